@@ -362,6 +362,142 @@ aa_status aa_step_host(aa_ctx* ctx, const aa_feat* feat, aa_assistant* assistant
                        void* staging, size_t staging_bytes);
 
 /*
+ * Operators that train the Boss on the batch the generator chose (Algorithm 3: Boss.Forward, Boss.Backward on the batch B).
+ * They take the batch as the generator leaves it on the device: the list of stored rows (out_idx of aa_score_shrink) as the
+ * instances' identities, token offsets of ragged sentences (out_offsets of aa_batch_cut) and device counts.  As everywhere in
+ * this header a call only enqueues kernels, and only the instances below the device count are touched.
+ *
+ * Row-major matrix the library reads or writes: row r at data + r*row_stride elements.
+ */
+typedef struct {
+    void* data;
+    int32_t dtype;           /* aa_dtype */
+    int32_t reserved;
+    int64_t rows;
+    int64_t cols;
+    int64_t row_stride;      /* elements */
+} aa_rows;
+
+/*
+ * Dropout by a counter-based generator: the mask is a function of (seed, step, instance id, site, element) and is never stored.
+ * The instance id of instance k is id_base + row_idx[k] (id_base + k without row_idx), so an instance draws the same mask in any
+ * batch slot, batch size or shard.  site numbers the dropouts of a model.
+ *   instance key  (k0, k1) = output words 2 and 3 of Philox4x32-10(key = seed, counter = (id, step)); the screen's draw is word 0;
+ *   block of 8    = Philox4x32-10(key = (k0, k1), counter = (block number as 64 bits, site, 0)): eight 16-bit draws, draw h =
+ *                   bits 16 (h % 2) .. +15 of word h / 2;
+ *   an element is dropped iff its draw is below t = floor(65536 p + 1/2) (at most 65535); kept ones are scaled by
+ *   65536 / (65536 - t): the rate is p rounded to a multiple of 2^-16 and the scale is exact for that rate.
+ */
+typedef struct {
+    float p;                 /* in [0, 1) */
+    uint32_t site;
+    uint64_t seed;
+    uint64_t step;
+    const int32_t* row_idx;  /* nullable DEVICE list, one entry per instance */
+    int64_t id_base;
+} aa_dropout_rule;
+
+/*
+ * out = residual + dropout(x) (residual nullable: out = dropout(x), which applied to the gradient of out is also the backward
+ * pass; the residual's gradient is the gradient of out itself).  Element (a, c), row a of its instance and column c, takes draw
+ * c % 8 of block a * ceil(cols / 8) + c / 8.  Computed in fp32 and rounded once; dropped elements are 0 whatever x holds.
+ *   offsets == NULL: row k is instance k; M = min(*count_dev, rows) instances, or rows without count_dev.
+ *   offsets != NULL: offsets[n_seg + 1] ascending; instance s is the rows [offsets[s], offsets[s+1]); M = min(*count_dev, n_seg).
+ * Rows of no counted instance are left untouched.  Offsets outside [0, rows] or descending latch AA_ERR_BAD_INDEX; rows that they
+ * would misplace are left untouched or take the draws of a neighbouring instance, nothing outside the matrices is accessed.
+ * x, residual and out have one dtype and shape, strides of their own; out may be x or residual itself, not a shifted overlap.
+ */
+aa_status aa_dropout(aa_ctx* ctx, const aa_rows* x, const aa_dropout_rule* rule, const int32_t* offsets, int64_t n_seg,
+                     const int32_t* count_dev, const aa_rows* residual, const aa_rows* out);
+
+typedef enum { AA_REDUCE_SUM = 0, AA_REDUCE_MEAN = 1 } aa_reduce_mode;
+
+/*
+ * Gradient of the batch objective  F = scale * c * sum_i weight_i f_i  with respect to the logits, f_i the instance losses of
+ * aa_instance_loss, c = 1 (AA_REDUCE_SUM) or 1 / M (AA_REDUCE_MEAN; M is the device count where there is one):
+ *   out_grad[r][k] = scale * c * weight_i * (exp(logit[r][k] - lse_r) - [k = labels[r]]),   i the instance of row r.
+ * weight nullable (all 1), one fp32 per instance, e.g. 1 / p_i of the screen.  out_loss nullable: f_i as aa_instance_loss writes it.
+ * Rows with a label < 0 (padding) get a zero gradient; labels >= cols too, and latch AA_ERR_BAD_INDEX.
+ *   offsets / n_seg: as in aa_instance_loss; count_dev counts instances, that is rows without offsets and segments with them.
+ * Rows of no counted instance are left untouched.  out_grad has the logits' dtype and shape; it may be the logits' own memory
+ * (same pointer and stride).  Offsets that descend or leave [0, rows] latch AA_ERR_BAD_INDEX; the rows concerned are then unspecified.
+ */
+aa_status aa_instance_loss_grad(aa_ctx* ctx, const aa_logits* logits, const int32_t* labels, const int32_t* offsets, int64_t n_seg,
+                                const int32_t* count_dev, const float* weight, float scale, int32_t reduce_mode,
+                                float* out_loss, const aa_rows* out_grad);
+
+/*
+ * Attention over ragged sentences with a learned relative position bias.  For sequence s with Lq queries and Lk keys, head h
+ * (key head h / (heads / kv_heads)), query i at position pos_i = i + Lk - Lq (the last query sits at the last key: a single new
+ * token over its context is Lq = 1), key j at position j, delta = j - pos_i:
+ *   s_ij = scale * q_i . k_j + table[bucket(delta)][h]       (causal: keys with delta > 0 are masked)
+ *   p_ij = softmax over the unmasked keys,   o_i = sum_j dropout(p)_ij v_j.
+ * A query that sees no key (Lk = 0, a position before the first key, a bias of -inf everywhere) gives o_i = 0 and no gradient.
+ *
+ * Tokens: element (token t, head h, e) at data + t*token_stride + h*head_stride + e, so that q, k and v may be views of one packed
+ * projection.  Sequence s owns the query tokens [q_offsets[s], q_offsets[s+1]) and the key tokens [k_offsets[s], k_offsets[s+1]).
+ * max_q, max_k: HOST upper bounds of one sequence's lengths.  A sequence that breaks them, or whose offsets descend or leave
+ * [0, q_rows] / [0, k_rows], latches AA_ERR_BAD_INDEX and is skipped.  M = min(*count_dev, n_seq) sequences are evaluated; token
+ * rows of no evaluated sequence are left untouched.
+ *
+ * aa_rel_bias: buckets halve into the two directions when bidirectional (delta > 0 takes the upper half); with n buckets per
+ * direction, distances below E = n / 2 have a bucket each and the rest grow geometrically up to max_distance: bucket k >= E starts
+ * at ceil(E (max_distance / E)^((k - E) / (n - E)) (1 - 1e-9)), the last one has no end.  Not bidirectional: delta > 0 counts as 0.
+ * table is [buckets][heads] fp32.  Limits: buckets per direction 2..128 (even totals when bidirectional), E < max_distance <= 2048.
+ * A NULL bias is no bias.
+ *
+ * Dropout (NULL: none): probability (h, i, j) takes draw 2 ((j / 8) % 4) + j % 2 of block ((h Lq + i) ceil(Lk / 32) + j / 32) 4 +
+ * (j / 2) % 4; the instance of sequence s is rule->row_idx[s].
+ *
+ * dtype AA_BF16 with 16-byte aligned tokens (base and strides), head_dim a multiple of 8 up to 128 runs on the tensor cores: scores and
+ * sums in fp32, probabilities and score gradients rounded to bf16 as operands of the products with v, k, q and do.  Everything
+ * else (AA_F32, other widths up to 256, other strides) takes an fp32 kernel.
+ */
+typedef struct {
+    void* data;
+    int64_t token_stride;    /* elements */
+    int64_t head_stride;     /* elements */
+} aa_tokens;
+
+typedef struct {
+    int32_t dtype;           /* aa_dtype of every token array */
+    int32_t causal;
+    int32_t heads, kv_heads, head_dim;
+    float scale;
+    int64_t n_seq;
+    const int32_t* q_offsets;   /* DEVICE, n_seq + 1 */
+    const int32_t* k_offsets;   /* DEVICE, n_seq + 1; may be q_offsets */
+    int64_t q_rows, k_rows;     /* stored tokens */
+    int64_t max_q, max_k;
+    const int32_t* count_dev;   /* nullable */
+    aa_tokens q, k, v;
+} aa_attn;
+
+typedef struct {
+    int32_t buckets;
+    int32_t max_distance;
+    int32_t bidirectional;
+    int32_t reserved;
+    const float* table;      /* DEVICE [buckets][heads] */
+} aa_rel_bias;
+
+/* HOST: bucket of a relative position delta (-1 for a malformed descriptor; table is not read). */
+int32_t aa_rel_bucket(const aa_rel_bias* bias, int64_t delta);
+
+aa_status aa_rel_attention(aa_ctx* ctx, const aa_attn* attn, const aa_rel_bias* bias, const aa_dropout_rule* dropout, const aa_tokens* out);
+
+/*
+ * Gradients of aa_rel_attention from dout, the gradient of its output: dq, dk, dv in the tokens' dtype (written, not added to; shared key
+ * heads get the sum over their query heads), dtable[buckets][heads] fp32 (nullable; summed over all evaluated sequences in a fixed
+ * order, 0 for buckets that no pair takes).  bias and dropout as in the forward call.  The probabilities are evaluated again, nothing
+ * is kept from the forward call.  scratch: DEVICE memory of at least aa_rel_attention_scratch_bytes(...) bytes, 256-byte aligned.
+ */
+aa_status aa_rel_attention_scratch_bytes(const aa_attn* attn, const aa_rel_bias* bias, size_t* bytes);
+aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_bias* bias, const aa_dropout_rule* dropout,
+                                const aa_tokens* dout, const aa_tokens* dq, const aa_tokens* dk, const aa_tokens* dv, float* dtable,
+                                void* scratch, size_t scratch_bytes);
+
+/*
  * Synchronises the context's stream, returns the first device-side condition latched since the
  * last call in *latched (HOST pointer; AA_OK if none) and clears it.
  */

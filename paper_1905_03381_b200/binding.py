@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
+from ctypes import POINTER, Structure, byref, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 
 import torch
 
@@ -22,12 +22,14 @@ AA_F32, AA_BF16 = 0, 1
 AA_FEAT_DENSE, AA_FEAT_CSR = 0, 1
 AA_ASSIST_LINEAR, AA_ASSIST_MLP = 0, 1
 AA_THRESH_VALUE, AA_THRESH_BATCH_MEAN = 0, 1
+AA_REDUCE_SUM, AA_REDUCE_MEAN = 0, 1
 
 EXPORTS = (
     "aa_status_string", "aa_workspace_bytes", "aa_create", "aa_destroy", "aa_score_shrink",
     "aa_shrink_compact", "aa_instance_loss", "aa_assistant_step", "aa_step_host_staging_bytes", "aa_step_host",
     "aa_device_status", "aa_launch_count", "aa_shrink_compact_static", "aa_batch_cut", "aa_threshold_compact", "aa_sk_threshold", "aa_assistant_step_adam",
     "aa_instance_loss_rows", "aa_assistant_step_scored", "aa_conv_pool_features",
+    "aa_dropout", "aa_instance_loss_grad", "aa_rel_bucket", "aa_rel_attention", "aa_rel_attention_scratch_bytes", "aa_rel_attention_grad",
 )
 AA_STATIC_MAX_CANDIDATES = 1 << 22
 
@@ -73,6 +75,96 @@ def conv_layer(weight: torch.Tensor, bias, height: int, width: int, pool: int) -
     cv.weight, cv.bias = weight.data_ptr(), _ptr(bias)
     cv._keep = (weight, bias)
     return cv
+
+
+class aa_rows(Structure):
+    _fields_ = [("data", c_void_p), ("dtype", c_int32), ("reserved", c_int32), ("rows", c_int64), ("cols", c_int64), ("row_stride", c_int64)]
+
+
+class aa_dropout_rule(Structure):
+    _fields_ = [("p", c_float), ("site", c_uint32), ("seed", c_uint64), ("step", c_uint64), ("row_idx", c_void_p), ("id_base", c_int64)]
+
+
+class aa_tokens(Structure):
+    _fields_ = [("data", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64)]
+
+
+class aa_attn(Structure):
+    _fields_ = [
+        ("dtype", c_int32), ("causal", c_int32), ("heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32), ("scale", c_float),
+        ("n_seq", c_int64), ("q_offsets", c_void_p), ("k_offsets", c_void_p), ("q_rows", c_int64), ("k_rows", c_int64),
+        ("max_q", c_int64), ("max_k", c_int64), ("count_dev", c_void_p), ("q", aa_tokens), ("k", aa_tokens), ("v", aa_tokens),
+    ]
+
+
+class aa_rel_bias(Structure):
+    _fields_ = [("buckets", c_int32), ("max_distance", c_int32), ("bidirectional", c_int32), ("reserved", c_int32), ("table", c_void_p)]
+
+
+def rows_desc(x: torch.Tensor) -> aa_rows:
+    """Descriptor of a 2-D fp32/bf16 matrix with contiguous rows (row stride free)."""
+    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1) or not x.is_cuda:
+        raise TypeError("expected a 2-D CUDA tensor with contiguous rows")
+    m = aa_rows()
+    m.data, m.dtype, m.rows, m.cols = x.data_ptr(), _dtype_code(x), x.shape[0], x.shape[1]
+    m.row_stride = x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return m
+
+
+def dropout_rule(p: float, seed: int, step: int, site: int = 0, row_idx=None, id_base: int = 0) -> aa_dropout_rule:
+    """Dropout of rate p whose mask is a function of (seed, step, instance id, site, element); row_idx: the batch list (int32)."""
+    _check(row_idx, torch.int32, "row_idx")
+    r = aa_dropout_rule()
+    r.p, r.site, r.seed, r.step, r.row_idx, r.id_base = p, site, seed, step, _ptr(row_idx), id_base
+    r._keep = row_idx
+    return r
+
+
+def rel_bias(table: torch.Tensor, max_distance: int, bidirectional: bool = True) -> aa_rel_bias:
+    """Learned bias by relative position: table fp32 [buckets, heads]."""
+    _check(table, torch.float32, "table")
+    if table.dim() != 2:
+        raise TypeError("table must be [buckets, heads]")
+    b = aa_rel_bias()
+    b.buckets, b.max_distance, b.bidirectional, b.table = table.shape[0], max_distance, int(bidirectional), table.data_ptr()
+    b._keep = table
+    return b
+
+
+def _tokens(x: torch.Tensor, name: str, like=None) -> aa_tokens:
+    if x.dim() != 3 or not x.is_cuda or (x.stride(2) != 1 and x.shape[2] > 1):
+        raise TypeError(f"{name} must be a 3-D CUDA tensor [tokens, heads, head_dim] with a contiguous last dimension")
+    if like is not None and (x.shape != like.shape or x.dtype != like.dtype):
+        raise TypeError(f"{name} must have the shape and dtype of the tensor it belongs to")
+    t = aa_tokens()
+    t.data, t.token_stride, t.head_stride = x.data_ptr(), x.stride(0), x.stride(1)
+    return t
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets=None, max_q=None, max_k=None,
+              scale=None, causal: bool = False, count_dev=None, n_seq=None) -> aa_attn:
+    """Ragged attention problem: q [tokens, heads, dim], k and v [tokens, kv_heads, dim] (views of a packed projection are fine),
+    int32 offsets of the sequences' tokens; max_q / max_k bound one sequence's length (default: all tokens); scale defaults to
+    1 / sqrt(dim)."""
+    k_offsets = q_offsets if k_offsets is None else k_offsets
+    _check(q_offsets, torch.int32, "q_offsets")
+    _check(k_offsets, torch.int32, "k_offsets")
+    _check(count_dev, torch.int32, "count_dev")
+    a = aa_attn()
+    a.q, a.k, a.v = _tokens(q, "q"), _tokens(k, "k"), _tokens(v, "v", k)
+    if q.dtype != k.dtype or q.shape[2] != k.shape[2]:
+        raise TypeError("q, k and v must share dtype and head_dim")
+    if n_seq is None and q_offsets.numel() != k_offsets.numel():
+        raise TypeError("q_offsets and k_offsets must have the same length")
+    a.dtype, a.causal, a.heads, a.kv_heads, a.head_dim = _dtype_code(q), int(causal), q.shape[1], k.shape[1], q.shape[2]
+    a.scale = 1.0 / float(q.shape[2]) ** 0.5 if scale is None else scale
+    a.n_seq = q_offsets.numel() - 1 if n_seq is None else n_seq
+    a.q_offsets, a.k_offsets, a.count_dev = q_offsets.data_ptr(), k_offsets.data_ptr(), _ptr(count_dev)
+    a.q_rows, a.k_rows = q.shape[0], k.shape[0]
+    a.max_q = q.shape[0] if max_q is None else max_q
+    a.max_k = k.shape[0] if max_k is None else max_k
+    a._keep = (q, k, v, q_offsets, k_offsets, count_dev)
+    return a
 
 
 class aa_adam(Structure):
@@ -139,6 +231,16 @@ def lib() -> ctypes.CDLL:
         L.aa_step_host.argtypes = [c_void_p, POINTER(aa_feat), POINTER(aa_assistant), c_float, c_uint64, c_uint64,
                                    POINTER(aa_logits), c_void_p, c_float, c_int32, c_float,
                                    c_void_p, c_void_p, c_void_p, c_void_p, c_size_t]
+        L.aa_dropout.argtypes = [c_void_p, POINTER(aa_rows), POINTER(aa_dropout_rule), c_void_p, c_int64, c_void_p, POINTER(aa_rows),
+                                 POINTER(aa_rows)]
+        L.aa_instance_loss_grad.argtypes = [c_void_p, POINTER(aa_logits), c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_float, c_int32,
+                                            c_void_p, POINTER(aa_rows)]
+        L.aa_rel_bucket.restype = c_int32
+        L.aa_rel_bucket.argtypes = [POINTER(aa_rel_bias), c_int64]
+        L.aa_rel_attention.argtypes = [c_void_p, POINTER(aa_attn), POINTER(aa_rel_bias), POINTER(aa_dropout_rule), POINTER(aa_tokens)]
+        L.aa_rel_attention_scratch_bytes.argtypes = [POINTER(aa_attn), POINTER(aa_rel_bias), POINTER(c_size_t)]
+        L.aa_rel_attention_grad.argtypes = [c_void_p, POINTER(aa_attn), POINTER(aa_rel_bias), POINTER(aa_dropout_rule), POINTER(aa_tokens),
+                                            POINTER(aa_tokens), POINTER(aa_tokens), POINTER(aa_tokens), c_void_p, c_void_p, c_size_t]
         L.aa_device_status.argtypes = [c_void_p, POINTER(c_int32)]
         L.aa_launch_count.restype = c_int64
         L.aa_launch_count.argtypes = [c_void_p]
@@ -371,6 +473,69 @@ class AutoAssist:
         self._ok(self._L.aa_assistant_step_adam(self._ctx, byref(feat), loss.data_ptr(), _ptr(count_dev), byref(assistant),
                                                 byref(state), lr, mode, 0.0 if threshold is None else threshold),
                  "aa_assistant_step_adam")
+
+    # ---- operators that train the Boss on the generated batch
+
+    def aa_dropout(self, x: torch.Tensor, rule: aa_dropout_rule, out: torch.Tensor, residual=None, offsets=None, count_dev=None, n_seg=None):
+        """out = residual + dropout(x); without residual also the backward pass (x = the gradient of out).  offsets: token offsets of
+        the instances (int32, ragged sentences); without them every row is an instance."""
+        _check(offsets, torch.int32, "offsets")
+        _check(count_dev, torch.int32, "count_dev")
+        xm, om = rows_desc(x), rows_desc(out)
+        rm = None if residual is None else byref(rows_desc(residual))
+        if offsets is None:
+            n_seg = 0
+        elif n_seg is None:
+            n_seg = offsets.numel() - 1
+        self._ok(self._L.aa_dropout(self._ctx, byref(xm), byref(rule), _ptr(offsets), n_seg, _ptr(count_dev), rm, byref(om)), "aa_dropout")
+
+    def aa_instance_loss_grad(self, logits: aa_logits, labels: torch.Tensor, out_grad: torch.Tensor, offsets=None, n_seg=None, count_dev=None,
+                              weight=None, scale: float = 1.0, mean: bool = True, out_loss=None):
+        """Gradient of scale * (mean or sum over the instances of weight_i f_i) with respect to the logits; out_loss receives f_i.
+        out_grad may be the logits themselves."""
+        for t, name, dtype in ((labels, "labels", torch.int32), (offsets, "offsets", torch.int32), (count_dev, "count_dev", torch.int32),
+                               (weight, "weight", torch.float32), (out_loss, "out_loss", torch.float32)):
+            _check(t, dtype, name)
+        if offsets is None:
+            n_seg = 0
+        elif n_seg is None:
+            n_seg = offsets.numel() - 1
+        self._ok(self._L.aa_instance_loss_grad(self._ctx, byref(logits), labels.data_ptr(), _ptr(offsets), n_seg, _ptr(count_dev), _ptr(weight),
+                                               scale, AA_REDUCE_MEAN if mean else AA_REDUCE_SUM, _ptr(out_loss), byref(rows_desc(out_grad))),
+                 "aa_instance_loss_grad")
+
+    def aa_rel_attention(self, attn: aa_attn, out: torch.Tensor, bias=None, dropout=None):
+        """Attention over ragged sequences with a learned relative position bias and instance-keyed dropout (both optional)."""
+        self._check_bias(attn, bias)
+        o = _tokens(out, "out", attn._keep[0])
+        self._ok(self._L.aa_rel_attention(self._ctx, byref(attn), None if bias is None else byref(bias), None if dropout is None else byref(dropout),
+                                          byref(o)), "aa_rel_attention")
+
+    @staticmethod
+    def _check_bias(attn: aa_attn, bias):
+        if bias is not None and bias._keep.shape[1] != attn.heads:
+            raise TypeError("the bias table must be [buckets, heads]")
+
+    def rel_attention_scratch(self, attn: aa_attn, bias=None) -> torch.Tensor:
+        """Device scratch for aa_rel_attention_grad on problems of this size."""
+        nbytes = c_size_t(0)
+        self._ok(self._L.aa_rel_attention_scratch_bytes(byref(attn), None if bias is None else byref(bias), byref(nbytes)),
+                 "aa_rel_attention_scratch_bytes")
+        return torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
+
+    def aa_rel_attention_grad(self, attn: aa_attn, dout: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, scratch: torch.Tensor,
+                              bias=None, dropout=None, dtable=None):
+        """dq, dk, dv (and the bias table's gradient) of aa_rel_attention from the gradient of its output."""
+        self._check_bias(attn, bias)
+        q, k, v = attn._keep[:3]
+        _check(dtable, torch.float32, "dtable")
+        if dtable is not None and (bias is None or dtable.shape != bias._keep.shape):
+            raise TypeError("dtable must have the bias table's shape")
+        ts = [_tokens(dout, "dout", q), _tokens(dq, "dq", q), _tokens(dk, "dk", k), _tokens(dv, "dv", v)]
+        base = (scratch.data_ptr() + 255) // 256 * 256
+        self._ok(self._L.aa_rel_attention_grad(self._ctx, byref(attn), None if bias is None else byref(bias), None if dropout is None else byref(dropout),
+                                               *[byref(t) for t in ts], _ptr(dtable), base, scratch.data_ptr() + scratch.numel() - base),
+                 "aa_rel_attention_grad")
 
     def host_step_plan(self, x_host: torch.Tensor, logits_host: torch.Tensor):
         """Descriptors and a device staging buffer for aa_step_host on HOST tensors of these shapes."""

@@ -5,6 +5,7 @@
 // t = x * log2(e), so that sum_c 2^(t_c) = S * 2^M; thread states are merged by warp shuffles
 // (and through shared memory when a CTA shares a row).  For sequence tasks the token rows of
 // a sentence are then summed in row order (fp64 accumulator) by a second small kernel.
+#include "boss_common.cuh"
 #include "loss_common.cuh"
 
 namespace aa {
@@ -206,7 +207,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) row_loss_cta_kernel(L
 
 // Per-sentence sums of token-row losses, one warp per segment, rows added in fp64.
 __global__ void __launch_bounds__(256) segment_sum_kernel(const float* __restrict__ row_loss, const int32_t* __restrict__ offsets,
-                                                          int64_t n_seg, int64_t rows, float* __restrict__ out, Control* ctl) {
+                                                          int64_t n_seg, int64_t rows, float* __restrict__ out, Control* ctl,
+                                                          const int32_t* __restrict__ count_dev) {
+    n_seg = counted(count_dev, n_seg);
     const int lane = threadIdx.x & 31;
     const int64_t warp = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
     const int64_t nwarps = ((int64_t)gridDim.x * blockDim.x) >> 5;
@@ -278,6 +281,18 @@ aa_status launch_rows(aa_ctx_impl* c, LossParams& p) {
 
 }  // namespace
 
+aa_status launch_segment_sum(aa_ctx_impl* c, const float* row_loss, const int32_t* offsets, int64_t n_seg, const int32_t* count_dev,
+                             int64_t rows, float* out) {
+    Control* ctl = c->ctl;
+    void* args[] = {&row_loss, &offsets, &n_seg, &rows, &out, &ctl, &count_dev};
+    const int64_t want = (n_seg + 7) / 8;   // 8 warps per CTA
+    const int cap = c->sm_count * 8;
+    const int grid = (int)(want < cap ? want : cap);
+    if (cudaLaunchKernel((const void*)segment_sum_kernel, dim3(grid), dim3(256), args, 0, c->stream) != cudaSuccess) return AA_ERR_CUDA;
+    ++c->launches;
+    return AA_OK;
+}
+
 aa_status launch_instance_loss(aa_ctx_impl* c, const aa_logits& lg, const int32_t* labels, const int32_t* offsets,
                                int64_t n_seg, const int32_t* count_dev, float* out_loss, const int32_t* row_idx, int64_t n_rows) {
     LossParams p;
@@ -295,18 +310,7 @@ aa_status launch_instance_loss(aa_ctx_impl* c, const aa_logits& lg, const int32_
         const aa_status st = lg.dtype == AA_BF16 ? launch_rows<uint16_t>(c, p) : launch_rows<float>(c, p);
         if (st != AA_OK) return st;
     }
-    if (offsets && n_seg > 0) {
-        const float* row_loss = c->row_scratch;
-        int64_t rows = p.rows;
-        Control* ctl = c->ctl;
-        void* args[] = {&row_loss, &offsets, &n_seg, &rows, &out_loss, &ctl};
-        const int64_t want = (n_seg + 7) / 8;   // 8 warps per CTA
-        const int cap = c->sm_count * 8;
-        const int grid = (int)(want < cap ? want : cap);
-        if (cudaLaunchKernel((const void*)segment_sum_kernel, dim3(grid), dim3(256), args, 0, c->stream) != cudaSuccess)
-            return AA_ERR_CUDA;
-        ++c->launches;
-    }
+    if (offsets && n_seg > 0) return launch_segment_sum(c, c->row_scratch, offsets, n_seg, nullptr, p.rows, out_loss);
     return AA_OK;
 }
 

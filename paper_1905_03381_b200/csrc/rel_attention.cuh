@@ -1,0 +1,143 @@
+// Attention over ragged sequences with a learned relative position bias: parameters, the bias by distance, the draws of its dropout
+// and the tile bookkeeping that the kernels share.
+//
+// Scores are kept in base 2:  t_ij = scale log2(e) q_i.k_j + log2(e) table[bucket(delta)][h],  p_ij = 2^(t_ij - m_i) / l_i.
+// A finite bias is clamped to +-3e38 after the change of base, so that the type's lowest value stays a finite mask.
+#pragma once
+
+#include "boss_common.cuh"
+
+namespace aa {
+
+constexpr int kMaxPerDir = 128;          // buckets per direction
+constexpr int kMaxReach = 2048;          // largest max_distance
+constexpr float kAttnLog2e = 1.4426950408889634f;
+
+struct TokArg {
+    const void* data;
+    int64_t tok, head;                   // strides in elements
+};
+
+struct RelParams {
+    TokArg q, k, v, out, dout, dq, dk, dv;
+    int heads, kv_heads, group, dim, causal;
+    float scale2;                        // scale * log2(e)
+    float scale;
+    int64_t n_seq, q_rows, k_rows, max_q, max_k;
+    const int32_t* q_off;
+    const int32_t* k_off;
+    const int32_t* count_dev;
+    // bias: distances below `reach` have an entry each in the kernels' distance table, the rest are the last bucket's
+    const float* table;                  // nullable
+    int buckets, per_dir, bidir, reach;
+    int lower[kMaxPerDir];               // first distance of every bucket of a direction
+    DropRule drop;
+    Control* ctl;
+    // backward
+    float4* stats;                       // [heads][q_rows]: m, 1 / l, D
+    float* parts;                        // [n_parts][heads][buckets] partial sums of the table's gradient
+    int n_parts;
+    float* dtable;                       // nullable
+};
+
+// First distances of the buckets of one direction; false: malformed.
+bool rel_bucket_bounds(const aa_rel_bias* b, int* per_dir, int* lower);
+// Shapes and offsets of one problem; AA_OK or the argument error.
+aa_status make_rel_params(const aa_attn* a, const aa_rel_bias* b, const aa_dropout_rule* d, RelParams& p);
+int rel_grad_parts(int heads);                                       // CTAs per head that share the table's gradient
+
+aa_status launch_rel_attention_plain(aa_ctx_impl* c, const RelParams& p, int dtype);
+aa_status launch_rel_attention_grad_plain(aa_ctx_impl* c, const RelParams& p, int dtype);
+aa_status launch_rel_table_grad(aa_ctx_impl* c, const RelParams& p);  // parts -> dtable
+
+#ifdef __CUDACC__
+
+struct Seq {
+    int64_t q0, k0;                      // first tokens
+    int lq, lk;
+};
+
+// Sequence s; false: not counted, or its offsets are bad (latched).
+__device__ __forceinline__ bool load_seq(const RelParams& p, int64_t s, Seq& q) {
+    if (s >= counted(p.count_dev, p.n_seq)) return false;
+    const int a = __ldg(p.q_off + s), b = __ldg(p.q_off + s + 1), c = __ldg(p.k_off + s), d = __ldg(p.k_off + s + 1);
+    if (a < 0 || b < a || b > p.q_rows || b - a > p.max_q || c < 0 || d < c || d > p.k_rows || d - c > p.max_k) {
+        latch(p.ctl, AA_ERR_BAD_INDEX);
+        return false;
+    }
+    q.q0 = a;
+    q.lq = b - a;
+    q.k0 = c;
+    q.lk = d - c;
+    return true;
+}
+
+__device__ __forceinline__ int bucket_of(const RelParams& p, int delta) {
+    const int n = p.bidir ? abs(delta) : max(-delta, 0);
+    int lo = 0, hi = p.per_dir;          // lower[lo] <= n, lower[hi] > n (or hi = per_dir)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.lower[mid] <= n) lo = mid; else hi = mid;
+    }
+    return lo + (p.bidir && delta > 0 ? p.per_dir : 0);
+}
+
+// Base-2 bias by distance for head h: bias[delta + reach], delta in [-reach, reach]; farther ones are clamped to the ends.
+__device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias) {
+    if (!p.table) return;
+    for (int i = threadIdx.x; i <= 2 * p.reach; i += blockDim.x) {
+        const float b = __ldg(p.table + (int64_t)bucket_of(p, i - p.reach) * p.heads + h);
+        const float b2 = b * kAttnLog2e;
+        bias[i] = isinf(b) || isnan(b) ? b : fminf(fmaxf(b2, -3.0e38f), 3.0e38f);
+    }
+}
+__device__ __forceinline__ float bias_at(const RelParams& p, const float* bias, int delta) {
+    return p.table ? bias[min(max(delta, -p.reach), p.reach) + p.reach] : 0.0f;
+}
+
+// Number of the first draw block of query row i, head h.
+__device__ __forceinline__ uint64_t draw_row(const Seq& s, int h, int i) {
+    return ((uint64_t)h * (uint64_t)s.lq + (uint64_t)i) * (uint64_t)((s.lk + 31) >> 5) * 4ull;
+}
+
+// Keys [0, n) that some query of rows [i0, i1) sees.
+__device__ __forceinline__ int keys_seen(const RelParams& p, const Seq& s, int i1) {
+    return p.causal ? max(0, min(s.lk, i1 + s.lk - s.lq)) : s.lk;
+}
+// First query row that sees key j.
+__device__ __forceinline__ int first_query(const RelParams& p, const Seq& s, int j) {
+    return p.causal ? max(0, j - (s.lk - s.lq)) : 0;
+}
+
+// Partial sums of the table's gradient by distance, then by bucket.  Distances inside the table's reach have a bin of their own,
+// [delta + reach] for -reach < delta < reach (and delta <= 0 when one-directional); the rest are summed per side.
+struct FarSums {
+    float neg, pos;
+};
+__device__ __forceinline__ void bin_diagonal(const RelParams& p, float* bins, FarSums& far, int delta, float sum) {
+    if (delta <= -p.reach) far.neg += sum;
+    else if (delta >= p.reach || (!p.bidir && delta > 0)) far.pos += sum;
+    else bins[delta + p.reach] += sum;
+}
+
+// Bins and the threads' far sums -> this CTA's partial sums by bucket (bins and far sums visible to the CTA).
+__device__ __forceinline__ void write_table_part(const RelParams& p, int h, const float* bins, const float* far_neg, const float* far_pos, int n_far) {
+    float* part = p.parts + ((int64_t)blockIdx.x * p.heads + h) * p.buckets;
+    for (int b = threadIdx.x; b < p.buckets; b += blockDim.x) {
+        const int k = b % p.per_dir;
+        const bool up = b >= p.per_dir, last = k == p.per_dir - 1;
+        double sum = 0.0;
+        const int hi = last ? p.reach : p.lower[k + 1];                 // distances [lower[k], hi); up: delta > 0
+        for (int n = max(p.lower[k], up ? 1 : 0); n < hi; ++n) sum += (double)bins[p.reach + (up ? n : -n)];
+        const float* far = last ? (up ? far_pos : far_neg) : nullptr;
+        if (far)
+            for (int i = 0; i < n_far; ++i) sum += (double)far[i];
+        if (!p.bidir && k == 0)                                         // delta > 0 counts as 0
+            for (int i = 0; i < n_far; ++i) sum += (double)far_pos[i];
+        part[b] = (float)sum;
+    }
+}
+
+#endif  // __CUDACC__
+
+}  // namespace aa
