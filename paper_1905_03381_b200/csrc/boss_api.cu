@@ -171,7 +171,7 @@ aa_status aa_rel_attention(aa_ctx* ctx, const aa_attn* attn, const aa_rel_bias* 
     aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
     p.out = tok(*out);
     p.ctl = c->ctl;
-    return launch_rel_attention_plain(c, p, attn->dtype);
+    return attn->dtype == AA_BF16 && rel_mma_fits(p) ? launch_rel_attention_mma(c, p) : launch_rel_attention_plain(c, p, attn->dtype);
 }
 
 aa_status aa_rel_attention_scratch_bytes(const aa_attn* attn, const aa_rel_bias* bias, size_t* bytes) {
@@ -179,7 +179,8 @@ aa_status aa_rel_attention_scratch_bytes(const aa_attn* attn, const aa_rel_bias*
     RelParams p;
     const aa_status st = make_rel_params(attn, bias, nullptr, p);
     if (st != AA_OK) return st;
-    *bytes = stats_bytes(attn) + (size_t)rel_grad_parts(p.heads) * (size_t)p.heads * (size_t)p.buckets * sizeof(float);
+    // up to three launches (short, middle and long sequences) leave partial sums of the table's gradient
+    *bytes = stats_bytes(attn) + 3 * (size_t)rel_grad_parts(p.heads) * (size_t)p.heads * (size_t)p.buckets * sizeof(float);
     return AA_OK;
 }
 
@@ -209,7 +210,7 @@ aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_b
     p.stats = static_cast<float4*>(scratch);
     p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(attn));
     p.n_parts = rel_grad_parts(p.heads);
-    st = launch_rel_attention_grad_plain(c, p, attn->dtype);
+    st = attn->dtype == AA_BF16 && rel_mma_fits(p) ? launch_rel_attention_grad_mma(c, p, &p.n_parts) : launch_rel_attention_grad_plain(c, p, attn->dtype);
     if (st != AA_OK || !dtable) return st;
     return launch_rel_table_grad(c, p);
 }

@@ -48,6 +48,10 @@ int rel_grad_parts(int heads);                                       // CTAs per
 
 aa_status launch_rel_attention_plain(aa_ctx_impl* c, const RelParams& p, int dtype);
 aa_status launch_rel_attention_grad_plain(aa_ctx_impl* c, const RelParams& p, int dtype);
+// bf16 kernels on the tensor cores: aligned tokens, head width a multiple of 8 up to 128.
+bool rel_mma_fits(const RelParams& p);
+aa_status launch_rel_attention_mma(aa_ctx_impl* c, const RelParams& p);
+aa_status launch_rel_attention_grad_mma(aa_ctx_impl* c, const RelParams& p, int* n_parts);
 aa_status launch_rel_table_grad(aa_ctx_impl* c, const RelParams& p);  // parts -> dtable
 
 #ifdef __CUDACC__
@@ -120,21 +124,24 @@ __device__ __forceinline__ void bin_diagonal(const RelParams& p, float* bins, Fa
     else bins[delta + p.reach] += sum;
 }
 
-// Bins and the threads' far sums -> this CTA's partial sums by bucket (bins and far sums visible to the CTA).
-__device__ __forceinline__ void write_table_part(const RelParams& p, int h, const float* bins, const float* far_neg, const float* far_pos, int n_far) {
-    float* part = p.parts + ((int64_t)blockIdx.x * p.heads + h) * p.buckets;
-    for (int b = threadIdx.x; b < p.buckets; b += blockDim.x) {
+// Bins and the threads' far sums -> one CTA's partial sums by bucket (bins and far sums visible to the CTA).  A warp per bucket, lanes
+// over its distances, joined in a fixed order.
+__device__ __forceinline__ void write_table_part(const RelParams& p, int64_t index, int h, const float* bins, const float* far_neg, const float* far_pos, int n_far) {
+    float* part = p.parts + (index * p.heads + h) * p.buckets;
+    const int lane = threadIdx.x & 31;
+    for (int b = threadIdx.x >> 5; b < p.buckets; b += blockDim.x >> 5) {
         const int k = b % p.per_dir;
         const bool up = b >= p.per_dir, last = k == p.per_dir - 1;
         double sum = 0.0;
         const int hi = last ? p.reach : p.lower[k + 1];                 // distances [lower[k], hi); up: delta > 0
-        for (int n = max(p.lower[k], up ? 1 : 0); n < hi; ++n) sum += (double)bins[p.reach + (up ? n : -n)];
-        const float* far = last ? (up ? far_pos : far_neg) : nullptr;
-        if (far)
-            for (int i = 0; i < n_far; ++i) sum += (double)far[i];
+        for (int n = max(p.lower[k], up ? 1 : 0) + lane; n < hi; n += 32) sum += (double)bins[p.reach + (up ? n : -n)];
+        if (last)
+            for (int i = lane; i < n_far; i += 32) sum += (double)(up ? far_pos : far_neg)[i];
         if (!p.bidir && k == 0)                                         // delta > 0 counts as 0
-            for (int i = 0; i < n_far; ++i) sum += (double)far_pos[i];
-        part[b] = (float)sum;
+            for (int i = lane; i < n_far; i += 32) sum += (double)far_pos[i];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        if (lane == 0) part[b] = (float)sum;
     }
 }
 

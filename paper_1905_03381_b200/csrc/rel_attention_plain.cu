@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(kThreads) grad_q_kernel(RelParams p, int tiles
     far_sum[0][threadIdx.x] = far.neg;
     far_sum[1][threadIdx.x] = far.pos;
     __syncthreads();
-    write_table_part(p, h, bins, far_sum[0], far_sum[1], kThreads);
+    write_table_part(p, blockIdx.x, h, bins, far_sum[0], far_sum[1], kThreads);
 }
 
 // dk and dv of one key tile and key head: the query heads that share it and the query tiles that see it, in order.
