@@ -51,6 +51,9 @@ aa_status launch_rel_attention_grad_plain(aa_ctx_impl* c, const RelParams& p, in
 // bf16 kernels on the tensor cores: aligned tokens, head width a multiple of 8 up to 128.
 bool rel_mma_fits(const RelParams& p);
 aa_status launch_rel_attention_mma(aa_ctx_impl* c, const RelParams& p);
+// ... of them the sequences of at most *covered tokens on both sides (set by the call; -1: none)
+aa_status launch_rel_sentences(aa_ctx_impl* c, const RelParams& p, int* covered);
+aa_status launch_rel_sentences_grad(aa_ctx_impl* c, const RelParams& p, int* covered, int* n_parts);
 aa_status launch_rel_attention_grad_mma(aa_ctx_impl* c, const RelParams& p, int* n_parts);
 aa_status launch_rel_table_grad(aa_ctx_impl* c, const RelParams& p);  // parts -> dtable
 
@@ -76,26 +79,33 @@ __device__ __forceinline__ bool load_seq(const RelParams& p, int64_t s, Seq& q) 
     return true;
 }
 
-__device__ __forceinline__ int bucket_of(const RelParams& p, int delta) {
-    const int n = p.bidir ? abs(delta) : max(-delta, 0);
-    int lo = 0, hi = p.per_dir;          // lower[lo] <= n, lower[hi] > n (or hi = per_dir)
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.lower[mid] <= n) lo = mid; else hi = mid;
-    }
-    return lo + (p.bidir && delta > 0 ? p.per_dir : 0);
-}
-
-// Base-2 bias by distance for head h: bias[delta + reach], delta in [-reach, reach]; farther ones are clamped to the ends.
+// Base-2 bias by distance for head h: bias[delta + reach + MARGIN]; the ends beyond the reach repeat the last buckets' values for MARGIN
+// distances, so that a tile that touches the reach needs no clamping.  A warp per bucket: the bounds are read at one address.
+template <int MARGIN>
 __device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias) {
     if (!p.table) return;
-    for (int i = threadIdx.x; i <= 2 * p.reach; i += blockDim.x) {
-        const float b = __ldg(p.table + (int64_t)bucket_of(p, i - p.reach) * p.heads + h);
-        const float b2 = b * kAttnLog2e;
-        bias[i] = isinf(b) || isnan(b) ? b : fminf(fmaxf(b2, -3.0e38f), 3.0e38f);
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    float* zero = bias + p.reach + MARGIN;
+    for (int b0 = 0; b0 < p.buckets; b0 += 32) {
+        float v = 0.0f;                                                 // a lane per bucket: one trip to memory for 32 of them
+        if (b0 + lane < p.buckets) {
+            const float x = __ldg(p.table + (int64_t)(b0 + lane) * p.heads + h);
+            v = isinf(x) || isnan(x) ? x : fminf(fmaxf(x * kAttnLog2e, -3.0e38f), 3.0e38f);
+        }
+        const int b1 = min(p.buckets - b0, 32);
+        for (int i = threadIdx.x >> 5; i < b1; i += warps) {
+            const float x = __shfl_sync(0xFFFFFFFFu, v, i);
+            const bool up = b0 + i >= p.per_dir;
+            const int k = up ? b0 + i - p.per_dir : b0 + i;
+            const int end = k == p.per_dir - 1 ? p.reach + MARGIN + 1 : p.lower[k + 1];
+            for (int n = max(p.lower[k], up ? 1 : 0) + lane; n < end; n += 32) zero[up ? n : -n] = x;
+            if (!p.bidir && k == 0)                                     // one direction: later keys count as distance 0
+                for (int n = 1 + lane; n <= p.reach + MARGIN; n += 32) zero[n] = x;
+        }
     }
 }
-__device__ __forceinline__ float bias_at(const RelParams& p, const float* bias, int delta) {
+__host__ __device__ constexpr int bias_floats(int reach, int margin) { return 2 * (reach + margin) + 1; }
+__device__ __forceinline__ float bias_at(const RelParams& p, const float* bias, int delta) {      // a table without margins
     return p.table ? bias[min(max(delta, -p.reach), p.reach) + p.reach] : 0.0f;
 }
 
@@ -124,21 +134,26 @@ __device__ __forceinline__ void bin_diagonal(const RelParams& p, float* bins, Fa
     else bins[delta + p.reach] += sum;
 }
 
-// Bins and the threads' far sums -> one CTA's partial sums by bucket (bins and far sums visible to the CTA).  A warp per bucket, lanes
-// over its distances, joined in a fixed order.
-__device__ __forceinline__ void write_table_part(const RelParams& p, int64_t index, int h, const float* bins, const float* far_neg, const float* far_pos, int n_far) {
+// Bins -> one CTA's partial sums by bucket.  `copies` arrays `pitch` floats apart, each 2 reach bins, then n_far sums of the far past and
+// n_far of the far future (visible to the CTA).  A warp per bucket, lanes over its distances, joined in a fixed order.
+__device__ __forceinline__ void write_table_part(const RelParams& p, int64_t index, int h, const float* bins, int pitch, int copies, int n_far) {
     float* part = p.parts + (index * p.heads + h) * p.buckets;
     const int lane = threadIdx.x & 31;
     for (int b = threadIdx.x >> 5; b < p.buckets; b += blockDim.x >> 5) {
-        const int k = b % p.per_dir;
-        const bool up = b >= p.per_dir, last = k == p.per_dir - 1;
-        double sum = 0.0;
+        const bool up = b >= p.per_dir;
+        const int k = up ? b - p.per_dir : b;
+        const bool last = k == p.per_dir - 1;
         const int hi = last ? p.reach : p.lower[k + 1];                 // distances [lower[k], hi); up: delta > 0
-        for (int n = max(p.lower[k], up ? 1 : 0) + lane; n < hi; n += 32) sum += (double)bins[p.reach + (up ? n : -n)];
-        if (last)
-            for (int i = lane; i < n_far; i += 32) sum += (double)(up ? far_pos : far_neg)[i];
-        if (!p.bidir && k == 0)                                         // delta > 0 counts as 0
-            for (int i = lane; i < n_far; i += 32) sum += (double)far_pos[i];
+        double sum = 0.0;
+        for (int c = 0; c < copies; ++c) {
+            const float* one = bins + c * pitch;
+            const float* far_neg = one + 2 * p.reach;
+            for (int n = max(p.lower[k], up ? 1 : 0) + lane; n < hi; n += 32) sum += (double)one[p.reach + (up ? n : -n)];
+            if (last)
+                for (int i = lane; i < n_far; i += 32) sum += (double)far_neg[i + (up ? n_far : 0)];
+            if (!p.bidir && k == 0)                                     // delta > 0 counts as 0
+                for (int i = lane; i < n_far; i += 32) sum += (double)far_neg[i + n_far];
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
         if (lane == 0) part[b] = (float)sum;

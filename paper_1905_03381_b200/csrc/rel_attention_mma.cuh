@@ -41,20 +41,20 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Tokens [row0, row0 + ROWS) of one head into a tile of DT columns; rows from n on and columns from p.dim on are zero.
+// Tokens [row0, row0 + ROWS) of one head into a tile of DT columns; rows from n up to the next multiple of 16 and columns from p.dim on are
+// zero, rows behind that are left as they are (no product reads them).  A thread keeps its column and walks down the rows: an address is
+// one 32 x 32 + 64 bit multiply-add (strides are below 2^30 elements).
 template <int ROWS, int DT, int THREADS>
 __device__ __forceinline__ void load_tile_async(const RelParams& p, const TokArg& a, int head, int64_t row0, int n, uint16_t* dst) {
-    constexpr int CH = DT / 8;
-    const uint16_t* base = static_cast<const uint16_t*>(a.data) + row0 * a.tok + (int64_t)head * a.head;
-    const uint32_t d = smem_u32(dst);
+    constexpr int CH = DT / 8, STEP = THREADS / CH;
+    const int c = threadIdx.x % CH, r0 = threadIdx.x / CH;
+    const char* base = reinterpret_cast<const char*>(static_cast<const uint16_t*>(a.data) + row0 * a.tok + (int64_t)head * a.head + (c * 8 < p.dim ? c * 8 : 0));
+    const uint32_t d = smem_u32(dst) + (uint32_t)(r0 * pitch_of(DT) + c * 8) * 2u, pitch = (uint32_t)a.tok * 2u;
+    const int live = c * 8 < p.dim ? n : 0, rows = (n + 15) & ~15;
 #pragma unroll
-    for (int i = 0; i < (ROWS * CH + THREADS - 1) / THREADS; ++i) {
-        const int at = i * THREADS + (int)threadIdx.x;
-        if ((ROWS * CH) % THREADS == 0 || at < ROWS * CH) {
-            const int r = at / CH, c = at % CH;
-            const bool live = r < n && c * 8 < p.dim;
-            cp_async16(d + (uint32_t)(r * pitch_of(DT) + c * 8) * 2u, live ? base + (int64_t)r * a.tok + c * 8 : base, live);
-        }
+    for (int i = 0; i < (ROWS + STEP - 1) / STEP; ++i) {
+        const int r = r0 + i * STEP;
+        if (r < rows) cp_async16(d + (uint32_t)(i * STEP * pitch_of(DT)) * 2u, base + (uint64_t)(uint32_t)min(r, n - 1) * pitch, r < live);
     }
 }
 
@@ -110,60 +110,75 @@ struct Block {
     int i0, j0;
 };
 
-// Products -> base-2 scores with bias and masks.
-__device__ __forceinline__ void block_scores(const RelParams& p, const Seq& s, const float* bias, const Block& b, int lane, float (&acc)[8][4]) {
+// A block that touches the reach of the bias holds distances up to 78 beyond it.
+constexpr int kBiasMargin = 80;
+
+// Products -> base-2 scores with bias and masks, for the first n16 groups of 16 keys (the others are left as they are).
+__device__ __forceinline__ void block_scores(const RelParams& p, const Seq& s, const float* bias, const Block& b, int n16, int lane, float (&acc)[8][4]) {
     const int shift = s.lk - s.lq, g = lane >> 2, t = lane & 3;
     const int dmin = b.j0 - (b.i0 + 15 + shift), dmax = b.j0 + 63 - (b.i0 + shift);
     const bool whole = b.j0 + 64 <= s.lk && b.i0 + 16 <= s.lq && (!p.causal || dmax <= 0);
     if (!p.table) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < 8; ++n) {
+            if (n / 2 >= n16) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[n][e] *= p.scale2;
+        }
     } else if (dmax <= -p.reach || dmin >= p.reach) {      // one bucket for the whole block
-        const float far = bias[dmax <= -p.reach ? 0 : 2 * p.reach];
+        const float far = bias[dmax <= -p.reach ? 0 : 2 * (p.reach + kBiasMargin)];
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < 8; ++n) {
+            if (n / 2 >= n16) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[n][e] = fmaf(acc[n][e], p.scale2, far);
+        }
     } else {
-        const int d0 = b.j0 + 2 * t - (b.i0 + g + shift) + p.reach, top = 2 * p.reach;
+        const float* at = bias + (b.j0 + 2 * t - (b.i0 + g + shift) + p.reach + kBiasMargin);
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < 8; ++n) {
+            if (n / 2 >= n16) continue;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int at = d0 + 8 * n + (e & 1) - 8 * (e >> 1);
-                acc[n][e] = fmaf(acc[n][e], p.scale2, bias[min(max(at, 0), top)]);
-            }
+            for (int e = 0; e < 4; ++e) acc[n][e] = fmaf(acc[n][e], p.scale2, at[8 * n + (e & 1) - 8 * (e >> 1)]);
+        }
     }
     if (!whole) {
+        int lim[2];                                        // keys of this lane's columns that row r sees: those below lim[r]
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int r = 0; r < 2; ++r) {
+            const int i = b.i0 + g + 8 * r;
+            lim[r] = i < s.lq ? min(s.lk, p.causal ? i + shift + 1 : s.lk) - (b.j0 + 2 * t) : -0x40000000;
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = b.i0 + g + 8 * (e >> 1), j = b.j0 + 8 * n + 2 * t + (e & 1);
-                if (i >= s.lq || j >= s.lk || (p.causal && j > i + shift)) acc[n][e] = -INFINITY;
-            }
+        for (int n = 0; n < 8; ++n) {
+            if (n / 2 >= n16) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (8 * n + (e & 1) >= lim[e >> 1]) acc[n][e] = -INFINITY;
+        }
     }
 }
 
-// Bits of dropped elements: bit 4 nt + e of the answer.  Four draw blocks per lane: two rows, two chunks of 32 keys.
-__device__ __forceinline__ uint32_t block_drops(const RelParams& p, const Seq& s, uint2 key, int h, const Block& b, int lane) {
-    uint32_t bits = 0;
+// Calls drop(n, e, dropped) for every element of the block.  Four draw blocks per lane: two rows, two chunks of 32 keys.  Draw x of a
+// block is key tile 4 c + x / 2, element x % 2 of its row; the high half of a word compares in place, the low half shifted up.
+template <typename F>
+__device__ __forceinline__ void block_drops(const RelParams& p, const Seq& s, uint2 key, int h, const Block& b, int n16, int lane, F drop) {
+    const uint32_t top = p.drop.thr << 16;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const uint64_t first = draw_row(s, h, b.i0 + (lane >> 2) + 8 * r) + (uint64_t)((b.j0 >> 5) * 4 + (lane & 3));
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
+            if (2 * c >= n16) continue;
             const Words4 w = draw_block(p.drop, key, first + 4 * c);
 #pragma unroll
-            for (int x = 0; x < 8; ++x)                     // draw x: key tile 4 c + x / 2, element x % 2 of row r
-                if (draw_half(w, x) < p.drop.thr) bits |= 1u << (4 * (4 * c + (x >> 1)) + 2 * r + (x & 1));
+            for (int x = 0; x < 4; ++x) {
+                drop(4 * c + x, 2 * r, (w.w[x] << 16) < top);
+                drop(4 * c + x, 2 * r + 1, w.w[x] < top);
+            }
         }
     }
-    return bits;
 }
-
 // 16-key groups of the block that hold an unmasked pair.
 __device__ __forceinline__ int block_groups(const RelParams& p, const Seq& s, const Block& b) {
     if (b.i0 >= s.lq) return 0;
@@ -181,6 +196,120 @@ __device__ __forceinline__ float quad_sum(float x) {
     return x + __shfl_xor_sync(0xFFFFFFFFu, x, 2);
 }
 
+// ---- softmax and gradient steps of a block, for its first n16 groups of 16 keys
+
+// Running maximum and sum of rows g and g + 8, t -> 2^(t - m), earlier output rescaled.
+template <int DT>
+__device__ __forceinline__ void block_softmax(float (&t)[8][4], int n16, float (&m)[2], float (&l)[2], float (&o)[DT / 8][4]) {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        float top = m[r];
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+            if (n / 2 < n16) top = fmaxf(top, fmaxf(t[n][2 * r], t[n][2 * r + 1]));
+        top = quad_max(top);
+        const float ref = top == -INFINITY ? 0.0f : top, corr = ex2_approx(m[r] - ref);
+        float sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            if (n / 2 >= n16) continue;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float e = ex2_approx(t[n][2 * r + c] - ref);
+                sum += e;
+                t[n][2 * r + c] = e;
+            }
+        }
+        l[r] = fmaf(l[r], corr, sum);                      // this lane's part of the row
+        m[r] = top;
+#pragma unroll
+        for (int j = 0; j < DT / 8; ++j) {
+            o[j][2 * r] *= corr;
+            o[j][2 * r + 1] *= corr;
+        }
+    }
+}
+// o += x . tile rows [n0, n0 + 64).  x (probabilities of at most 1, or score gradients) is rounded to bf16 as the left operand: 2^-9 of each
+// term of a result that is bf16 itself.
+template <int DT>
+__device__ __forceinline__ void block_times(const RelParams& p, const float (&x)[8][4], uint32_t tile, int n0, int n16, int lane, float (&o)[DT / 8][4]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (k >= n16) continue;
+        const uint32_t a[4] = {pack_bf16(x[2 * k][0], x[2 * k][1]), pack_bf16(x[2 * k][2], x[2 * k][3]), pack_bf16(x[2 * k + 1][0], x[2 * k + 1][1]),
+                               pack_bf16(x[2 * k + 1][2], x[2 * k + 1][3])};
+#pragma unroll
+        for (int j = 0; j < DT / 16; ++j) {
+            if (DT > 64 && j * 16 >= p.dim) continue;
+            uint32_t v[4];
+            ldsm4t(v, frag_rows<pitch_of(DT)>(tile, n0 + k * 16, j * 16, lane));
+            mma16816(o[2 * j], a, v[0], v[1]);
+            mma16816(o[2 * j + 1], a, v[2], v[3]);
+        }
+    }
+}
+
+// Row statistics of lane (g, t)'s rows g and g + 8.
+struct RowStats {
+    float m[2], rl[2], D[2];
+};
+// this lane's maximum of row r
+__device__ __forceinline__ float block_max(const float (&t)[8][4], int n16, int r, float top) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+        if (n / 2 < n16) top = fmaxf(top, fmaxf(t[n][2 * r], t[n][2 * r + 1]));
+    return top;
+}
+// t -> e = 2^(t - ref); adds this lane's sums
+__device__ __forceinline__ void block_exp(int n16, const float (&ref)[2], float (&t)[8][4], float (&sum)[2]) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+        if (n / 2 >= n16) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            t[n][e] = ex2_approx(t[n][e] - ref[e >> 1]);
+            sum[e >> 1] += t[n][e];
+        }
+    }
+}
+// dp of dropped probabilities is 0, of kept ones scaled; the sign of e (which is not negative) remembers which were dropped.
+__device__ __forceinline__ void block_drop(const RelParams& p, const Seq& s, uint2 key, int h, const Block& b, int n16, int lane, float (&t)[8][4], float (&dp)[8][4]) {
+    if (!p.drop.thr) return;
+    block_drops(p, s, key, h, b, n16, lane, [&](int n, int e, bool d) {
+        dp[n][e] = d ? 0.0f : __fmul_rn(dp[n][e], p.drop.scale);
+        t[n][e] = d ? -t[n][e] : t[n][e];
+    });
+}
+// this lane's sums of e dp
+__device__ __forceinline__ void block_dsum(int n16, const float (&t)[8][4], const float (&dp)[8][4], float (&dsum)[2]) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+        if (n / 2 >= n16) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dsum[e >> 1] = fmaf(fabsf(t[n][e]), dp[n][e], dsum[e >> 1]);
+    }
+}
+// e (signed) -> p, dropped and scaled, in t;  dp -> ds = p (dp - D).  rl includes whatever turns e into p.
+__device__ __forceinline__ void block_ds(const RelParams& p, const RowStats& st, int n16, float (&t)[8][4], float (&dp)[8][4]) {
+    const float f[2] = {st.rl[0] * p.drop.scale, st.rl[1] * p.drop.scale};
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+        if (n / 2 >= n16) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = e >> 1;
+            dp[n][e] = fabsf(t[n][e]) * st.rl[r] * (dp[n][e] - st.D[r]);
+            t[n][e] = fmaxf(t[n][e], 0.0f) * f[r];
+        }
+    }
+}
+__device__ __forceinline__ float block_total(const float (&ds)[8][4]) {
+    float a = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) a += (ds[n][0] + ds[n][1]) + (ds[n][2] + ds[n][3]);
+    return a;
+}
+
 // ---- diagonal sums.  A lane's elements of one 16 x 64 block are first added along the diagonal inside the lane (row g + 8 of key tile
 // nt + 1 lies on the diagonal of row g of key tile nt); the 8 x 72 values left are stored skewed, row g shifted by 7 - g, so that a column
 // of the staging area is a diagonal: column key - row + 15 (rows and keys relative to the block), columns 0..78.
@@ -196,21 +325,51 @@ __device__ __forceinline__ void stage_diagonals(float* stage, const float (&ds)[
 #pragma unroll
         for (int c = 0; c < 2; ++c) at[8 * (u + 1) + c] = (u >= 0 ? ds[u < 0 ? 0 : u][c] : 0.0f) + (u < 7 ? ds[u < 7 ? u + 1 : 7][2 + c] : 0.0f);
 }
+// Row r holds columns 7 - r .. 78 - r.
 __device__ __forceinline__ float diagonal_sum(const float* stage, int col) {
     float sum = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) sum += stage[r * kDiagPitch + col];
+    for (int r = 0; r < 8; ++r) {
+        const float x = stage[r * kDiagPitch + col];
+        sum += col + r >= 7 && col + r < 79 ? x : 0.0f;
+    }
     return sum;
 }
 
-// acc rows (g, g + 8 of a 16-row block) times f, as bf16; rows from n on are not written.
-template <int DT>
-__device__ __forceinline__ void store_block(const RelParams& p, const TokArg& a, int head, int64_t row0, int n, int lane, const float (&acc)[DT / 8][4], float f0, float f1) {
+// The same 18 values of a lane, added up over blocks that lie at the same distances: acc[u + 1][lane] of 9 x 32 pairs, this lane's own.
+constexpr int kDiagAccFloats = 9 * 64;
+__device__ __forceinline__ void add_diagonals(float* acc, const float (&ds)[8][4], int lane) {
+    float2* mine = reinterpret_cast<float2*>(acc) + lane;
+#pragma unroll
+    for (int u = -1; u < 8; ++u) {
+        float2 x = mine[(u + 1) * 32];
+        x.x += (u >= 0 ? ds[u < 0 ? 0 : u][0] : 0.0f) + (u < 7 ? ds[u < 7 ? u + 1 : 7][2] : 0.0f);
+        x.y += (u >= 0 ? ds[u < 0 ? 0 : u][1] : 0.0f) + (u < 7 ? ds[u < 7 ? u + 1 : 7][3] : 0.0f);
+        mine[(u + 1) * 32] = x;
+    }
+}
+__device__ __forceinline__ void stage_accumulated(float* stage, float* acc, int lane) {
     const int g = lane >> 2, t = lane & 3;
-    uint16_t* base = const_cast<uint16_t*>(static_cast<const uint16_t*>(a.data)) + row0 * a.tok + (int64_t)head * a.head + 2 * t;
+    float* at = stage + g * kDiagPitch + 2 * t + 7 - g;
+    float2* mine = reinterpret_cast<float2*>(acc) + lane;
+#pragma unroll
+    for (int u = 0; u < 9; ++u) {
+        const float2 x = mine[u * 32];
+        mine[u * 32] = make_float2(0.0f, 0.0f);
+        at[8 * u] = x.x;
+        at[8 * u + 1] = x.y;
+    }
+}
+
+// acc rows (g, g + 8 of a 16-row block) times f, as bf16, into DT columns from c0 on; rows from n on are not written.
+template <int DT>
+__device__ __forceinline__ void store_block(const RelParams& p, const TokArg& a, int head, int64_t row0, int n, int lane, const float (&acc)[DT / 8][4], float f0, float f1,
+                                            int c0 = 0) {
+    const int g = lane >> 2, t = lane & 3;
+    uint16_t* base = const_cast<uint16_t*>(static_cast<const uint16_t*>(a.data)) + row0 * a.tok + (int64_t)head * a.head + c0 + 2 * t;
 #pragma unroll
     for (int j = 0; j < DT / 8; ++j) {
-        if (j * 8 >= p.dim) continue;
+        if (c0 + j * 8 >= p.dim) continue;
         if (g < n) *reinterpret_cast<uint32_t*>(base + (int64_t)g * a.tok + j * 8) = pack_bf16(acc[j][0] * f0, acc[j][1] * f0);
         if (g + 8 < n) *reinterpret_cast<uint32_t*>(base + (int64_t)(g + 8) * a.tok + j * 8) = pack_bf16(acc[j][2] * f1, acc[j][3] * f1);
     }

@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kThreads) forward_kernel(RelParams p, int tile
     if (!load_seq(p, sn, s) || i0 >= s.lq) return;
     const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
     const uint2 key = p.drop.thr ? instance_key(p.drop, sn) : make_uint2(0, 0);
-    fill_bias(p, h, bias);
+    fill_bias<0>(p, h, bias);
     const int nq = min(G::B, s.lq - i0), end = keys_seen(p, s, i0 + nq);
     load_tile<T, DT>(p, p.q, h, s.q0 + i0, nq, Qs);
     float m[G::M], l[G::M], acc[G::M][G::W];
@@ -234,12 +234,11 @@ __global__ void __launch_bounds__(kThreads) grad_q_kernel(RelParams p, int tiles
     float* Ps = Vs + G::B * G::LD;
     float* bias = Ps + G::B * G::LP;
     float* bins = bias + (p.table ? 2 * p.reach + 1 : 0);
-    __shared__ float far_sum[2][kThreads];
     grid_dependency_wait();
     grid_dependency_release();
     const int h = blockIdx.y, ty = threadIdx.x / 16, tx = threadIdx.x % 16;
     const bool want_table = p.table && p.dtable;
-    fill_bias(p, h, bias);
+    fill_bias<0>(p, h, bias);
     if (want_table)
         for (int i = threadIdx.x; i < 2 * p.reach; i += kThreads) bins[i] = 0.0f;
     FarSums far = {0.0f, 0.0f};
@@ -330,10 +329,10 @@ __global__ void __launch_bounds__(kThreads) grad_q_kernel(RelParams p, int tiles
         store_rows<T, DT>(p, p.dq, h, s.q0 + i0, nq, ty, tx, acc, f);
     }
     if (!want_table) return;
-    far_sum[0][threadIdx.x] = far.neg;
-    far_sum[1][threadIdx.x] = far.pos;
+    bins[2 * p.reach + threadIdx.x] = far.neg;
+    bins[2 * p.reach + kThreads + threadIdx.x] = far.pos;
     __syncthreads();
-    write_table_part(p, blockIdx.x, h, bins, far_sum[0], far_sum[1], kThreads);
+    write_table_part(p, blockIdx.x, h, bins, 0, 1, kThreads);
 }
 
 // dk and dv of one key tile and key head: the query heads that share it and the query tiles that see it, in order.
@@ -365,7 +364,7 @@ __global__ void __launch_bounds__(kThreads) grad_kv_kernel(RelParams p, int tile
         for (int w = 0; w < G::W; ++w) gk[a][w] = gv[a][w] = 0.0f;
     for (int h = hk * p.group; h < (hk + 1) * p.group; ++h) {
         __syncthreads();
-        fill_bias(p, h, bias);
+        fill_bias<0>(p, h, bias);
         for (int i0 = first_query(p, s, j0) / G::B * G::B; i0 < s.lq; i0 += G::B) {
             const int nq = min(G::B, s.lq - i0);
             __syncthreads();
@@ -409,16 +408,18 @@ __global__ void __launch_bounds__(kThreads) grad_kv_kernel(RelParams p, int tile
     store_rows<T, DT>(p, p.dv, hk, s.k0 + j0, nk, ty, tx, gv, one);
 }
 
-// dtable[b][h] = sum of the parts in their order.
+// dtable[b][h] = sum of the parts: a warp per entry, lanes over the parts, joined in a fixed order.
 __global__ void __launch_bounds__(256) table_grad_kernel(RelParams p) {
     grid_dependency_wait();
     grid_dependency_release();
-    const int n = p.buckets * p.heads;
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
-        const int b = i / p.heads, h = i % p.heads;
+    const int n = p.buckets * p.heads, lane = threadIdx.x & 31;
+    for (int i = (blockIdx.x * 256 + threadIdx.x) >> 5; i < n; i += gridDim.x * 8) {
+        const int h = i / p.buckets, b = i % p.buckets;
         double sum = 0.0;
-        for (int g = 0; g < p.n_parts; ++g) sum += (double)p.parts[((int64_t)g * p.heads + h) * p.buckets + b];
-        p.dtable[i] = (float)sum;
+        for (int g = lane; g < p.n_parts; g += 32) sum += (double)p.parts[((int64_t)g * p.heads + h) * p.buckets + b];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        if (lane == 0) p.dtable[b * p.heads + h] = (float)sum;
     }
 }
 
@@ -447,7 +448,7 @@ aa_status backward(aa_ctx_impl* c, RelParams p) {
     const void* kq = (const void*)grad_q_kernel<T, DT>;
     const void* kkv = (const void*)grad_kv_kernel<T, DT>;
     const int reach = p.table ? 2 * p.reach + 1 : 0;
-    const size_t smem_q = G::smem(4, reach + (p.table && p.dtable ? 2 * p.reach : 0)), smem_kv = G::smem(4, reach);
+    const size_t smem_q = G::smem(4, reach + (p.table && p.dtable ? 2 * p.reach + 2 * kThreads : 0)), smem_kv = G::smem(4, reach);
     if (set_smem(kq, smem_q) != AA_OK || set_smem(kkv, smem_kv) != AA_OK) return AA_ERR_CUDA;
     int tiles_q = (int)((p.max_q + G::B - 1) / G::B), tiles_k = (int)((p.max_k + G::B - 1) / G::B);
     if (p.n_seq * tiles_k > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
@@ -479,7 +480,7 @@ aa_status launch_rel_table_grad(aa_ctx_impl* c, const RelParams& p) {
     RelParams q = p;
     void* args[] = {&q};
     const int n = p.buckets * p.heads;
-    if (launch_overlapped(c, (const void*)table_grad_kernel, dim3((n + 255) / 256), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+    if (launch_overlapped(c, (const void*)table_grad_kernel, dim3((n + 7) / 8), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     return AA_OK;
 }
