@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(256) grad_keys_kernel(RelParams p, int lo, int
             load_tile_async<64, DT, THREADS>(p, p.dout, h, s.q0 + i0, nq, Os);
             cp_async_commit();
             const Block b = {i0 + wq * 16, j0 + wk * 64};
-            const int n16 = block_groups(p, s, b);
+            const bool live = block_live(p, s, b);
             RowStats st;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
@@ -76,30 +76,23 @@ __global__ void __launch_bounds__(256) grad_keys_kernel(RelParams p, int lo, int
             }
             cp_async_wait<0>();
             __syncthreads();
-            float t[8][4], dp[8][4];
-            {
+            uint16_t* prow = Ps + (wq * 16 + (lane >> 2)) * PP + wk * 64 + 2 * (lane & 3);
+            uint16_t* srow = Ss + (wq * 16 + (lane >> 2)) * PP + wk * 64 + 2 * (lane & 3);
+            if (live) {
+                float t[8][4], dp[8][4], unused[2] = {0.0f, 0.0f};
                 uint32_t f[DT / 16][4];
                 load_frags<DT>(p, f, qS, wq * 16, lane);
-                block_dot<DT>(p, f, kS, wk * 64, n16, lane, t);
+                block_dot<DT, 8>(p, f, kS, wk * 64, lane, t);
                 load_frags<DT>(p, f, oS, wq * 16, lane);
-                block_dot<DT>(p, f, vS, wk * 64, n16, lane, dp);
-            }
-            block_scores(p, s, bias, b, n16, lane, t);
-            float unused[2] = {0.0f, 0.0f};
-            block_exp(n16, st.m, t, unused);
-            block_drop(p, s, key, h, b, n16, lane, t, dp);
-            block_ds(p, st, n16, t, dp);                                    // dead groups stay zero
-            {
-                const int g = lane >> 2, q2 = 2 * (lane & 3);
-                uint16_t* prow = Ps + (wq * 16 + g) * PP + wk * 64 + q2;
-                uint16_t* srow = Ss + (wq * 16 + g) * PP + wk * 64 + q2;
-#pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    *reinterpret_cast<uint32_t*>(prow + 8 * n) = pack_bf16(t[n][0], t[n][1]);
-                    *reinterpret_cast<uint32_t*>(prow + 8 * PP + 8 * n) = pack_bf16(t[n][2], t[n][3]);
-                    *reinterpret_cast<uint32_t*>(srow + 8 * n) = pack_bf16(dp[n][0], dp[n][1]);
-                    *reinterpret_cast<uint32_t*>(srow + 8 * PP + 8 * n) = pack_bf16(dp[n][2], dp[n][3]);
-                }
+                block_dot<DT, 8>(p, f, vS, wk * 64, lane, dp);
+                block_scores(p, s, bias, b, lane, t);
+                block_exp(st.m, t, unused);
+                block_drop(p, s, key, h, b, lane, t, dp);
+                block_ds(p, st, t, dp);
+                store_scores(prow, srow, PP, t, dp);
+            } else {
+                const float zero[8][4] = {};
+                store_scores(prow, srow, PP, zero, zero);
             }
             __syncthreads();
             // dV += P^T dO, dK += dS^T Q: this warp's 16 keys, contraction over the tile's rows
@@ -223,26 +216,26 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(RelParams p, int lo, int
             }
             const uint32_t kS = smem_u32(KV + (it & 1) * 2 * 64 * P), vS = kS + 64 * P * 2;
             const Block b = {i0 + warp * 16, j0};
-            const int n16 = block_groups(p, s, b);
+            const bool live = block_live(p, s, b);
             float t[8][4], dp[8][4];
-            if (n16 > 0) {
-                block_dot<DT>(p, qf, kS, 0, n16, lane, t);
-                block_dot<DT>(p, of, vS, 0, n16, lane, dp);
-                block_scores(p, s, bias, b, n16, lane, t);
+            if (live) {
+                block_dot<DT, 8>(p, qf, kS, 0, lane, t);
+                block_dot<DT, 8>(p, of, vS, 0, lane, dp);
+                block_scores(p, s, bias, b, lane, t);
             }
             if (it < n_tiles) {
-                if (n16 > 0) {
+                if (live) {
                     float ref[2], sum[2] = {0.0f, 0.0f}, dsum[2] = {0.0f, 0.0f}, corr[2];
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float top = quad_max(block_max(t, n16, r, m[r]));
+                        const float top = quad_max(block_max(t, r, m[r]));
                         ref[r] = top == -INFINITY ? 0.0f : top;
                         corr[r] = ex2_approx(m[r] - ref[r]);
                         m[r] = top;
                     }
-                    block_exp(n16, ref, t, sum);
-                    block_drop(p, s, key, h, b, n16, lane, t, dp);
-                    block_dsum(n16, t, dp, dsum);
+                    block_exp(ref, t, sum);
+                    block_drop(p, s, key, h, b, lane, t, dp);
+                    block_dsum(t, dp, dsum);
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         l[r] = fmaf(l[r], corr[r], sum[r]);
@@ -255,17 +248,17 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(RelParams p, int lo, int
             const int shift = s.lk - s.lq;
             // distances of the whole CTA's tile: one side's last bucket throughout needs no diagonals
             const bool past = j0 + 63 - (i0 + shift) <= -p.reach, ahead = j0 - (i0 + 127 + shift) >= p.reach;
-            if (n16 > 0) {
+            if (live) {
                 float unused[2] = {0.0f, 0.0f};
-                block_exp(n16, st.m, t, unused);
-                block_drop(p, s, key, h, b, n16, lane, t, dp);
-                block_ds(p, st, n16, t, dp);
+                block_exp(st.m, t, unused);
+                block_drop(p, s, key, h, b, lane, t, dp);
+                block_ds(p, st, t, dp);
                 if (want_table && past) far_neg += block_total(dp);
                 if (want_table && ahead) far_pos += block_total(dp);
-                block_times<DT>(p, dp, kS, 0, n16, lane, gq);
+                block_times<DT, 8>(p, dp, kS, 0, lane, gq);
             }
             if (want_table && !past && !ahead) {
-                if (n16 == 0) {
+                if (!live) {
 #pragma unroll
                     for (int n = 0; n < 8; ++n)
 #pragma unroll

@@ -46,15 +46,14 @@ __global__ void __launch_bounds__(NW * 32) forward_mma_kernel(RelParams p, int l
         }
         if (tile == 0) load_frags<DT>(p, qf, smem_u32(Qs), warp * 16, lane);
         const Block b = {i0 + warp * 16, tile * 64};
-        const int n16 = block_groups(p, s, b);
-        if (n16 == 0) continue;
+        if (!block_live(p, s, b)) continue;
         const uint32_t Ks = smem_u32(KV + (tile & 1) * 2 * 64 * P), Vs = Ks + 64 * P * 2;
         float t[8][4];
-        block_dot<DT>(p, qf, Ks, 0, n16, lane, t);
-        block_scores(p, s, bias, b, n16, lane, t);
-        block_softmax<DT>(t, n16, m, l, o);
-        if (p.drop.thr) block_drops(p, s, key, h, b, n16, lane, [&](int n, int e, bool d) { t[n][e] = d ? 0.0f : t[n][e]; });
-        block_times<DT>(p, t, Vs, 0, n16, lane, o);
+        block_dot<DT, 8>(p, qf, Ks, 0, lane, t);
+        block_scores(p, s, bias, b, lane, t);
+        block_softmax<DT, 8>(t, m, l, o);
+        if (p.drop.thr) block_drops<8>(p, s, key, h, b, lane, [&](int n, int e, bool d) { t[n][e] = d ? 0.0f : t[n][e]; });
+        block_times<DT, 8>(p, t, Vs, 0, lane, o);
     }
     cp_async_wait<0>();                                    // a tile that sees no key has loaded its queries all the same
     float f[2];

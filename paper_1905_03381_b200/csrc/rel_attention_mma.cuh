@@ -41,20 +41,21 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Tokens [row0, row0 + ROWS) of one head into a tile of DT columns; rows from n up to the next multiple of 16 and columns from p.dim on are
-// zero, rows behind that are left as they are (no product reads them).  A thread keeps its column and walks down the rows: an address is
-// one 32 x 32 + 64 bit multiply-add (strides are below 2^30 elements).
-template <int ROWS, int DT, int THREADS>
+// Tokens [row0, row0 + ROWS) of one head into a tile of DT columns; rows from n up to the next multiple of ROUND and columns from p.dim on are
+// zero, rows behind that are left as they are (nothing may read them: not even a masked score's product, which would pass a NaN on).  A
+// thread keeps its column and walks down the rows: an address is one 32 x 32 + 64 bit multiply-add (strides are below 2^30 elements).
+template <int ROWS, int DT, int THREADS, int ROUND = ROWS>
 __device__ __forceinline__ void load_tile_async(const RelParams& p, const TokArg& a, int head, int64_t row0, int n, uint16_t* dst) {
     constexpr int CH = DT / 8, STEP = THREADS / CH;
+    static_assert(STEP <= ROWS && ROWS % STEP == 0, "a pass of the threads covers whole rows");
     const int c = threadIdx.x % CH, r0 = threadIdx.x / CH;
     const char* base = reinterpret_cast<const char*>(static_cast<const uint16_t*>(a.data) + row0 * a.tok + (int64_t)head * a.head + (c * 8 < p.dim ? c * 8 : 0));
     const uint32_t d = smem_u32(dst) + (uint32_t)(r0 * pitch_of(DT) + c * 8) * 2u, pitch = (uint32_t)a.tok * 2u;
-    const int live = c * 8 < p.dim ? n : 0, rows = (n + 15) & ~15;
+    const int live = c * 8 < p.dim ? n : 0, rows = ROUND == ROWS ? ROWS : (n + ROUND - 1) / ROUND * ROUND;
 #pragma unroll
-    for (int i = 0; i < (ROWS + STEP - 1) / STEP; ++i) {
+    for (int i = 0; i < ROWS / STEP; ++i) {
         const int r = r0 + i * STEP;
-        if (r < rows) cp_async16(d + (uint32_t)(i * STEP * pitch_of(DT)) * 2u, base + (uint64_t)(uint32_t)min(r, n - 1) * pitch, r < live);
+        if (ROUND == ROWS || r < rows) cp_async16(d + (uint32_t)(i * STEP * pitch_of(DT)) * 2u, base + (uint64_t)(uint32_t)max(0, min(r, n - 1)) * pitch, r < live);
     }
 }
 
@@ -75,21 +76,23 @@ __device__ __forceinline__ uint32_t frag_trans(uint32_t tile, int k, int m, int 
     return tile + (uint32_t)((k + (lane & 7) + ((lane >> 4) << 3)) * PITCH + m + (((lane >> 3) & 1) << 3)) * 2u;
 }
 
-// acc (16 rows x 64 columns) = A (16 x DT from registers) . tile rows^T, for the first n16 groups of 16 columns.
-template <int DT>
-__device__ __forceinline__ void block_dot(const RelParams& p, const uint32_t (&a)[DT / 16][4], uint32_t tile, int n0, int n16, int lane, float (&acc)[8][4]) {
+// A score block is 16 rows x 8 NT keys, NT = 4 or 8, fully unrolled and without a test per group of keys: groups that see nothing are masked
+// like any other key (a test each made the block's code twice as long in instructions executed).
+// acc = A (16 x DT from registers) . tile rows [n0, n0 + 8 NT)^T
+template <int DT, int NT>
+__device__ __forceinline__ void block_dot(const RelParams& p, const uint32_t (&a)[DT / 16][4], uint32_t tile, int n0, int lane, float (&acc)[NT][4]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
+    const uint32_t at = frag_cols<pitch_of(DT)>(tile, n0, 0, lane);
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        if (g >= n16) continue;
+    for (int k = 0; k < DT / 16; ++k) {
+        if (DT > 64 && k * 16 >= p.dim) continue;
 #pragma unroll
-        for (int k = 0; k < DT / 16; ++k) {
-            if (DT > 64 && k * 16 >= p.dim) continue;
+        for (int g = 0; g < NT / 2; ++g) {
             uint32_t b[4];
-            ldsm4(b, frag_cols<pitch_of(DT)>(tile, n0 + g * 16, k * 16, lane));
+            ldsm4(b, at + (uint32_t)(g * 16 * pitch_of(DT) + k * 16) * 2u);
             mma16816(acc[2 * g], a[k], b[0], b[1]);
             mma16816(acc[2 * g + 1], a[k], b[2], b[3]);
         }
@@ -105,7 +108,7 @@ __device__ __forceinline__ void load_frags(const RelParams& p, uint32_t (&a)[DT 
     }
 }
 
-// Where a warp's 16 x 64 score block lies: query rows i0 + g, i0 + g + 8 and keys j0 + 8 nt + 2 t + {0, 1} of lane (g, t).
+// Where a block lies: lane (g, t) holds query rows i0 + g, i0 + g + 8 and keys j0 + 8 nt + 2 t + {0, 1}.
 struct Block {
     int i0, j0;
 };
@@ -113,34 +116,29 @@ struct Block {
 // A block that touches the reach of the bias holds distances up to 78 beyond it.
 constexpr int kBiasMargin = 80;
 
-// Products -> base-2 scores with bias and masks, for the first n16 groups of 16 keys (the others are left as they are).
-__device__ __forceinline__ void block_scores(const RelParams& p, const Seq& s, const float* bias, const Block& b, int n16, int lane, float (&acc)[8][4]) {
+// Products -> base-2 scores with bias and masks.
+template <int NT>
+__device__ __forceinline__ void block_scores(const RelParams& p, const Seq& s, const float* bias, const Block& b, int lane, float (&acc)[NT][4]) {
     const int shift = s.lk - s.lq, g = lane >> 2, t = lane & 3;
-    const int dmin = b.j0 - (b.i0 + 15 + shift), dmax = b.j0 + 63 - (b.i0 + shift);
-    const bool whole = b.j0 + 64 <= s.lk && b.i0 + 16 <= s.lq && (!p.causal || dmax <= 0);
+    const int dmin = b.j0 - (b.i0 + 15 + shift), dmax = b.j0 + 8 * NT - 1 - (b.i0 + shift);
+    const bool whole = b.j0 + 8 * NT <= s.lk && b.i0 + 16 <= s.lq && (!p.causal || dmax <= 0);
     if (!p.table) {
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            if (n / 2 >= n16) continue;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[n][e] *= p.scale2;
-        }
     } else if (dmax <= -p.reach || dmin >= p.reach) {      // one bucket for the whole block
         const float far = bias[dmax <= -p.reach ? 0 : 2 * (p.reach + kBiasMargin)];
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            if (n / 2 >= n16) continue;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[n][e] = fmaf(acc[n][e], p.scale2, far);
-        }
     } else {
         const float* at = bias + (b.j0 + 2 * t - (b.i0 + g + shift) + p.reach + kBiasMargin);
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            if (n / 2 >= n16) continue;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[n][e] = fmaf(acc[n][e], p.scale2, at[8 * n + (e & 1) - 8 * (e >> 1)]);
-        }
     }
     if (!whole) {
         int lim[2];                                        // keys of this lane's columns that row r sees: those below lim[r]
@@ -150,26 +148,22 @@ __device__ __forceinline__ void block_scores(const RelParams& p, const Seq& s, c
             lim[r] = i < s.lq ? min(s.lk, p.causal ? i + shift + 1 : s.lk) - (b.j0 + 2 * t) : -0x40000000;
         }
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            if (n / 2 >= n16) continue;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (8 * n + (e & 1) >= lim[e >> 1]) acc[n][e] = -INFINITY;
-        }
+            for (int e = 0; e < 4; ++e) acc[n][e] = 8 * n + (e & 1) >= lim[e >> 1] ? -INFINITY : acc[n][e];
     }
 }
 
 // Calls drop(n, e, dropped) for every element of the block.  Four draw blocks per lane: two rows, two chunks of 32 keys.  Draw x of a
 // block is key tile 4 c + x / 2, element x % 2 of its row; the high half of a word compares in place, the low half shifted up.
-template <typename F>
-__device__ __forceinline__ void block_drops(const RelParams& p, const Seq& s, uint2 key, int h, const Block& b, int n16, int lane, F drop) {
+template <int NT, typename F>
+__device__ __forceinline__ void block_drops(const RelParams& p, const Seq& s, uint2 key, int h, const Block& b, int lane, F drop) {
     const uint32_t top = p.drop.thr << 16;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const uint64_t first = draw_row(s, h, b.i0 + (lane >> 2) + 8 * r) + (uint64_t)((b.j0 >> 5) * 4 + (lane & 3));
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            if (2 * c >= n16) continue;
+        for (int c = 0; c < NT / 4; ++c) {
             const Words4 w = draw_block(p.drop, key, first + 4 * c);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
@@ -179,12 +173,10 @@ __device__ __forceinline__ void block_drops(const RelParams& p, const Seq& s, ui
         }
     }
 }
-// 16-key groups of the block that hold an unmasked pair.
-__device__ __forceinline__ int block_groups(const RelParams& p, const Seq& s, const Block& b) {
-    if (b.i0 >= s.lq) return 0;
-    int end = s.lk;
-    if (p.causal) end = min(end, min(b.i0 + 16, s.lq) + s.lk - s.lq);
-    return min(4, max(0, (end - b.j0 + 15) >> 4));
+
+// Whether some query of the block sees its first key.
+__device__ __forceinline__ bool block_live(const RelParams& p, const Seq& s, const Block& b) {
+    return b.i0 < s.lq && b.j0 < keys_seen(p, s, min(b.i0 + 16, s.lq));
 }
 
 __device__ __forceinline__ float quad_max(float x) {
@@ -196,30 +188,27 @@ __device__ __forceinline__ float quad_sum(float x) {
     return x + __shfl_xor_sync(0xFFFFFFFFu, x, 2);
 }
 
-// ---- softmax and gradient steps of a block, for its first n16 groups of 16 keys
+// ---- softmax and gradient steps of a block
 
 // Running maximum and sum of rows g and g + 8, t -> 2^(t - m), earlier output rescaled.
-template <int DT>
-__device__ __forceinline__ void block_softmax(float (&t)[8][4], int n16, float (&m)[2], float (&l)[2], float (&o)[DT / 8][4]) {
+template <int DT, int NT>
+__device__ __forceinline__ void block_softmax(float (&t)[NT][4], float (&m)[2], float (&l)[2], float (&o)[DT / 8][4]) {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         float top = m[r];
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
-            if (n / 2 < n16) top = fmaxf(top, fmaxf(t[n][2 * r], t[n][2 * r + 1]));
+        for (int n = 0; n < NT; ++n) top = fmaxf(top, fmaxf(t[n][2 * r], t[n][2 * r + 1]));
         top = quad_max(top);
         const float ref = top == -INFINITY ? 0.0f : top, corr = ex2_approx(m[r] - ref);
         float sum = 0.0f;
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            if (n / 2 >= n16) continue;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const float e = ex2_approx(t[n][2 * r + c] - ref);
                 sum += e;
                 t[n][2 * r + c] = e;
             }
-        }
         l[r] = fmaf(l[r], corr, sum);                      // this lane's part of the row
         m[r] = top;
 #pragma unroll
@@ -229,20 +218,20 @@ __device__ __forceinline__ void block_softmax(float (&t)[8][4], int n16, float (
         }
     }
 }
-// o += x . tile rows [n0, n0 + 64).  x (probabilities of at most 1, or score gradients) is rounded to bf16 as the left operand: 2^-9 of each
+// o += x . tile rows [n0, n0 + 8 NT).  x (probabilities of at most 1, or score gradients) is rounded to bf16 as the left operand: 2^-9 of each
 // term of a result that is bf16 itself.
-template <int DT>
-__device__ __forceinline__ void block_times(const RelParams& p, const float (&x)[8][4], uint32_t tile, int n0, int n16, int lane, float (&o)[DT / 8][4]) {
+template <int DT, int NT>
+__device__ __forceinline__ void block_times(const RelParams& p, const float (&x)[NT][4], uint32_t tile, int n0, int lane, float (&o)[DT / 8][4]) {
+    const uint32_t at = frag_rows<pitch_of(DT)>(tile, n0, 0, lane);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (k >= n16) continue;
+    for (int k = 0; k < NT / 2; ++k) {
         const uint32_t a[4] = {pack_bf16(x[2 * k][0], x[2 * k][1]), pack_bf16(x[2 * k][2], x[2 * k][3]), pack_bf16(x[2 * k + 1][0], x[2 * k + 1][1]),
                                pack_bf16(x[2 * k + 1][2], x[2 * k + 1][3])};
 #pragma unroll
         for (int j = 0; j < DT / 16; ++j) {
             if (DT > 64 && j * 16 >= p.dim) continue;
             uint32_t v[4];
-            ldsm4t(v, frag_rows<pitch_of(DT)>(tile, n0 + k * 16, j * 16, lane));
+            ldsm4t(v, at + (uint32_t)(k * 16 * pitch_of(DT) + j * 16) * 2u);
             mma16816(o[2 * j], a, v[0], v[1]);
             mma16816(o[2 * j + 1], a, v[2], v[3]);
         }
@@ -254,60 +243,70 @@ struct RowStats {
     float m[2], rl[2], D[2];
 };
 // this lane's maximum of row r
-__device__ __forceinline__ float block_max(const float (&t)[8][4], int n16, int r, float top) {
+template <int NT>
+__device__ __forceinline__ float block_max(const float (&t)[NT][4], int r, float top) {
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
-        if (n / 2 < n16) top = fmaxf(top, fmaxf(t[n][2 * r], t[n][2 * r + 1]));
+    for (int n = 0; n < NT; ++n) top = fmaxf(top, fmaxf(t[n][2 * r], t[n][2 * r + 1]));
     return top;
 }
 // t -> e = 2^(t - ref); adds this lane's sums
-__device__ __forceinline__ void block_exp(int n16, const float (&ref)[2], float (&t)[8][4], float (&sum)[2]) {
+template <int NT>
+__device__ __forceinline__ void block_exp(const float (&ref)[2], float (&t)[NT][4], float (&sum)[2]) {
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-        if (n / 2 >= n16) continue;
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             t[n][e] = ex2_approx(t[n][e] - ref[e >> 1]);
             sum[e >> 1] += t[n][e];
         }
-    }
 }
 // dp of dropped probabilities is 0, of kept ones scaled; the sign of e (which is not negative) remembers which were dropped.
-__device__ __forceinline__ void block_drop(const RelParams& p, const Seq& s, uint2 key, int h, const Block& b, int n16, int lane, float (&t)[8][4], float (&dp)[8][4]) {
+template <int NT>
+__device__ __forceinline__ void block_drop(const RelParams& p, const Seq& s, uint2 key, int h, const Block& b, int lane, float (&t)[NT][4], float (&dp)[NT][4]) {
     if (!p.drop.thr) return;
-    block_drops(p, s, key, h, b, n16, lane, [&](int n, int e, bool d) {
+    block_drops<NT>(p, s, key, h, b, lane, [&](int n, int e, bool d) {
         dp[n][e] = d ? 0.0f : __fmul_rn(dp[n][e], p.drop.scale);
         t[n][e] = d ? -t[n][e] : t[n][e];
     });
 }
 // this lane's sums of e dp
-__device__ __forceinline__ void block_dsum(int n16, const float (&t)[8][4], const float (&dp)[8][4], float (&dsum)[2]) {
+template <int NT>
+__device__ __forceinline__ void block_dsum(const float (&t)[NT][4], const float (&dp)[NT][4], float (&dsum)[2]) {
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-        if (n / 2 >= n16) continue;
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) dsum[e >> 1] = fmaf(fabsf(t[n][e]), dp[n][e], dsum[e >> 1]);
-    }
 }
 // e (signed) -> p, dropped and scaled, in t;  dp -> ds = p (dp - D).  rl includes whatever turns e into p.
-__device__ __forceinline__ void block_ds(const RelParams& p, const RowStats& st, int n16, float (&t)[8][4], float (&dp)[8][4]) {
+template <int NT>
+__device__ __forceinline__ void block_ds(const RelParams& p, const RowStats& st, float (&t)[NT][4], float (&dp)[NT][4]) {
     const float f[2] = {st.rl[0] * p.drop.scale, st.rl[1] * p.drop.scale};
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-        if (n / 2 >= n16) continue;
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int r = e >> 1;
             dp[n][e] = fabsf(t[n][e]) * st.rl[r] * (dp[n][e] - st.D[r]);
             t[n][e] = fmaxf(t[n][e], 0.0f) * f[r];
         }
-    }
 }
-__device__ __forceinline__ float block_total(const float (&ds)[8][4]) {
+template <int NT>
+__device__ __forceinline__ float block_total(const float (&ds)[NT][4]) {
     float a = 0.0f;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) a += (ds[n][0] + ds[n][1]) + (ds[n][2] + ds[n][3]);
+    for (int n = 0; n < NT; ++n) a += (ds[n][0] + ds[n][1]) + (ds[n][2] + ds[n][3]);
     return a;
+}
+// t and dp (p and ds by now) as bf16 into rows g and g + 8 of two tiles, at this lane's columns
+template <int NT>
+__device__ __forceinline__ void store_scores(uint16_t* prow, uint16_t* srow, int pitch, const float (&t)[NT][4], const float (&dp)[NT][4]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        *reinterpret_cast<uint32_t*>(prow + 8 * n) = pack_bf16(t[n][0], t[n][1]);
+        *reinterpret_cast<uint32_t*>(prow + 8 * pitch + 8 * n) = pack_bf16(t[n][2], t[n][3]);
+        *reinterpret_cast<uint32_t*>(srow + 8 * n) = pack_bf16(dp[n][0], dp[n][1]);
+        *reinterpret_cast<uint32_t*>(srow + 8 * pitch + 8 * n) = pack_bf16(dp[n][2], dp[n][3]);
+    }
 }
 
 // ---- diagonal sums.  A lane's elements of one 16 x 64 block are first added along the diagonal inside the lane (row g + 8 of key tile
@@ -338,13 +337,14 @@ __device__ __forceinline__ float diagonal_sum(const float* stage, int col) {
 
 // The same 18 values of a lane, added up over blocks that lie at the same distances: acc[u + 1][lane] of 9 x 32 pairs, this lane's own.
 constexpr int kDiagAccFloats = 9 * 64;
-__device__ __forceinline__ void add_diagonals(float* acc, const float (&ds)[8][4], int lane) {
+template <int NT>
+__device__ __forceinline__ void add_diagonals(float* acc, const float (&ds)[NT][4], int lane) {
     float2* mine = reinterpret_cast<float2*>(acc) + lane;
 #pragma unroll
-    for (int u = -1; u < 8; ++u) {
+    for (int u = -1; u < NT; ++u) {
         float2 x = mine[(u + 1) * 32];
-        x.x += (u >= 0 ? ds[u < 0 ? 0 : u][0] : 0.0f) + (u < 7 ? ds[u < 7 ? u + 1 : 7][2] : 0.0f);
-        x.y += (u >= 0 ? ds[u < 0 ? 0 : u][1] : 0.0f) + (u < 7 ? ds[u < 7 ? u + 1 : 7][3] : 0.0f);
+        x.x += (u >= 0 ? ds[u < 0 ? 0 : u][0] : 0.0f) + (u < NT - 1 ? ds[u < NT - 1 ? u + 1 : NT - 1][2] : 0.0f);
+        x.y += (u >= 0 ? ds[u < 0 ? 0 : u][1] : 0.0f) + (u < NT - 1 ? ds[u < NT - 1 ? u + 1 : NT - 1][3] : 0.0f);
         mine[(u + 1) * 32] = x;
     }
 }

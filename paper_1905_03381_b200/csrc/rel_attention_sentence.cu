@@ -77,9 +77,9 @@ __global__ void __launch_bounds__(128, DT == 128 ? 2 : 4) sentence_forward_kerne
     Item it = walk.next();
     if (!it.live) return;
     const auto load = [&](const Item& x) {
-        load_tile_async<LT, DT, THREADS>(p, p.q, h, x.s.q0, x.s.lq, tiles);
-        load_tile_async<LT, DT, THREADS>(p, p.k, hk, x.s.k0, x.s.lk, tiles + TILE);
-        load_tile_async<LT, DT, THREADS>(p, p.v, hk, x.s.k0, x.s.lk, tiles + 2 * TILE);
+        load_tile_async<LT, DT, THREADS, 16>(p, p.q, h, x.s.q0, x.s.lq, tiles);
+        load_tile_async<LT, DT, THREADS, 32>(p, p.k, hk, x.s.k0, x.s.lk, tiles + TILE);
+        load_tile_async<LT, DT, THREADS, 32>(p, p.v, hk, x.s.k0, x.s.lk, tiles + 2 * TILE);
         cp_async_commit();
     };
     load(it);
@@ -100,21 +100,18 @@ __global__ void __launch_bounds__(128, DT == 128 ? 2 : 4) sentence_forward_kerne
             for (int j = 0; j < DT / 8; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
+            uint32_t qf[DT / 16][4];
+            load_frags<DT>(p, qf, qS, i0, lane);
+            const int end = keys_seen(p, s, min(i0 + 16, s.lq));
 #pragma unroll 1
-            for (int j0 = 0; j0 < LT; j0 += 64) {
+            for (int j0 = 0; j0 < end; j0 += 32) {
                 const Block b = {i0, j0};
-                const int n16 = block_groups(p, s, b);
-                if (n16 == 0) break;
-                float t[8][4];
-                {
-                    uint32_t qf[DT / 16][4];
-                    load_frags<DT>(p, qf, qS, i0, lane);
-                    block_dot<DT>(p, qf, kS, j0, n16, lane, t);
-                }
-                block_scores(p, s, bias, b, n16, lane, t);
-                block_softmax<DT>(t, n16, m, l, o);
-                if (p.drop.thr) block_drops(p, s, it.key, h, b, n16, lane, [&](int n, int e, bool d) { t[n][e] = d ? 0.0f : t[n][e]; });
-                block_times<DT>(p, t, vS, j0, n16, lane, o);
+                float t[4][4];
+                block_dot<DT, 4>(p, qf, kS, j0, lane, t);
+                block_scores(p, s, bias, b, lane, t);
+                block_softmax<DT, 4>(t, m, l, o);
+                if (p.drop.thr) block_drops<4>(p, s, it.key, h, b, lane, [&](int n, int e, bool d) { t[n][e] = d ? 0.0f : t[n][e]; });
+                block_times<DT, 4>(p, t, vS, j0, lane, o);
             }
             float f[2];
 #pragma unroll
@@ -147,6 +144,85 @@ struct BackGeo {
     }
 };
 
+// A half of a strip that sees no key: what it adds to the row statistics.
+template <int LT>
+__device__ __forceinline__ void join_nothing(const Block b, int lane, float* stat) {
+    if (LT == 64) return;
+    float* mine = stat + (b.j0 / 64 * LT + b.i0 + (lane >> 2)) * 3;
+    if ((lane & 3) == 0)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            mine[24 * r] = -INFINITY;
+            mine[24 * r + 1] = mine[24 * r + 2] = 0.0f;
+        }
+    asm volatile("bar.sync %0, 64;" ::"r"(1 + (b.i0 >> 4)) : "memory");
+}
+
+// p and dS of a warp's block, from scores to shared memory, with the strip's row statistics.
+template <int DT, int LT, int NT>
+__device__ __forceinline__ void strip_scores(const RelParams& p, const Seq& s, uint2 key, int h, const Block b, int lane, uint32_t qS, uint32_t kS, uint32_t oS, uint32_t vS,
+                                             const float* bias, float* stat, uint16_t* PS, float* dacc) {
+    constexpr int HALVES = LT / 64, PP = BackGeo<DT, LT>::PP;
+    float t[NT][4], dp[NT][4];
+    RowStats st;
+    float m[2], l[2] = {0.0f, 0.0f}, D[2] = {0.0f, 0.0f};
+    {
+        uint32_t f[DT / 16][4];
+        load_frags<DT>(p, f, qS, b.i0, lane);
+        block_dot<DT, NT>(p, f, kS, b.j0, lane, t);
+    }
+    block_scores(p, s, bias, b, lane, t);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        m[r] = quad_max(block_max(t, r, -INFINITY));
+        st.m[r] = m[r] == -INFINITY ? 0.0f : m[r];
+    }
+    block_exp(st.m, t, l);
+    {
+        uint32_t f[DT / 16][4];
+        load_frags<DT>(p, f, oS, b.i0, lane);
+        block_dot<DT, NT>(p, f, vS, b.j0, lane, dp);
+    }
+    block_drop(p, s, key, h, b, lane, t, dp);
+    block_dsum(t, dp, D);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        l[r] = quad_sum(l[r]);
+        D[r] = quad_sum(D[r]);
+    }
+    float own[2] = {1.0f, 1.0f};
+    if (HALVES > 1) {                                                      // join with the strip's other keys
+        const int half = b.j0 / 64;
+        float* mine = stat + (half * LT + b.i0 + (lane >> 2)) * 3;
+        const float* other = stat + ((half ^ 1) * LT + b.i0 + (lane >> 2)) * 3;
+        if ((lane & 3) == 0)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                mine[24 * r] = m[r];
+                mine[24 * r + 1] = l[r];
+                mine[24 * r + 2] = D[r];
+            }
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + (b.i0 >> 4)) : "memory");
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const float mo = other[24 * r], top = fmaxf(m[r], mo), ref = top == -INFINITY ? 0.0f : top, fo = ex2_approx(mo - ref);
+            own[r] = ex2_approx(m[r] - ref);
+            l[r] = l[r] * own[r] + other[24 * r + 1] * fo;
+            D[r] = D[r] * own[r] + other[24 * r + 2] * fo;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const float rl = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+        st.D[r] = D[r] * rl;
+        st.rl[r] = rl * own[r];
+    }
+    block_ds(p, st, t, dp);
+    if (dacc) add_diagonals(dacc, dp, lane);
+    uint16_t* row = PS + (b.i0 + (lane >> 2)) * PP + b.j0 + 2 * (lane & 3);
+    store_scores(row, row + LT, PP, t, dp);
+}
+
 // A strip's rows belong to HALVES warps, one per 64 keys, which join their row statistics.  SHARED: several query heads per key head.
 // Dropping LT = 64 to four warps keeps three CTAs on an SM; LT = 128 fills it with 16 warps and fetches the next sentence's K and Q meanwhile,
 // its V as soon as this one's is used up, its dO last.
@@ -172,7 +248,7 @@ __global__ void __launch_bounds__(LT * 2 * (LT / 64), LT == 64 && DT <= 64 ? (SH
     Walk<LT> walk(p, lo);
     Item it = walk.next();
     int slot = 0;                                                          // 0 or 4: where this sentence's K and Q are
-    const auto load = [&](const TokArg& t, int head, int64_t row0, int n, int at) { load_tile_async<LT, DT, THREADS>(p, t, head, row0, n, tiles + at * TILE); };
+    const auto load = [&](const TokArg& t, int head, int64_t row0, int n, int at) { load_tile_async<LT, DT, THREADS, 32>(p, t, head, row0, n, tiles + at * TILE); };
     if (it.live) {
         load(p.k, hk, it.s.k0, it.s.lk, 0);
         load(p.q, h0, it.s.q0, it.s.lq, 1);
@@ -244,73 +320,9 @@ __global__ void __launch_bounds__(LT * 2 * (LT / 64), LT == 64 && DT <= 64 ? (SH
             __syncthreads();
             const int end = i0 < s.lq ? keys_seen(p, s, min(i0 + 16, s.lq)) : 0;      // keys this strip sees
             if (i0 < s.lq) {
-                const Block b = {i0, j0};
-                const int n16 = min(4, max(0, (end - j0 + 15) >> 4));
-                float t[8][4], dp[8][4];
-                RowStats st;
-                float m[2], l[2] = {0.0f, 0.0f}, D[2] = {0.0f, 0.0f};
-                {
-                    uint32_t f[DT / 16][4];
-                    load_frags<DT>(p, f, qS, i0, lane);
-                    block_dot<DT>(p, f, kS, j0, n16, lane, t);
-                }
-                block_scores(p, s, bias + a * bias_len, b, n16, lane, t);
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    m[r] = quad_max(block_max(t, n16, r, -INFINITY));
-                    st.m[r] = m[r] == -INFINITY ? 0.0f : m[r];
-                }
-                block_exp(n16, st.m, t, l);
-                {
-                    uint32_t f[DT / 16][4];
-                    load_frags<DT>(p, f, oS, i0, lane);
-                    block_dot<DT>(p, f, vS, j0, n16, lane, dp);
-                }
-                block_drop(p, s, it.key, h, b, n16, lane, t, dp);
-                block_dsum(n16, t, dp, D);
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    l[r] = quad_sum(l[r]);
-                    D[r] = quad_sum(D[r]);
-                }
-                float own[2] = {1.0f, 1.0f};
-                if (HALVES > 1) {                                          // join with the strip's other keys
-                    float* mine = stat + (half * LT + i0 + (lane >> 2)) * 3;
-                    const float* other = stat + ((half ^ 1) * LT + i0 + (lane >> 2)) * 3;
-                    if ((lane & 3) == 0)
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            mine[24 * r] = m[r];
-                            mine[24 * r + 1] = l[r];
-                            mine[24 * r + 2] = D[r];
-                        }
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + strip) : "memory");
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float mo = other[24 * r], top = fmaxf(m[r], mo), ref = top == -INFINITY ? 0.0f : top, fo = ex2_approx(mo - ref);
-                        own[r] = ex2_approx(m[r] - ref);
-                        l[r] = l[r] * own[r] + other[24 * r + 1] * fo;
-                        D[r] = D[r] * own[r] + other[24 * r + 2] * fo;
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float rl = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
-                    st.D[r] = D[r] * rl;
-                    st.rl[r] = rl * own[r];
-                }
-                block_ds(p, st, n16, t, dp);
-                if (want_table && n16 > 0) add_diagonals(dacc + (a * WARPS + warp) * kDiagAccFloats, dp, lane);
-                uint16_t* row = PS + (i0 + (lane >> 2)) * PP + j0 + 2 * (lane & 3);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (j / 2 >= n16) continue;
-                    uint16_t* at = row + 8 * j;
-                    *reinterpret_cast<uint32_t*>(at) = pack_bf16(t[j][0], t[j][1]);
-                    *reinterpret_cast<uint32_t*>(at + 8 * PP) = pack_bf16(t[j][2], t[j][3]);
-                    *reinterpret_cast<uint32_t*>(at + LT) = pack_bf16(dp[j][0], dp[j][1]);
-                    *reinterpret_cast<uint32_t*>(at + 8 * PP + LT) = pack_bf16(dp[j][2], dp[j][3]);
-                }
+                if (end <= j0) join_nothing<LT>(Block{i0, j0}, lane, stat);
+                else if (end - j0 > 32) strip_scores<DT, LT, 8>(p, s, it.key, h, Block{i0, j0}, lane, qS, kS, oS, vS, bias + a * bias_len, stat, PS, want_table ? dacc + (a * WARPS + warp) * kDiagAccFloats : nullptr);
+                else strip_scores<DT, LT, 4>(p, s, it.key, h, Block{i0, j0}, lane, qS, kS, oS, vS, bias + a * bias_len, stat, PS, want_table ? dacc + (a * WARPS + warp) * kDiagAccFloats : nullptr);
             }
             __syncthreads();
             if (AHEAD && nx.live) load(p.v, hk, nx.s.k0, nx.s.lk, 2);
