@@ -51,6 +51,9 @@ aa_status launch_rel_attention_grad_plain(aa_ctx_impl* c, const RelParams& p, in
 // bf16 kernels on the tensor cores: aligned tokens, head width a multiple of 8 up to 128.
 bool rel_mma_fits(const RelParams& p);
 aa_status launch_rel_attention_mma(aa_ctx_impl* c, const RelParams& p);
+// ... a few new tokens over long contexts
+bool rel_decode_fits(const RelParams& p);
+aa_status launch_rel_decode(aa_ctx_impl* c, const RelParams& p);
 // ... of them the sequences of at most *covered tokens on both sides (set by the call; -1: none)
 aa_status launch_rel_sentences(aa_ctx_impl* c, const RelParams& p, int* covered);
 aa_status launch_rel_sentences_grad(aa_ctx_impl* c, const RelParams& p, int* covered, int* n_parts);

@@ -91,6 +91,7 @@ bool rel_mma_fits(const RelParams& p) {
 }
 
 aa_status launch_rel_attention_mma(aa_ctx_impl* c, const RelParams& p) {
+    if (rel_decode_fits(p)) return launch_rel_decode(c, p);
     int covered = -1;
     const aa_status st = launch_rel_sentences(c, p, &covered);
     if (st != AA_OK || (p.max_q <= covered && p.max_k <= covered)) return st;
