@@ -163,20 +163,17 @@ struct RowPart {
         eh = rank < sp.head ? load1(row + rank) : -INFINITY;
         et = sp.tail0 + rank < cols ? load1(row + sp.tail0 + rank) : -INFINITY;
     }
-    // vectors v0 + rank + k n < v0 + nv of `body` (memory or shared)
+    // vectors rank + k n < nv of `body` (memory or shared); what is missing reads as -inf
     __device__ __forceinline__ void load_body(const T* body, int nv, int rank, int n) {
+        constexpr uint32_t kNegInf = VE == 8 ? 0xFF80FF80u : 0xFF800000u;
+        uint4 w[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            if (rank + k * n < nv) {
-                float x[VE];
-                Vec<T>::unpack(*reinterpret_cast<const uint4*>(body + (int64_t)(rank + k * n) * VE), x);
-#pragma unroll
-                for (int i = 0; i < VE; ++i) e[k][i] = x[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < VE; ++i) e[k][i] = -INFINITY;
-            }
+            w[k] = make_uint4(kNegInf, kNegInf, kNegInf, kNegInf);
+            if (rank + k * n < nv) w[k] = *reinterpret_cast<const uint4*>(body + (int64_t)(rank + k * n) * VE);
         }
+#pragma unroll
+        for (int k = 0; k < V; ++k) Vec<T>::unpack(w[k], e[k]);
     }
     __device__ __forceinline__ void exponentials() {
         m = fmaxf(eh, et);
@@ -205,8 +202,9 @@ struct RowPart {
         if (rank < sp.head) store1(out + rank, fmaf(eh, f, rank == y ? -g : 0.0f));
         if (sp.tail0 + rank < cols) store1(out + sp.tail0 + rank, fmaf(et, f, sp.tail0 + rank == y ? -g : 0.0f));
     }
-    // at_y: element of `body` that is the label's (negative: none here)
-    __device__ __forceinline__ void store_body(T* body, int nv, int rank, int n, float f, float g, int at_y) {
+    // at_y: element of `body` that is the label's (negative: none here), fy: its gradient.  The thread that owns it writes it again: an index into
+    // the exponentials would put them into local memory.
+    __device__ __forceinline__ void store_body(T* body, int nv, int rank, int n, float f, int at_y, float fy) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const int v = rank + k * n;
@@ -214,16 +212,15 @@ struct RowPart {
             float x[VE];
 #pragma unroll
             for (int i = 0; i < VE; ++i) x[i] = e[k][i] * f;
-            if (at_y >= 0 && at_y / VE == v) {
-#pragma unroll
-                for (int i = 0; i < VE; ++i)
-                    if (at_y % VE == i) x[i] -= g;
-            }
             if constexpr (VE == 8) store8(body + (int64_t)v * VE, x);
             else *reinterpret_cast<float4*>(body + (int64_t)v * VE) = make_float4(x[0], x[1], x[2], x[3]);
         }
+        if (at_y >= 0 && (at_y / VE) % n == rank) store1(body + at_y, fy);
     }
 };
+
+// Gradient of the label's logit.
+__device__ __forceinline__ float label_grad(const NatState& all, float label_logit, float g) { return fmaf(exp_from(label_logit, all.m), g / all.s, -g); }
 
 // LPR lanes per row (LPR * V vectors at least; at least 16 / sizeof(T) - 1 lanes for the ends).
 template <typename T, int LPR, int V>
@@ -254,7 +251,7 @@ __global__ void __launch_bounds__(256) row_grad_lanes_kernel(GradParams p) {
             if (y >= 0) {
                 const float f = part.factor(all, g);
                 part.store_ends(out, sp, cols, gl, f, g, y);
-                part.store_body(out + sp.head, sp.nvec, gl, LPR, f, g, y >= sp.head && y < sp.tail0 ? y - sp.head : -1);
+                part.store_body(out + sp.head, sp.nvec, gl, LPR, f, y >= sp.head && y < sp.tail0 ? y - sp.head : -1, label_grad(all, label_logit, g));
             } else {
                 zero_row<T>(out, cols, gl, LPR);
             }
@@ -293,7 +290,7 @@ __global__ void __launch_bounds__(128) row_grad_block_kernel(GradParams p) {
             const NatState all = merge(merge(warp_state[turn][0], warp_state[turn][1]), merge(warp_state[turn][2], warp_state[turn][3]));
             const float f = part.factor(all, g);
             part.store_ends(out, sp, cols, threadIdx.x, f, g, y);
-            part.store_body(out + sp.head, sp.nvec, threadIdx.x, 128, f, g, y >= sp.head && y < sp.tail0 ? y - sp.head : -1);
+            part.store_body(out + sp.head, sp.nvec, threadIdx.x, 128, f, y >= sp.head && y < sp.tail0 ? y - sp.head : -1, label_grad(all, label_logit, g));
             if (p.loss.out && threadIdx.x == 0) p.loss.out[r] = row_loss(all, label_logit);
         } else {
             zero_row<T>(out, cols, threadIdx.x, 128);
@@ -304,8 +301,9 @@ __global__ void __launch_bounds__(128) row_grad_block_kernel(GradParams p) {
 
 // --------------------------------------------------------------------------------------------- ring of long rows
 
-constexpr int kRingThreads = 512;          // consumers; a producer warp comes on top
-constexpr int kRingVecs = 8;               // vectors per consumer: slices of up to 64 KB
+constexpr int kRingThreads = 480;          // consumers; with the producer warp 16 warps, 128 registers a thread
+constexpr int kRingVecs = 9;               // vectors per consumer: slices of up to 67.5 KB
+constexpr int kRingSliceVecs = 4096;       // ... of which 64 KB are used: three stages
 constexpr int kRingMaxStages = 6;
 constexpr int kMaxCluster = 8;
 
@@ -319,7 +317,7 @@ struct RingRow {
 struct RingControl {
     uint64_t full[kRingMaxStages], empty[kRingMaxStages], joined[2];
     RingRow meta[kRingMaxStages];
-    NatState warp_state[2][16];
+    NatState warp_state[2][kRingThreads / 32];
     NatState peer[2][kMaxCluster];
     int abort_flag;
 };
@@ -400,41 +398,51 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
             if (bad) latch(p.loss.ctl, AA_ERR_BAD_INDEX);
         }
         int64_t j = 0;
-        bool ok = true;
-        for (int64_t r = first;; r += step) {
-            const bool more = r < p.loss.rows;
-            float g = 0.0f;
-            if (more && !row_factor(p, n_inst, r, g)) continue;
-            const int y = more ? checked_label(p.loss, r) : -1;
-            const T* row = static_cast<const T*>(p.loss.logits) + (more ? r : 0) * p.loss.row_stride;
-            const RowSpan<T> sp(row, cols);
-            const float label_logit = y >= 0 ? load1(row + y) : 0.0f;
-            float end = 0.0f;              // lanes 0..7: head, 8..15: tail
-            if (y >= 0 && lane < sp.head) end = load1(row + lane);
-            if (y >= 0 && lane >= 8 && lane < 16 && sp.tail0 + lane - 8 < cols) end = load1(row + sp.tail0 + lane - 8);
-            const int stage = (int)(j % stages);
-            if (j >= stages && !mbar_wait(&ctl.empty[stage], (uint32_t)((j / stages - 1) & 1), abort_flag)) {
-                ok = false;
-                break;
+        bool ok = true, more = true;
+        for (int64_t r0 = first; ok && more; r0 += 32 * step) {
+            // a lane per row: 32 rows' searches, labels and label logits cost one chain of loads
+            const int64_t mine = r0 + lane * step;
+            float my_g = 0.0f, my_logit = 0.0f;
+            int my_y = -2;                 // not counted
+            if (mine < p.loss.rows && row_factor(p, n_inst, mine, my_g)) {
+                my_y = checked_label(p.loss, mine);
+                if (my_y >= 0) my_logit = load1(static_cast<const T*>(p.loss.logits) + mine * p.loss.row_stride + my_y);
             }
-            RingRow* meta = &ctl.meta[stage];
-            if (lane < 16) meta->ends[lane] = end;
-            __syncwarp();
-            if (lane == 0) {
-                meta->row = more ? r : -1;
-                meta->g = g;
-                meta->y = y;
-                meta->label_logit = label_logit;
-                const int per = (sp.nvec + C - 1) / C, nv = max(0, min(per, sp.nvec - rank * per));
-                if (y >= 0 && nv > 0) {
-                    mbar_arrive_expect_tx(&ctl.full[stage], (uint32_t)nv * 16u);
-                    bulk_g2s(ring + (size_t)stage * stage_bytes, row + sp.head + (int64_t)rank * per * VE, (uint32_t)nv * 16u, &ctl.full[stage]);
-                } else {
+            for (int i = 0; i < 32; ++i) {
+                const int64_t r = r0 + i * step;
+                more = r < p.loss.rows;
+                const int y = __shfl_sync(0xFFFFFFFFu, my_y, i);
+                const float g = __shfl_sync(0xFFFFFFFFu, my_g, i), label_logit = __shfl_sync(0xFFFFFFFFu, my_logit, i);
+                if (more && y == -2) continue;
+                const int stage = (int)(j % stages);
+                if (j >= stages && !mbar_wait(&ctl.empty[stage], (uint32_t)((j / stages - 1) & 1), abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                const T* row = static_cast<const T*>(p.loss.logits) + (more ? r : 0) * p.loss.row_stride;
+                const RowSpan<T> sp(row, cols);
+                const int per = (sp.nvec + C - 1) / C, nv = more && y >= 0 ? max(0, min(per, sp.nvec - rank * per)) : 0;
+                // one copy per lane: many in flight at once (the barrier's phase cannot complete before lane 0's arrival below)
+                const int piece = (nv + 31) >> 5, v0 = lane * piece, n = min(piece, nv - v0);
+                if (lane == 0) mbar_expect_tx(&ctl.full[stage], (uint32_t)nv * 16u);
+                __syncwarp();
+                if (n > 0) bulk_g2s(ring + (size_t)stage * stage_bytes + v0 * 16, row + sp.head + ((int64_t)rank * per + v0) * VE, (uint32_t)n * 16u, &ctl.full[stage]);
+                float end = 0.0f;          // lanes 0..7: head, 8..15: tail
+                if (more && y >= 0 && lane < sp.head) end = load1(row + lane);
+                if (more && y >= 0 && lane >= 8 && lane < 16 && sp.tail0 + lane - 8 < cols) end = load1(row + sp.tail0 + lane - 8);
+                RingRow* meta = &ctl.meta[stage];
+                if (lane < 16) meta->ends[lane] = end;
+                __syncwarp();
+                if (lane == 0) {
+                    meta->row = more ? r : -1;
+                    meta->g = g;
+                    meta->y = y;
+                    meta->label_logit = label_logit;
                     mbar_arrive(&ctl.full[stage]);
                 }
+                ++j;
+                if (!more) break;
             }
-            ++j;
-            if (!more) break;
         }
         if (!ok) {                         // the copies in flight still write to this CTA's memory
             ctl.abort_flag = 1;
@@ -479,7 +487,7 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
             if (r < 0) break;              // every consumer has seen the same hand-over
             float f = 0.0f;
             if (y >= 0) {
-                NatState all = group_merge_nat<16>(ctl.warp_state[turn][lane & 15]);
+                NatState all = group_merge_nat<16>((lane & 15) < kRingThreads / 32 ? ctl.warp_state[turn][lane & 15] : NatState{-INFINITY, 0.0f});
                 if (C > 1) {
                     const int slot = (int)(joins & 1);
                     if (tid < C) send_state(&ctl.peer[slot][rank], &ctl.joined[slot], tid, all);
@@ -490,7 +498,7 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
                 }
                 f = part.factor(all, g);
                 const int at = y - sp.head - rank * per * VE;
-                part.store_body(body, nv, tid, kRingThreads, f, g, y >= sp.head && y < sp.tail0 && at >= 0 && at < nv * VE ? at : -1);
+                part.store_body(body, nv, tid, kRingThreads, f, y >= sp.head && y < sp.tail0 && at >= 0 && at < nv * VE ? at : -1, label_grad(all, label_logit, g));
                 if (p.loss.out && rank == 0 && tid == 0) p.loss.out[r] = row_loss(all, label_logit);
             } else {
                 for (int v = tid; v < nv; v += kRingThreads) reinterpret_cast<uint4*>(body)[v] = make_uint4(0, 0, 0, 0);
@@ -503,19 +511,21 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
                 ok = false;
                 break;
             }
-            if (tid == 0) {
-                if (nv > 0) bulk_s2g(out + sp.head + (int64_t)rank * per * VE, body, (uint32_t)nv * 16u);
+            if (warp == 0) {
+                const int piece = (nv + 31) >> 5, v0 = lane * piece, n = min(piece, nv - v0);
+                if (n > 0) bulk_s2g(out + sp.head + ((int64_t)rank * per + v0) * VE, body + (int64_t)v0 * VE, (uint32_t)n * 16u);
                 else asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                // the previous row's copy has been read out of its stage once only this one is pending
+                // the previous row's copies have been read out of their stage once only these are pending
                 bulk_wait_read<1>();
-                if (j > 0) mbar_arrive(&ctl.empty[(j - 1) % stages]);
+                __syncwarp();
+                if (lane == 0 && j > 0) mbar_arrive(&ctl.empty[(j - 1) % stages]);
             }
         }
         if (!ok) {
             ctl.abort_flag = 1;
             if (tid == 0) latch(p.loss.ctl, AA_ERR_SCAN_TIMEOUT);
         }
-        if (tid == 0) bulk_wait_read<0>();
+        if (warp == 0) bulk_wait_read<0>();
     }
     __syncthreads();
     cluster_sync();                        // peers may still send here until they are done
@@ -652,9 +662,9 @@ aa_status launch_rows(aa_ctx_impl* c, GradParams& p) {
         kernel = (const void*)row_grad_block_kernel<T, 8>;
         want = p.loss.rows;
         threads = 128;
-    } else if (alike && vecs <= (int64_t)kRingThreads * kRingVecs * kMaxCluster) {
+    } else if (alike && vecs <= (int64_t)kRingSliceVecs * kMaxCluster) {
         int C = 1;
-        while ((vecs + C - 1) / C > kRingThreads * kRingVecs) C *= 2;
+        while ((vecs + C - 1) / C > kRingSliceVecs) C *= 2;
         return launch_ring<T>(c, p, C);
     } else if (row_bytes > 8 * 1024) {
         kernel = (const void*)row_grad_cta_kernel<T>;
