@@ -82,19 +82,6 @@ int resident_ctas(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_sm
     return ctas;
 }
 
-int resident_clusters(aa_ctx_impl* c, const void* kernel, const cudaLaunchConfig_t* cfg, int size) {
-    aa_ctx* ctx = reinterpret_cast<aa_ctx*>(c);
-    const int shape = -((int)cfg->blockDim.x * 16 + size);        // negative: not a thread count of resident_ctas
-    for (int i = 0; i < ctx->occ_used; ++i) {
-        const OccEntry& e = ctx->occ[i];
-        if (e.kernel == kernel && e.threads == shape && e.smem == cfg->dynamicSmemBytes) return e.ctas;
-    }
-    int clusters = 0;
-    if (cudaOccupancyMaxActiveClusters(&clusters, kernel, cfg) != cudaSuccess || clusters < 1) return -1;
-    if (ctx->occ_used < kOccSlots) ctx->occ[ctx->occ_used++] = OccEntry{kernel, shape, cfg->dynamicSmemBytes, clusters};
-    return clusters;
-}
-
 cudaError_t launch_overlapped(aa_ctx_impl* c, const void* kernel, dim3 grid, dim3 block, void** args, size_t smem, bool cooperative) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;

@@ -297,9 +297,6 @@ aa_status launch_conv_pool_features(aa_ctx_impl* c, const void* x, int dtype, in
 // Persistent-grid size for a kernel: CTAs that fit on the device at once.
 int resident_ctas(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_smem);
 
-// The same for a launch in clusters of `size` CTAs (cfg: its block, shared memory and cluster attribute): clusters that fit at once.
-int resident_clusters(aa_ctx_impl* c, const void* kernel, const cudaLaunchConfig_t* cfg, int size);
-
 inline aa_status cuda_ok(cudaError_t e) { return e == cudaSuccess ? AA_OK : AA_ERR_CUDA; }
 
 }  // namespace aa

@@ -1,10 +1,8 @@
 // Gradient of the weighted instance losses with respect to the logits:  G_rc = g_r (softmax(x_r)_c - [c = y_r]).
 //
 // One read and one write of the logits: a row stays on chip between its sum and its gradient.  Rows of up to 4 KB sit in the registers of up to
-// a warp, rows of up to 16 KB in those of a small CTA; longer ones stream through a ring of shared-memory stages (bulk copies in and out,
-// in place), split over a cluster of CTAs where a slice would pass 64 KB.  Every exponential is evaluated once, against the thread's own
-// maximum, and rescaled by one factor per thread.  What is left (rows past 512 KB, gradients that are not aligned like the logits) is swept
-// twice through L2.
+// a warp, rows of up to 16 KB in those of a small CTA, rows of up to 64 KB in a stage of a shared-memory ring (bulk copies in and out, in place).
+// Longer rows, and gradients that are not aligned like the logits, are swept twice, the second time out of L2.
 #include "async_copy.cuh"
 #include "boss_common.cuh"
 #include "loss_common.cuh"
@@ -158,7 +156,7 @@ template <typename T, int V>
 struct RowPart {
     static constexpr int VE = Vec<T>::kElems;
     float e[V][VE], eh, et;    // logits, then exponentials against the thread's own maximum
-    float m, s;
+    float m, s, undo;          // s and what they stand for include the factor `undo`
     __device__ __forceinline__ void load_ends(const T* row, const RowSpan<T>& sp, int cols, int rank) {
         eh = rank < sp.head ? load1(row + rank) : -INFINITY;
         et = sp.tail0 + rank < cols ? load1(row + sp.tail0 + rank) : -INFINITY;
@@ -182,21 +180,41 @@ struct RowPart {
 #pragma unroll
             for (int i = 0; i < VE; ++i) m = fmaxf(m, e[k][i]);
         const float ref = m == -INFINITY ? 0.0f : m;
-        eh = exp_from(eh, ref);
-        et = exp_from(et, ref);
-        float s0 = eh, s1 = et;
+        float s0, s1;
+        if (fabsf(ref) < 1e38f) {
+            // 2^(x log2 e - fl(m log2 e)): one multiply-add; the rounding of the product is common to all and taken out of the sum and the factor
+            const float shift = -ref * kLog2e;
+            undo = ex2_approx(-fmaf(ref, kLog2e, shift));
+            eh = ex2_approx(fmaf(eh, kLog2e, shift));
+            et = ex2_approx(fmaf(et, kLog2e, shift));
+            s0 = eh;
+            s1 = et;
 #pragma unroll
-        for (int k = 0; k < V; ++k)
+            for (int k = 0; k < V; ++k)
 #pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                e[k][i] = exp_from(e[k][i], ref);
-                (i & 1 ? s1 : s0) += e[k][i];
-            }
-        s = s0 + s1;
+                for (int i = 0; i < VE; ++i) {
+                    e[k][i] = ex2_approx(fmaf(e[k][i], kLog2e, shift));
+                    (i & 1 ? s1 : s0) += e[k][i];
+                }
+        } else {
+            undo = 1.0f;
+            eh = exp_from(eh, ref);
+            et = exp_from(et, ref);
+            s0 = eh;
+            s1 = et;
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+#pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    e[k][i] = exp_from(e[k][i], ref);
+                    (i & 1 ? s1 : s0) += e[k][i];
+                }
+        }
+        s = (s0 + s1) * undo;
     }
     // What turns this thread's exponentials into g p.  A thread that saw only -inf holds zeros; a row of nothing else is NaN, as its loss is.
     __device__ __forceinline__ float factor(const NatState& all, float g) const {
-        return (m == -INFINITY && all.m != -INFINITY ? 0.0f : exp_from(m, all.m)) * (g / all.s);
+        return (m == -INFINITY && all.m != -INFINITY ? 0.0f : exp_from(m, all.m)) * undo * (g / all.s);
     }
     __device__ __forceinline__ void store_ends(T* out, const RowSpan<T>& sp, int cols, int rank, float f, float g, int y) {
         if (rank < sp.head) store1(out + rank, fmaf(eh, f, rank == y ? -g : 0.0f));
@@ -301,11 +319,9 @@ __global__ void __launch_bounds__(128) row_grad_block_kernel(GradParams p) {
 
 // --------------------------------------------------------------------------------------------- ring of long rows
 
-constexpr int kRingThreads = 480;          // consumers; with the producer warp 16 warps, 128 registers a thread
-constexpr int kRingVecs = 9;               // vectors per consumer: slices of up to 67.5 KB
-constexpr int kRingSliceVecs = 4096;       // ... of which 64 KB are used: three stages
+constexpr int kRingThreads = 512;          // consumers; a producer warp and a storing warp come on top
+constexpr int kRingVecs = 8;                // vectors per consumer: rows of up to 64 KB
 constexpr int kRingMaxStages = 6;
-constexpr int kMaxCluster = 8;
 
 // What the producer hands over with a row.
 struct RingRow {
@@ -315,80 +331,139 @@ struct RingRow {
     float ends[16];            // head elements, then tail elements
 };
 struct RingControl {
-    uint64_t full[kRingMaxStages], empty[kRingMaxStages], joined[2];
-    RingRow meta[kRingMaxStages];
+    uint64_t full[kRingMaxStages], done[kRingMaxStages], empty[kRingMaxStages];
+    RingRow rows[kRingMaxStages];
     NatState warp_state[2][kRingThreads / 32];
-    NatState peer[2][kMaxCluster];
     int abort_flag;
 };
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-}
 // All consumers: true iff `ok` in every one of them.
 __device__ __forceinline__ bool consumers_all(bool ok) {
     int r;
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbarrier.red.and.pred q, 1, %2, p;\n\tselp.s32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"((int)ok), "n"(kRingThreads) : "memory");
     return r != 0;
 }
-// This CTA's row state into every CTA of the cluster; completes one arrival on their barriers.
-__device__ __forceinline__ void send_state(NatState* slot, uint64_t* bar, int rank, const NatState& st) {
-    uint32_t a, b;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(slot)), "r"(rank));
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(smem_u32(bar)), "r"(rank));
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(st.m), "f"(st.s) : "memory");
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(b) : "memory");
-}
-__device__ __forceinline__ bool wait_states(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    const long long t0 = clock64();
-    while (true) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity)
-            : "memory");
-        if (ok) return true;
-        if (*abort_flag || clock64() - t0 > kWaitCycles) return false;
-    }
-}
 __device__ __forceinline__ void bulk_s2g(void* dst, const void* src_smem, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src_smem)), "r"(bytes) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-template <int N>
-__device__ __forceinline__ void bulk_wait_read() {
-    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
+// 2^((x - m) log2 e) / undo: one multiply-add and the exponential; `undo` takes the rounding of m log2 e out of sums and factors.  Near the
+// type's limits, where that product overflows, the difference is taken first.
+struct ExpAt {
+    float ref, shift, undo;
+    bool plain;
+    __device__ __forceinline__ explicit ExpAt(float m) {
+        ref = m == -INFINITY ? 0.0f : m;
+        plain = !(fabsf(ref) < 1e38f);
+        shift = plain ? 0.0f : -ref * kLog2e;
+        undo = plain ? 1.0f : ex2_approx(-fmaf(ref, kLog2e, shift));
+    }
+    __device__ __forceinline__ float fast(float x) const { return ex2_approx(fmaf(x, kLog2e, shift)); }
+    __device__ __forceinline__ float operator()(float x) const { return plain ? exp_from(x, ref) : fast(x); }
+};
+
+__device__ __forceinline__ float vec_max(const uint4& w, const float*) {
+    return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+}
+__device__ __forceinline__ float vec_max(const uint4& w, const uint16_t*) {
+    float x[8];
+    Vec<uint16_t>::unpack(w, x);
+    return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+}
+template <typename T>
+__device__ __forceinline__ float slice_max(const T* body, int nv, int tid) {
+    const uint4* w = reinterpret_cast<const uint4*>(body);
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int v = tid; v < nv; v += kRingThreads) {
+        const uint4 q = w[v];              // one 16-byte load
+        m = fmaxf(m, vec_max(q, body));
+    }
+    return m;
+}
+// The thread's exponentials of the row in `body`, and their sum.
+template <typename T>
+__device__ __forceinline__ float row_exponentials(const T* body, int nv, int tid, const ExpAt& at, float (&e)[kRingVecs][Vec<T>::kElems]) {
+    constexpr int VE = Vec<T>::kElems;
+    const uint4* w = reinterpret_cast<const uint4*>(body);
+    float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kRingVecs; ++k) {
+        if (tid + k * kRingThreads < nv) {
+            const uint4 q = w[tid + k * kRingThreads];
+            Vec<T>::unpack(q, e[k]);
+            if (at.plain) {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) e[k][i] = exp_from(e[k][i], at.ref);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VE; ++i) e[k][i] = at.fast(e[k][i]);
+            }
+#pragma unroll
+            for (int i = 0; i < VE; ++i) (i & 1 ? s1 : s0) += e[k][i];
+        }
+    }
+    return s0 + s1;
+}
+template <typename T>
+__device__ __forceinline__ void row_gradient(T* body, int nv, int tid, float f, const float (&e)[kRingVecs][Vec<T>::kElems]) {
+    constexpr int VE = Vec<T>::kElems;
+#pragma unroll
+    for (int k = 0; k < kRingVecs; ++k) {
+        const int v = tid + k * kRingThreads;
+        if (v < nv) {
+            float x[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) x[i] = e[k][i] * f;
+            if constexpr (VE == 8) store8(body + (int64_t)v * VE, x);
+            else *reinterpret_cast<float4*>(body + (int64_t)v * VE) = make_float4(x[0], x[1], x[2], x[3]);
+        }
+    }
 }
 
-// A cluster of `C` CTAs per row, rows handed out in turn; CTA `rank` owns the vectors [rank * per, rank * per + nv) of a row.
+// One persistent CTA per SM, rows handed out in turn, one ring stage each: fetched once, read for the maximum and again for the exponentials,
+// which stay in registers until the sum is known, overwritten by the gradient and copied out.
 template <typename T>
-__global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradParams p, int C, int stages, int stage_bytes) {
+__global__ void __launch_bounds__(kRingThreads + 64, 1) row_grad_ring_kernel(GradParams p, int stages, int stage_vecs) {
     constexpr int VE = Vec<T>::kElems;
     extern __shared__ uint4 smem16[];
     __shared__ RingControl ctl;
     grid_dependency_wait();
     grid_dependency_release();
-    const int rank = (int)(blockIdx.x % C), cols = (int)p.loss.cols;
-    const int64_t first = blockIdx.x / C, step = gridDim.x / C;
-    const int64_t n_inst = counted(p.count_dev, p.n_inst);
-    char* ring = reinterpret_cast<char*>(smem16);
+    const int cols = (int)p.loss.cols;
+    const int64_t n_inst = counted(p.count_dev, p.n_inst), step = gridDim.x;
+    uint4* ring = smem16;
     volatile int* abort_flag = &ctl.abort_flag;
     if (threadIdx.x == 0) {
         for (int i = 0; i < stages; ++i) {
             mbar_init(&ctl.full[i], 1);
+            mbar_init(&ctl.done[i], kRingThreads / 32);
             mbar_init(&ctl.empty[i], 1);
         }
-        mbar_init(&ctl.joined[0], C);
-        mbar_init(&ctl.joined[1], C);
         ctl.abort_flag = 0;
         mbar_fence_init();
     }
     __syncthreads();
-    cluster_sync();                        // nobody sends before every barrier stands
-    if (threadIdx.x >= kRingThreads) {
-        // ---- producer warp: looks a row's factor and label up, fetches its ends and its slice
-        const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x >= kRingThreads + 32) {
+        // ---- storing warp: a finished row goes out, and its stage is free as soon as the copies have read it
+        for (int64_t j = 0;; ++j) {
+            const int stage = (int)(j % stages);
+            if (!mbar_wait(&ctl.done[stage], (uint32_t)((j / stages) & 1), abort_flag) || *abort_flag) break;
+            const int64_t r = ctl.rows[stage].row;
+            if (r < 0) break;
+            T* out = static_cast<T*>(p.grad) + r * p.grad_stride;
+            const RowSpan<T> sp(static_cast<const T*>(p.loss.logits) + r * p.loss.row_stride, cols);
+            const int piece = (sp.nvec + 31) >> 5, v0 = lane * piece, n = min(piece, sp.nvec - v0);
+            if (n > 0) bulk_s2g(out + sp.head + (int64_t)v0 * VE, ring + (size_t)stage * stage_vecs + v0, (uint32_t)n * 16u);
+            bulk_wait_read();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.empty[stage]);
+        }
+    } else if (threadIdx.x >= kRingThreads) {
+        // ---- producer warp
         if (p.offsets && blockIdx.x == 0) {
             bool bad = false;
             for (int64_t s = lane; s < n_inst; s += 32) {
@@ -399,7 +474,7 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
         }
         int64_t j = 0;
         bool ok = true, more = true;
-        for (int64_t r0 = first; ok && more; r0 += 32 * step) {
+        for (int64_t r0 = blockIdx.x; ok && more; r0 += 32 * step) {
             // a lane per row: 32 rows' searches, labels and label logits cost one chain of loads
             const int64_t mine = r0 + lane * step;
             float my_g = 0.0f, my_logit = 0.0f;
@@ -408,7 +483,7 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
                 my_y = checked_label(p.loss, mine);
                 if (my_y >= 0) my_logit = load1(static_cast<const T*>(p.loss.logits) + mine * p.loss.row_stride + my_y);
             }
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; more && i < 32; ++i) {
                 const int64_t r = r0 + i * step;
                 more = r < p.loss.rows;
                 const int y = __shfl_sync(0xFFFFFFFFu, my_y, i);
@@ -421,27 +496,27 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
                 }
                 const T* row = static_cast<const T*>(p.loss.logits) + (more ? r : 0) * p.loss.row_stride;
                 const RowSpan<T> sp(row, cols);
-                const int per = (sp.nvec + C - 1) / C, nv = more && y >= 0 ? max(0, min(per, sp.nvec - rank * per)) : 0;
-                // one copy per lane: many in flight at once (the barrier's phase cannot complete before lane 0's arrival below)
-                const int piece = (nv + 31) >> 5, v0 = lane * piece, n = min(piece, nv - v0);
-                if (lane == 0) mbar_expect_tx(&ctl.full[stage], (uint32_t)nv * 16u);
-                __syncwarp();
-                if (n > 0) bulk_g2s(ring + (size_t)stage * stage_bytes + v0 * 16, row + sp.head + ((int64_t)rank * per + v0) * VE, (uint32_t)n * 16u, &ctl.full[stage]);
-                float end = 0.0f;          // lanes 0..7: head, 8..15: tail
-                if (more && y >= 0 && lane < sp.head) end = load1(row + lane);
-                if (more && y >= 0 && lane >= 8 && lane < 16 && sp.tail0 + lane - 8 < cols) end = load1(row + sp.tail0 + lane - 8);
-                RingRow* meta = &ctl.meta[stage];
-                if (lane < 16) meta->ends[lane] = end;
-                __syncwarp();
+                const bool load = more && y >= 0;                     // padding rows are only written
+                const int nv = load ? sp.nvec : 0;
+                RingRow* c = &ctl.rows[stage];
                 if (lane == 0) {
-                    meta->row = more ? r : -1;
-                    meta->g = g;
-                    meta->y = y;
-                    meta->label_logit = label_logit;
-                    mbar_arrive(&ctl.full[stage]);
+                    c->row = more ? r : -1;
+                    c->g = g;
+                    c->y = y;
+                    c->label_logit = label_logit;
+                    mbar_expect_tx(&ctl.full[stage], (uint32_t)nv * 16u);
                 }
+                __syncwarp();
+                // one copy per lane: many in flight at once (the phase cannot complete before lane 0's arrival below)
+                const int piece = (nv + 31) >> 5, v0 = lane * piece, n = min(piece, nv - v0);
+                if (n > 0) bulk_g2s(ring + (size_t)stage * stage_vecs + v0, row + sp.head + (int64_t)v0 * VE, (uint32_t)n * 16u, &ctl.full[stage]);
+                float end = 0.0f;          // lanes 0..7: head, 8..15: tail
+                if (load && lane < sp.head) end = load1(row + lane);
+                if (load && lane >= 8 && lane < 16 && sp.tail0 + lane - 8 < cols) end = load1(row + sp.tail0 + lane - 8);
+                if (lane < 16) c->ends[lane] = end;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.full[stage]);
                 ++j;
-                if (!more) break;
             }
         }
         if (!ok) {                         // the copies in flight still write to this CTA's memory
@@ -454,81 +529,68 @@ __global__ void __launch_bounds__(kRingThreads + 32) row_grad_ring_kernel(GradPa
         }
     } else {
         // ---- consumers
-        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+        const int tid = threadIdx.x, warp = tid >> 5;
         bool ok = true;
-        int64_t joins = 0;
         for (int64_t j = 0;; ++j) {
             const int stage = (int)(j % stages), turn = (int)(j & 1);
             ok = mbar_wait(&ctl.full[stage], (uint32_t)((j / stages) & 1), abort_flag);
-            const RingRow* meta = &ctl.meta[stage];
-            const int64_t r = ok ? meta->row : 0;
-            const int y = ok ? meta->y : -1;
-            const T* row = static_cast<const T*>(p.loss.logits) + (r < 0 ? 0 : r) * p.loss.row_stride;
-            T* out = static_cast<T*>(p.grad) + (r < 0 ? 0 : r) * p.grad_stride;
-            const RowSpan<T> sp(row, cols);
-            const int per = (sp.nvec + C - 1) / C, nv = max(0, min(per, sp.nvec - rank * per));
-            T* body = reinterpret_cast<T*>(ring + (size_t)stage * stage_bytes);
-            // the row's ends: rank 0 has the head, the last rank the tail
-            const int nh = rank == 0 ? sp.head : 0, nt = rank == C - 1 ? cols - sp.tail0 : 0;
-            RowPart<T, kRingVecs> part;
+            const RingRow* c = &ctl.rows[stage];
+            const int64_t r = ok ? c->row : 0;
+            const int y = ok && r >= 0 ? c->y : -1;
+            const RowSpan<T> sp(static_cast<const T*>(p.loss.logits) + (r < 0 ? 0 : r) * p.loss.row_stride, cols);
+            T* body = reinterpret_cast<T*>(ring + (size_t)stage * stage_vecs);
+            const int nh = sp.head, nt = cols - sp.tail0;
+            float e[kRingVecs][VE];
+            float eh = -INFINITY, et = -INFINITY;
+            NatState mine = {-INFINITY, 0.0f};
+            float undo = 1.0f;
             if (y >= 0) {
-                part.eh = tid < nh ? meta->ends[tid] : -INFINITY;
-                part.et = tid < nt ? meta->ends[8 + tid] : -INFINITY;
-                part.load_body(body, nv, tid, kRingThreads);
-                part.exponentials();
-                const NatState mine = group_merge_nat<32>(NatState{part.m, part.s});
-                if (lane == 0) ctl.warp_state[turn][warp] = mine;
+                if (tid < nh) eh = c->ends[tid];
+                if (tid < nt) et = c->ends[8 + tid];
+                mine.m = fmaxf(fmaxf(eh, et), slice_max(body, sp.nvec, tid));
+                const ExpAt at(mine.m);
+                undo = at.undo;
+                eh = at(eh);
+                et = at(et);
+                mine.s = (eh + et + row_exponentials(body, sp.nvec, tid, at, e)) * undo;
+                const NatState w = group_merge_nat<32>(mine);
+                if (lane == 0) ctl.warp_state[turn][warp] = w;
             }
-            const float g = ok ? meta->g : 0.0f, label_logit = ok ? meta->label_logit : 0.0f;
-            if (!consumers_all(ok)) {
+            if (!consumers_all(ok)) {      // a wait that gave up: all leave here
                 ok = false;
                 break;
             }
-            if (r < 0) break;              // every consumer has seen the same hand-over
-            float f = 0.0f;
+            if (r < 0) {
+                if (lane == 0) mbar_arrive(&ctl.done[stage]);
+                break;
+            }
+            T* out = static_cast<T*>(p.grad) + r * p.grad_stride;
             if (y >= 0) {
-                NatState all = group_merge_nat<16>((lane & 15) < kRingThreads / 32 ? ctl.warp_state[turn][lane & 15] : NatState{-INFINITY, 0.0f});
-                if (C > 1) {
-                    const int slot = (int)(joins & 1);
-                    if (tid < C) send_state(&ctl.peer[slot][rank], &ctl.joined[slot], tid, all);
-                    ok = wait_states(&ctl.joined[slot], (uint32_t)((joins >> 1) & 1), abort_flag);
-                    ++joins;
-                    all = ctl.peer[slot][0];
-                    for (int c = 1; c < C; ++c) all = merge(all, ctl.peer[slot][c]);
-                }
-                f = part.factor(all, g);
-                const int at = y - sp.head - rank * per * VE;
-                part.store_body(body, nv, tid, kRingThreads, f, y >= sp.head && y < sp.tail0 && at >= 0 && at < nv * VE ? at : -1, label_grad(all, label_logit, g));
-                if (p.loss.out && rank == 0 && tid == 0) p.loss.out[r] = row_loss(all, label_logit);
+                const NatState all = group_merge_nat<16>(ctl.warp_state[turn][lane & 15]);
+                const float g = c->g, label_logit = c->label_logit;
+                // this thread's exponentials -> g p; one that saw only -inf holds zeros, a row of nothing else is NaN as its loss is
+                const float f = (mine.m == -INFINITY && all.m != -INFINITY ? 0.0f : exp_from(mine.m, all.m)) * undo * (g / all.s);
+                row_gradient(body, sp.nvec, tid, f, e);
+                const int idx = y - sp.head;
+                if (idx >= 0 && y < sp.tail0 && (idx / VE) % kRingThreads == tid) store1(body + idx, label_grad(all, label_logit, g));
+                if (tid < nh) store1(out + tid, fmaf(eh, f, tid == y ? -g : 0.0f));
+                if (tid < nt) store1(out + sp.tail0 + tid, fmaf(et, f, sp.tail0 + tid == y ? -g : 0.0f));
+                if (p.loss.out && tid == 0) p.loss.out[r] = row_loss(all, label_logit);
             } else {
-                for (int v = tid; v < nv; v += kRingThreads) reinterpret_cast<uint4*>(body)[v] = make_uint4(0, 0, 0, 0);
-                if (p.loss.out && rank == 0 && tid == 0) p.loss.out[r] = 0.0f;
+                for (int v = tid; v < sp.nvec; v += kRingThreads) reinterpret_cast<uint4*>(body)[v] = make_uint4(0, 0, 0, 0);
+                if (tid < nh) store1(out + tid, 0.0f);
+                if (tid < nt) store1(out + sp.tail0 + tid, 0.0f);
+                if (p.loss.out && tid == 0) p.loss.out[r] = 0.0f;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            if (tid < nh) store1(out + tid, y >= 0 ? fmaf(part.eh, f, tid == y ? -g : 0.0f) : 0.0f);
-            if (tid < nt) store1(out + sp.tail0 + tid, y >= 0 ? fmaf(part.et, f, sp.tail0 + tid == y ? -g : 0.0f) : 0.0f);
-            if (!consumers_all(ok)) {
-                ok = false;
-                break;
-            }
-            if (warp == 0) {
-                const int piece = (nv + 31) >> 5, v0 = lane * piece, n = min(piece, nv - v0);
-                if (n > 0) bulk_s2g(out + sp.head + ((int64_t)rank * per + v0) * VE, body + (int64_t)v0 * VE, (uint32_t)n * 16u);
-                else asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                // the previous row's copies have been read out of their stage once only these are pending
-                bulk_wait_read<1>();
-                __syncwarp();
-                if (lane == 0 && j > 0) mbar_arrive(&ctl.empty[(j - 1) % stages]);
-            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.done[stage]);
         }
         if (!ok) {
             ctl.abort_flag = 1;
             if (tid == 0) latch(p.loss.ctl, AA_ERR_SCAN_TIMEOUT);
         }
-        if (warp == 0) bulk_wait_read<0>();
     }
-    __syncthreads();
-    cluster_sync();                        // peers may still send here until they are done
 }
 
 // ------------------------------------------------------------------------------------------- two sweeps
@@ -600,34 +662,19 @@ __global__ void __launch_bounds__(256) row_grad_cta_kernel(GradParams p) {
 }
 
 template <typename T>
-aa_status launch_ring(aa_ctx_impl* c, GradParams& p, int C) {
+aa_status launch_ring(aa_ctx_impl* c, GradParams& p) {
     const void* kernel = (const void*)row_grad_ring_kernel<T>;
     const int64_t vecs = p.loss.cols * (int64_t)sizeof(T) / 16;
-    int stage_bytes = (int)((vecs + C - 1) / C * 16 + 127) / 128 * 128;
-    int stages = 210 * 1024 / stage_bytes;
+    int stage_vecs = (int)((vecs + 7) / 8 * 8);
+    int stages = 208 * 1024 / (stage_vecs * 16);                      // three of 64 KB
     if (stages > kRingMaxStages) stages = kRingMaxStages;
-    const size_t smem = (size_t)stages * stage_bytes;
+    const size_t smem = (size_t)stages * stage_vecs * 16;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(kRingThreads + 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = c->stream;
-    cudaLaunchAttribute attrs[2];
-    attrs[0].id = cudaLaunchAttributeClusterDimension;
-    attrs[0].val.clusterDim.x = (unsigned)C;
-    attrs[0].val.clusterDim.y = attrs[0].val.clusterDim.z = 1;
-    attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attrs[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attrs;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3((unsigned)(c->sm_count / C * C));
-    int clusters = resident_clusters(c, kernel, &cfg, C);
-    if (clusters < 1) return AA_ERR_CUDA;
-    if (clusters > p.loss.rows) clusters = (int)p.loss.rows;
-    cfg.gridDim = dim3((unsigned)(clusters * C));
-    cfg.numAttrs = 2;
-    void* args[] = {&p, &C, &stages, &stage_bytes};
-    if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) return AA_ERR_CUDA;
+    const int cap = resident_ctas(c, kernel, kRingThreads + 64, smem);
+    if (cap <= 0) return AA_ERR_CUDA;
+    void* args[] = {&p, &stages, &stage_vecs};
+    const unsigned grid = (unsigned)(p.loss.rows < cap ? p.loss.rows : cap);
+    if (launch_overlapped(c, kernel, dim3(grid), dim3(kRingThreads + 64), args, smem, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     return AA_OK;
 }
@@ -662,10 +709,8 @@ aa_status launch_rows(aa_ctx_impl* c, GradParams& p) {
         kernel = (const void*)row_grad_block_kernel<T, 8>;
         want = p.loss.rows;
         threads = 128;
-    } else if (alike && vecs <= (int64_t)kRingSliceVecs * kMaxCluster) {
-        int C = 1;
-        while ((vecs + C - 1) / C > kRingSliceVecs) C *= 2;
-        return launch_ring<T>(c, p, C);
+    } else if (alike && vecs <= kRingThreads * kRingVecs) {
+        return launch_ring<T>(c, p);
     } else if (row_bytes > 8 * 1024) {
         kernel = (const void*)row_grad_cta_kernel<T>;
         want = p.loss.rows;
