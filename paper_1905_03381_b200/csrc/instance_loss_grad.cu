@@ -119,15 +119,28 @@ __device__ __forceinline__ void write_row(const T* row, T* out, int64_t cols, fl
         if (head > cols) head = cols;
         nvec = (cols - head) / VE;
     }
-    for (int64_t v = rank; v < nvec; v += nthreads) {
+    const auto put = [&](const uint4& q, int64_t v) {
         const int64_t c = head + v * VE;
         float x[VE];
-        Vec<T>::unpack(*reinterpret_cast<const uint4*>(row + c), x);
+        Vec<T>::unpack(q, x);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) x[e] = at(x[e], c + e);
+        for (int e = 0; e < VE; ++e) x[e] = a * exp_from(x[e], m);
+        if ((uint64_t)(y - c) < (uint64_t)VE) {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) x[e] -= c + e == y ? g : 0.0f;
+        }
         if constexpr (VE == 8) store8(out + c, x);
         else *reinterpret_cast<float4*>(out + c) = make_float4(x[0], x[1], x[2], x[3]);
+    };
+    int64_t v = rank;
+    for (; v + 3 * (int64_t)nthreads < nvec; v += 4 * (int64_t)nthreads) {
+        uint4 q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = *reinterpret_cast<const uint4*>(row + head + (v + k * (int64_t)nthreads) * VE);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) put(q[k], v + k * (int64_t)nthreads);
     }
+    for (; v < nvec; v += nthreads) put(*reinterpret_cast<const uint4*>(row + head + v * VE), v);
     for (int64_t c = rank; c < head; c += nthreads) store1(out + c, at(load1(row + c), c));
     for (int64_t c = head + nvec * VE + rank; c < cols; c += nthreads) store1(out + c, at(load1(row + c), c));
 }
@@ -629,9 +642,12 @@ __global__ void __launch_bounds__(256) row_grad_group_kernel(GradParams p) {
     }
 }
 
+// A CTA of 512 threads per row, two on an SM: the rows in flight (296) fit L2 up to 400 KB each.
+constexpr int kSweepThreads = 512;
+
 template <typename T>
-__global__ void __launch_bounds__(256) row_grad_cta_kernel(GradParams p) {
-    __shared__ NatState warp_state[8];
+__global__ void __launch_bounds__(kSweepThreads, 2) row_grad_cta_kernel(GradParams p) {
+    __shared__ NatState warp_state[kSweepThreads / 32];
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t n_inst = counted(p.count_dev, p.n_inst);
@@ -644,19 +660,19 @@ __global__ void __launch_bounds__(256) row_grad_cta_kernel(GradParams p) {
         const T* row = static_cast<const T*>(p.loss.logits) + r * p.loss.row_stride;
         T* out = static_cast<T*>(p.grad) + r * p.grad_stride;
         if (y < 0) {
-            zero_row<T>(out, p.loss.cols, threadIdx.x, 256);
+            zero_row<T>(out, p.loss.cols, threadIdx.x, kSweepThreads);
             if (p.loss.out && threadIdx.x == 0) p.loss.out[r] = 0.0f;
             continue;
         }
         const float label_logit = load1(row + y);
         NatState st = {-INFINITY, 0.0f};
-        scan_row_nat<T>(st, row, p.loss.cols, threadIdx.x, 256);
+        scan_row_nat<T>(st, row, p.loss.cols, threadIdx.x, kSweepThreads);
         st = group_merge_nat<32>(st);
         __syncthreads();                                 // the previous row's states have been read
         if (lane == 0) warp_state[warp] = st;
         __syncthreads();
-        st = group_merge_nat<32>(lane < 8 ? warp_state[lane] : NatState{-INFINITY, 0.0f});
-        write_row<T>(row, out, p.loss.cols, st.m, g / st.s, g, y, threadIdx.x, 256);
+        st = group_merge_nat<32>(lane < kSweepThreads / 32 ? warp_state[lane] : NatState{-INFINITY, 0.0f});
+        write_row<T>(row, out, p.loss.cols, st.m, g / st.s, g, y, threadIdx.x, kSweepThreads);
         if (p.loss.out && threadIdx.x == 0) p.loss.out[r] = row_loss(st, label_logit);
     }
 }
@@ -714,6 +730,7 @@ aa_status launch_rows(aa_ctx_impl* c, GradParams& p) {
     } else if (row_bytes > 8 * 1024) {
         kernel = (const void*)row_grad_cta_kernel<T>;
         want = p.loss.rows;
+        threads = kSweepThreads;
     } else {
         kernel = (const void*)row_grad_group_kernel<T>;
         want = (p.loss.rows + 7) / 8;
