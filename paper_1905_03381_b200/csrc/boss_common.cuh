@@ -59,12 +59,14 @@ __device__ __forceinline__ Words4 philox4x32_10(uint32_t c0, uint32_t c1, uint32
     return Words4{{c0, c1, c2, c3}};
 }
 
-// Key of one instance's draws: words 2 and 3 of the block whose word 0 is the screen's draw.
-__device__ __forceinline__ uint2 instance_key(const DropRule& r, int64_t instance) {
-    const int64_t id = r.id_base + (r.row_idx ? (int64_t)__ldg(r.row_idx + instance) : instance);
+// Key of the draws of the instance with this id: words 2 and 3 of the block whose word 0 is the screen's draw.
+__device__ __forceinline__ uint2 id_key(const DropRule& r, int64_t id) {
     const Words4 w = philox4x32_10((uint32_t)id, (uint32_t)((uint64_t)id >> 32), r.step_lo, r.step_hi, r.seed_lo, r.seed_hi);
     return make_uint2(w.w[2], w.w[3]);
 }
+
+__device__ __forceinline__ int64_t instance_row(const DropRule& r, int64_t instance) { return r.row_idx ? (int64_t)__ldg(r.row_idx + instance) : instance; }
+__device__ __forceinline__ uint2 instance_key(const DropRule& r, int64_t instance) { return id_key(r, r.id_base + instance_row(r, instance)); }
 
 __device__ __forceinline__ Words4 draw_block(const DropRule& r, uint2 key, uint64_t block) {
     return philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), r.site, 0u, key.x, key.y);
@@ -84,6 +86,22 @@ __device__ __forceinline__ int64_t find_segment(const int32_t* __restrict__ offs
     while (hi - lo > 1) {
         const int64_t mid = (lo + hi) >> 1;
         if ((int64_t)__ldg(offsets + mid) <= r) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// The same by WIDTH lanes together (lane `l` of them, `mask` theirs): WIDTH probes a round instead of one.
+template <int WIDTH>
+__device__ __forceinline__ int64_t find_segment_lanes(const int32_t* __restrict__ offsets, int64_t n, int64_t r, int l, unsigned mask) {
+    int64_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + WIDTH) / (WIDTH + 1);      // probes lo + step, lo + 2 step, ...
+        const int64_t at = lo + (int64_t)(l + 1) * step;
+        const bool below = at < hi && (int64_t)__ldg(offsets + at) <= r;
+        const int count = __popc(__ballot_sync(mask, below) & mask);  // offsets ascend: the probes that hold are the first ones
+        const int64_t next = lo + (int64_t)(count + 1) * step;
+        lo += (int64_t)count * step;
+        hi = next < hi ? next : hi;
     }
     return lo;
 }
