@@ -51,6 +51,8 @@ aa_status launch_rel_attention_grad_plain(aa_ctx_impl* c, const RelParams& p, in
 // bf16 kernels on the tensor cores: aligned tokens, head width a multiple of 8 up to 128.
 bool rel_mma_fits(const RelParams& p);
 aa_status launch_rel_attention_mma(aa_ctx_impl* c, const RelParams& p);
+// ... of them the sequences of more than `lo` tokens on either side, on the tcgen05 tensor cores
+aa_status launch_rel_attention_tc(aa_ctx_impl* c, const RelParams& p, int lo);
 // ... a few new tokens over long contexts
 bool rel_decode_fits(const RelParams& p);
 aa_status launch_rel_decode(aa_ctx_impl* c, const RelParams& p);

@@ -95,7 +95,7 @@ aa_status launch_rel_attention_mma(aa_ctx_impl* c, const RelParams& p) {
     int covered = -1;
     const aa_status st = launch_rel_sentences(c, p, &covered);
     if (st != AA_OK || (p.max_q <= covered && p.max_k <= covered)) return st;
-    return p.dim <= 32 ? forward_rows<32>(c, p, covered) : p.dim <= 64 ? forward_rows<64>(c, p, covered) : forward_rows<128>(c, p, covered);
+    return launch_rel_attention_tc(c, p, covered);
 }
 
 }  // namespace aa
