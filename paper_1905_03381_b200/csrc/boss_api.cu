@@ -101,6 +101,28 @@ aa_status make_rel_params(const aa_attn* a, const aa_rel_bias* b, const aa_dropo
     return make_drop_rule(d, p.drop) ? AA_OK : AA_ERR_INVALID_ARG;
 }
 
+bool rel_bf16_fits(const RelParams& p) {
+    const auto ok = [&](const TokArg& a) { return !a.data || ((uintptr_t)a.data % 16 == 0 && a.tok % 8 == 0 && a.head % 8 == 0 && a.tok < (1 << 30)); };
+    return p.dim % 8 == 0 && p.dim <= 128 && ok(p.q) && ok(p.k) && ok(p.v) && ok(p.out) && ok(p.dout) && ok(p.dq) && ok(p.dk) && ok(p.dv);
+}
+
+// A few new tokens: split over the context.  Sentences: a CTA each.  What is longer: tiles on the tcgen05 tensor cores.
+aa_status launch_rel_attention_bf16(aa_ctx_impl* c, const RelParams& p) {
+    if (rel_decode_fits(p)) return launch_rel_decode(c, p);
+    int covered = -1;
+    const aa_status st = launch_rel_sentences(c, p, &covered);
+    if (st != AA_OK || (p.max_q <= covered && p.max_k <= covered)) return st;
+    return launch_rel_attention_tc(c, p, covered);
+}
+
+aa_status launch_rel_attention_grad_bf16(aa_ctx_impl* c, const RelParams& p, int* n_parts) {
+    *n_parts = 0;
+    int covered = -1;
+    const aa_status st = launch_rel_sentences_grad(c, p, &covered, n_parts);
+    if (st != AA_OK || (p.max_q <= covered && p.max_k <= covered)) return st;
+    return launch_rel_attention_grad_tc(c, p, covered, n_parts);
+}
+
 int rel_grad_parts(int heads) { return (1184 + heads - 1) / heads; }
 
 namespace {
@@ -171,7 +193,7 @@ aa_status aa_rel_attention(aa_ctx* ctx, const aa_attn* attn, const aa_rel_bias* 
     aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
     p.out = tok(*out);
     p.ctl = c->ctl;
-    return attn->dtype == AA_BF16 && rel_mma_fits(p) ? launch_rel_attention_mma(c, p) : launch_rel_attention_plain(c, p, attn->dtype);
+    return attn->dtype == AA_BF16 && rel_bf16_fits(p) ? launch_rel_attention_bf16(c, p) : launch_rel_attention_plain(c, p, attn->dtype);
 }
 
 aa_status aa_rel_attention_scratch_bytes(const aa_attn* attn, const aa_rel_bias* bias, size_t* bytes) {
@@ -210,7 +232,7 @@ aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_b
     p.stats = static_cast<float4*>(scratch);
     p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(attn));
     p.n_parts = rel_grad_parts(p.heads);
-    st = attn->dtype == AA_BF16 && rel_mma_fits(p) ? launch_rel_attention_grad_mma(c, p, &p.n_parts) : launch_rel_attention_grad_plain(c, p, attn->dtype);
+    st = attn->dtype == AA_BF16 && rel_bf16_fits(p) ? launch_rel_attention_grad_bf16(c, p, &p.n_parts) : launch_rel_attention_grad_plain(c, p, attn->dtype);
     if (st != AA_OK || !dtable) return st;
     return launch_rel_table_grad(c, p);
 }

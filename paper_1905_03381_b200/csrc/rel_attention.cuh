@@ -49,8 +49,8 @@ int rel_grad_parts(int heads);                                       // CTAs per
 aa_status launch_rel_attention_plain(aa_ctx_impl* c, const RelParams& p, int dtype);
 aa_status launch_rel_attention_grad_plain(aa_ctx_impl* c, const RelParams& p, int dtype);
 // bf16 kernels on the tensor cores: aligned tokens, head width a multiple of 8 up to 128.
-bool rel_mma_fits(const RelParams& p);
-aa_status launch_rel_attention_mma(aa_ctx_impl* c, const RelParams& p);
+bool rel_bf16_fits(const RelParams& p);
+aa_status launch_rel_attention_bf16(aa_ctx_impl* c, const RelParams& p);
 // ... of them the sequences of more than `lo` tokens on either side, on the tcgen05 tensor cores
 aa_status launch_rel_attention_tc(aa_ctx_impl* c, const RelParams& p, int lo);
 // ... a few new tokens over long contexts
@@ -59,7 +59,8 @@ aa_status launch_rel_decode(aa_ctx_impl* c, const RelParams& p);
 // ... of them the sequences of at most *covered tokens on both sides (set by the call; -1: none)
 aa_status launch_rel_sentences(aa_ctx_impl* c, const RelParams& p, int* covered);
 aa_status launch_rel_sentences_grad(aa_ctx_impl* c, const RelParams& p, int* covered, int* n_parts);
-aa_status launch_rel_attention_grad_mma(aa_ctx_impl* c, const RelParams& p, int* n_parts);
+aa_status launch_rel_attention_grad_tc(aa_ctx_impl* c, const RelParams& p, int lo, int* n_parts);
+aa_status launch_rel_attention_grad_bf16(aa_ctx_impl* c, const RelParams& p, int* n_parts);
 aa_status launch_rel_table_grad(aa_ctx_impl* c, const RelParams& p);  // parts -> dtable
 
 #ifdef __CUDACC__
@@ -87,9 +88,9 @@ __device__ __forceinline__ bool load_seq(const RelParams& p, int64_t s, Seq& q) 
 // Base-2 bias by distance for head h: bias[delta + reach + MARGIN]; the ends beyond the reach repeat the last buckets' values for MARGIN
 // distances, so that a tile that touches the reach needs no clamping.  A warp per bucket: the bounds are read at one address.
 template <int MARGIN>
-__device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias) {
+__device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias, int warps) {      // the CTA's first `warps` warps call
     if (!p.table) return;
-    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31;
     float* zero = bias + p.reach + MARGIN;
     for (int b0 = 0; b0 < p.buckets; b0 += 32) {
         float v = 0.0f;                                                 // a lane per bucket: one trip to memory for 32 of them
@@ -108,6 +109,10 @@ __device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias
                 for (int n = 1 + lane; n <= p.reach + MARGIN; n += 32) zero[n] = x;
         }
     }
+}
+template <int MARGIN>
+__device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias) {
+    fill_bias<MARGIN>(p, h, bias, (int)(blockDim.x >> 5));
 }
 __host__ __device__ constexpr int bias_floats(int reach, int margin) { return 2 * (reach + margin) + 1; }
 __device__ __forceinline__ float bias_at(const RelParams& p, const float* bias, int delta) {      // a table without margins

@@ -174,11 +174,6 @@ __device__ __forceinline__ void block_drops(const RelParams& p, const Seq& s, ui
     }
 }
 
-// Whether some query of the block sees its first key.
-__device__ __forceinline__ bool block_live(const RelParams& p, const Seq& s, const Block& b) {
-    return b.i0 < s.lq && b.j0 < keys_seen(p, s, min(b.i0 + 16, s.lq));
-}
-
 __device__ __forceinline__ float quad_max(float x) {
     x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1));
     return fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2));
@@ -289,13 +284,6 @@ __device__ __forceinline__ void block_ds(const RelParams& p, const RowStats& st,
             dp[n][e] = fabsf(t[n][e]) * st.rl[r] * (dp[n][e] - st.D[r]);
             t[n][e] = fmaxf(t[n][e], 0.0f) * f[r];
         }
-}
-template <int NT>
-__device__ __forceinline__ float block_total(const float (&ds)[NT][4]) {
-    float a = 0.0f;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) a += (ds[n][0] + ds[n][1]) + (ds[n][2] + ds[n][3]);
-    return a;
 }
 // t and dp (p and ds by now) as bf16 into rows g and g + 8 of two tiles, at this lane's columns
 template <int NT>

@@ -121,9 +121,9 @@ __device__ __forceinline__ void load_row(uint32_t tmem, float (&t)[64]) {
     }
 }
 
-// COLS accumulator columns of this thread's lane times f, as bf16, to `out` (nullptr: read only, the instruction is the warp's).
+// COLS accumulator columns of this thread's lane times f, as bf16, to `out` from element `from` on (nullptr: read only, the instruction is the warp's).
 template <int COLS>
-__device__ __forceinline__ void store_accumulator(const RelParams& p, uint32_t tmem, uint16_t* out, float f) {
+__device__ __forceinline__ void store_accumulator(const RelParams& p, uint32_t tmem, uint16_t* out, float f, int from = 0) {
 #pragma unroll
     for (int c0 = 0; c0 < COLS; c0 += 32) {
         uint32_t v[32];
@@ -132,11 +132,11 @@ __device__ __forceinline__ void store_accumulator(const RelParams& p, uint32_t t
         if (out) {
 #pragma unroll
             for (int c = 0; c < 32; c += 8) {
-                if (c0 + c >= p.dim) continue;
+                if (from + c0 + c >= p.dim) continue;
                 uint32_t w[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) w[k] = pack_bf16(__uint_as_float(v[c + 2 * k]) * f, __uint_as_float(v[c + 2 * k + 1]) * f);
-                *reinterpret_cast<uint4*>(out + c0 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(out + from + c0 + c) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
         __syncwarp();                      // the next load is the whole warp's
