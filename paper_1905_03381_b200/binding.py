@@ -103,12 +103,11 @@ class aa_rel_bias(Structure):
 
 def rows_desc(x: torch.Tensor) -> aa_rows:
     """Descriptor of a 2-D fp32/bf16 matrix with contiguous rows (row stride free)."""
-    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1) or not x.is_cuda:
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1) or not x.is_cuda:
         raise TypeError("expected a 2-D CUDA tensor with contiguous rows")
-    m = aa_rows()
-    m.data, m.dtype, m.rows, m.cols = x.data_ptr(), _dtype_code(x), x.shape[0], x.shape[1]
-    m.row_stride = x.stride(0) if x.shape[0] > 1 else x.shape[1]
-    return m
+    rows, cols = shape
+    return aa_rows(x.data_ptr(), _dtype_code(x), 0, rows, cols, stride[0] if rows > 1 else cols)
 
 
 def dropout_rule(p: float, seed: int, step: int, site: int = 0, row_idx=None, id_base: int = 0) -> aa_dropout_rule:
@@ -132,13 +131,12 @@ def rel_bias(table: torch.Tensor, max_distance: int, bidirectional: bool = True)
 
 
 def _tokens(x: torch.Tensor, name: str, like=None) -> aa_tokens:
-    if x.dim() != 3 or not x.is_cuda or (x.stride(2) != 1 and x.shape[2] > 1):
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or not x.is_cuda or (stride[2] != 1 and shape[2] > 1):
         raise TypeError(f"{name} must be a 3-D CUDA tensor [tokens, heads, head_dim] with a contiguous last dimension")
-    if like is not None and (x.shape != like.shape or x.dtype != like.dtype):
+    if like is not None and (shape != like.shape or x.dtype != like.dtype):
         raise TypeError(f"{name} must have the shape and dtype of the tensor it belongs to")
-    t = aa_tokens()
-    t.data, t.token_stride, t.head_stride = x.data_ptr(), x.stride(0), x.stride(1)
-    return t
+    return aa_tokens(x.data_ptr(), stride[0], stride[1])
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets=None, max_q=None, max_k=None,
