@@ -13,8 +13,8 @@ constexpr int kStages = 3;
 
 struct DecodeParams {
     RelParams p;
-    int splits, row_tiles;
-    float* part;             // [sequence][key head][row tile][split][16][dim + 2]: o, m, l
+    int splits, row_tiles, part_rows;   // rows kept of a pass: 16, or all there can be
+    float* part;             // [sequence][key head][row tile][split][part_rows][dim + 2]: o, m, l
 };
 
 // Row r of the pass: query head h0 + r / lq, new token r % lq.
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(128) decode_kernel(DecodeParams d) {
         }
     }
     __syncthreads();
-    float* part = d.part + (((sn * p.kv_heads + hk) * d.row_tiles + rt) * d.splits + split) * 16 * (p.dim + 2);
+    float* part = d.part + (((sn * p.kv_heads + hk) * d.row_tiles + rt) * d.splits + split) * d.part_rows * (p.dim + 2);
     for (int r = warp; r < 16 && r0 + r < rows; r += 4) {
         float mw[4], top = -INFINITY;
 #pragma unroll
@@ -171,16 +171,16 @@ __global__ void __launch_bounds__(128) decode_join_kernel(DecodeParams d) {
     Seq s;
     if (!load_seq(p, sn, s) || row >= p.group * s.lq) return;
     const int pitch = p.dim + 2;
-    const float* part = d.part + ((sn * p.kv_heads + hk) * d.row_tiles + row / 16) * d.splits * 16 * pitch + row % 16 * pitch;
+    const float* part = d.part + ((sn * p.kv_heads + hk) * d.row_tiles + row / 16) * d.splits * d.part_rows * pitch + row % 16 * pitch;
     float top = -INFINITY;
-    for (int i = lane; i < d.splits; i += 32) top = fmaxf(top, part[(int64_t)i * 16 * pitch + p.dim]);
+    for (int i = lane; i < d.splits; i += 32) top = fmaxf(top, part[(int64_t)i * d.part_rows * pitch + p.dim]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     const float ref = top == -INFINITY ? 0.0f : top;
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sum = 0.0f;
 #pragma unroll 4
     for (int i = 0; i < d.splits; ++i) {
-        const float* at = part + (int64_t)i * 16 * pitch;
+        const float* at = part + (int64_t)i * d.part_rows * pitch;
         const float w = ex2_approx(at[p.dim] - ref);
         sum = fmaf(at[p.dim + 1], w, sum);
 #pragma unroll
@@ -204,11 +204,12 @@ aa_status decode(aa_ctx_impl* c, const RelParams& p) {
     const int cap = resident_ctas(c, kernel, 128, smem);
     if (cap <= 0) return AA_ERR_CUDA;
     d.row_tiles = (int)((p.group * p.max_q + 15) / 16);
+    d.part_rows = p.group * p.max_q < 16 ? (int)(p.group * p.max_q) : 16;
     // one wave of CTAs, at least two tiles each, and as many parts as the context's partial sums hold
     const int64_t units = p.n_seq * p.kv_heads * d.row_tiles, tiles = (p.max_k + 63) / 64;
     int64_t splits = cap / units;
     if (splits > (tiles + 1) / 2) splits = (tiles + 1) / 2;
-    const int64_t room = c->partial_floats / (units * 16 * (p.dim + 2));
+    const int64_t room = c->partial_floats / (units * d.part_rows * (p.dim + 2));
     if (splits > room) splits = room;
     d.splits = splits > 1 ? (int)splits : 1;
     d.part = c->partials;
