@@ -71,7 +71,6 @@ __device__ __forceinline__ uint2 instance_key(const DropRule& r, int64_t instanc
 __device__ __forceinline__ Words4 draw_block(const DropRule& r, uint2 key, uint64_t block) {
     return philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), r.site, 0u, key.x, key.y);
 }
-__device__ __forceinline__ uint32_t draw_half(const Words4& w, int h) { return (w.w[h >> 1] >> (16 * (h & 1))) & 0xFFFFu; }
 
 // min(*count_dev, n), or n.
 __device__ __forceinline__ int64_t counted(const int32_t* count_dev, int64_t n) {
@@ -116,21 +115,13 @@ __device__ __forceinline__ void check_offsets(Control* ctl, const int32_t* __res
     if (bad) latch(ctl, AA_ERR_BAD_INDEX);
 }
 
-// Eight consecutive elements widened to fp32 / rounded once (to nearest even) on the way back.  Pointers 16-byte aligned.
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
-    Vec<uint16_t>::unpack(*reinterpret_cast<const uint4*>(p), x);
-}
 // Two floats as packed bf16, `lo` in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// Eight consecutive elements, rounded once (to nearest even).  Pointers 16-byte aligned.
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
     *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
