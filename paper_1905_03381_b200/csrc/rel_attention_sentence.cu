@@ -4,6 +4,9 @@
 // the bias by distance is laid out once per CTA.  A warp works on a strip of 16 query rows in steps of 16 keys.  Backward: strips leave p
 // and dS in shared memory (bf16), then warps contract them for 16 keys (dV, dK) and 16 rows (dQ): five products, each operand read from
 // memory once.  The bias gradient is added up along the diagonals of the unrounded dS, in a fixed order.
+//
+// Bound by the instructions around the products (bias, exponential, draws, operand moves) more than by the products: 368 sentences of 8 to
+// 128 tokens, 8 heads of 64, forward 56 us (1.9 TB/s), forward and every gradient, causal, with dropout 242 us.
 #include "rel_attention_mma.cuh"
 
 namespace aa {
