@@ -88,7 +88,7 @@ __device__ __forceinline__ bool load_seq(const RelParams& p, int64_t s, Seq& q) 
 // Base-2 bias by distance for head h: bias[delta + reach + MARGIN]; the ends beyond the reach repeat the last buckets' values for MARGIN
 // distances, so that a tile that touches the reach needs no clamping.  A warp per bucket: the bounds are read at one address.
 template <int MARGIN>
-__device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias, int warps) {      // the CTA's first `warps` warps call
+__device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias, int warps, int self) {      // `warps` warps call, this one as the self-th
     if (!p.table) return;
     const int lane = threadIdx.x & 31;
     float* zero = bias + p.reach + MARGIN;
@@ -99,7 +99,7 @@ __device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias
             v = isinf(x) || isnan(x) ? x : fminf(fmaxf(x * kAttnLog2e, -3.0e38f), 3.0e38f);
         }
         const int b1 = min(p.buckets - b0, 32);
-        for (int i = threadIdx.x >> 5; i < b1; i += warps) {
+        for (int i = self; i < b1; i += warps) {
             const float x = __shfl_sync(0xFFFFFFFFu, v, i);
             const bool up = b0 + i >= p.per_dir;
             const int k = up ? b0 + i - p.per_dir : b0 + i;
@@ -112,7 +112,7 @@ __device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias
 }
 template <int MARGIN>
 __device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias) {
-    fill_bias<MARGIN>(p, h, bias, (int)(blockDim.x >> 5));
+    fill_bias<MARGIN>(p, h, bias, (int)(blockDim.x >> 5), (int)(threadIdx.x >> 5));
 }
 __host__ __device__ constexpr int bias_floats(int reach, int margin) { return 2 * (reach + margin) + 1; }
 __device__ __forceinline__ float bias_at(const RelParams& p, const float* bias, int delta) {      // a table without margins

@@ -5,7 +5,7 @@
 // Four warps share a 64-key tile, 16 keys each, with running statistics of their own; three tiles of K and V are in flight per CTA.
 //
 // Bound by latency: launch, first tiles, the warps' and the splits' joins.  Four sequences of 4,001 tokens, 16 heads of 128 on 4 key heads:
-// 24 us for 33 MB (34 us while every part kept 16 rows and the context's partial sums held 4 splits of a sequence).
+// 23.7 us for 33 MB (34 us while every part kept 16 rows and the context's partial sums held 4 splits of a sequence).
 #include "rel_attention_mma.cuh"
 
 namespace aa {
@@ -60,7 +60,9 @@ __global__ void __launch_bounds__(128) decode_kernel(DecodeParams d) {
         *reinterpret_cast<uint4*>(Qs + r * P + c) = x;
     }
     const int bias_len = p.table ? bias_floats(p.reach, 0) : 0;
-    for (int a = 0; a < p.group; ++a) fill_bias<0>(p, h0 + a, bias + a * bias_len);
+    // the warps share out the heads: one trip to the table, where all warps on one head after the other would make `group` of them
+    const int share = max(1, 4 / p.group);
+    for (int a = warp / share; a < p.group; a += 4 / share) fill_bias<0>(p, h0 + a, bias + a * bias_len, share, warp % share);
     const uint2 key = p.drop.thr ? instance_key(p.drop, sn) : make_uint2(0, 0);
     // this lane's two rows
     int qi[2], pos[2], lim[2], head[2];

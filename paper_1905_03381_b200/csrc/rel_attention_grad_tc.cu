@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) grad_keys_tc_kernel(RelParams
             const int h = h0 + g / per_head, i0 = (first + g % per_head) * 128, i = i0 + r, w0 = i0 + (warp & 3) * 32;
             if (h != filled) {                               // both groups meet at a head's first tile
                 group_barrier(1, 256);
-                fill_bias<kTcMargin>(p, h, bias, 8);
+                fill_bias<kTcMargin>(p, h, bias, 8, (int)(threadIdx.x >> 5));
                 group_barrier(1, 256);
                 filled = h;
             }
