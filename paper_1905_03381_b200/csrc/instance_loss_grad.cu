@@ -48,6 +48,9 @@ struct NatState {
     float m, s;
 };
 __device__ __forceinline__ float exp_from(float x, float m) { return ex2_approx((x - m) * kLog2e); }
+// Below this size of m, 2^(x log2 e - fl(m log2 e)) may stand for it: the rounding of m log2 e is at most 2^-4 (half an ulp below 2^21) and a
+// factor close to one takes it out of sums and gradients.  It doubles with every doubling of m and passes the exponent's range at a few 1e9.
+constexpr float kFusedLimit = 1048576.0f;
 template <int N>
 __device__ __forceinline__ void absorb_nat(NatState& st, const float (&x)[N]) {
     float top = x[0];
@@ -196,7 +199,7 @@ struct RowPart {
             for (int i = 0; i < VE; ++i) m = fmaxf(m, e[k][i]);
         const float ref = m == -INFINITY ? 0.0f : m;
         float s0, s1;
-        if (fabsf(ref) < 1e38f) {
+        if (fabsf(ref) < kFusedLimit) {
             // 2^(x log2 e - fl(m log2 e)): one multiply-add; the rounding of the product is common to all and taken out of the sum and the factor
             const float shift = -ref * kLog2e;
             undo = ex2_approx(-fmaf(ref, kLog2e, shift));
@@ -364,14 +367,14 @@ __device__ __forceinline__ void bulk_s2g(void* dst, const void* src_smem, uint32
 }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
-// 2^((x - m) log2 e) / undo: one multiply-add and the exponential; `undo` takes the rounding of m log2 e out of sums and factors.  Near the
-// type's limits, where that product overflows, the difference is taken first.
+// 2^((x - m) log2 e) / undo: one multiply-add and the exponential; `undo` takes the rounding of m log2 e out of sums and factors.  Where that
+// rounding is no longer small the difference is taken first.
 struct ExpAt {
     float ref, shift, undo;
     bool plain;
     __device__ __forceinline__ explicit ExpAt(float m) {
         ref = m == -INFINITY ? 0.0f : m;
-        plain = !(fabsf(ref) < 1e38f);
+        plain = !(fabsf(ref) < kFusedLimit);
         shift = plain ? 0.0f : -ref * kLog2e;
         undo = plain ? 1.0f : ex2_approx(-fmaf(ref, kLog2e, shift));
     }
