@@ -3,7 +3,8 @@
 // Row cross-entropy  l_r = log sum_c exp(x_rc) - x_{r,y_r}  in a single pass over the row:
 // every thread keeps a running maximum M and a sum S of 2^(t - M) over its elements, with
 // t = x * log2(e), so that sum_c 2^(t_c) = S * 2^M; thread states are merged by warp shuffles
-// (and through shared memory when a CTA shares a row).  For sequence tasks the token rows of
+// (and through shared memory when a CTA shares a row).  A row whose logits are too large for
+// that form (loss_common.cuh: settled) is read a second time once it is done.  For sequence tasks the token rows of
 // a sentence are then summed in row order (fp64 accumulator) by a second small kernel.
 #include "boss_common.cuh"
 #include "loss_common.cuh"
@@ -56,6 +57,38 @@ __device__ __forceinline__ void scan_row(RunState& st, const T* row, int64_t col
     }
 }
 
+// The same with differences first, for logits of any size.  Small code and few registers: it must cost the kernels' ordinary rows nothing.
+template <typename T>
+__device__ __forceinline__ NatState scan_row_wide(const T* row, int64_t cols, int rank, int nthreads) {
+    constexpr int VE = Vec<T>::kElems;
+    NatState st = {-INFINITY, 0.0f};
+    const int head = (int)(((16 - ((uintptr_t)row & 15)) & 15) / sizeof(T));
+    // unit 0: the elements before the first 16-byte boundary, unit u: the VE elements from head + (u - 1) VE on
+#pragma unroll 1
+    for (int64_t c = (int64_t)rank * VE + head - VE; c < cols; c += (int64_t)nthreads * VE) {
+        float x[VE];
+        if (c >= 0 && c + VE <= cols) {
+            Vec<T>::load(row + c, x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) x[e] = c + e >= 0 && c + e < cols ? Vec<T>::one(row + c + e) : -INFINITY;
+        }
+        absorb_nat(st, x);
+    }
+    return st;
+}
+
+// Rows that are to be read again, LPR lanes each (whole warps call).  Everything is looked up anew: nothing of it is kept beside an ordinary row.
+template <typename T, int LPR>
+__device__ __forceinline__ void reread_rows(const LossParams& p, int64_t r, int gl, bool again) {
+    const int64_t src = again ? source_row(p, r) : 0;
+    const T* row = static_cast<const T*>(p.logits) + src * p.row_stride;
+    NatState st = {-INFINITY, 0.0f};
+    if (again) st = scan_row_wide<T>(row, p.cols, gl, LPR);
+    st = group_merge_nat<LPR>(st);
+    if (again && gl == 0) p.out[r] = row_loss(st, Vec<T>::one(row + __ldg(p.labels + src)));
+}
+
 // Short rows: LPR lanes per row, several rows per warp.
 template <typename T, int LPR>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 6 : 4) row_loss_group_kernel(LossParams p) {
@@ -83,6 +116,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 4 ? 6 : 4) row_loss_group_ke
             if (y >= 0) loss = finish_row(st, Vec<T>::one(static_cast<const T*>(p.logits) + src * p.row_stride + y));
             p.out[r] = loss;
         }
+        const bool again = y >= 0 && !settled(st.m, st.s);
+        if (__builtin_expect(__any_sync(0xFFFFFFFFu, again), 0)) reread_rows<T, LPR>(p, r, gl, again);
     }
 }
 
@@ -151,6 +186,8 @@ __global__ void __launch_bounds__(256) row_loss_short_kernel(LossParams p) {
             RunState st = {m * kLog2e, ssum};
             p.out[r] = y >= 0 ? finish_row(st, label_logit) : 0.0f;
         }
+        const bool again = live && y >= 0 && !settled(m * kLog2e, 0.0f);     // the reference is the row's own maximum: the sum is right if that is small
+        if (__builtin_expect(__any_sync(0xFFFFFFFFu, again), 0)) reread_rows<T, LPR>(p, r, gl, again);
     }
 }
 
@@ -162,6 +199,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) row_loss_cta_kernel(L
     constexpr int kRowThreads = THREADS;
     __shared__ RunState warp_state[kRowThreads / 32];
     __shared__ unsigned int s_row[2];
+    __shared__ NatState wide_state[kRowThreads / 32];
+    __shared__ int s_again;                // the last row to read again, or -1; out[] links to the one before until then
     grid_dependency_wait();      // the row count and the logits may come from the previous kernel of the stream
     grid_dependency_release();
     const int64_t rows = effective_rows(p);
@@ -171,6 +210,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) row_loss_cta_kernel(L
     if (threadIdx.x == 0) {
         s_row[0] = blockIdx.x;
         s_row[1] = gridDim.x + atomicAdd(&p.ctl->ticket, 1u);
+        s_again = -1;
     }
     __syncthreads();
     for (int it = 0;; ++it) {
@@ -190,7 +230,31 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) row_loss_cta_kernel(L
         if (warp == 0) {
             RunState t = lane < kRowThreads / 32 ? warp_state[lane] : RunState{-INFINITY, 0.0f};
             t = group_merge<32>(t);
-            if (lane == 0) p.out[r] = y >= 0 ? finish_row(t, Vec<T>::one(row + y)) : 0.0f;
+            if (lane == 0) {
+                float loss = y >= 0 ? finish_row(t, Vec<T>::one(row + y)) : 0.0f;
+                if (y >= 0 && !settled(t.m, t.s)) {
+                    loss = __int_as_float(s_again);
+                    s_again = (int)r;
+                }
+                p.out[r] = loss;
+            }
+        }
+        __syncthreads();
+    }
+    // behind the loop, where it takes no register from it (inside: 340 us instead of 258 for 25,000 x 32,000 bf16)
+    while (s_again >= 0) {
+        const int r = s_again;
+        const int64_t src = source_row(p, r);
+        const T* row = static_cast<const T*>(p.logits) + src * p.row_stride;
+        const NatState st = group_merge_nat<32>(scan_row_wide<T>(row, p.cols, threadIdx.x, kRowThreads));
+        if (lane == 0) wide_state[warp] = st;
+        __syncthreads();
+        if (warp == 0) {
+            const NatState t = group_merge_nat<32>(lane < kRowThreads / 32 ? wide_state[lane] : NatState{-INFINITY, 0.0f});
+            if (lane == 0) {
+                s_again = __float_as_int(p.out[r]);
+                p.out[r] = row_loss(t, Vec<T>::one(row + __ldg(p.labels + src)));
+            }
         }
         __syncthreads();
     }

@@ -42,43 +42,6 @@ __device__ __forceinline__ bool row_factor(const GradParams& p, int64_t n_inst, 
     return true;
 }
 
-// Running maximum and sum of a row in the logits' own scale: exponents are 2^((x - m) log2 e), so that logits near the type's limits do not
-// overflow in a change of base (one subtraction more per element than the loss kernels' fused form; these kernels have the room).
-struct NatState {
-    float m, s;
-};
-__device__ __forceinline__ float exp_from(float x, float m) { return ex2_approx((x - m) * kLog2e); }
-// Below this size of m, 2^(x log2 e - fl(m log2 e)) may stand for it: the rounding of m log2 e is at most 2^-4 (half an ulp below 2^21) and a
-// factor close to one takes it out of sums and gradients.  It doubles with every doubling of m and passes the exponent's range at a few 1e9.
-constexpr float kFusedLimit = 1048576.0f;
-template <int N>
-__device__ __forceinline__ void absorb_nat(NatState& st, const float (&x)[N]) {
-    float top = x[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
-    if (top > st.m) {
-        st.s *= exp_from(st.m, top);       // st.m = -inf gives 0 * 0
-        st.m = top;
-    }
-    const float ref = st.m == -INFINITY ? 0.0f : st.m;      // only -inf so far: every term is 0
-    float a = 0.0f, b = 0.0f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) (e & 1 ? b : a) += exp_from(x[e], ref);
-    st.s += a + b;
-}
-__device__ __forceinline__ NatState merge(const NatState& a, const NatState& b) {
-    const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.0f : m;
-    return NatState{m, a.s * exp_from(a.m, ref) + b.s * exp_from(b.m, ref)};
-}
-template <int WIDTH>
-__device__ __forceinline__ NatState group_merge_nat(NatState st) {
-#pragma unroll
-    for (int o = WIDTH / 2; o > 0; o >>= 1)
-        st = merge(st, NatState{__shfl_xor_sync(0xFFFFFFFFu, st.m, o), __shfl_xor_sync(0xFFFFFFFFu, st.s, o)});
-    return st;
-}
-__device__ __forceinline__ float row_loss(const NatState& st, float label_logit) { return (st.m - label_logit) + lg2_approx(st.s) * kLn2; }
-
 // First sweep: elements rank, rank + nthreads, ... in 16-byte vectors between the row's 16-byte boundaries.
 template <typename T>
 __device__ __forceinline__ void scan_row_nat(NatState& st, const T* row, int64_t cols, int rank, int nthreads) {
@@ -156,6 +119,10 @@ __device__ __forceinline__ void zero_row(T* out, int64_t cols, int rank, int nth
 }
 
 // ------------------------------------------------------------------------------------------- rows in registers
+
+// Below this size of m, 2^(x log2 e - fl(m log2 e)) may stand for it: the rounding of m log2 e is at most 2^-4 (half an ulp below 2^21) and a
+// factor close to one takes it out of sums and gradients.  It doubles with every doubling of m and passes the exponent's range at a few 1e9.
+constexpr float kFusedLimit = 1048576.0f;
 
 // Where a row's 16-byte vectors lie: `head` elements before them, nvec vectors, the rest behind.
 template <typename T>

@@ -1,10 +1,10 @@
 // Pieces shared by the per-instance-loss kernels: the running (max, sum) state of a one-pass
-// log-sum-exp in base 2, its merge, and the label checks (Sec. "Asynchronous joint learning with CPU/GPU": the loss f of each batch instance).
+// log-sum-exp in base 2, its merge, the same for logits of any size, and the label checks (Sec. "Asynchronous joint learning with CPU/GPU": the loss f of each batch instance).
 #pragma once
 
 #include <math.h>
 
-#include "aa_internal.cuh"
+#include "boss_common.cuh"
 
 namespace aa {
 
@@ -26,6 +26,12 @@ struct RunState {
     float m;   // running maximum of t = x*log2(e)
     float s;   // sum of 2^(t - m)
 };
+// The rounding of m (half an ulp) reaches the loss, and what a thread whose logits are all large holds in s is wrong by 2^ of it: too small or infinite
+// from a few 1e9 on, where a share masked by -1e10, say, turned the row into NaN.  Such a share has no weight in a row of ordinary logits unless it is
+// infinite, so a finished row is right as it stands if its maximum is small (the rounding below 2^-14, the loss within 1e-4) and its sum finite.
+// Any other row is read again with differences first (NatState).
+constexpr float kFusedMax2 = 1024.0f;
+__device__ __forceinline__ bool settled(float m, float s) { return fabsf(m) < kFusedMax2 && s < INFINITY; }
 
 __device__ __forceinline__ void absorb(RunState& st, const float* t, int n) {
     float vmax = t[0];
@@ -110,6 +116,40 @@ __device__ __forceinline__ RunState group_merge(RunState st) {
 __device__ __forceinline__ float finish_row(const RunState& st, float label_logit) {
     return (st.m + lg2_approx(st.s)) * kLn2 - label_logit;
 }
+
+// Running maximum and sum of a row in the logits' own scale: exponents are 2^((x - m) log2 e), right for logits of any size; one subtraction more
+// per element than RunState's fused form.
+struct NatState {
+    float m, s;
+};
+__device__ __forceinline__ float exp_from(float x, float m) { return ex2_approx((x - m) * kLog2e); }
+template <int N>
+__device__ __forceinline__ void absorb_nat(NatState& st, const float (&x)[N]) {
+    float top = x[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
+    if (top > st.m) {
+        st.s *= exp_from(st.m, top);       // st.m = -inf gives 0 * 0
+        st.m = top;
+    }
+    const float ref = st.m == -INFINITY ? 0.0f : st.m;      // only -inf so far: every term is 0
+    float a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) (e & 1 ? b : a) += exp_from(x[e], ref);
+    st.s += a + b;
+}
+__device__ __forceinline__ NatState merge(const NatState& a, const NatState& b) {
+    const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.0f : m;
+    return NatState{m, a.s * exp_from(a.m, ref) + b.s * exp_from(b.m, ref)};
+}
+template <int WIDTH>
+__device__ __forceinline__ NatState group_merge_nat(NatState st) {
+#pragma unroll
+    for (int o = WIDTH / 2; o > 0; o >>= 1)
+        st = merge(st, NatState{__shfl_xor_sync(0xFFFFFFFFu, st.m, o), __shfl_xor_sync(0xFFFFFFFFu, st.s, o)});
+    return st;
+}
+__device__ __forceinline__ float row_loss(const NatState& st, float label_logit) { return (st.m - label_logit) + lg2_approx(st.s) * kLn2; }
 
 __device__ __forceinline__ int64_t effective_rows(const LossParams& p) {
     int64_t rows = p.rows;

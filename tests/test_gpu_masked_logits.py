@@ -94,3 +94,41 @@ def test_loss_gradient_of_classes_masked_by_a_finite_value(aa, dtype, cols):
 def test_loss_gradient_of_shifted_rows(aa, dtype, cols):
     for shift in SHIFTS:
         check_gradient(aa, *shifted_rows(cols, dtype, shift), dtype)
+
+
+def check_instance_losses(aa, x, y):
+    rows, labels = len(y), torch.tensor(y, device=DEV)
+    out = torch.full((rows,), 7.0, device=DEV)
+    aa.aa_instance_loss(B.logits_desc(x), labels, out)
+    check_losses(out, x, y)
+    order = np.random.default_rng(rows).permutation(rows).astype(np.int32)
+    listed = torch.full((rows,), 7.0, device=DEV)
+    aa.aa_instance_loss_rows(B.logits_desc(x), labels, torch.tensor(order, device=DEV), listed)
+    check_losses(listed, x[torch.tensor(order, device=DEV).long()], y[order])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_instance_loss_of_classes_masked_by_a_finite_value(aa, dtype, cols):
+    for value in VALUES:
+        check_instance_losses(aa, *masked_rows(cols, dtype, value_of(value, dtype)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_instance_loss_of_shifted_rows(aa, dtype, cols):
+    for shift in SHIFTS:
+        check_instance_losses(aa, *shifted_rows(cols, dtype, shift))
+
+
+def test_instance_loss_of_rows_of_nothing_but_infinities_stays_undefined(aa):
+    """As before: no class left is NaN, a class of +inf is NaN, a label of -inf is +inf."""
+    for cols in WIDTHS:
+        x = W.normal((3, cols), 1.0, 5, F32, DEV)
+        x[0] = -float("inf")
+        x[1, 0] = float("inf")
+        x[2, 1] = -float("inf")
+        out = torch.empty(3, device=DEV)
+        aa.aa_instance_loss(B.logits_desc(x), torch.tensor([0, 1, 1], dtype=torch.int32, device=DEV), out)
+        got = f64(out)
+        assert np.isnan(got[0]) and np.isnan(got[1]) and np.isposinf(got[2])
