@@ -405,7 +405,7 @@ typedef struct {
  *   offsets != NULL: offsets[n_seg + 1] ascending; instance s is the rows [offsets[s], offsets[s+1]); M = min(*count_dev, n_seg).
  * Rows of no counted instance are left untouched.  Offsets outside [0, rows] or descending latch AA_ERR_BAD_INDEX; rows that they
  * would misplace are left untouched or take the draws of a neighbouring instance, nothing outside the matrices is accessed.
- * x, residual and out have one dtype and shape, strides of their own; out may be x or residual itself, not a shifted overlap.
+ * x, residual and out have one dtype and shape (at most 2^31 - 1024 columns, else AA_ERR_UNSUPPORTED), strides of their own; out may be x or residual itself, not a shifted overlap.
  */
 aa_status aa_dropout(aa_ctx* ctx, const aa_rows* x, const aa_dropout_rule* rule, const int32_t* offsets, int64_t n_seg,
                      const int32_t* count_dev, const aa_rows* residual, const aa_rows* out);

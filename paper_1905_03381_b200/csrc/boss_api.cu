@@ -141,6 +141,7 @@ aa_status aa_dropout(aa_ctx* ctx, const aa_rows* x, const aa_dropout_rule* rule,
     if (!ctx || !rule || check_rows(x) != AA_OK || check_rows(out) != AA_OK || !same_shape(*x, *out)) return AA_ERR_INVALID_ARG;
     if (residual && (check_rows(residual) != AA_OK || !same_shape(*x, *residual))) return AA_ERR_INVALID_ARG;
     if (offsets ? n_seg < 0 : n_seg != 0) return AA_ERR_INVALID_ARG;
+    if (x->cols > kMaxDropoutCols) return AA_ERR_UNSUPPORTED;
     DropParams p = {};
     if (!make_drop_rule(rule, p.rule)) return AA_ERR_INVALID_ARG;
     if (x->rows == 0 || (offsets && n_seg == 0)) return AA_OK;

@@ -20,6 +20,9 @@ struct RowsArg {             // one matrix operand
     int64_t stride;          // elements
 };
 
+// Column numbers are 32 bits and those of the last unit's idle lanes pass the row's end, by less than 1,024.
+constexpr int64_t kMaxDropoutCols = 0x7FFFFFFFll - 1023;
+
 struct DropParams {
     RowsArg x, res, out;     // res.data nullable
     int64_t rows, cols;

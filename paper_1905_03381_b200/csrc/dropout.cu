@@ -224,6 +224,7 @@ __global__ void __launch_bounds__(kThreads, 3) dropout_kernel(DropParams p, int 
 template <typename T, int LPR>
 aa_status launch(aa_ctx_impl* c, const DropParams& p, bool vec) {
     const int kGroups = vec ? kGroupsOf<T, true> : kGroupsOf<T, false>;
+    static_assert(LPR * 2 * 8 + 8 <= 1024, "kMaxDropoutCols leaves room for a unit behind the last column");
     const void* kernel = vec ? (const void*)dropout_kernel<T, LPR, true> : (const void*)dropout_kernel<T, LPR, false>;
     const int64_t groups = (p.cols + 7) / 8;
     int chunks = (int)((groups + LPR * kGroups - 1) / (LPR * kGroups));

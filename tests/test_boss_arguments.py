@@ -1,0 +1,37 @@
+"""Host-side refusals of the Boss operators that need no GPU: the calls end before anything is enqueued."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_1905_03381_b200 import binding as B
+from paper_1905_03381_b200 import build
+
+# the descriptors below hold no real addresses, so no call may get as far as a device
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="refusals are looked at where nothing can run")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return B.lib()
+
+
+def matrix(rows, cols):
+    return B.aa_rows(1 << 20, B.AA_BF16, 0, rows, cols, cols)
+
+
+def test_dropout_of_rows_whose_column_numbers_do_not_fit(lib):
+    """A lane's column number may pass the row's end by a unit of the kernel; it has to stay below 2^31."""
+    ctx = ctypes.create_string_buffer(1 << 16)
+    rule = B.aa_dropout_rule()
+    rule.p = 0.5
+
+    def status(cols):
+        m = matrix(1, cols)
+        return lib.aa_dropout(ctx, ctypes.byref(m), ctypes.byref(rule), None, 0, None, None, ctypes.byref(m))
+
+    for cols in (2**31 - 16, 2**31 - 600, 2**31 - 1023):
+        assert status(cols) == B.AA_ERR_UNSUPPORTED
+    assert status(2**31) == status(0) == B.AA_ERR_INVALID_ARG
+    assert status(2**31 - 1024) not in (B.AA_ERR_UNSUPPORTED, B.AA_ERR_INVALID_ARG)
