@@ -43,6 +43,9 @@ aa_status launch_segment_sum(aa_ctx_impl* c, const float* row_loss, const int32_
 
 #ifdef __CUDACC__
 
+// The kernels that include this may start while the launch before theirs still runs (grid_dependency_wait).  What that launch may have written - lists,
+// counts, offsets, weights, row statistics - is read by ordinary loads: those of the read-only path need memory that nothing writes meanwhile.
+
 struct Words4 {
     uint32_t w[4];
 };
@@ -68,7 +71,7 @@ __device__ __forceinline__ uint2 id_key(const DropRule& r, int64_t id) {
     return make_uint2(w.w[2], w.w[3]);
 }
 
-__device__ __forceinline__ int64_t instance_row(const DropRule& r, int64_t instance) { return r.row_idx ? (int64_t)__ldg(r.row_idx + instance) : instance; }
+__device__ __forceinline__ int64_t instance_row(const DropRule& r, int64_t instance) { return r.row_idx ? (int64_t)r.row_idx[instance] : instance; }
 __device__ __forceinline__ uint2 instance_key(const DropRule& r, int64_t instance) { return id_key(r, r.id_base + instance_row(r, instance)); }
 
 __device__ __forceinline__ Words4 draw_block(const DropRule& r, uint2 key, uint64_t block) {
@@ -78,28 +81,28 @@ __device__ __forceinline__ Words4 draw_block(const DropRule& r, uint2 key, uint6
 // min(*count_dev, n), or n.
 __device__ __forceinline__ int64_t counted(const int32_t* count_dev, int64_t n) {
     if (!count_dev) return n;
-    const int64_t c = __ldg(count_dev);
+    const int64_t c = *count_dev;
     return c < 0 ? 0 : (c < n ? c : n);
 }
 
 // The last segment s in [0, n) with offsets[s] <= r (0 if there is none); reads offsets[0..n-1] only, whatever they hold.
-__device__ __forceinline__ int64_t find_segment(const int32_t* __restrict__ offsets, int64_t n, int64_t r) {
+__device__ __forceinline__ int64_t find_segment(const int32_t* offsets, int64_t n, int64_t r) {
     int64_t lo = 0, hi = n;          // offsets[lo] <= r (or lo = 0), offsets[hi] > r (or hi = n)
     while (hi - lo > 1) {
         const int64_t mid = (lo + hi) >> 1;
-        if ((int64_t)__ldg(offsets + mid) <= r) lo = mid; else hi = mid;
+        if ((int64_t)offsets[mid] <= r) lo = mid; else hi = mid;
     }
     return lo;
 }
 
 // The same by WIDTH lanes together (lane `l` of them, `mask` theirs): WIDTH probes a round instead of one.
 template <int WIDTH>
-__device__ __forceinline__ int64_t find_segment_lanes(const int32_t* __restrict__ offsets, int64_t n, int64_t r, int l, unsigned mask) {
+__device__ __forceinline__ int64_t find_segment_lanes(const int32_t* offsets, int64_t n, int64_t r, int l, unsigned mask) {
     int64_t lo = 0, hi = n;
     while (hi - lo > 1) {
         const int64_t step = (hi - lo + WIDTH) / (WIDTH + 1);      // probes lo + step, lo + 2 step, ...
         const int64_t at = lo + (int64_t)(l + 1) * step;
-        const bool below = at < hi && (int64_t)__ldg(offsets + at) <= r;
+        const bool below = at < hi && (int64_t)offsets[at] <= r;
         const int count = __popc(__ballot_sync(mask, below) & mask);  // offsets ascend: the probes that hold are the first ones
         const int64_t next = lo + (int64_t)(count + 1) * step;
         lo += (int64_t)count * step;
@@ -109,10 +112,10 @@ __device__ __forceinline__ int64_t find_segment_lanes(const int32_t* __restrict_
 }
 
 // One CTA looks every counted segment's offsets over.
-__device__ __forceinline__ void check_offsets(Control* ctl, const int32_t* __restrict__ offsets, int64_t n, int64_t rows) {
+__device__ __forceinline__ void check_offsets(Control* ctl, const int32_t* offsets, int64_t n, int64_t rows) {
     bool bad = false;
     for (int64_t s = threadIdx.x; s < n; s += blockDim.x) {
-        const int a = __ldg(offsets + s), b = __ldg(offsets + s + 1);
+        const int a = offsets[s], b = offsets[s + 1];
         bad |= a < 0 || b < a || b > rows;
     }
     if (bad) latch(ctl, AA_ERR_BAD_INDEX);

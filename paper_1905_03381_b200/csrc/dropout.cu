@@ -54,7 +54,7 @@ struct Run {
     int64_t u, u_end, row;
     int chunk, chunks;
     int64_t inst, first, last;             // rows [first, last)
-    int64_t next_last, next_row;           // what the next instance will need, on its way
+    int32_t next_last, next_row;           // what the next instance will need of the lists, on its way
     uint2 key;
     __device__ __forceinline__ void next() {
         ++u;
@@ -72,24 +72,24 @@ struct Run {
             ++inst;
             first = last;
             last = p.offsets ? next_last : row + 1;
-            stored = next_row;
+            stored = p.rule.row_idx ? (int64_t)next_row : inst;
         } else {
             inst = p.offsets ? find_segment_lanes<LPR>(p.offsets, n_inst, row, sl, mask) : row;
-            first = p.offsets ? (int64_t)__ldg(p.offsets + inst) : row;
-            last = p.offsets ? (int64_t)__ldg(p.offsets + inst + 1) : row + 1;
+            first = p.offsets ? (int64_t)p.offsets[inst] : row;
+            last = p.offsets ? (int64_t)p.offsets[inst + 1] : row + 1;
             stored = instance_row(p.rule, inst);
         }
         if (inst >= n_inst) return false;
         while (last <= row) {              // empty segments
             if (++inst >= n_inst) return false;
             first = last;
-            last = __ldg(p.offsets + inst + 1);
+            last = p.offsets[inst + 1];
             stored = instance_row(p.rule, inst);
         }
         key = id_key(p.rule, p.rule.id_base + stored);
         if (inst + 1 < n_inst) {
-            if (p.offsets) next_last = __ldg(p.offsets + inst + 2);
-            next_row = instance_row(p.rule, inst + 1);
+            if (p.offsets) next_last = p.offsets[inst + 2];
+            if (p.rule.row_idx) next_row = p.rule.row_idx[inst + 1];
         }
         return true;
     }
@@ -114,7 +114,8 @@ __global__ void __launch_bounds__(kThreads, 3) dropout_kernel(DropParams p, int 
     run.chunk = (int)(run.u - run.row * chunks);
     run.chunks = chunks;
     run.inst = -1;
-    run.first = run.last = run.next_last = run.next_row = 0;
+    run.first = run.last = 0;
+    run.next_last = run.next_row = 0;
     run.key = make_uint2(0, 0);
     const int cols = (int)p.cols, groups = (cols + 7) >> 3;
     const uint32_t top = p.rule.thr << 16;

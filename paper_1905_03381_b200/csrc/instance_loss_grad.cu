@@ -32,13 +32,13 @@ __device__ __forceinline__ bool row_factor(const GradParams& p, int64_t n_inst, 
         if (n_inst == 0) return false;
         inst = find_segment(p.offsets, n_inst, r);
         // empty segments share their start with the next one; the search ends at the last of them
-        if (r < __ldg(p.offsets + inst) || r >= __ldg(p.offsets + inst + 1)) return false;
+        if (r < p.offsets[inst] || r >= p.offsets[inst + 1]) return false;
     } else if (r >= n_inst) {
         return false;
     }
     g = p.scale;
     if (p.mean) g = g / (float)n_inst;
-    if (p.weight) g *= __ldg(p.weight + inst);
+    if (p.weight) g *= p.weight[inst];
     return true;
 }
 
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(kRingThreads + 64, 1) row_grad_ring_kernel(Gra
         if (p.offsets && blockIdx.x == 0) {
             bool bad = false;
             for (int64_t s = lane; s < n_inst; s += 32) {
-                const int a = __ldg(p.offsets + s), b = __ldg(p.offsets + s + 1);
+                const int a = p.offsets[s], b = p.offsets[s + 1];
                 bad |= a < 0 || b < a || b > p.loss.rows;
             }
             if (bad) latch(p.loss.ctl, AA_ERR_BAD_INDEX);

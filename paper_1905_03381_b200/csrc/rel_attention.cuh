@@ -73,7 +73,7 @@ struct Seq {
 // Sequence s; false: not counted, or its offsets are bad (latched).
 __device__ __forceinline__ bool load_seq(const RelParams& p, int64_t s, Seq& q) {
     if (s >= counted(p.count_dev, p.n_seq)) return false;
-    const int a = __ldg(p.q_off + s), b = __ldg(p.q_off + s + 1), c = __ldg(p.k_off + s), d = __ldg(p.k_off + s + 1);
+    const int a = p.q_off[s], b = p.q_off[s + 1], c = p.k_off[s], d = p.k_off[s + 1];
     if (a < 0 || b < a || b > p.q_rows || b - a > p.max_q || c < 0 || d < c || d > p.k_rows || d - c > p.max_k) {
         latch(p.ctl, AA_ERR_BAD_INDEX);
         return false;
@@ -95,7 +95,7 @@ __device__ __forceinline__ void fill_bias(const RelParams& p, int h, float* bias
     for (int b0 = 0; b0 < p.buckets; b0 += 32) {
         float v = 0.0f;                                                 // a lane per bucket: one trip to memory for 32 of them
         if (b0 + lane < p.buckets) {
-            const float x = __ldg(p.table + (int64_t)(b0 + lane) * p.heads + h);
+            const float x = p.table[(int64_t)(b0 + lane) * p.heads + h];
             v = isinf(x) || isnan(x) ? x : fminf(fmaxf(x * kAttnLog2e, -3.0e38f), 3.0e38f);
         }
         const int b1 = min(p.buckets - b0, 32);

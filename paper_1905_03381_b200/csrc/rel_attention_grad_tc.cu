@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) grad_keys_tc_kernel(RelParams
                 filled = h;
             }
             if ((g & 1) != grp) continue;
-            const float4 st = i < s.lq ? __ldg(p.stats + (int64_t)h * p.q_rows + s.q0 + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            const float4 st = i < s.lq ? p.stats[(int64_t)h * p.q_rows + s.q0 + i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (!mbar_wait(&ctl.s_full[grp], (uint32_t)((g / 2) & 1), abort_flag)) *abort_flag = 1, ok = false;
             tc_fence_after_sync();
             __syncwarp();

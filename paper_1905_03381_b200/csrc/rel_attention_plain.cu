@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) forward_kernel(RelParams p, int tile
 // dq, the row statistics (m, 1 / l, D) and this CTA's share of the table's gradient.  grid (parts, heads): a CTA walks query tiles of
 // its head.  First pass: m, l and D = sum_j p_ij dp_ij from unrounded probabilities; second pass: dS, its diagonal sums, dq.
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads) grad_q_kernel(RelParams p, int tiles) {
+__global__ void __launch_bounds__(kThreads, DT == 64 ? 2 : 1) grad_q_kernel(RelParams p, int tiles) {
     using G = Geo<DT>;
     extern __shared__ float4 smem4[];
     float* Qs = reinterpret_cast<float*>(smem4);
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kThreads) grad_q_kernel(RelParams p, int tiles
 
 // dk and dv of one key tile and key head: the query heads that share it and the query tiles that see it, in order.
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads) grad_kv_kernel(RelParams p, int tiles) {
+__global__ void __launch_bounds__(kThreads, DT == 64 ? 2 : 1) grad_kv_kernel(RelParams p, int tiles) {
     using G = Geo<DT>;
     extern __shared__ float4 smem4[];
     float* Qs = reinterpret_cast<float*>(smem4);

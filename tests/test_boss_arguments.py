@@ -35,3 +35,19 @@ def test_dropout_of_rows_whose_column_numbers_do_not_fit(lib):
         assert status(cols) == B.AA_ERR_UNSUPPORTED
     assert status(2**31) == status(0) == B.AA_ERR_INVALID_ARG
     assert status(2**31 - 1024) not in (B.AA_ERR_UNSUPPORTED, B.AA_ERR_INVALID_ARG)
+
+
+def test_kernels_that_start_early_read_what_the_call_before_may_write_by_ordinary_loads():
+    """Every kernel of the Boss operators may start while the launch before it still runs and waits for it on the device.  Loads of the read-only path
+    are defined for memory that nothing writes while the kernel lives, and may be moved above that wait; the lists, counts, offsets, weights and row
+    statistics that the launch before may have written have to be read by ordinary loads."""
+    import glob
+    import os
+    import re
+
+    files = [os.path.join(build.CSRC, f) for f in ("boss_common.cuh", "dropout.cu", "instance_loss_grad.cu")] + glob.glob(os.path.join(build.CSRC, "rel_attention*"))
+    assert len(files) >= 11
+    for path in files:
+        for n, line in enumerate(open(path), 1):
+            code = line.split("//")[0]
+            assert not re.search(r"__ldg\(|\.nc\b|__restrict__", code), f"{os.path.basename(path)}:{n}: {line.strip()}"
