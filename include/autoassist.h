@@ -405,7 +405,8 @@ typedef struct {
  *   offsets != NULL: offsets[n_seg + 1] ascending; instance s is the rows [offsets[s], offsets[s+1]); M = min(*count_dev, n_seg).
  * Rows of no counted instance are left untouched.  Offsets outside [0, rows] or descending latch AA_ERR_BAD_INDEX; rows that they
  * would misplace are left untouched or take the draws of a neighbouring instance, nothing outside the matrices is accessed.
- * x, residual and out have one dtype and shape (at most 2^31 - 1024 columns, else AA_ERR_UNSUPPORTED), strides of their own; out may be x or residual itself, not a shifted overlap.
+ * x, residual and out have one dtype and shape (at most 2^31 - 1024 columns, else AA_ERR_UNSUPPORTED), strides of their own; out
+ * may be x or residual itself, or lie beside them in one array (column slices of a matrix), but have no other element in common.
  */
 aa_status aa_dropout(aa_ctx* ctx, const aa_rows* x, const aa_dropout_rule* rule, const int32_t* offsets, int64_t n_seg,
                      const int32_t* count_dev, const aa_rows* residual, const aa_rows* out);
@@ -420,7 +421,7 @@ typedef enum { AA_REDUCE_SUM = 0, AA_REDUCE_MEAN = 1 } aa_reduce_mode;
  * Rows with a label < 0 (padding) get a zero gradient; labels >= cols too, and latch AA_ERR_BAD_INDEX.
  *   offsets / n_seg: as in aa_instance_loss; count_dev counts instances, that is rows without offsets and segments with them.
  * Rows of no counted instance are left untouched.  out_grad has the logits' dtype and shape; it may be the logits' own memory
- * (same pointer and stride).  Offsets that descend or leave [0, rows] latch AA_ERR_BAD_INDEX; the rows concerned are then unspecified.
+ * (same pointer and stride) or lie beside them in one array, but have no other element in common.  Offsets that descend or leave [0, rows] latch AA_ERR_BAD_INDEX; the rows concerned are then unspecified.
  */
 aa_status aa_instance_loss_grad(aa_ctx* ctx, const aa_logits* logits, const int32_t* labels, const int32_t* offsets, int64_t n_seg,
                                 const int32_t* count_dev, const float* weight, float scale, int32_t reduce_mode,
