@@ -437,6 +437,8 @@ aa_status aa_instance_loss_grad(aa_ctx* ctx, const aa_logits* logits, const int3
  *
  * Tokens: element (token t, head h, e) at data + t*token_stride + h*head_stride + e, so that q, k and v may be views of one packed
  * projection.  Sequence s owns the query tokens [q_offsets[s], q_offsets[s+1]) and the key tokens [k_offsets[s], k_offsets[s+1]).
+ * What a call writes (out; dq, dk, dv) must have no element in common with its other operands, except that out may be q itself (same pointer
+ * and strides); views of one packed array with the same strides are told apart exactly, other interleaving address ranges are refused.
  * max_q, max_k: HOST upper bounds of one sequence's lengths.  A sequence that breaks them, or whose offsets descend or leave
  * [0, q_rows] / [0, k_rows], latches AA_ERR_BAD_INDEX and is skipped.  M = min(*count_dev, n_seq) sequences are evaluated; token
  * rows of no evaluated sequence are left untouched.

@@ -91,6 +91,9 @@ aa_status check_tokens(const aa_tokens& t, int64_t es, int64_t rows, int heads, 
 
 TokArg tok(const aa_tokens& t) { return TokArg{t.data, t.token_stride, t.head_stride}; }
 
+Extent query_extent(const aa_tokens& t, const RelParams& p) { return Extent{t.data, p.q_rows, t.token_stride, p.heads, t.head_stride, p.dim}; }
+Extent key_extent(const aa_tokens& t, const RelParams& p) { return Extent{t.data, p.k_rows, t.token_stride, p.kv_heads, t.head_stride, p.dim}; }
+
 }  // namespace
 
 aa_status make_rel_params(const aa_attn* a, const aa_rel_bias* b, const aa_dropout_rule* d, RelParams& p) {
@@ -223,6 +226,10 @@ aa_status aa_rel_attention(aa_ctx* ctx, const aa_attn* attn, const aa_rel_bias* 
     if (st != AA_OK) return st;
     const int64_t es = attn->dtype == AA_BF16 ? 2 : 4;
     if ((st = check_tokens(*out, es, p.q_rows, p.heads, p.dim, true)) != AA_OK) return st;
+    // the output may take the queries' place: whoever writes a row has read it, and nobody else reads it
+    const Extent o = query_extent(*out, p);
+    const bool in_place = out->data == attn->q.data && (p.q_rows <= 1 || out->token_stride == attn->q.token_stride) && (p.heads == 1 || out->head_stride == attn->q.head_stride);
+    if ((!in_place && !apart(o, query_extent(attn->q, p), es)) || !apart(o, key_extent(attn->k, p), es) || !apart(o, key_extent(attn->v, p), es)) return AA_ERR_INVALID_ARG;
     if (p.n_seq == 0 || p.max_q == 0) return AA_OK;
     aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
     p.out = tok(*out);
@@ -250,6 +257,15 @@ aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_b
     if ((st = check_tokens(*dout, es, p.q_rows, p.heads, p.dim, false)) != AA_OK || (st = check_tokens(*dq, es, p.q_rows, p.heads, p.dim, true)) != AA_OK ||
         (st = check_tokens(*dk, es, p.k_rows, p.kv_heads, p.dim, true)) != AA_OK || (st = check_tokens(*dv, es, p.k_rows, p.kv_heads, p.dim, true)) != AA_OK)
         return st;
+    // gradients are written while operands are still to be read (those of long sequences by a later kernel): nothing in common
+    const Extent in[4] = {query_extent(attn->q, p), key_extent(attn->k, p), key_extent(attn->v, p), query_extent(*dout, p)};
+    const Extent to[3] = {query_extent(*dq, p), key_extent(*dk, p), key_extent(*dv, p)};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < 4; ++j)
+            if (!apart(to[i], in[j], es)) return AA_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (!apart(to[i], to[j], es)) return AA_ERR_INVALID_ARG;
+    }
     size_t need = 0;
     if ((st = aa_rel_attention_scratch_bytes(attn, bias, &need)) != AA_OK) return st;
     if (need > 0 && (!scratch || (uintptr_t)scratch % 256)) return AA_ERR_INVALID_ARG;

@@ -1,4 +1,5 @@
 """What the Boss operators accept as memory of their operands: views of one packed array, the operand itself where the call says so, no overlap."""
+import numpy as np
 import pytest
 import torch
 
@@ -20,10 +21,88 @@ def aa():
     ctx.close()
 
 
+def offs(lens):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=torch.int32, device=DEV)
+
+
 def refused(call):
     with pytest.raises(B.AutoAssistError) as e:
         call()
     assert e.value.status == B.AA_ERR_INVALID_ARG
+
+
+# ---- attention
+
+def problem(dtype, lens, heads=4, kv=2, dim=64):
+    n = sum(lens)
+    q, k, v, g = (W.normal((n, h, dim), 1.0, 50 + i, dtype, DEV) for i, h in enumerate((heads, kv, kv, heads)))
+    return q, k, v, g, B.attention(q, k, v, offs(lens), max_q=max(lens), max_k=max(lens), causal=True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens", [[9, 40, 3], [300, 20]])
+def test_attention_output_may_be_the_queries_themselves_and_no_other_operand(aa, dtype, lens):
+    q, k, v, g, attn = problem(dtype, lens)
+    want = torch.empty_like(q)
+    aa.aa_rel_attention(attn, want)
+    aa.aa_rel_attention(attn, q)
+    assert torch.equal(q, want)
+    q, k, v, g, attn = problem(dtype, lens, kv=4)
+    for out in (k, v):
+        refused(lambda: aa.aa_rel_attention(attn, out))
+    flat = torch.zeros(q.numel() + 64, dtype=dtype, device=DEV)
+    shifted = B.attention(flat[:-64].view(q.shape), k, v, offs(lens), causal=True)
+    refused(lambda: aa.aa_rel_attention(shifted, flat[64:].view(q.shape)))           # one head further on
+
+
+def test_one_new_token_over_its_own_queries(aa):
+    q, kv = W.normal((3, 8, 64), 1.0, 1, BF16, DEV), W.normal((900, 2, 2, 64), 1.0, 2, BF16, DEV)
+    attn = B.attention(q, kv[:, 0], kv[:, 1], offs([1, 1, 1]), offs([700, 150, 50]), 1, 700)
+    want = torch.empty_like(q)
+    aa.aa_rel_attention(attn, want)
+    aa.aa_rel_attention(attn, q)
+    assert torch.equal(q, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens", [[9, 40, 3], [300, 20]])
+def test_attention_gradients_overlap_nothing(aa, dtype, lens):
+    q, k, v, g, attn = problem(dtype, lens, kv=4)
+    scratch = aa.rel_attention_scratch(attn)
+    fresh = lambda: [torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)]  # noqa: E731
+    for at in range(3):
+        for other in (q, k, v, g):
+            grads = fresh()
+            grads[at] = other
+            refused(lambda: aa.aa_rel_attention_grad(attn, g, *grads, scratch))
+    grads = fresh()
+    for at in range(3):
+        twice = list(grads)
+        twice[at] = grads[at - 1]
+        refused(lambda: aa.aa_rel_attention_grad(attn, g, *twice, scratch))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens", [[9, 40, 3], [300, 20], [1]])
+@pytest.mark.parametrize("head_major", [False, True])
+def test_gradients_as_views_of_one_packed_array(aa, dtype, lens, head_major):
+    """q, k, v, dout, out and the gradients interleaved in one array: nothing overlaps, nothing is refused."""
+    heads, kv, dim, n = 4, 2, 64, sum(lens)
+    q, k, v, g, attn = problem(dtype, lens)
+    out, dq, dk, dv = torch.empty_like(q), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    aa.aa_rel_attention(attn, out)
+    aa.aa_rel_attention_grad(attn, g, dq, dk, dv, aa.rel_attention_scratch(attn))
+    sizes = [heads, kv, kv, heads, heads, heads, kv, kv]
+    buf = torch.zeros((sum(sizes), n, dim) if head_major else (n, sum(sizes), dim), dtype=dtype, device=DEV)
+    views = [x.transpose(0, 1) for x in buf.split(sizes, 0)] if head_major else buf.split(sizes, 1)
+    for view, x in zip(views, (q, k, v, g)):
+        view.copy_(x)
+    packed = B.attention(*views[:3], offs(lens), max_q=max(lens), max_k=max(lens), causal=True)
+    aa.aa_rel_attention(packed, views[4])
+    aa.aa_rel_attention_grad(packed, views[3], *views[5:], aa.rel_attention_scratch(packed))
+    torch.cuda.synchronize()
+    for view, x in zip(views[4:], (out, dq, dk, dv)):
+        assert torch.equal(view, x)
 
 
 # ---- matrices
