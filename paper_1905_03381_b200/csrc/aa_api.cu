@@ -55,6 +55,11 @@ struct OccEntry {
     int ctas;
 };
 constexpr int kOccSlots = 64;
+struct SmemEntry {
+    const void* kernel;
+    size_t limit;
+};
+constexpr int kSmemSlots = 64;
 
 }  // namespace
 
@@ -64,6 +69,8 @@ struct aa_ctx {
     aa::aa_ctx_impl impl;
     aa::OccEntry occ[aa::kOccSlots];
     int occ_used;
+    aa::SmemEntry smem[aa::kSmemSlots];
+    int smem_used;
 };
 
 namespace aa {
@@ -80,6 +87,22 @@ int resident_ctas(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_sm
     const int ctas = per_sm * c->sm_count;
     if (ctx->occ_used < kOccSlots) ctx->occ[ctx->occ_used++] = OccEntry{kernel, threads, dyn_smem, ctas};
     return ctas;
+}
+
+// The limit belongs to the function, not to the context: set to each call's own size, one host thread's call lowered it between another's setting and
+// launch, which was then refused.  It is set to all that the device grants, once per context and kernel.
+aa_status allow_smem(aa_ctx_impl* c, const void* kernel, size_t dyn_smem) {
+    aa_ctx* ctx = reinterpret_cast<aa_ctx*>(c);
+    for (int i = 0; i < ctx->smem_used; ++i)
+        if (ctx->smem[i].kernel == kernel) return dyn_smem <= ctx->smem[i].limit ? AA_OK : AA_ERR_CUDA;
+    int most = 0;
+    cudaFuncAttributes attr;
+    if (cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, c->device) != cudaSuccess || cudaFuncGetAttributes(&attr, kernel) != cudaSuccess)
+        return AA_ERR_CUDA;
+    const int limit = most - (int)attr.sharedSizeBytes;
+    if (limit < 0 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return AA_ERR_CUDA;
+    if (ctx->smem_used < kSmemSlots) ctx->smem[ctx->smem_used++] = SmemEntry{kernel, (size_t)limit};
+    return dyn_smem <= (size_t)limit ? AA_OK : AA_ERR_CUDA;
 }
 
 cudaError_t launch_overlapped(aa_ctx_impl* c, const void* kernel, dim3 grid, dim3 block, void** args, size_t smem, bool cooperative) {

@@ -294,6 +294,9 @@ cudaError_t launch_overlapped(aa_ctx_impl* c, const void* kernel, dim3 grid, dim
 aa_status launch_conv_pool_features(aa_ctx_impl* c, const void* x, int dtype, int64_t n, int64_t row_stride, const aa_conv& cv,
                                     float* phi, int64_t phi_stride);
 
+// Lets launches of `kernel` through this context have dyn_smem bytes of dynamic shared memory; an error if the device has not that much.
+aa_status allow_smem(aa_ctx_impl* c, const void* kernel, size_t dyn_smem);
+
 // Persistent-grid size for a kernel: CTAs that fit on the device at once.
 int resident_ctas(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_smem);
 

@@ -353,7 +353,7 @@ aa_status launch_assistant_step_dense(aa_ctx_impl* c, const DenseFeat& f, const 
     const void* kernel = f.dtype == AA_BF16 ? (vec ? pick_dense_kernel<uint16_t, true>(ci) : pick_dense_kernel<uint16_t, false>(ci))
                                             : (vec ? pick_dense_kernel<float, true>(ci) : pick_dense_kernel<float, false>(ci));
     if (smem > 48 * 1024 &&
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        allow_smem(c, kernel, smem) != AA_OK)
         return AA_ERR_CUDA;
     int grid = resident_ctas(c, kernel, kStepThreads, smem);
     if (grid <= 0) return AA_ERR_CUDA;

@@ -443,7 +443,7 @@ aa_status launch_assistant_grad_dense_scored(aa_ctx_impl* c, StepParams& p, int*
     if ((int64_t)grid * (p.d_pad + 1) > c->partial_floats) return AA_ERR_UNSUPPORTED;
     p.loss_sums = nullptr;
     const void* kernel = (const void*)linear_grad_scored_kernel;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     void* args[] = {&p, &g};
     // cooperative: the CTAs wait for one another before the update, so all of them must be resident at once
     const cudaError_t le = launch_overlapped(c, kernel, dim3(grid), dim3(kMThreads), args, smem, true);

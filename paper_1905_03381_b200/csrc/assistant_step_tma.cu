@@ -383,7 +383,7 @@ aa_status launch_assistant_grad_dense_tma(aa_ctx_impl* c, StepParams& p, int* pa
     if ((int64_t)grid * (p.d_pad + 1) > c->partial_floats) return AA_ERR_UNSUPPORTED;
 
     const void* kernel = p.f.dtype == AA_BF16 ? pick_grad_kernel<uint16_t>(ci) : pick_grad_kernel<float>(ci);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     void* args[] = {&p, &g};
     if (cudaLaunchKernel(kernel, dim3(grid), dim3(kGradThreads), args, smem, c->stream) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;

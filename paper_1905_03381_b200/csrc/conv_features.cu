@@ -279,7 +279,7 @@ aa_status launch_conv_pool_features(aa_ctx_impl* c, const void* x, int dtype, in
     else
         kernel = cv.ksize == 1 ? (const void*)conv_pool_features_kernel<float, 1>
                  : cv.ksize == 3 ? (const void*)conv_pool_features_kernel<float, 3> : (const void*)conv_pool_features_kernel<float, 5>;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    if (smem > 48 * 1024 && allow_smem(c, kernel, smem) != AA_OK)
         return AA_ERR_CUDA;
     int grid = resident_ctas(c, kernel, kConvThreads, smem);
     if (grid <= 0) return AA_ERR_CUDA;

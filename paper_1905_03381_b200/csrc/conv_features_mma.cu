@@ -348,7 +348,7 @@ aa_status launch_conv_pool_features_mma(aa_ctx_impl* c, const void* x, int dtype
     p.by_width.set((uint32_t)cv.width);
     p.by_strips.set((uint32_t)(cv.width / 16));
     const void* kernel = taps > 16 ? (const void*)conv_pool_mma_kernel<2> : (const void*)conv_pool_mma_kernel<1>;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    if (smem > 48 * 1024 && allow_smem(c, kernel, smem) != AA_OK)
         return AA_ERR_CUDA;
     int grid = resident_ctas(c, kernel, kCmThreads, smem);
     if (grid <= 0) return AA_ERR_CUDA;

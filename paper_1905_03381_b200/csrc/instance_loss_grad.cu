@@ -657,7 +657,7 @@ aa_status launch_ring(aa_ctx_impl* c, GradParams& p) {
     int stages = 208 * 1024 / (stage_vecs * 16);                      // three of 64 KB
     if (stages > kRingMaxStages) stages = kRingMaxStages;
     const size_t smem = (size_t)stages * stage_vecs * 16;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     const int cap = resident_ctas(c, kernel, kRingThreads + 64, smem);
     if (cap <= 0) return AA_ERR_CUDA;
     void* args[] = {&p, &stages, &stage_vecs};

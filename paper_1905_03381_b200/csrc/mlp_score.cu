@@ -239,7 +239,7 @@ aa_status launch_score_shrink_mlp(aa_ctx_impl* c, const MlpFeat& f, ShrinkParams
     const size_t smem = 1024 + (size_t)kMlpStages * mp.g.stage_bytes + sizeof(float) * (2 * kMaxHidden + 2 * kSuperRows) +
                         sizeof(ScoreControl) + 64;
     const void* kernel = gather ? (const void*)mlp_score_shrink_kernel<true> : (const void*)mlp_score_shrink_kernel<false>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     int grid = c->sm_count;
     if ((unsigned int)grid > sp.n_tiles) grid = (int)sp.n_tiles;
     void* args[] = {&map_x, &map_w, &mp, &sp};

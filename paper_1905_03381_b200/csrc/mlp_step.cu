@@ -869,7 +869,7 @@ aa_status launch_assistant_step_mlp(aa_ctx_impl* c, const MlpFeat& f, float* W1_
         const size_t smem = 1024 + (size_t)kHalfStages * p.g.stage_bytes + sizeof(float) * (2 * kMaxHidden + kStepEpiWarps * 2 * kMaxHidden) +
                             sizeof(double) * (kStepMlpThreads / 32) + sizeof(float) * kStepEpiWarps + sizeof(TilePipe) + 64;
         const void* kernel = gather ? (const void*)mlp_residual_kernel<true> : (const void*)mlp_residual_kernel<false>;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+        if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
         const int64_t tiles = (m_host + kHalfRows - 1) / kHalfRows;
         int grid = max_ctas;
         if (grid > tiles) grid = (int)tiles;
@@ -888,7 +888,7 @@ aa_status launch_assistant_step_mlp(aa_ctx_impl* c, const MlpFeat& f, float* W1_
         // 2. G = P^T X
         const size_t smem2 = 1024 + (size_t)kXStages * kXStageBytes + (size_t)kATiles * kATileBytes + sizeof(GradPipe) + 64;
         const void* k2 = gather ? (const void*)mlp_w1_grad_kernel<true> : (const void*)mlp_w1_grad_kernel<false>;
-        if (cudaFuncSetAttribute(k2, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem2) != cudaSuccess) return AA_ERR_CUDA;
+        if (allow_smem(c, k2, smem2) != AA_OK) return AA_ERR_CUDA;
         void* args2[] = {&map_xg, &p};
         if (cudaLaunchKernel(k2, dim3(p.n_chunks * p.splits), dim3(kStepMlpThreads), args2, smem2, c->stream) != cudaSuccess)
             return AA_ERR_CUDA;

@@ -205,7 +205,7 @@ aa_status decode(aa_ctx_impl* c, const RelParams& p) {
     d.p = p;
     const void* kernel = (const void*)decode_kernel<DT>;
     const size_t smem = (size_t)(16 + kStages * 2 * 64) * pitch_of(DT) * 2 + (p.table ? (size_t)p.group * bias_floats(p.reach, 0) : 0) * sizeof(float);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     const int cap = resident_ctas(c, kernel, 128, smem);
     if (cap <= 0) return AA_ERR_CUDA;
     d.row_tiles = (int)((p.group * p.max_q + 15) / 16);

@@ -612,8 +612,8 @@ aa_status backward(aa_ctx_impl* c, RelParams p, int lo, int* n_parts) {
     int pairs = KeysTcGeo<DT>::smem(2, p.reach, p.table) <= 227 * 1024 ? 2 : 1;       // ... or for one pair of p and dS tiles
     const size_t smem_k = KeysTcGeo<DT>::smem(pairs, p.reach, p.table);
     int blocks_q = (int)((p.max_q + 127) / 128), blocks_k = (int)((p.max_k + kTcKeys - 1) / kTcKeys);
-    if (cudaFuncSetAttribute(rows, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_r) != cudaSuccess ||
-        cudaFuncSetAttribute(keys, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_k) != cudaSuccess)
+    if (allow_smem(c, rows, smem_r) != AA_OK ||
+        allow_smem(c, keys, smem_k) != AA_OK)
         return AA_ERR_CUDA;
     if (p.n_seq * blocks_k > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
     int64_t grid = c->sm_count / p.heads > 0 ? c->sm_count / p.heads : 1;             // one CTA an SM, one wave

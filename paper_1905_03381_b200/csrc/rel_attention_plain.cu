@@ -429,16 +429,12 @@ __global__ void __launch_bounds__(256) table_grad_kernel(RelParams p) {
     }
 }
 
-aa_status set_smem(const void* kernel, size_t bytes) {
-    return cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-}
-
 template <typename T, int DT>
 aa_status forward(aa_ctx_impl* c, RelParams p) {
     using G = Geo<DT>;
     const void* kernel = (const void*)forward_kernel<T, DT>;
     const size_t smem = G::smem(3, p.table ? 2 * p.reach + 1 : 0);
-    if (set_smem(kernel, smem) != AA_OK) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     int tiles = (int)((p.max_q + G::B - 1) / G::B);
     if (p.n_seq * tiles > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
     void* args[] = {&p, &tiles};
@@ -455,7 +451,7 @@ aa_status backward(aa_ctx_impl* c, RelParams p) {
     const void* kkv = (const void*)grad_kv_kernel<T, DT>;
     const int reach = p.table ? 2 * p.reach + 1 : 0;
     const size_t smem_q = G::smem(4, reach + (p.table && p.dtable ? 2 * p.reach + 2 * kThreads : 0)), smem_kv = G::smem(4, reach);
-    if (set_smem(kq, smem_q) != AA_OK || set_smem(kkv, smem_kv) != AA_OK) return AA_ERR_CUDA;
+    if (allow_smem(c, kq, smem_q) != AA_OK || allow_smem(c, kkv, smem_kv) != AA_OK) return AA_ERR_CUDA;
     int tiles_q = (int)((p.max_q + G::B - 1) / G::B), tiles_k = (int)((p.max_k + G::B - 1) / G::B);
     if (p.n_seq * tiles_k > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
     void* args_q[] = {&p, &tiles_q};

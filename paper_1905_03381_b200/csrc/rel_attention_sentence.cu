@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(LT * 2 * (LT / 64), LT == 64 && DT <= 64 ? (SH
 }
 
 aa_status prepare(aa_ctx_impl* c, const void* kernel, int threads, size_t smem, int* resident) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     *resident = resident_ctas(c, kernel, threads, smem);
     return *resident > 0 ? AA_OK : AA_ERR_CUDA;
 }

@@ -224,7 +224,7 @@ template <int DT>
 aa_status forward(aa_ctx_impl* c, RelParams p, int lo) {
     const void* kernel = (const void*)forward_tc_kernel<DT>;
     const size_t smem = FwdGeo<DT>::smem(p.reach, p.table);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     int tiles = (int)((p.max_q + 255) / 256);
     if (p.n_seq * tiles > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
     void* args[] = {&p, &lo, &tiles};

@@ -230,7 +230,7 @@ int choose_tile_rows(const aa_ctx_impl* c, int64_t n_cand, double bytes_per_row,
 template <typename K>
 aa_status launch_scan(aa_ctx_impl* c, K kernel, size_t smem, const ShrinkParams& sp, void** args) {
     if (smem > 48 * 1024) {
-        if (cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        if (allow_smem(c, (const void*)kernel, smem) != AA_OK)
             return AA_ERR_CUDA;
     }
     int grid = resident_ctas(c, (const void*)kernel, kScanThreads, smem);

@@ -400,7 +400,7 @@ aa_status launch_score_shrink_dense_tma(aa_ctx_impl* c, const DenseFeat& f_in, S
     aa_status st = finish_shrink_params(c, sp, tile_rows);
     if (st != AA_OK) return st;
     const void* kernel = f.dtype == AA_BF16 ? pick_kernel<uint16_t>(lpr) : pick_kernel<float>(lpr);
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return AA_ERR_CUDA;
+    if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     int grid = resident_ctas(c, kernel, kTmaThreads, smem);     // two per SM; every CTA's first tile is its block index, so all must be resident
     if (grid <= 0) return AA_ERR_CUDA;
     if ((unsigned int)grid > sp.n_tiles) grid = (int)sp.n_tiles;
