@@ -52,6 +52,7 @@ class aa_assistant(Structure):
 
 
 class aa_logits(Structure):
+    _stored = 2**63 - 1              # rows of the tensor, where logits_desc made the descriptor
     _fields_ = [
         ("data", c_void_p), ("dtype", c_int32), ("reserved", c_int32),
         ("rows", c_int64), ("cols", c_int64), ("row_stride", c_int64),
@@ -82,6 +83,7 @@ class aa_rows(Structure):
 
 
 class aa_dropout_rule(Structure):
+    _keep = _entries = None          # the list and its length, where dropout_rule made the descriptor
     _fields_ = [("p", c_float), ("site", c_uint32), ("seed", c_uint64), ("step", c_uint64), ("row_idx", c_void_p), ("id_base", c_int64)]
 
 
@@ -115,7 +117,7 @@ def dropout_rule(p: float, seed: int, step: int, site: int = 0, row_idx=None, id
     _check(row_idx, torch.int32, "row_idx")
     r = aa_dropout_rule()
     r.p, r.site, r.seed, r.step, r.row_idx, r.id_base = p, site, seed, step, _ptr(row_idx), id_base
-    r._keep = row_idx
+    r._keep, r._entries = row_idx, None if row_idx is None else row_idx.numel()
     return r
 
 
@@ -157,6 +159,9 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torc
     a.dtype, a.causal, a.heads, a.kv_heads, a.head_dim = _dtype_code(q), int(causal), q.shape[1], k.shape[1], q.shape[2]
     a.scale = 1.0 / float(q.shape[2]) ** 0.5 if scale is None else scale
     a.n_seq = q_offsets.numel() - 1 if n_seq is None else n_seq
+    for t, n, name in ((q_offsets, a.n_seq + 1, "q_offsets"), (k_offsets, a.n_seq + 1, "k_offsets"), (count_dev, 1, "count_dev")):
+        if t is not None and t.numel() < n:
+            _short(t, n, name)
     a.q_offsets, a.k_offsets, a.count_dev = q_offsets.data_ptr(), k_offsets.data_ptr(), _ptr(count_dev)
     a.q_rows, a.k_rows = q.shape[0], k.shape[0]
     a.max_q = q.shape[0] if max_q is None else max_q
@@ -287,6 +292,11 @@ def _check(t, dtype, name):
         raise TypeError(f"{name} must be a contiguous CUDA tensor of {dtype}")
 
 
+def _short(t, n: int, name: str):
+    """Raises for a list the kernels would read or write n entries of."""
+    raise TypeError(f"{name} must have at least {n} entries, got {t.numel()}")
+
+
 def dense_features(x: torch.Tensor, row_idx=None, n_rows=None, id_base: int = 0) -> aa_feat:
     """Descriptor of a row-major [n, d] fp32/bf16 matrix (last dim contiguous; row stride free)."""
     if x.dim() != 2 or x.stride(1) != 1 or not x.is_cuda:
@@ -351,7 +361,7 @@ def logits_desc(logits: torch.Tensor, rows=None) -> aa_logits:
     g.rows = logits.shape[0] if rows is None else rows
     g.cols = logits.shape[1]
     g.row_stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
-    g._keep = logits
+    g._keep, g._stored = logits, logits.shape[0]
     return g
 
 
@@ -485,32 +495,56 @@ class AutoAssist:
             n_seg = 0
         elif n_seg is None:
             n_seg = offsets.numel() - 1
+        if offsets is not None and offsets.numel() <= n_seg:
+            _short(offsets, n_seg + 1, "offsets")
+        if count_dev is not None and count_dev.numel() < 1:
+            _short(count_dev, 1, "count_dev")
+        if rule._entries is not None and rule._entries < (xm.rows if offsets is None else n_seg):
+            _short(rule._keep, xm.rows if offsets is None else n_seg, "the rule's row_idx")
         self._ok(self._L.aa_dropout(self._ctx, byref(xm), byref(rule), _ptr(offsets), n_seg, _ptr(count_dev), rm, byref(om)), "aa_dropout")
 
     def aa_instance_loss_grad(self, logits: aa_logits, labels: torch.Tensor, out_grad: torch.Tensor, offsets=None, n_seg=None, count_dev=None,
                               weight=None, scale: float = 1.0, mean: bool = True, out_loss=None):
         """Gradient of scale * (mean or sum over the instances of weight_i f_i) with respect to the logits; out_loss receives f_i.
         out_grad may be the logits themselves."""
-        for t, name, dtype in ((labels, "labels", torch.int32), (offsets, "offsets", torch.int32), (count_dev, "count_dev", torch.int32),
-                               (weight, "weight", torch.float32), (out_loss, "out_loss", torch.float32)):
-            _check(t, dtype, name)
+        _check(labels, torch.int32, "labels")
+        _check(offsets, torch.int32, "offsets")
+        _check(count_dev, torch.int32, "count_dev")
+        _check(weight, torch.float32, "weight")
+        _check(out_loss, torch.float32, "out_loss")
         if offsets is None:
             n_seg = 0
         elif n_seg is None:
             n_seg = offsets.numel() - 1
+        rows = logits.rows
+        instances = rows if offsets is None else n_seg
+        if rows > logits._stored:
+            raise TypeError("the logits have fewer rows than their descriptor says")
+        if labels.numel() < rows:
+            _short(labels, rows, "labels")
+        if weight is not None and weight.numel() < instances:
+            _short(weight, instances, "weight")
+        if out_loss is not None and out_loss.numel() < instances:
+            _short(out_loss, instances, "out_loss")
+        if offsets is not None and offsets.numel() <= n_seg:
+            _short(offsets, n_seg + 1, "offsets")
+        if count_dev is not None and count_dev.numel() < 1:
+            _short(count_dev, 1, "count_dev")
         self._ok(self._L.aa_instance_loss_grad(self._ctx, byref(logits), labels.data_ptr(), _ptr(offsets), n_seg, _ptr(count_dev), _ptr(weight),
                                                scale, AA_REDUCE_MEAN if mean else AA_REDUCE_SUM, _ptr(out_loss), byref(rows_desc(out_grad))),
                  "aa_instance_loss_grad")
 
     def aa_rel_attention(self, attn: aa_attn, out: torch.Tensor, bias=None, dropout=None):
         """Attention over ragged sequences with a learned relative position bias and instance-keyed dropout (both optional)."""
-        self._check_bias(attn, bias)
+        self._check_lists(attn, bias, dropout)
         o = _tokens(out, "out", attn._keep[0])
         self._ok(self._L.aa_rel_attention(self._ctx, byref(attn), None if bias is None else byref(bias), None if dropout is None else byref(dropout),
                                           byref(o)), "aa_rel_attention")
 
     @staticmethod
-    def _check_bias(attn: aa_attn, bias):
+    def _check_lists(attn: aa_attn, bias, dropout):
+        if dropout is not None and dropout._entries is not None and dropout._entries < attn.n_seq:
+            _short(dropout._keep, attn.n_seq, "the rule's row_idx")
         if bias is not None and bias._keep.shape[1] != attn.heads:
             raise TypeError("the bias table must be [buckets, heads]")
 
@@ -524,7 +558,7 @@ class AutoAssist:
     def aa_rel_attention_grad(self, attn: aa_attn, dout: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, scratch: torch.Tensor,
                               bias=None, dropout=None, dtable=None):
         """dq, dk, dv (and the bias table's gradient) of aa_rel_attention from the gradient of its output."""
-        self._check_bias(attn, bias)
+        self._check_lists(attn, bias, dropout)
         q, k, v = attn._keep[:3]
         _check(dtable, torch.float32, "dtable")
         if dtable is not None and (bias is None or dtable.shape != bias._keep.shape):

@@ -126,3 +126,37 @@ def test_rows_as_column_slices_of_one_matrix(aa, dtype, cols):
     wide = torch.zeros((37, 2 * cols - 1), dtype=dtype, device=DEV)
     refused(lambda: aa.aa_dropout(wide[:, :cols], rule, wide[:, cols - 1:]))
     refused(lambda: aa.aa_instance_loss_grad(B.logits_desc(wide[:, :cols]), y, wide[:, cols - 1:]))
+
+
+# ---- lists
+
+def test_lists_shorter_than_what_is_read_or_written_are_refused(aa):
+    x, n = torch.zeros((6, 16), device=DEV), 6
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)  # noqa: E731
+    f32 = lambda n: torch.zeros(n, device=DEV)  # noqa: E731
+    rule = lambda n: B.dropout_rule(0.5, 1, 2, row_idx=i32(n))  # noqa: E731
+    off = offs([2, 4])
+    logits = B.logits_desc(x)
+    q = torch.zeros((6, 2, 16), device=DEV)
+    attn = B.attention(q, q, q, off)
+    many = B.logits_desc(x[:5])
+    many.rows = 6
+    for bad in (
+            lambda: aa.aa_dropout(x, rule(n - 1), x), lambda: aa.aa_dropout(x, rule(1), x, offsets=off), lambda: aa.aa_dropout(x, rule(3), x, offsets=off, n_seg=3),
+            lambda: aa.aa_dropout(x, rule(n), x, count_dev=i32(0)),
+            lambda: aa.aa_instance_loss_grad(logits, i32(n - 1), x), lambda: aa.aa_instance_loss_grad(logits, i32(n), x, weight=f32(n - 1)),
+            lambda: aa.aa_instance_loss_grad(logits, i32(n), x, out_loss=f32(n - 1)), lambda: aa.aa_instance_loss_grad(logits, i32(n), x, offsets=off, n_seg=3),
+            lambda: aa.aa_instance_loss_grad(logits, i32(n), x, offsets=off, weight=f32(1)), lambda: aa.aa_instance_loss_grad(logits, i32(n), x, offsets=off, out_loss=f32(1)),
+            lambda: aa.aa_instance_loss_grad(logits, i32(n), x, count_dev=i32(0)), lambda: aa.aa_instance_loss_grad(many, i32(n), x),
+            lambda: B.attention(q, q, q, off, n_seq=3), lambda: B.attention(q, q, q, off, i32(2), n_seq=2), lambda: B.attention(q, q, q, off, count_dev=i32(0)),
+            lambda: aa.aa_rel_attention(attn, torch.empty_like(q), dropout=rule(1)),
+            lambda: aa.aa_rel_attention_grad(attn, q.clone(), q.clone(), q.clone(), q.clone(), aa.rel_attention_scratch(attn), dropout=rule(1))):
+        with pytest.raises(TypeError):
+            bad()
+    # exactly as long as needed, and longer
+    aa.aa_dropout(x, rule(2), x, offsets=off)
+    aa.aa_dropout(x, rule(9), x, offsets=off, n_seg=1)
+    aa.aa_instance_loss_grad(logits, i32(n), x, offsets=off, weight=f32(2), out_loss=f32(2))
+    aa.aa_rel_attention(B.attention(q, q, q, off, n_seq=1), torch.empty_like(q), dropout=rule(1))
+    torch.cuda.synchronize()
+    assert aa.aa_device_status() == B.AA_OK
