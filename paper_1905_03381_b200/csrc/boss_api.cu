@@ -230,11 +230,12 @@ aa_status aa_rel_attention(aa_ctx* ctx, const aa_attn* attn, const aa_rel_bias* 
     const Extent o = query_extent(*out, p);
     const bool in_place = out->data == attn->q.data && (p.q_rows <= 1 || out->token_stride == attn->q.token_stride) && (p.heads == 1 || out->head_stride == attn->q.head_stride);
     if ((!in_place && !apart(o, query_extent(attn->q, p), es)) || !apart(o, key_extent(attn->k, p), es) || !apart(o, key_extent(attn->v, p), es)) return AA_ERR_INVALID_ARG;
-    if (p.n_seq == 0 || p.max_q == 0) return AA_OK;
+    if (p.n_seq == 0) return AA_OK;
     aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
     p.out = tok(*out);
     p.ctl = c->ctl;
-    return attn->dtype == AA_BF16 && rel_bf16_fits(p) ? launch_rel_attention_bf16(c, p) : launch_rel_attention_plain(c, p, attn->dtype);
+    // a bound of zero leaves only the sequences to be looked over, which the fp32 kernel does
+    return attn->dtype == AA_BF16 && p.max_q > 0 && rel_bf16_fits(p) ? launch_rel_attention_bf16(c, p) : launch_rel_attention_plain(c, p, attn->dtype);
 }
 
 aa_status aa_rel_attention_scratch_bytes(const aa_attn* attn, const aa_rel_bias* bias, size_t* bytes) {
@@ -271,7 +272,7 @@ aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_b
     if (need > 0 && (!scratch || (uintptr_t)scratch % 256)) return AA_ERR_INVALID_ARG;
     if (scratch_bytes < need) return AA_ERR_WORKSPACE;
     aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
-    if (p.n_seq == 0 || (p.max_q == 0 && p.max_k == 0))
+    if (p.n_seq == 0)
         return dtable ? cuda_ok(cudaMemsetAsync(dtable, 0, sizeof(float) * (size_t)p.buckets * (size_t)p.heads, c->stream)) : AA_OK;
     p.dout = tok(*dout);
     p.dq = tok(*dq);
@@ -282,7 +283,7 @@ aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_b
     p.stats = static_cast<float4*>(scratch);
     p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats_bytes(attn));
     p.n_parts = rel_grad_parts(p.heads);
-    st = attn->dtype == AA_BF16 && rel_bf16_fits(p) ? launch_rel_attention_grad_bf16(c, p, &p.n_parts) : launch_rel_attention_grad_plain(c, p, attn->dtype);
+    st = attn->dtype == AA_BF16 && (p.max_q > 0 || p.max_k > 0) && rel_bf16_fits(p) ? launch_rel_attention_grad_bf16(c, p, &p.n_parts) : launch_rel_attention_grad_plain(c, p, attn->dtype);
     if (st != AA_OK || !dtable) return st;
     return launch_rel_table_grad(c, p);
 }

@@ -435,7 +435,7 @@ aa_status forward(aa_ctx_impl* c, RelParams p) {
     const void* kernel = (const void*)forward_kernel<T, DT>;
     const size_t smem = G::smem(3, p.table ? 2 * p.reach + 1 : 0);
     if (allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
-    int tiles = (int)((p.max_q + G::B - 1) / G::B);
+    int tiles = p.max_q > 0 ? (int)((p.max_q + G::B - 1) / G::B) : 1;      // one: sequences are looked over even if none may have a query
     if (p.n_seq * tiles > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
     void* args[] = {&p, &tiles};
     if (launch_overlapped(c, kernel, dim3((unsigned)(p.n_seq * tiles), p.heads), dim3(kThreads), args, smem, false) != cudaSuccess)
@@ -452,7 +452,7 @@ aa_status backward(aa_ctx_impl* c, RelParams p) {
     const int reach = p.table ? 2 * p.reach + 1 : 0;
     const size_t smem_q = G::smem(4, reach + (p.table && p.dtable ? 2 * p.reach + 2 * kThreads : 0)), smem_kv = G::smem(4, reach);
     if (allow_smem(c, kq, smem_q) != AA_OK || allow_smem(c, kkv, smem_kv) != AA_OK) return AA_ERR_CUDA;
-    int tiles_q = (int)((p.max_q + G::B - 1) / G::B), tiles_k = (int)((p.max_k + G::B - 1) / G::B);
+    int tiles_q = p.max_q > 0 ? (int)((p.max_q + G::B - 1) / G::B) : 1, tiles_k = (int)((p.max_k + G::B - 1) / G::B);
     if (p.n_seq * tiles_k > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
     void* args_q[] = {&p, &tiles_q};
     void* args_kv[] = {&p, &tiles_k};

@@ -160,3 +160,27 @@ def test_lists_shorter_than_what_is_read_or_written_are_refused(aa):
     aa.aa_rel_attention(B.attention(q, q, q, off, n_seq=1), torch.empty_like(q), dropout=rule(1))
     torch.cuda.synchronize()
     assert aa.aa_device_status() == B.AA_OK
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_sequences_that_break_a_bound_of_zero_are_latched(aa, dtype):
+    """A bound of no token at all is a bound like any other: sequences beyond it are skipped and reported."""
+    q, k, v, g, _ = problem(dtype, [4, 6])
+    table = torch.zeros((16, 4), device=DEV)
+    none = torch.zeros((0, 4, 64), dtype=dtype, device=DEV)
+    for attn in (B.attention(q, k, v, offs([4, 6]), max_q=0, max_k=6), B.attention(none, k, v, offs([4, 6]), max_k=6)):
+        out = torch.full_like(q, 7.0) if attn._keep[0] is q else none
+        aa.aa_rel_attention(attn, out, bias=B.rel_bias(table, 40))
+        torch.cuda.synchronize()
+        assert aa.aa_device_status() == B.AA_ERR_BAD_INDEX and torch.all(out == 7.0)
+    attn, bias = B.attention(q, k, v, offs([4, 6]), max_q=0, max_k=0), B.rel_bias(table, 40)
+    dq, dk, dv, dt = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(v, 7.0), torch.full_like(table, 7.0)
+    aa.aa_rel_attention_grad(attn, g, dq, dk, dv, aa.rel_attention_scratch(attn, bias), bias=bias, dtable=dt)
+    torch.cuda.synchronize()
+    assert aa.aa_device_status() == B.AA_ERR_BAD_INDEX and all(torch.all(t == 7.0) for t in (dq, dk, dv)) and not dt.any()
+    # empty sequences keep to it
+    attn = B.attention(q, k, v, offs([0, 0]), max_q=0, max_k=0)
+    aa.aa_rel_attention(attn, dq, bias=bias)
+    aa.aa_rel_attention_grad(attn, g, dq, dk, dv, aa.rel_attention_scratch(attn, bias), bias=bias, dtable=dt)
+    torch.cuda.synchronize()
+    assert aa.aa_device_status() == B.AA_OK and all(torch.all(t == 7.0) for t in (dq, dk, dv)) and not dt.any()
