@@ -415,7 +415,11 @@ struct KeysTcGeo {
 // grid (sequences x key blocks, key heads).  Tiles are counted over the heads of the group: tile g works on head h0 + g / per_head.
 template <int DT>
 __global__ void __launch_bounds__(kGradThreads, 1) grad_keys_tc_kernel(RelParams p, int lo, int blocks, int pairs) {
+    // Two at least: the scores of tile g + 1 are issued before the products of tile g (below), so both tiles' q and dO are held at once; with one
+    // stage the issuing warp would wait for a tile that cannot be loaded before its own next products.  (Without that look-ahead one stage gives the
+    // same dk and dv under these barriers.)
     constexpr int stages = 2;
+    static_assert(stages >= 2, "look-ahead of one tile");
     using G = KeysTcGeo<DT>;
     extern __shared__ char smem_raw[];
     char* KV = reinterpret_cast<char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);     // K, V
