@@ -434,13 +434,16 @@ aa_status aa_instance_loss_grad(aa_ctx* ctx, const aa_logits* logits, const int3
  *   s_ij = scale * q_i . k_j + table[bucket(delta)][h]       (causal: keys with delta > 0 are masked)
  *   p_ij = softmax over the unmasked keys,   o_i = sum_j dropout(p)_ij v_j.
  * A query that sees no key (Lk = 0, a position before the first key, a bias of -inf everywhere) gives o_i = 0 and no gradient.
+ * A masked key and a dropped probability enter the sums as 0 * v_j (in the gradient call 0 * k_j, 0 * q_i, 0 * dout_i too): a sequence's own tokens must
+ * be finite there as well.  What lies outside of every evaluated sequence may hold anything.
  *
  * Tokens: element (token t, head h, e) at data + t*token_stride + h*head_stride + e, so that q, k and v may be views of one packed
  * projection.  Sequence s owns the query tokens [q_offsets[s], q_offsets[s+1]) and the key tokens [k_offsets[s], k_offsets[s+1]).
  * What a call writes (out; dq, dk, dv) must have no element in common with its other operands, except that out may be q itself (same pointer
  * and strides); views of one packed array with the same strides are told apart exactly, other interleaving address ranges are refused.
  * max_q, max_k: HOST upper bounds of one sequence's lengths.  A sequence that breaks them, or whose offsets descend or leave
- * [0, q_rows] / [0, k_rows], latches AA_ERR_BAD_INDEX and is skipped.  M = min(*count_dev, n_seq) sequences are evaluated; token
+ * [0, q_rows] / [0, k_rows], latches AA_ERR_BAD_INDEX and is skipped.  The bounds also choose the kernels: true ones matter (max_q = 1 for
+ * single new tokens, else their context is not split over the GPU).  M = min(*count_dev, n_seq) sequences are evaluated; token
  * rows of no evaluated sequence are left untouched.
  *
  * aa_rel_bias: buckets halve into the two directions when bidirectional (delta > 0 takes the upper half); with n buckets per

@@ -145,7 +145,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torc
               scale=None, causal: bool = False, count_dev=None, n_seq=None) -> aa_attn:
     """Ragged attention problem: q [tokens, heads, dim], k and v [tokens, kv_heads, dim] (views of a packed projection are fine),
     int32 offsets of the sequences' tokens; max_q / max_k bound one sequence's length (default: all tokens); scale defaults to
-    1 / sqrt(dim)."""
+    1 / sqrt(dim).  The bounds choose the kernels, so give true ones: without max_q=1 a batch of single new tokens is taken for
+    long sequences, and its contexts are not split over the GPU."""
     k_offsets = q_offsets if k_offsets is None else k_offsets
     _check(q_offsets, torch.int32, "q_offsets")
     _check(k_offsets, torch.int32, "k_offsets")

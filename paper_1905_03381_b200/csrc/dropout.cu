@@ -1,10 +1,11 @@
 // Dropout whose mask is a function of (seed, step, instance id, site, element): out = residual + mask * scale * x.
 //
-// One Philox block decides eight elements (16 bits each): about 8 of the 16 instructions an element costs, so the kernel stays bound by memory
-// only if the next unit's loads are under way while this one's draws are made.  Work is handed out in units of one row's chunk of kGroups *
+// One Philox block decides eight elements (16 bits each): about 8 of the 29 instructions an element costs, so the kernel stays near memory's
+// time only if the next unit's loads are under way while this one's draws are made.  Work is handed out in units of one row's chunk of kGroups *
 // LPR groups of eight: a sub-warp of LPR lanes takes a contiguous run of units, so that the segment search and the instance's key are paid
-// once per run and again only where a new instance begins.  Bound by the draws' instructions together with memory: 25,000 x 512 bf16 with
-// residual 20.8 us (78 MB, 3.8 TB/s), 30,011 x 1,001 fp32, whose rows are not aligned, 51 us (240 MB, 4.7 TB/s), one sentence 7 us (launch).
+// once per run and again only where a new instance begins.  Bound by instructions (44 and 56 % of the issue slots) together with loads that 24
+// warps an SM do not hide: 25,000 x 512 bf16 with residual 21 us (78 MB, 3.7 TB/s), 30,011 x 1,001 fp32, whose rows are not aligned, 52 us (240 MB,
+// 4.6 TB/s), one sentence 7 us (launch).
 #include "boss_common.cuh"
 
 namespace aa {
@@ -13,7 +14,7 @@ namespace {
 
 constexpr int kThreads = 256;
 // Groups of eight per lane and unit.  Two where their operands fit the registers of three CTAs on an SM without spilling (fp32 vectors with
-// their successors do not); one and more CTAs instead is slower where both fit (25,000 x 512 bf16: 21.4 against 20.8 us).
+// their successors do not); one and more CTAs instead is slower where both fit (25,000 x 512 bf16, at the time: 21.4 against 20.8 us).
 template <typename T, bool VEC>
 constexpr int kGroupsOf = VEC == (sizeof(T) == 2) ? 2 : 1;
 

@@ -3,8 +3,8 @@
 // One read and one write of the logits: a row stays on chip between its sum and its gradient.  Rows of up to 4 KB sit in the registers of up to
 // a warp, rows of up to 16 KB in those of a small CTA, rows of up to 64 KB in a stage of a shared-memory ring (bulk copies in and out, in place).
 // Longer rows, and gradients that are not aligned like the logits, are swept twice, the second time out of L2.  Measured: 39,000 x 100 fp32 8 us
-// (31 MB), of which 6 are the launch; about 25,000 rows x 32,000 bf16 (ring) 3.26 GB in 0.61 ms, 5.3 TB/s: the maximum and the sum of a row are
-// two barriers that the copies have to bridge; 4,096 rows x 131,071 bf16 (two sweeps) 2.15 GB in 0.50 ms, 4.3 TB/s, the second sweep out of L2.
+// (31 MB), of which 6 are the launch; about 25,000 rows x 32,000 bf16 (ring) 3.26 GB in 0.63 ms, 5.2 TB/s: the maximum and the sum of a row are
+// two barriers that the copies have to bridge; 4,096 rows x 131,071 bf16 (two sweeps) 2.15 GB in 0.51 ms, 4.2 TB/s, the second sweep out of L2.
 #include "async_copy.cuh"
 #include "boss_common.cuh"
 #include "loss_common.cuh"

@@ -3,8 +3,10 @@
 //
 // A CTA of 256 threads holds a B x B score tile, each thread an M x M part of it (rows ty*M + a, columns tx + 16 b), and loops over the
 // other axis with the running maximum and sum of a softmax.  Operand tiles sit in shared memory as fp32, zero past the sequence's end.
-// Bound by shared memory and, for short sentences, by the tail of unequal CTAs: 24 sentences of up to 301 tokens, 5 heads of 40, forward and
-// every gradient with dropout 0.40 ms for 1.9 GFLOP.
+// Bound by the loads that feed the multiply-adds (eight 16-byte reads for 64 of them at best), by a width of 40 padded to 64, and by unequal CTAs (the
+// busiest SM is active 1.4 to 1.5 times as long as the mean one): 24 sentences of up to 301 tokens, 5 heads of 40, forward and every gradient with
+// dropout 0.39 ms for 1.9 GFLOP.  Operands split into two or three narrower terms would bring these products onto the tensor cores within the same
+// bounds; that is not built.
 #include "rel_attention.cuh"
 
 namespace aa {
@@ -468,7 +470,7 @@ aa_status backward(aa_ctx_impl* c, RelParams p) {
 
 }  // namespace
 
-// Operand tiles of 64, 128 or 256 columns (48 as a fourth was slower for a width of 40: 436 against 401 us for 24 sentences of up to 301 tokens,
+// Operand tiles of 64, 128 or 256 columns (48 as a fourth was slower for a width of 40, at the time: 436 against 401 us for 24 sentences of up to 301 tokens,
 // 5 heads, forward and every gradient).
 template <typename T>
 aa_status forward_width(aa_ctx_impl* c, const RelParams& p) {

@@ -5,8 +5,10 @@
 // and dS in shared memory (bf16), then warps contract them for 16 keys (dV, dK) and 16 rows (dQ): five products, each operand read from
 // memory once.  The bias gradient is added up along the diagonals of the unrounded dS, in a fixed order.
 //
-// Bound by the instructions around the products (bias, exponential, draws, operand moves) more than by the products: 368 sentences of 8 to
-// 128 tokens, 8 heads of 64, forward 56 us (1.9 TB/s), forward and every gradient, causal, with dropout 242 us.
+// Bound by unequal CTAs and by what a CTA waits for: sentences are dealt out by a fixed stride, whatever their length, so that the busiest SM is
+// active 1.3 to 1.5 times as long as the mean one, and the forward pass fetches a sentence only after the last one; the issue slots are in use for
+// 22 to 34 %, the tensor pipe for 5 to 16 %.  368 sentences of 8 to 128 tokens, 8 heads of 64: forward 56 us (1.9 TB/s), forward and every
+// gradient, causal, with dropout 242 us.
 #include "rel_attention_mma.cuh"
 
 namespace aa {
