@@ -339,13 +339,20 @@ def _philox(c0, c1, c2, c3, k0, k1):
     return c0, c1, c2, c3
 
 
-def _to_e4m3(x, u):
-    """x in units of its block's scale -> e4m3, up where the 16 random bits u (int32) reach the remainder."""
+def _to_e4m3(x, u, squares):
+    """x in units of its block's scale -> e4m3.  u: 16 random bits (int32).  Up where they reach the remainder, or where x^2 is above that part
+    of the way from the lower neighbour's square to the upper one's, so that the stored number's square has the mean x^2."""
     a = x.abs()
     low = a < 2.0**-6                                        # below the normal numbers steps are equal: those of [2^-6, 2^-5)
     y = torch.where(low, a + 2.0**-6, a)
-    y = ((y.view(torch.int32) + (u << 4)) & ~0xFFFFF).view(torch.float32)
+    bits = y.view(torch.int32)
+    y = ((bits if squares else bits + (u << 4)) & ~0xFFFFF).view(torch.float32)
+    if squares:
+        z = ((bits & ~0xFFFFF) + 0x100000).view(torch.float32)
+        z = torch.where(low, z - 2.0**-6, z)
     y = torch.where(low, y - 2.0**-6, y)
+    if squares:
+        return torch.where((a - y) * (a + y) > u.float() * 2.0**-16 * ((z - y) * (z + y)), z, y)
     return torch.where(x < 0, -y, y)
 
 
@@ -379,7 +386,7 @@ def _plain_adamw(s, case):
         scale = _scale_of(x)
         unit = scale.float()[:, None]
         unit = torch.where(unit < 2.0**-126, torch.ones((), device=DEV), unit)      # blocks of zeros
-        code = _to_e4m3((x.view(blocks) / unit).view(-1), u.to(torch.int32))
+        code = _to_e4m3((x.view(blocks) / unit).view(-1), u.to(torch.int32), name == "root")
         if name == "root":
             code = torch.where((x > 0) & (code == 0), torch.full((), 2.0**-9, device=DEV), code)
         s[name].copy_(code.to(torch.float8_e4m3fn))
@@ -461,8 +468,12 @@ def _exact_adamw(s, case):
         scale = torch.where(top > 0, 2.0 ** (torch.floor(torch.log2(top.clamp(min=1e-300))) - 7), torch.full_like(top, 2.0**-127))
         y = rows / scale
         step = 2.0 ** (torch.floor(torch.log2(y.clamp(min=2.0**-6))) - 3)            # e4m3 steps; equal ones below 2^-6
-        code = torch.floor(y / step + u.view(-1, 256).double() / 65536) * step
-        if name == "root":
+        u64 = u.view(-1, 256).double() / 65536
+        if name == "m":
+            code = torch.floor(y / step + u64) * step
+        else:
+            low = torch.floor(y / step) * step
+            code = torch.where(y**2 - low**2 > u64 * ((low + step) ** 2 - low**2), low + step, low)
             code = torch.where((rows > 0) & (code == 0), torch.full_like(code, 2.0**-9), code)
         got[name] = (code * torch.sign(x.view(-1, 256))).view(-1)
         got[name + "_scale"] = scale[:, 0]
