@@ -504,6 +504,97 @@ aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_b
                                 void* scratch, size_t scratch_bytes);
 
 /*
+ * The rest of the Boss's training step: linear layers, layer normalisation, AdamW.
+ *
+ * Rows: the token rows of a batch of ragged sentences, of which only the first R are evaluated; later rows are left untouched and may hold anything.
+ *   offsets == NULL: R = min(*count_dev, rows), or rows without count_dev (n_seg is 0).
+ *   offsets != NULL: offsets[n_seg + 1] are the sentences' token offsets as for aa_dropout; with M = min(*count_dev, n_seg) counted sentences
+ *                    R = offsets[M] (0 if M = 0).  Only that entry is read; one outside [0, rows] latches AA_ERR_BAD_INDEX and counts as 0.
+ *
+ * Linear layer:  pre = x w^T + bias,  out = act(pre) + residual.
+ *   x [rows x inner], w [cols x inner] (one output per row), residual and out and pre [rows x cols] of one dtype; bias fp32 [cols].
+ *   bias, residual and pre are nullable; pre is what aa_linear_grad needs of a layer with an activation.
+ *   AA_ACT_RELU max(z, 0); AA_ACT_GELU z (1 + erf(z / sqrt 2)) / 2; AA_ACT_SILU z / (1 + exp(-z)).
+ * Products are summed in fp32, bias, activation and residual are applied in fp32, and the result is rounded once.  fp32 operands enter
+ * the products with all their bits.  A factor of zero against an infinity or NaN gives NaN, as in the formula.
+ * out may be residual itself (same pointer and stride); what is written has otherwise no element in common with another operand.
+ * rows may be 0 (dw and dbias of no rows are 0); cols and inner are 1 to 2^30.
+ */
+typedef enum { AA_ACT_NONE = 0, AA_ACT_RELU = 1, AA_ACT_GELU = 2, AA_ACT_SILU = 3 } aa_activation;
+
+aa_status aa_linear(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, const float* bias, int32_t activation, const aa_rows* residual,
+                    const int32_t* offsets, int64_t n_seg, const int32_t* count_dev, const aa_rows* pre, const aa_rows* out);
+
+/*
+ * Gradients of aa_linear from dout, the gradient of its output:  G = dout * act'(pre) (AA_ACT_NONE: G = dout, pre is NULL),
+ *   dx = G w + residual,   dw = G^T x,   dbias = column sums of G.
+ * dx, dw, dbias are nullable (not computed), written and not added to; residual (nullable, needs dx) is a gradient that reaches x past the layer, dx may
+ * be residual itself.  dx and dw have the dtype of x and w, dbias is fp32.  With an activation and bf16 operands G is rounded to bf16 before the
+ * two products (dbias sums it unrounded).  Sums run in an order that depends on the sizes alone, so equal calls give equal bits.
+ * scratch: DEVICE memory of at least aa_linear_grad_scratch_bytes(...) bytes, 256-byte aligned.
+ */
+aa_status aa_linear_grad_scratch_bytes(const aa_rows* x, const aa_rows* w, int32_t activation, size_t* bytes);
+aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_t activation, const aa_rows* pre, const aa_rows* dout,
+                         const aa_rows* residual, const int32_t* offsets, int64_t n_seg, const int32_t* count_dev,
+                         const aa_rows* dx, const aa_rows* dw, float* dbias, void* scratch, size_t scratch_bytes);
+
+/*
+ * Layer normalisation of every row:  h = (x - mean(x)) / sqrt(var(x) + eps),  out = h * gamma + beta; var is the mean of the squared
+ * distances from the mean, gamma and beta fp32 [cols], nullable (1 and 0).  Computed in fp32, rounded once.  out may be x itself.
+ * Gradients, with g = dout * gamma:  dx = (g - mean(g) - h mean(g h)) / sqrt(var + eps) + residual,  dgamma = sum over the rows of dout h,  dbeta =
+ * sum over the rows of dout (fp32, nullable, written, summed in an order that depends on the sizes alone).  residual is nullable; dx may be
+ * x, dout or residual itself.  Mean and variance are taken from x again, nothing is kept from the forward call.
+ * scratch: DEVICE memory of at least aa_layer_norm_grad_scratch_bytes(...) bytes, 256-byte aligned.
+ */
+aa_status aa_layer_norm(aa_ctx* ctx, const aa_rows* x, const float* gamma, const float* beta, float eps, const int32_t* offsets, int64_t n_seg,
+                        const int32_t* count_dev, const aa_rows* out);
+aa_status aa_layer_norm_grad_scratch_bytes(const aa_rows* x, size_t* bytes);
+aa_status aa_layer_norm_grad(aa_ctx* ctx, const aa_rows* x, const float* gamma, float eps, const aa_rows* dout, const aa_rows* residual,
+                             const int32_t* offsets, int64_t n_seg, const int32_t* count_dev, const aa_rows* dx, float* dgamma, float* dbeta,
+                             void* scratch, size_t scratch_bytes);
+
+/*
+ * One AdamW step (decoupled weight decay) on a HOST list of tensors with fp32 parameters.  With t the step's number (from 1),
+ *   g = grad_scale * grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   param = (1 - lr weight_decay) param - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps);   copy = param rounded to bf16.
+ * grad_scale: nullable DEVICE scalar (for instance the factor of a clipped gradient norm).  If it is not finite the step writes nothing.
+ * The call advances rule->t; the rule's values are read when the call is made, so that a captured graph replays one t.
+ *
+ * state_bits 32: m and v are fp32 [n].
+ * state_bits 8:  m and root = sqrt(v) are e4m3 [n] in units of a power of two per block of 256 consecutive elements, m_scale and v_scale
+ *   [ceil(n / 256)] holding its exponent + 127 as a byte (0: a block of zeros), chosen so that the block's largest magnitude lies in [128, 256) units.
+ *   Rounding is random and without bias in m and in v, else a moment that moves by less than half a step would stand still.  For x in units
+ *   between the e4m3 magnitudes lo <= x < hi (those below 2^-6 are multiples of 2^-9), m goes up iff (x - lo) / (hi - lo) + u / 65536 >= 1, and root iff
+ *   x^2 - lo^2 > u / 65536 (hi^2 - lo^2).  u are 16 bits of Philox4x32-10 (key = seed, counter = (i / 4, index of the tensor in the list, t as
+ *   64 bits)): word i % 4 of it, the low half for m, the high half for root.
+ *   A positive root never becomes 0 (it is 2^-9 units at least), so that a step is not divided by less than was seen.  The step itself uses
+ *   the moments before they are rounded.  Start from zero bytes.  Gradients are to be finite: the blocks of one that is not hold no numbers afterwards.
+ * grad is fp32 or bf16 [n]; copy is nullable.  All arrays are contiguous and have no element in common with one another, whichever tensors they belong
+ * to, except that gradients may be shared.  n <= 2^33.
+ */
+typedef struct {
+    float* param;
+    const void* grad;
+    void* m;
+    void* v;
+    uint8_t* m_scale;        /* state_bits 8 */
+    uint8_t* v_scale;
+    void* copy;              /* nullable bf16 */
+    int64_t n;
+    double weight_decay;
+    int32_t grad_dtype;      /* aa_dtype */
+    int32_t state_bits;      /* 32 or 8 */
+} aa_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t t;               /* steps taken so far */
+    uint64_t seed;
+} aa_adamw_rule;
+
+aa_status aa_adamw(aa_ctx* ctx, const aa_adamw_tensor* tensors, int64_t n_tensors, aa_adamw_rule* rule, const float* grad_scale);
+
+/*
  * Synchronises the context's stream, returns the first device-side condition latched since the
  * last call in *latched (HOST pointer; AA_OK if none) and clears it.
  */

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
+from ctypes import POINTER, Structure, byref, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 
 import torch
 
@@ -23,6 +23,8 @@ AA_FEAT_DENSE, AA_FEAT_CSR = 0, 1
 AA_ASSIST_LINEAR, AA_ASSIST_MLP = 0, 1
 AA_THRESH_VALUE, AA_THRESH_BATCH_MEAN = 0, 1
 AA_REDUCE_SUM, AA_REDUCE_MEAN = 0, 1
+AA_ACT_NONE, AA_ACT_RELU, AA_ACT_GELU, AA_ACT_SILU = 0, 1, 2, 3
+ACTIVATIONS = {None: AA_ACT_NONE, "relu": AA_ACT_RELU, "gelu": AA_ACT_GELU, "silu": AA_ACT_SILU}
 
 EXPORTS = (
     "aa_status_string", "aa_workspace_bytes", "aa_create", "aa_destroy", "aa_score_shrink",
@@ -30,6 +32,7 @@ EXPORTS = (
     "aa_device_status", "aa_launch_count", "aa_shrink_compact_static", "aa_batch_cut", "aa_threshold_compact", "aa_sk_threshold", "aa_assistant_step_adam",
     "aa_instance_loss_rows", "aa_assistant_step_scored", "aa_conv_pool_features",
     "aa_dropout", "aa_instance_loss_grad", "aa_rel_bucket", "aa_rel_attention", "aa_rel_attention_scratch_bytes", "aa_rel_attention_grad",
+    "aa_linear", "aa_linear_grad_scratch_bytes", "aa_linear_grad", "aa_layer_norm", "aa_layer_norm_grad_scratch_bytes", "aa_layer_norm_grad", "aa_adamw",
 )
 AA_STATIC_MAX_CANDIDATES = 1 << 22
 
@@ -112,6 +115,10 @@ def rows_desc(x: torch.Tensor) -> aa_rows:
     return aa_rows(x.data_ptr(), _dtype_code(x), 0, rows, cols, stride[0] if rows > 1 else cols)
 
 
+def _rows_or_none(x):
+    return None if x is None else byref(rows_desc(x))
+
+
 def dropout_rule(p: float, seed: int, step: int, site: int = 0, row_idx=None, id_base: int = 0) -> aa_dropout_rule:
     """Dropout of rate p whose mask is a function of (seed, step, instance id, site, element); row_idx: the batch list (int32)."""
     _check(row_idx, torch.int32, "row_idx")
@@ -187,6 +194,79 @@ def adam_state(m: torch.Tensor, v: torch.Tensor, beta1: float = 0.9, beta2: floa
     return st
 
 
+class aa_adamw_tensor(Structure):
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p), ("copy", c_void_p),
+                ("n", c_int64), ("weight_decay", c_double), ("grad_dtype", c_int32), ("state_bits", c_int32)]
+
+
+class aa_adamw_rule(Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("t", c_int64), ("seed", c_uint64)]
+
+
+def adamw_rule(lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, t: int = 0, seed: int = 0) -> aa_adamw_rule:
+    """Constants of AdamW; t counts the steps taken and advances with every aa_adamw.  seed: of the rounding of 8-bit moments."""
+    return aa_adamw_rule(lr, beta1, beta2, eps, t, seed)
+
+
+def adamw_moments8(param: torch.Tensor) -> dict:
+    """Zero moments in 8 bits for a parameter, as the keyword arguments of adamw_tensor."""
+    n, dev = param.numel(), param.device
+    got = {k: torch.zeros(n, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn) for k in ("m", "v")}
+    got.update({k: torch.zeros((n + 255) // 256, dtype=torch.uint8, device=dev) for k in ("m_scale", "v_scale")})
+    return got
+
+
+def adamw_tensor(param: torch.Tensor, grad: torch.Tensor, m: torch.Tensor, v: torch.Tensor, m_scale=None, v_scale=None, copy=None,
+                 weight_decay: float = 0.0) -> aa_adamw_tensor:
+    """One tensor of an AdamW step: fp32 param, fp32 or bf16 grad, fp32 moments m and v - or, with m_scale and v_scale (bytes, one per 256
+    elements), e4m3 moments m and sqrt(v) - and an optional bf16 copy of the parameters."""
+    _check(param, torch.float32, "param")
+    _check(grad, grad.dtype, "grad")
+    _check(copy, torch.bfloat16, "copy")
+    if (m_scale is None) != (v_scale is None):
+        raise TypeError("m_scale and v_scale come together")
+    narrow = m_scale is not None
+    n = param.numel()
+    for t, name in ((m, "m"), (v, "v")):
+        _check(t, torch.float8_e4m3fn if narrow else torch.float32, name)
+    for t, name in ((m_scale, "m_scale"), (v_scale, "v_scale")):
+        if narrow:
+            _check(t, t.dtype if t.dtype == torch.float8_e8m0fnu else torch.uint8, name)
+    want = {"grad": (grad, n), "m": (m, n), "v": (v, n), "copy": (copy, n), "m_scale": (m_scale, (n + 255) // 256), "v_scale": (v_scale, (n + 255) // 256)}
+    for name, (t, size) in want.items():
+        if t is not None and t.numel() != size:
+            raise TypeError(f"{name} must have {size} elements, got {t.numel()}")
+        if t is not None and t.device != param.device:
+            raise TypeError(f"{name} must be on the parameter's device")
+    e = aa_adamw_tensor(param.data_ptr(), grad.data_ptr(), m.data_ptr(), v.data_ptr(), _ptr(m_scale), _ptr(v_scale), _ptr(copy), n, weight_decay,
+                        _dtype_code(grad), 8 if narrow else 32)
+    e._keep = (param, grad, m, v, m_scale, v_scale, copy)
+    return e
+
+
+def adamw_list(tensors) -> ctypes.Array:
+    """The tensors of a step, laid out once.  What a step writes may lie in no other array of the list."""
+    tensors = list(tensors)
+    spans = []
+    for e in tensors:
+        for i, t in enumerate(e._keep):
+            if t is not None and t.numel():
+                spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i != 1))
+    # in address order: a written span may meet nothing, a gradient only gradients
+    end = end_written = 0
+    for a, b, written in sorted(spans):
+        if a < (end if written else end_written):
+            raise TypeError("arrays of the list overlap")
+        end = max(end, b)
+        if written:
+            end_written = max(end_written, b)
+    if len({t.device for e in tensors for t in e._keep if t is not None}) > 1:
+        raise TypeError("the tensors must be on one device")
+    got = (aa_adamw_tensor * len(tensors))(*tensors)
+    got._keep = [e._keep for e in tensors]
+    return got
+
+
 class AutoAssistError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -245,6 +325,16 @@ def lib() -> ctypes.CDLL:
         L.aa_rel_attention_scratch_bytes.argtypes = [POINTER(aa_attn), POINTER(aa_rel_bias), POINTER(c_size_t)]
         L.aa_rel_attention_grad.argtypes = [c_void_p, POINTER(aa_attn), POINTER(aa_rel_bias), POINTER(aa_dropout_rule), POINTER(aa_tokens),
                                             POINTER(aa_tokens), POINTER(aa_tokens), POINTER(aa_tokens), c_void_p, c_void_p, c_size_t]
+        live = [c_void_p, c_int64, c_void_p]
+        L.aa_linear.argtypes = [c_void_p, POINTER(aa_rows), POINTER(aa_rows), c_void_p, c_int32, POINTER(aa_rows), *live, POINTER(aa_rows), POINTER(aa_rows)]
+        L.aa_linear_grad_scratch_bytes.argtypes = [POINTER(aa_rows), POINTER(aa_rows), c_int32, POINTER(c_size_t)]
+        L.aa_linear_grad.argtypes = [c_void_p, POINTER(aa_rows), POINTER(aa_rows), c_int32, POINTER(aa_rows), POINTER(aa_rows), POINTER(aa_rows), *live,
+                                     POINTER(aa_rows), POINTER(aa_rows), c_void_p, c_void_p, c_size_t]
+        L.aa_layer_norm.argtypes = [c_void_p, POINTER(aa_rows), c_void_p, c_void_p, c_float, *live, POINTER(aa_rows)]
+        L.aa_layer_norm_grad_scratch_bytes.argtypes = [POINTER(aa_rows), POINTER(c_size_t)]
+        L.aa_layer_norm_grad.argtypes = [c_void_p, POINTER(aa_rows), c_void_p, c_float, POINTER(aa_rows), POINTER(aa_rows), *live, POINTER(aa_rows), c_void_p,
+                                         c_void_p, c_void_p, c_size_t]
+        L.aa_adamw.argtypes = [c_void_p, POINTER(aa_adamw_tensor), c_int64, POINTER(aa_adamw_rule), c_void_p]
         L.aa_device_status.argtypes = [c_void_p, POINTER(c_int32)]
         L.aa_launch_count.restype = c_int64
         L.aa_launch_count.argtypes = [c_void_p]
@@ -569,6 +659,93 @@ class AutoAssist:
         self._ok(self._L.aa_rel_attention_grad(self._ctx, byref(attn), None if bias is None else byref(bias), None if dropout is None else byref(dropout),
                                                *[byref(t) for t in ts], _ptr(dtable), base, scratch.data_ptr() + scratch.numel() - base),
                  "aa_rel_attention_grad")
+
+    def _live(self, rows: int, offsets, n_seg, count_dev):
+        """offsets, n_seg and count_dev as the C calls take them."""
+        _check(offsets, torch.int32, "offsets")
+        _check(count_dev, torch.int32, "count_dev")
+        if offsets is None:
+            n_seg = 0
+        else:
+            if n_seg is None:
+                n_seg = offsets.numel() - 1
+            if offsets.numel() <= n_seg:
+                _short(offsets, n_seg + 1, "offsets")
+        if count_dev is not None and count_dev.numel() < 1:
+            _short(count_dev, 1, "count_dev")
+        return _ptr(offsets), n_seg, _ptr(count_dev)
+
+    def _scratch(self, nbytes: int) -> torch.Tensor:
+        return torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+
+    @staticmethod
+    def _within(scratch: torch.Tensor):
+        """The aligned part of a scratch tensor: address, bytes."""
+        _check(scratch, torch.uint8, "scratch")
+        base = (scratch.data_ptr() + 255) // 256 * 256
+        return base, max(0, scratch.data_ptr() + scratch.numel() - base)
+
+    @staticmethod
+    def _vector(t, n: int, name: str):
+        _check(t, torch.float32, name)
+        if t is not None and t.numel() != n:
+            raise TypeError(f"{name} must have {n} entries, got {t.numel()}")
+        return _ptr(t)
+
+    @staticmethod
+    def _activation(name) -> int:
+        if name not in ACTIVATIONS:
+            raise TypeError(f"activation must be one of {list(ACTIVATIONS)}, got {name!r}")
+        return ACTIVATIONS[name]
+
+    def aa_linear(self, x: torch.Tensor, w: torch.Tensor, out: torch.Tensor, bias=None, activation=None, residual=None, pre=None, offsets=None,
+                  count_dev=None, n_seg=None):
+        """out = activation(x w^T + bias) + residual; pre receives x w^T + bias.  w is [out, in], bias fp32, activation None, "relu", "gelu" or "silu".
+        offsets / count_dev: only the token rows of the counted sentences (without offsets: of the counted rows) are evaluated."""
+        xm = rows_desc(x)
+        self._ok(self._L.aa_linear(self._ctx, byref(xm), byref(rows_desc(w)), self._vector(bias, w.shape[0], "bias"), self._activation(activation),
+                                   _rows_or_none(residual), *self._live(xm.rows, offsets, n_seg, count_dev), _rows_or_none(pre), byref(rows_desc(out))), "aa_linear")
+
+    def linear_grad_scratch(self, x: torch.Tensor, w: torch.Tensor, activation=None) -> torch.Tensor:
+        """Device scratch for aa_linear_grad on operands of these shapes."""
+        nbytes = c_size_t(0)
+        self._ok(self._L.aa_linear_grad_scratch_bytes(byref(rows_desc(x)), byref(rows_desc(w)), self._activation(activation), byref(nbytes)),
+                 "aa_linear_grad_scratch_bytes")
+        return self._scratch(nbytes.value)
+
+    def aa_linear_grad(self, x: torch.Tensor, w: torch.Tensor, dout: torch.Tensor, scratch: torch.Tensor, dx=None, dw=None, dbias=None, activation=None,
+                       pre=None, residual=None, offsets=None, count_dev=None, n_seg=None):
+        """Gradients of aa_linear from dout; those that are None are not computed.  residual is added to dx.  pre: as aa_linear left it (layers with an
+        activation)."""
+        xm = rows_desc(x)
+        self._ok(self._L.aa_linear_grad(self._ctx, byref(xm), byref(rows_desc(w)), self._activation(activation), _rows_or_none(pre), byref(rows_desc(dout)),
+                                        _rows_or_none(residual), *self._live(xm.rows, offsets, n_seg, count_dev), _rows_or_none(dx), _rows_or_none(dw),
+                                        self._vector(dbias, w.shape[0], "dbias"), *self._within(scratch)), "aa_linear_grad")
+
+    def aa_layer_norm(self, x: torch.Tensor, out: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, offsets=None, count_dev=None, n_seg=None):
+        """out = (x - mean) / sqrt(var + eps) * gamma + beta, row by row; gamma and beta fp32.  out may be x."""
+        xm = rows_desc(x)
+        self._ok(self._L.aa_layer_norm(self._ctx, byref(xm), self._vector(gamma, xm.cols, "gamma"), self._vector(beta, xm.cols, "beta"), eps,
+                                       *self._live(xm.rows, offsets, n_seg, count_dev), byref(rows_desc(out))), "aa_layer_norm")
+
+    def layer_norm_grad_scratch(self, x: torch.Tensor) -> torch.Tensor:
+        """Device scratch for aa_layer_norm_grad on rows of this shape."""
+        nbytes = c_size_t(0)
+        self._ok(self._L.aa_layer_norm_grad_scratch_bytes(byref(rows_desc(x)), byref(nbytes)), "aa_layer_norm_grad_scratch_bytes")
+        return self._scratch(nbytes.value)
+
+    def aa_layer_norm_grad(self, x: torch.Tensor, dout: torch.Tensor, dx: torch.Tensor, scratch: torch.Tensor, gamma=None, eps: float = 1e-5, residual=None,
+                           dgamma=None, dbeta=None, offsets=None, count_dev=None, n_seg=None):
+        """Gradients of aa_layer_norm from dout; residual is added to dx.  dx may be x, dout or residual."""
+        xm = rows_desc(x)
+        self._ok(self._L.aa_layer_norm_grad(self._ctx, byref(xm), self._vector(gamma, xm.cols, "gamma"), eps, byref(rows_desc(dout)), _rows_or_none(residual),
+                                            *self._live(xm.rows, offsets, n_seg, count_dev), byref(rows_desc(dx)), self._vector(dgamma, xm.cols, "dgamma"),
+                                            self._vector(dbeta, xm.cols, "dbeta"), *self._within(scratch)), "aa_layer_norm_grad")
+
+    def aa_adamw(self, tensors: ctypes.Array, rule: aa_adamw_rule, grad_scale=None):
+        """One AdamW step on an adamw_list; rule.t advances.  grad_scale: fp32 device scalar that multiplies the gradients; if it is not finite the step
+        writes nothing."""
+        self._ok(self._L.aa_adamw(self._ctx, tensors, len(tensors), byref(rule), self._vector(grad_scale, 1, "grad_scale")), "aa_adamw")
 
     def host_step_plan(self, x_host: torch.Tensor, logits_host: torch.Tensor):
         """Descriptors and a device staging buffer for aa_step_host on HOST tensors of these shapes."""

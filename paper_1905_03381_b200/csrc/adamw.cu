@@ -1,0 +1,329 @@
+// One AdamW step over a list of tensors (see the header for the formulas and the 8-bit states).
+//
+// Bound by memory: with fp32 moments 24 bytes an element are read and written for the moments and parameters and 2 to 6 for gradient and copy; with e4m3
+// moments 12 and 2 to 6.  The list travels in the kernel's parameters, so that a step is one launch for up to 256 tensors and nothing is
+// copied to the device; a CTA finds its tensor by bisection over the running number of chunks.  A warp owns 256 consecutive elements, which is
+// one block of the 8-bit states: two runs of 128, four elements a lane in each, so that every access is contiguous over the warp, a lane's
+// four elements share one block of random words and the block's largest magnitude is a warp reduction.
+// Products, sums, roots and quotients are each rounded by themselves: a code's rounding depends on the last bits of what is rounded.
+#include <math.h>
+
+#include "boss_common.cuh"
+
+namespace aa {
+
+namespace {
+
+constexpr int kWarpsPerCta = 8, kPerCta = kWarpsPerCta * 256 * 2;      // a warp takes two blocks, one after the other
+
+struct Entry {
+    float* param;
+    const void* grad;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    uint16_t* copy;
+    int64_t n;
+    float keep;              // 1 - lr weight_decay
+    uint32_t first;          // chunks of the entries before
+    uint32_t index;          // in the caller's list
+    uint32_t flags;          // 1: bf16 gradient, 2: arrays aligned for vectors
+};
+
+template <int N>
+struct Table {
+    Entry e[N];
+    int n;
+    float b1, c1, b2, c2;    // betas and 1 - beta
+    float rate, root, eps;   // lr / (1 - beta1^t), 1 / (1 - beta2^t)
+    uint32_t t_lo, t_hi, seed_lo, seed_hi;
+    const float* grad_scale;
+};
+
+__device__ __forceinline__ void decode4(uint32_t w, float unit, float (&x)[4]) {
+    uint32_t a, b;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(a), "=r"(b) : "r"(w));
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(x[0]), "=f"(x[1]) : "r"(a));
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(x[2]), "=f"(x[3]) : "r"(b));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __fmul_rn(x[i], unit);
+}
+__device__ __forceinline__ uint32_t encode4(const float (&y)[4]) {
+    uint32_t w;
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+        : "=r"(w)
+        : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]));
+    return w;
+}
+
+// x in units, |x| < 256 -> a neighbouring e4m3 number, by 16 random bits.  What is not finite becomes NaN.
+__device__ __forceinline__ float to_e4m3(float x, uint32_t u) {
+    const float a = fabsf(x);
+    const bool low = a < 0.015625f;                        // below the normal numbers: the equal steps of [2^-6, 2^-5)
+    float y = low ? __fadd_rn(a, 0.015625f) : a;
+    y = __uint_as_float((__float_as_uint(y) + (u << 4)) & 0xFFF00000u);
+    y = low ? __fadd_rn(y, -0.015625f) : y;
+    return a < 512.0f ? copysignf(y, x) : __uint_as_float(0x7FFFFFFFu);
+}
+// The same for a root x >= 0 whose square is to keep its mean.
+__device__ __forceinline__ float root_to_e4m3(float x, uint32_t u) {
+    const bool low = x < 0.015625f;
+    const uint32_t bits = __float_as_uint(low ? __fadd_rn(x, 0.015625f) : x) & 0xFFF00000u;
+    float y = __uint_as_float(bits), z = __uint_as_float(bits + 0x100000u);
+    y = low ? __fadd_rn(y, -0.015625f) : y;
+    z = low ? __fadd_rn(z, -0.015625f) : z;
+    const float part = __fmul_rn(__fmul_rn((float)u, 1.52587890625e-5f), __fmul_rn(__fadd_rn(z, -y), __fadd_rn(z, y)));
+    y = __fmul_rn(__fadd_rn(x, -y), __fadd_rn(x, y)) > part ? z : y;
+    return x < 512.0f ? y : __uint_as_float(0x7FFFFFFFu);
+}
+
+__device__ __forceinline__ uint32_t scale_byte(float top) {
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+    return top > 0.0f ? (uint32_t)max((int)(__float_as_uint(top) >> 23) - 7, 1) : 0u;
+}
+
+template <bool VEC>
+__device__ __forceinline__ void load4(const float* p, int64_t left, float (&x)[4]) {
+    if (VEC && left >= 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < left ? p[i] : 0.0f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void load4(const uint16_t* p, int64_t left, float (&x)[4]) {
+    if (VEC && left >= 4) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < left ? load1(p + i) : 0.0f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(float* p, int64_t left, const float (&x)[4]) {
+    if (VEC && left >= 4) {
+        *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) p[i] = x[i];
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(uint16_t* p, int64_t left, const float (&x)[4]) {
+    if (VEC && left >= 4) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) store1(p + i, x[i]);
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t left) {
+    if (VEC && left >= 4) return *reinterpret_cast<const uint32_t*>(p);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) w |= (uint32_t)p[i] << (8 * i);
+    return w;
+}
+template <bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t* p, int64_t left, uint32_t w) {
+    if (VEC && left >= 4) {
+        *reinterpret_cast<uint32_t*>(p) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) p[i] = (uint8_t)(w >> (8 * i));
+    }
+}
+
+template <int N, int BITS, bool VEC>
+__device__ __forceinline__ void update(const Table<N>& tab, const Entry& e, int64_t block, float gs) {
+    const int lane = threadIdx.x & 31;
+    const int64_t at[2] = {block * 256 + lane * 4, block * 256 + 128 + lane * 4};
+    float p[2][4], g[2][4], m[2][4], v[2][4];
+    uint32_t mc[2], vc[2];
+    uint32_t mb = 0, vb = 0;
+    if (BITS == 8) {
+        mb = e.m_scale[block];
+        vb = e.v_scale[block];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t left = e.n - at[h];
+        load4<VEC>(e.param + at[h], left, p[h]);
+        if (e.flags & 1) load4<VEC>(static_cast<const uint16_t*>(e.grad) + at[h], left, g[h]);
+        else load4<VEC>(static_cast<const float*>(e.grad) + at[h], left, g[h]);
+        if (BITS == 32) {
+            load4<VEC>(static_cast<const float*>(e.m) + at[h], left, m[h]);
+            load4<VEC>(static_cast<const float*>(e.v) + at[h], left, v[h]);
+        } else {
+            mc[h] = load_codes<VEC>(static_cast<const uint8_t*>(e.m) + at[h], left);
+            vc[h] = load_codes<VEC>(static_cast<const uint8_t*>(e.v) + at[h], left);
+        }
+    }
+    float m_top = 0.0f, v_top = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (BITS == 8) {
+            decode4(mc[h], __uint_as_float(mb << 23), m[h]);
+            decode4(vc[h], __uint_as_float(vb << 23), v[h]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = tab.grad_scale ? __fmul_rn(g[h][i], gs) : g[h][i];
+            if (BITS == 8) v[h][i] = __fmul_rn(v[h][i], v[h][i]);
+            m[h][i] = __fadd_rn(__fmul_rn(m[h][i], tab.b1), __fmul_rn(x, tab.c1));
+            v[h][i] = __fadd_rn(__fmul_rn(v[h][i], tab.b2), __fmul_rn(__fmul_rn(x, x), tab.c2));
+            const float den = __fadd_rn(__fsqrt_rn(__fmul_rn(v[h][i], tab.root)), tab.eps);
+            p[h][i] = __fadd_rn(__fmul_rn(p[h][i], e.keep), -__fmul_rn(__fdiv_rn(m[h][i], den), tab.rate));
+            if (BITS == 8) {
+                v[h][i] = __fsqrt_rn(v[h][i]);
+                m_top = fmaxf(m_top, fabsf(m[h][i]));
+                v_top = fmaxf(v_top, v[h][i]);
+            }
+        }
+        const int64_t left = e.n - at[h];
+        store4<VEC>(e.param + at[h], left, p[h]);
+        if (e.copy) store4<VEC>(e.copy + at[h], left, p[h]);
+        if (BITS == 32) {
+            store4<VEC>(static_cast<float*>(e.m) + at[h], left, m[h]);
+            store4<VEC>(static_cast<float*>(e.v) + at[h], left, v[h]);
+        }
+    }
+    if (BITS == 32) return;
+    mb = scale_byte(m_top);
+    vb = scale_byte(v_top);
+    const float mi = mb ? __uint_as_float((254u - mb) << 23) : 1.0f, vi = vb ? __uint_as_float((254u - vb) << 23) : 1.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const Words4 w = philox4x32_10((uint32_t)(at[h] >> 2), e.index, tab.t_lo, tab.t_hi, tab.seed_lo, tab.seed_hi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool some = v[h][i] > 0.0f;
+            m[h][i] = to_e4m3(__fmul_rn(m[h][i], mi), w.w[i] & 0xFFFFu);
+            v[h][i] = root_to_e4m3(__fmul_rn(v[h][i], vi), w.w[i] >> 16);
+            if (some && v[h][i] == 0.0f) v[h][i] = 0.001953125f;      // 2^-9
+        }
+        const int64_t left = e.n - at[h];
+        store_codes<VEC>(static_cast<uint8_t*>(e.m) + at[h], left, encode4(m[h]));
+        store_codes<VEC>(static_cast<uint8_t*>(e.v) + at[h], left, encode4(v[h]));
+    }
+    if (lane == 0) {
+        e.m_scale[block] = (uint8_t)mb;
+        e.v_scale[block] = (uint8_t)vb;
+    }
+}
+
+template <int N, int BITS>
+__global__ void __launch_bounds__(kWarpsPerCta * 32) adamw_kernel(const __grid_constant__ Table<N> tab) {
+    int lo = 0, hi = tab.n;                  // the last entry with first <= blockIdx.x
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (tab.e[mid].first <= blockIdx.x) lo = mid; else hi = mid;
+    }
+    const Entry& e = tab.e[lo];
+    const int64_t block = (int64_t)(blockIdx.x - e.first) * (kPerCta / 256) + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    grid_dependency_release();
+    float gs = 1.0f;
+    if (tab.grad_scale) {
+        gs = *tab.grad_scale;
+        if (!(fabsf(gs) < INFINITY)) return;
+    }
+#pragma unroll 1
+    for (int i = 0; i < kPerCta / 256 / kWarpsPerCta; ++i) {
+        const int64_t b = block + i * kWarpsPerCta;
+        if (b * 256 >= e.n) return;
+        if (e.flags & 2) update<N, BITS, true>(tab, e, b, gs);
+        else update<N, BITS, false>(tab, e, b, gs);
+    }
+}
+
+template <int N, int BITS>
+aa_status launch_some(aa_ctx_impl* c, const aa_adamw_tensor* t, int64_t count, const aa_adamw_rule* r, const float* grad_scale) {
+    static_assert(sizeof(Table<N>) <= 32764, "kernel parameters");
+    Table<N> tab;
+    const double step = (double)(r->t + 1);
+    tab.b1 = (float)r->beta1;
+    tab.c1 = (float)(1.0 - r->beta1);
+    tab.b2 = (float)r->beta2;
+    tab.c2 = (float)(1.0 - r->beta2);
+    tab.rate = (float)(r->lr / (1.0 - pow(r->beta1, step)));
+    tab.root = (float)(1.0 / (1.0 - pow(r->beta2, step)));
+    tab.eps = (float)r->eps;
+    tab.t_lo = (uint32_t)(r->t + 1);
+    tab.t_hi = (uint32_t)((uint64_t)(r->t + 1) >> 32);
+    tab.seed_lo = (uint32_t)r->seed;
+    tab.seed_hi = (uint32_t)(r->seed >> 32);
+    tab.grad_scale = grad_scale;
+    int64_t at = 0;
+    while (at < count) {
+        tab.n = 0;
+        uint32_t chunks = 0;
+        for (; at < count && tab.n < N; ++at) {
+            if (t[at].state_bits != BITS || t[at].n == 0) continue;
+            const int64_t need = (t[at].n + kPerCta - 1) / kPerCta;
+            if (chunks + need > 0x7FFFFFFFll) break;
+            const auto on = [](const void* p, uintptr_t a) { return (uintptr_t)p % a == 0; };
+            const bool bf16 = t[at].grad_dtype == AA_BF16, wide = BITS == 32;
+            const bool vec = on(t[at].param, 16) && on(t[at].grad, bf16 ? 8 : 16) && on(t[at].m, wide ? 16 : 4) && on(t[at].v, wide ? 16 : 4) && on(t[at].copy, 8);
+            tab.e[tab.n++] = Entry{t[at].param, t[at].grad, t[at].m, t[at].v, t[at].m_scale, t[at].v_scale, static_cast<uint16_t*>(t[at].copy), t[at].n,
+                                   (float)(1.0 - r->lr * t[at].weight_decay), chunks, (uint32_t)at, (bf16 ? 1u : 0u) | (vec ? 2u : 0u)};
+            chunks += (uint32_t)need;
+        }
+        if (tab.n == 0) break;
+        void* args[] = {&tab};
+        if (launch_overlapped(c, (const void*)adamw_kernel<N, BITS>, dim3(chunks), dim3(kWarpsPerCta * 32), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+        ++c->launches;
+    }
+    return AA_OK;
+}
+
+}  // namespace
+
+}  // namespace aa
+
+using namespace aa;
+
+extern "C" aa_status aa_adamw(aa_ctx* ctx, const aa_adamw_tensor* tensors, int64_t n_tensors, aa_adamw_rule* rule, const float* grad_scale) {
+    if (!ctx || !rule || n_tensors < 0 || (n_tensors > 0 && !tensors)) return AA_ERR_INVALID_ARG;
+    const auto share = [](double x) { return x >= 0.0 && x < 1.0; };
+    if (!(rule->lr >= 0.0) || !isfinite(rule->lr) || !share(rule->beta1) || !share(rule->beta2) || !(rule->eps >= 0.0) || !isfinite(rule->eps) || rule->t < 0)
+        return AA_ERR_INVALID_ARG;
+    if (n_tensors > 0x7FFFFFFFll) return AA_ERR_UNSUPPORTED;
+    int64_t wide = 0, narrow = 0;
+    for (int64_t i = 0; i < n_tensors; ++i) {
+        const aa_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || (t.grad_dtype != AA_F32 && t.grad_dtype != AA_BF16) || (t.state_bits != 32 && t.state_bits != 8) || !isfinite(t.weight_decay)) return AA_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (t.n > (1ll << 33)) return AA_ERR_UNSUPPORTED;
+        const bool bytes = t.state_bits == 8;
+        if (!t.param || !t.grad || !t.m || !t.v || (bytes && (!t.m_scale || !t.v_scale))) return AA_ERR_INVALID_ARG;
+        const uintptr_t es = t.grad_dtype == AA_BF16 ? 2 : 4;
+        if ((uintptr_t)t.param % 4 || (uintptr_t)t.grad % es || (uintptr_t)t.copy % 2 || (!bytes && ((uintptr_t)t.m % 4 || (uintptr_t)t.v % 4))) return AA_ERR_INVALID_ARG;
+        // [begin, end) of each array: nothing written may lie in another
+        const uintptr_t n = (uintptr_t)t.n, sb = bytes ? 1 : 4, blocks = bytes ? (n + 255) / 256 : 0;
+        const struct { uintptr_t at, size; } a[7] = {{(uintptr_t)t.param, 4 * n},     {(uintptr_t)t.m, sb * n},         {(uintptr_t)t.v, sb * n},   {(uintptr_t)t.copy, t.copy ? 2 * n : 0},
+                                                      {(uintptr_t)t.m_scale, blocks}, {(uintptr_t)t.v_scale, blocks}, {(uintptr_t)t.grad, es * n}};
+        for (int x = 0; x < 7; ++x)
+            for (int y = 0; y < x; ++y)
+                if (a[x].size && a[y].size && a[x].at < a[y].at + a[y].size && a[y].at < a[x].at + a[x].size) return AA_ERR_INVALID_ARG;
+        ++(bytes ? narrow : wide);
+    }
+    aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
+    aa_status st = AA_OK;
+    // a long list takes a longer parameter block, which costs a launch little and saves several
+    if (wide) st = wide <= 32 ? launch_some<32, 32>(c, tensors, n_tensors, rule, grad_scale) : launch_some<256, 32>(c, tensors, n_tensors, rule, grad_scale);
+    if (st == AA_OK && narrow) st = narrow <= 32 ? launch_some<32, 8>(c, tensors, n_tensors, rule, grad_scale) : launch_some<256, 8>(c, tensors, n_tensors, rule, grad_scale);
+    if (st == AA_OK) ++rule->t;
+    return st;
+}

@@ -1,0 +1,234 @@
+// C entry points of linear layers and layer normalisation: argument checks and dispatch.
+#include <string.h>
+
+#include "boss_args.cuh"
+#include "layer_norm.cuh"
+#include "linear.cuh"
+
+namespace aa {
+
+namespace {
+
+constexpr int64_t kMaxWidth = 1ll << 30;
+
+MatArg mat(const aa_rows* m) { return m ? MatArg{m->data, m->row_stride} : MatArg{nullptr, 0}; }
+
+bool check_live(const int32_t* offsets, int64_t n_seg) { return offsets ? n_seg >= 0 : n_seg == 0; }
+
+LiveRows live_arg(const int32_t* offsets, int64_t n_seg, const int32_t* count_dev, int64_t rows) { return LiveRows{offsets, n_seg, count_dev, rows}; }
+
+// In bytes, so that matrices of different types compare.
+Extent bytes_of(const aa_rows* m) {
+    const int64_t es = m->dtype == AA_BF16 ? 2 : 4;
+    return Extent{m->data, m->rows, m->row_stride * es, 1, 0, m->cols * es};
+}
+Extent bytes_of(const float* v, int64_t n) { return Extent{v, v ? 1 : 0, 0, 1, 0, n * 4}; }
+bool clear_of(const aa_rows* out, const aa_rows* other) { return !out || !other || apart(bytes_of(out), bytes_of(other), 1); }
+bool clear_of(const aa_rows* out, const float* v, int64_t n) { return !out || !v || apart(bytes_of(out), bytes_of(v, n), 1); }
+bool clear_of(const float* a, const float* b, int64_t n) { return !a || !b || a + n <= b || b + n <= a; }
+// The same matrix, or nothing in common.
+bool same_or_clear(const aa_rows* out, const aa_rows* in) {
+    if (!out || !in) return true;
+    return in->data == out->data ? in->row_stride == out->row_stride || in->rows <= 1 : clear_of(out, in);
+}
+
+bool floats_ok(const float* p) { return (uintptr_t)p % 4 == 0; }
+bool act_ok(int32_t a) { return a >= AA_ACT_NONE && a <= AA_ACT_SILU; }
+
+struct LinearScratch {
+    size_t g, parts, total;
+};
+LinearScratch linear_scratch(int64_t rows, int64_t cols, int dtype, int act) {
+    const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    LinearScratch s;
+    s.g = act == AA_ACT_NONE ? 0 : up((size_t)rows * (size_t)((cols + 7) / 8 * 8) * (dtype == AA_BF16 ? 2 : 4));
+    s.parts = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));
+    s.total = s.g + s.parts;
+    return s;
+}
+
+aa_status check_linear(const aa_rows* x, const aa_rows* w) {
+    if (check_rows(x) != AA_OK || check_rows(w) != AA_OK || x->dtype != w->dtype || x->cols != w->cols || w->rows < 1) return AA_ERR_INVALID_ARG;
+    return x->cols > kMaxWidth || w->rows > kMaxWidth ? AA_ERR_UNSUPPORTED : AA_OK;
+}
+
+}  // namespace
+}  // namespace aa
+
+using namespace aa;
+
+extern "C" {
+
+aa_status aa_linear(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, const float* bias, int32_t activation, const aa_rows* residual, const int32_t* offsets,
+                    int64_t n_seg, const int32_t* count_dev, const aa_rows* pre, const aa_rows* out) {
+    if (!ctx || !act_ok(activation) || !check_live(offsets, n_seg) || !floats_ok(bias)) return AA_ERR_INVALID_ARG;
+    const aa_status st = check_linear(x, w);
+    if (st != AA_OK) return st;
+    const auto like_out = [&](const aa_rows* m) { return check_rows(m) == AA_OK && m->dtype == x->dtype && m->rows == x->rows && m->cols == w->rows; };
+    if (!like_out(out) || (residual && !like_out(residual)) || (pre && !like_out(pre))) return AA_ERR_INVALID_ARG;
+    for (const aa_rows* m : {pre, out})
+        if (!clear_of(m, x) || !clear_of(m, w) || !clear_of(m, bias, w->rows)) return AA_ERR_INVALID_ARG;
+    if (!same_or_clear(out, residual) || !clear_of(pre, residual) || !clear_of(pre, out)) return AA_ERR_INVALID_ARG;
+    if (x->rows == 0) return AA_OK;
+    aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
+    ProductParams p = {};
+    p.a = mat(x);
+    p.b = mat(w);
+    p.m = x->rows;
+    p.n = w->rows;
+    p.k = x->cols;
+    p.live = live_arg(offsets, n_seg, count_dev, x->rows);
+    p.bias = bias;
+    p.act = activation;
+    p.residual = mat(residual);
+    p.pre = mat(pre);
+    p.out = mat(out);
+    p.ctl = c->ctl;
+    return launch_product(c, p, x->dtype);
+}
+
+aa_status aa_linear_grad_scratch_bytes(const aa_rows* x, const aa_rows* w, int32_t activation, size_t* bytes) {
+    if (!bytes || !act_ok(activation)) return AA_ERR_INVALID_ARG;
+    const aa_status st = check_linear(x, w);
+    if (st != AA_OK) return st;
+    *bytes = linear_scratch(x->rows, w->rows, x->dtype, activation).total;
+    return AA_OK;
+}
+
+aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_t activation, const aa_rows* pre, const aa_rows* dout, const aa_rows* residual,
+                         const int32_t* offsets, int64_t n_seg, const int32_t* count_dev, const aa_rows* dx, const aa_rows* dw, float* dbias, void* scratch,
+                         size_t scratch_bytes) {
+    if (!ctx || !act_ok(activation) || !check_live(offsets, n_seg) || !floats_ok(dbias) || (activation == AA_ACT_NONE) != !pre || (residual && !dx)) return AA_ERR_INVALID_ARG;
+    const aa_status st = check_linear(x, w);
+    if (st != AA_OK) return st;
+    const auto like_out = [&](const aa_rows* m) { return check_rows(m) == AA_OK && m->dtype == x->dtype && m->rows == x->rows && m->cols == w->rows; };
+    if (!like_out(dout) || (pre && !like_out(pre))) return AA_ERR_INVALID_ARG;
+    for (const aa_rows* m : {residual, dx})
+        if (m && (check_rows(m) != AA_OK || !same_shape(*m, *x))) return AA_ERR_INVALID_ARG;
+    if (dw && (check_rows(dw) != AA_OK || !same_shape(*dw, *w))) return AA_ERR_INVALID_ARG;
+    for (const aa_rows* in : {x, w, pre, dout})
+        if (!clear_of(dx, in) || !clear_of(dw, in) || !clear_of(in, dbias, w->rows)) return AA_ERR_INVALID_ARG;
+    if (!same_or_clear(dx, residual) || !clear_of(dw, residual) || !clear_of(dw, dx) || !clear_of(dx, dbias, w->rows) || !clear_of(dw, dbias, w->rows) ||
+        !clear_of(residual, dbias, w->rows))
+        return AA_ERR_INVALID_ARG;
+    const LinearScratch need = linear_scratch(x->rows, w->rows, x->dtype, activation);
+    if (!scratch || (uintptr_t)scratch % 256) return AA_ERR_INVALID_ARG;
+    if (scratch_bytes < need.total) return AA_ERR_WORKSPACE;
+    aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
+    const LiveRows live = live_arg(offsets, n_seg, count_dev, x->rows);
+    if (x->rows == 0) {
+        aa_status zero = AA_OK;
+        if (dw) zero = cuda_ok(cudaMemset2DAsync(dw->data, (size_t)dw->row_stride * (dw->dtype == AA_BF16 ? 2 : 4), 0, (size_t)dw->cols * (dw->dtype == AA_BF16 ? 2 : 4), (size_t)dw->rows, c->stream));
+        if (zero == AA_OK && dbias) zero = cuda_ok(cudaMemsetAsync(dbias, 0, (size_t)w->rows * sizeof(float), c->stream));
+        return zero;
+    }
+    MatArg g = mat(dout);
+    if (activation != AA_ACT_NONE) g = MatArg{scratch, (w->rows + 7) / 8 * 8};
+    if (activation != AA_ACT_NONE || dbias) {
+        SlopeParams s = {};
+        s.dout = mat(dout);
+        s.pre = mat(pre);
+        if (activation != AA_ACT_NONE && (dx || dw)) s.g = g;
+        s.rows = x->rows;
+        s.cols = w->rows;
+        s.live = live;
+        s.act = activation;
+        s.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + need.g);
+        s.dbias = dbias;
+        s.ctl = c->ctl;
+        const aa_status done = launch_slope(c, s, x->dtype);
+        if (done != AA_OK) return done;
+    }
+    ProductParams p = {};
+    p.ctl = c->ctl;
+    p.live = live;
+    p.a = g;
+    if (dx) {
+        p.b = mat(w);
+        p.b_across = true;
+        p.m = x->rows;
+        p.n = x->cols;
+        p.k = w->rows;
+        p.residual = mat(residual);
+        p.out = mat(dx);
+        const aa_status done = launch_product(c, p, x->dtype);
+        if (done != AA_OK) return done;
+    }
+    if (!dw) return AA_OK;
+    p.b = mat(x);
+    p.a_across = p.b_across = p.live_k = true;
+    p.m = w->rows;
+    p.n = x->cols;
+    p.k = x->rows;
+    p.residual = MatArg{nullptr, 0};
+    p.out = mat(dw);
+    return launch_product(c, p, x->dtype);
+}
+
+aa_status aa_layer_norm(aa_ctx* ctx, const aa_rows* x, const float* gamma, const float* beta, float eps, const int32_t* offsets, int64_t n_seg,
+                        const int32_t* count_dev, const aa_rows* out) {
+    if (!ctx || !check_live(offsets, n_seg) || check_rows(x) != AA_OK || check_rows(out) != AA_OK || !same_shape(*x, *out)) return AA_ERR_INVALID_ARG;
+    if (!(eps >= 0.0f) || !floats_ok(gamma) || !floats_ok(beta) || !same_or_clear(out, x) || !clear_of(out, gamma, x->cols) || !clear_of(out, beta, x->cols)) return AA_ERR_INVALID_ARG;
+    if (x->cols > kMaxWidth) return AA_ERR_UNSUPPORTED;
+    if (x->rows == 0) return AA_OK;
+    aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
+    NormParams p = {};
+    p.x = mat(x);
+    p.out = mat(out);
+    p.cols = x->cols;
+    p.live = live_arg(offsets, n_seg, count_dev, x->rows);
+    p.gamma = gamma;
+    p.beta = beta;
+    p.eps = eps;
+    p.ctl = c->ctl;
+    return launch_layer_norm(c, p, x->dtype, false, nullptr, nullptr);
+}
+
+aa_status aa_layer_norm_grad_scratch_bytes(const aa_rows* x, size_t* bytes) {
+    if (!bytes || check_rows(x) != AA_OK) return AA_ERR_INVALID_ARG;
+    if (x->cols > kMaxWidth) return AA_ERR_UNSUPPORTED;
+    const size_t stats = x->cols > kNormInRegisters ? ((size_t)x->rows * sizeof(float2) + 255) / 256 * 256 : 0;
+    *bytes = stats + norm_scratch_floats(x->rows, x->cols) * sizeof(float);
+    return AA_OK;
+}
+
+aa_status aa_layer_norm_grad(aa_ctx* ctx, const aa_rows* x, const float* gamma, float eps, const aa_rows* dout, const aa_rows* residual, const int32_t* offsets,
+                             int64_t n_seg, const int32_t* count_dev, const aa_rows* dx, float* dgamma, float* dbeta, void* scratch, size_t scratch_bytes) {
+    if (!ctx || !check_live(offsets, n_seg) || check_rows(x) != AA_OK || !(eps >= 0.0f)) return AA_ERR_INVALID_ARG;
+    for (const aa_rows* m : {dout, dx})
+        if (check_rows(m) != AA_OK || !same_shape(*m, *x)) return AA_ERR_INVALID_ARG;
+    if (residual && (check_rows(residual) != AA_OK || !same_shape(*residual, *x))) return AA_ERR_INVALID_ARG;
+    const int64_t n = x->cols;
+    if (!floats_ok(gamma) || !floats_ok(dgamma) || !floats_ok(dbeta) || !same_or_clear(dx, x) || !same_or_clear(dx, dout) || !same_or_clear(dx, residual) || !clear_of(dx, gamma, n) ||
+        !clear_of(dgamma, dbeta, n) || !clear_of(gamma, dgamma, n) || !clear_of(gamma, dbeta, n))
+        return AA_ERR_INVALID_ARG;
+    for (const aa_rows* m : {x, dout, residual, dx})
+        if (!clear_of(m, dgamma, n) || !clear_of(m, dbeta, n)) return AA_ERR_INVALID_ARG;
+    size_t need = 0;
+    const aa_status st = aa_layer_norm_grad_scratch_bytes(x, &need);
+    if (st != AA_OK) return st;
+    if (need > 0 && (!scratch || (uintptr_t)scratch % 256)) return AA_ERR_INVALID_ARG;
+    if (scratch_bytes < need) return AA_ERR_WORKSPACE;
+    aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
+    if (x->rows == 0) {
+        aa_status zero = dgamma ? cuda_ok(cudaMemsetAsync(dgamma, 0, (size_t)n * sizeof(float), c->stream)) : AA_OK;
+        if (zero == AA_OK && dbeta) zero = cuda_ok(cudaMemsetAsync(dbeta, 0, (size_t)n * sizeof(float), c->stream));
+        return zero;
+    }
+    NormParams p = {};
+    p.x = mat(x);
+    p.dout = mat(dout);
+    p.residual = mat(residual);
+    p.out = mat(dx);
+    p.cols = n;
+    p.live = live_arg(offsets, n_seg, count_dev, x->rows);
+    p.gamma = gamma;
+    p.eps = eps;
+    p.ctl = c->ctl;
+    const size_t stats = n > kNormInRegisters ? ((size_t)x->rows * sizeof(float2) + 255) / 256 * 256 : 0;
+    p.stats = static_cast<float2*>(scratch);
+    if (dgamma || dbeta) p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats);
+    return launch_layer_norm(c, p, x->dtype, true, dgamma, dbeta);
+}
+
+}  // extern "C"
