@@ -36,6 +36,9 @@ struct ProductParams {
 };
 
 aa_status launch_product(aa_ctx_impl* c, const ProductParams& p, int dtype);
+// bf16 operands that TMA can fetch (16-byte aligned bases and rows).
+bool product_tc_fits(const ProductParams& p);
+aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p);
 // g = dout * act'(pre), rounded to the matrices' type; column sums of the unrounded g (or of dout alone where act is AA_ACT_NONE and g null) into dbias.
 struct SlopeParams {
     MatArg dout, pre, g;

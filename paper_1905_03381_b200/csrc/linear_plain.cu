@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(256) slope_join_kernel(const float* parts, flo
 
 aa_status launch_product(aa_ctx_impl* c, const ProductParams& in, int dtype) {
     ProductParams p = in;
+    if (dtype == AA_BF16 && product_tc_fits(p)) return launch_product_tc(c, p);
     const int64_t mt = (p.m + kT - 1) / kT, nt = (p.n + kT - 1) / kT;
     if (mt > 0x7FFFFFFFll || nt > 65535) return AA_ERR_UNSUPPORTED;
     const void* kernel = dtype == AA_BF16 ? (const void*)product_plain_kernel<uint16_t> : (const void*)product_plain_kernel<float>;
