@@ -54,12 +54,12 @@ struct OccEntry {
     size_t smem;
     int ctas;
 };
-constexpr int kOccSlots = 64;
+constexpr int kOccSlots = 128;
 struct SmemEntry {
     const void* kernel;
     size_t limit;
 };
-constexpr int kSmemSlots = 64;
+constexpr int kSmemSlots = 128;
 
 }  // namespace
 
@@ -87,6 +87,28 @@ int resident_ctas(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_sm
     const int ctas = per_sm * c->sm_count;
     if (ctx->occ_used < kOccSlots) ctx->occ[ctx->occ_used++] = OccEntry{kernel, threads, dyn_smem, ctas};
     return ctas;
+}
+
+int resident_clusters(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_smem, int cluster) {
+    aa_ctx* ctx = reinterpret_cast<aa_ctx*>(c);
+    for (int i = 0; i < ctx->occ_used; ++i) {
+        const OccEntry& e = ctx->occ[i];
+        if (e.kernel == kernel && e.threads == -threads && e.smem == dyn_smem) return e.ctas;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(c->sm_count / cluster * cluster));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = dyn_smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return -1;
+    if (ctx->occ_used < kOccSlots) ctx->occ[ctx->occ_used++] = OccEntry{kernel, -threads, dyn_smem, n};
+    return n;
 }
 
 // The limit belongs to the function, not to the context: set to each call's own size, one host thread's call lowered it between another's setting and

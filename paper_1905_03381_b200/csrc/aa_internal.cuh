@@ -300,6 +300,9 @@ aa_status allow_smem(aa_ctx_impl* c, const void* kernel, size_t dyn_smem);
 // Persistent-grid size for a kernel: CTAs that fit on the device at once.
 int resident_ctas(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_smem);
 
+// Clusters of `cluster` CTAs that fit on the device at once (SMs of a group that are left over count for nothing).
+int resident_clusters(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_smem, int cluster);
+
 inline aa_status cuda_ok(cudaError_t e) { return e == cudaSuccess ? AA_OK : AA_ERR_CUDA; }
 
 }  // namespace aa

@@ -35,14 +35,18 @@ bool same_or_clear(const aa_rows* out, const aa_rows* in) {
 bool floats_ok(const float* p) { return (uintptr_t)p % 4 == 0; }
 bool act_ok(int32_t a) { return a >= AA_ACT_NONE && a <= AA_ACT_SILU; }
 
+// G, then the column sums' parts or (later in the call) the products' parts.
 struct LinearScratch {
     size_t g, parts, total;
 };
+// The parts of a cut tile are 256 KB in fp32 on each pair of SMs; three rounds of them (58 MB) leave little to balance.
+constexpr size_t kProductParts = 3ull * 74 * 256 * 256 * sizeof(float);
 LinearScratch linear_scratch(int64_t rows, int64_t cols, int dtype, int act) {
     const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     LinearScratch s;
     s.g = act == AA_ACT_NONE ? 0 : up((size_t)rows * (size_t)((cols + 7) / 8 * 8) * (dtype == AA_BF16 ? 2 : 4));
-    s.parts = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));
+    const size_t sums = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));
+    s.parts = dtype == AA_BF16 && sums < kProductParts ? kProductParts : sums;
     s.total = s.g + s.parts;
     return s;
 }
@@ -143,6 +147,8 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
     p.ctl = c->ctl;
     p.live = live;
     p.a = g;
+    p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + need.g);
+    p.part_floats = (int64_t)(need.parts / sizeof(float));
     if (dx) {
         p.b = mat(w);
         p.b_across = true;

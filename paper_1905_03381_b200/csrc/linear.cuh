@@ -32,6 +32,8 @@ struct ProductParams {
     const float* bias;       // [n], nullable
     int act;                 // aa_activation
     MatArg residual, pre, out;   // nullable but out
+    float* parts;            // scratch for tiles cut along the contraction, nullable (then bias, act and pre are empty)
+    int64_t part_floats;
     Control* ctl;
 };
 

@@ -1,10 +1,16 @@
 // Products of linear layers on the 5th-generation tensor cores (tcgen05), bf16 operands that TMA can fetch.
 //
-// A persistent CTA per SM takes 128 x BN tiles of C = A B^T.  One warp fetches 64-wide slices of both operands into a ring (128-byte swizzle; an operand
-// whose contraction runs across its stored rows is fetched as it lies and read by the matrix unit in its other orientation, so nothing is
-// ever transposed in memory), one warp issues the products (M = 128, N = BN, K = 16, four a slice) into one of two accumulators in TMEM, and eight warps
-// take the finished accumulator through a 32 x 32 stage of their own - a thread holds a row of the accumulator but has to store along
-// rows - while the next tile's products run.  Bias, activation, residual and the single rounding happen on that way.
+// A persistent pair of CTAs (a cluster of two SMs) takes 256 x 256 tiles of C = A B^T, a single CTA 128 x BN tiles where there are few rows.  A warp fetches
+// 64-wide slices of its CTA's 128 rows of A and of its half of B into a ring (128-byte swizzle; an operand whose contraction runs across its
+// stored rows is fetched as it lies and read by the matrix unit in its other orientation, so nothing is ever transposed in memory).  One warp
+// of the pair issues the products (M = 256, N = BN, K = 16, four a slice), which read both CTAs' shared memory and leave 128 rows in each CTA's TMEM.
+// Two accumulators alternate: eight warps take the finished one through
+// a 32 x 32 stage of their own - a thread holds a row of the accumulator but has to store along rows - while the next tile's products run.
+// Bias, activation, residual and the single rounding happen on that way.
+// Pairs, because a tile of 128 x 256 needs 96 bytes a cycle and SM out of L2, which gives about 60, and one of 256 x 256 needs 64.
+//
+// Tiles that do not fill the last round of SMs can be cut along the contraction (the backward call has scratch memory): their parts go to
+// scratch in fp32 and a second kernel adds them up in order and finishes them.
 #include "linear.cuh"
 #include "tensor_core.cuh"
 
@@ -18,77 +24,166 @@ constexpr int kEpilogue = 8;
 constexpr int kStageFloats = 32 * 32;    // per epilogue warp
 constexpr int kMaxStages = 8;
 
-template <int BN>
+// CG CTAs share a tile of CG 128 rows and BN columns.
+template <int CG, int BN>
 struct Geo {
-    static constexpr int A = kBM * 128, B = BN * 128, STAGE = A + B;
-    static constexpr int STAGES = BN == 256 ? 4 : (BN == 128 ? 6 : 8);
-    static constexpr int TMEM = 2 * BN < 32 ? 32 : 2 * BN;
+    static constexpr int A = kBM * 128, ROWS_B = BN / CG, B = ROWS_B * 128, STAGE = A + B;
+    static constexpr int STAGES = STAGE == 49152 ? 4 : (STAGE == 32768 ? 6 : 8);
+    static constexpr int TMEM = 2 * BN;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + kEpilogue * kStageFloats * sizeof(float);
 };
 
 struct Ctl {
     uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    uint64_t ragged, cleared;            // the last slice of tokens: it has arrived (second CTA), its rest is zero there (first CTA)
     uint32_t tmem;
     int abort_flag;
 };
 
-struct Tiles {
-    int mt, nt, n;                       // of this launch
+// What a launch does in which order: the first `whole` tiles at once, the others in `splits` parts each.
+struct Plan {
+    int nt, whole, splits;
+    float* parts;                        // [part][CG 128][BN]
 };
 
-__device__ __forceinline__ void tile_at(const Tiles& t, int i, int& m, int& n) {
-    const int per = kGroupM * t.nt, g = i / per, in = i - g * per, rows = min(kGroupM, t.mt - g * kGroupM);
+struct Unit {
+    int m, n, s0, s1, part;              // slices [s0, s1); part < 0: the whole tile
+};
+
+__device__ __forceinline__ void tile_at(int mt, int nt, int i, int& m, int& n) {
+    const int per = kGroupM * nt, g = i / per, in = i - g * per, rows = min(kGroupM, mt - g * kGroupM);
     n = in / rows;
     m = g * kGroupM + (in - n * rows);
 }
+__device__ __forceinline__ int units_of(const Plan& p, int mt) {
+    const int tiles = mt * p.nt;
+    return tiles <= p.whole ? tiles : p.whole + (tiles - p.whole) * p.splits;
+}
+__device__ __forceinline__ Unit unit_at(const Plan& p, int mt, int slices, int i) {
+    Unit u;
+    if (i < p.whole) {
+        tile_at(mt, p.nt, i, u.m, u.n);
+        u.s0 = 0;
+        u.s1 = slices;
+        u.part = -1;
+    } else {
+        const int j = i - p.whole, t = j / p.splits, q = j - t * p.splits;
+        tile_at(mt, p.nt, p.whole + t, u.m, u.n);
+        u.s0 = (int)((int64_t)slices * q / p.splits);
+        u.s1 = (int)((int64_t)slices * (q + 1) / p.splits);
+        u.part = j;
+    }
+    return u;
+}
 
-template <int BN, bool A_ACROSS, bool B_ACROSS>
+// ---- a pair of CTAs
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same barrier of CTA `rank` of the pair.
+__device__ __forceinline__ uint32_t of_rank(const void* shared, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(shared)), "r"(rank));
+    return a;
+}
+// Orders the reads of TMEM and shared memory by tcgen05 only, which the barriers of a pair do at their default scope.
+__device__ __forceinline__ void mbar_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Orders ordinary writes before it too, over the pair (dear: not for every slice).
+__device__ __forceinline__ void mbar_release_at(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// A box into this CTA's shared memory whose bytes count on a barrier of either CTA.
+template <int CG>
+__device__ __forceinline__ void load_box(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar, uint32_t first_bar) {
+    if (CG == 1) tma_load_2d(dst, map, x, y, bar);
+    else
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)), "l"(map),
+                     "r"(first_bar), "r"(x), "r"(y)
+                     : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    if (CG == 1) umma_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    if (CG == 1) umma_bf16(d, a, b, idesc, accumulate);
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                     "r"((uint32_t)accumulate)
+                     : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void alloc(uint32_t* dst, uint32_t cols) {
+    if (CG == 1) {
+        tmem_alloc(dst, cols);
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void dealloc(uint32_t addr, uint32_t cols) {
+    if (CG == 1) tmem_dealloc(addr, cols);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+}
+
+template <int CG, int BN, bool A_ACROSS, bool B_ACROSS>
 __global__ void __launch_bounds__(kTcThreads, 1)
-product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductParams p, int mt, int nt, bool vec) {
-    using G = Geo<BN>;
+product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan,
+                  bool vec) {
+    using G = Geo<CG, BN>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Ctl ctl;
     unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     float* stage_f = reinterpret_cast<float*>(ring + (size_t)G::STAGES * G::STAGE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CG == 1 ? 0 : (int)cluster_rank();
     volatile int* abort_flag = &ctl.abort_flag;
     if (threadIdx.x == 0) {
         for (int s = 0; s < G::STAGES; ++s) {
-            mbar_init(&ctl.full[s], 1);
+            mbar_init(&ctl.full[s], 1);      // both CTAs' copies count on the first one's
             mbar_init(&ctl.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&ctl.acc_full[b], 1);
-            mbar_init(&ctl.acc_empty[b], kEpilogue);
+            mbar_init(&ctl.acc_empty[b], CG * kEpilogue);
         }
         mbar_init(&ctl.drain, 1);
+        mbar_init(&ctl.ragged, 1);
+        mbar_init(&ctl.cleared, 1);
         ctl.abort_flag = 0;
         mbar_fence_init();
         prefetch_tensormap(&map_a);
         prefetch_tensormap(&map_b);
     }
-    if (warp == 2) tmem_alloc(&ctl.tmem, G::TMEM);
+    if (warp == 2) alloc<CG>(&ctl.tmem, G::TMEM);
     tc_fence_before_sync();
     __syncthreads();
+    if (CG == 2) cluster_sync_all();
     tc_fence_after_sync();
     const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem;
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
     const int64_t m_end = p.live_k ? p.m : min(p.m, live), k_end = p.live_k ? min(p.k, live) : p.k;
-    const Tiles tiles{(int)((m_end + kBM - 1) / kBM), nt, (int)((m_end + kBM - 1) / kBM) * nt};
+    const int mt = (int)((m_end + CG * kBM - 1) / (CG * kBM)), units = units_of(plan, mt);
     const int slices = (int)((k_end + kSlice - 1) / kSlice);
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
     bool ok = true;
-    if (slices == 0) {
-        // no term at all: only the epilogue has work
-    } else if (warp == 0) {
+    if (warp == 0) {
         // ---- producer
         int stage = 0, sent = 0;
         uint32_t phase = 0;
-        for (int i = blockIdx.x; i < tiles.n && ok; i += gridDim.x) {
-            int m, n;
-            tile_at(tiles, i, m, n);
-            for (int s = 0; s < slices; ++s) {
+        for (int i = first; i < units && ok; i += step) {
+            const Unit u = unit_at(plan, mt, slices, i);
+            const int am = (u.m * CG + rank) * kBM, bn = u.n * BN + rank * G::ROWS_B;
+            for (int s = u.s0; s < u.s1; ++s) {
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.empty[stage], phase ^ 1u, abort_flag))) {
                     ok = false;
                     break;
@@ -96,18 +191,20 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 if (lane == 0) {
                     unsigned char* a = ring + (size_t)stage * G::STAGE;
                     unsigned char* b = a + G::A;
-                    mbar_arrive_expect_tx(&ctl.full[stage], G::STAGE);
+                    uint64_t* bar = &ctl.full[stage];
+                    const uint32_t bar0 = CG == 1 ? 0u : of_rank(bar, 0);
+                    if (rank == 0) mbar_arrive_expect_tx(bar, CG * G::STAGE);
                     if (A_ACROSS) {
 #pragma unroll
-                        for (int c = 0; c < kBM / 64; ++c) tma_load_2d(a + c * 8192, &map_a, m * kBM + c * 64, s * kSlice, &ctl.full[stage]);
+                        for (int c = 0; c < kBM / 64; ++c) load_box<CG>(a + c * 8192, &map_a, am + c * 64, s * kSlice, bar, bar0);
                     } else {
-                        tma_load_2d(a, &map_a, s * kSlice, m * kBM, &ctl.full[stage]);
+                        load_box<CG>(a, &map_a, s * kSlice, am, bar, bar0);
                     }
                     if (B_ACROSS) {
 #pragma unroll
-                        for (int c = 0; c < BN / 64; ++c) tma_load_2d(b + c * 8192, &map_b, n * BN + c * 64, s * kSlice, &ctl.full[stage]);
+                        for (int c = 0; c < G::ROWS_B / 64; ++c) load_box<CG>(b + c * 8192, &map_b, bn + c * 64, s * kSlice, bar, bar0);
                     } else {
-                        tma_load_2d(b, &map_b, s * kSlice, n * BN, &ctl.full[stage]);
+                        load_box<CG>(b, &map_b, s * kSlice, bn, bar, bar0);
                     }
                 }
                 __syncwarp();
@@ -118,8 +215,8 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
             }
         }
-        if (!ok) {
-            // copies still in flight land before the CTA's shared memory goes away
+        if (!ok && rank == 0) {
+            // copies still in flight land before the shared memory of either CTA goes away
             const int pending = sent < G::STAGES ? sent : G::STAGES;
             for (int back = 1; back <= pending; ++back) {
                 const int j = sent - back;
@@ -129,60 +226,75 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
         }
     } else if (warp == 1) {
-        // ---- issuer
-        constexpr uint32_t idesc = umma_idesc_bf16(kBM, BN, A_ACROSS, B_ACROSS);
-        int stage = 0, it = 0;
-        uint32_t phase = 0;
-        for (int i = blockIdx.x; i < tiles.n && ok; i += gridDim.x, ++it) {
+        // ---- issuer; in the second CTA it only clears what lies behind the last token
+        constexpr uint32_t idesc = umma_idesc_bf16(CG * kBM, BN, A_ACROSS, B_ACROSS);
+        int it = 0;
+        uint32_t sent = 0, ragged = 0;
+        for (int i = first; i < units && ok; i += step) {
+            const Unit u = unit_at(plan, mt, slices, i);
+            if (u.s0 == u.s1) continue;
             const int buf = it & 1;
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_empty[buf], (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag))) {
-                ok = false;
-                break;
-            }
-            tc_fence_after_sync();
             const uint32_t d = tmem + (uint32_t)(buf * BN);
-            for (int s = 0; s < slices; ++s) {
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], phase, abort_flag))) {
+            if (rank == 0) {
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_empty[buf], (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag))) {
                     ok = false;
                     break;
                 }
+                tc_fence_after_sync();
+            }
+            ++it;
+            for (int s = u.s0; s < u.s1; ++s, ++sent) {
+                const int stage = (int)(sent % G::STAGES), left = (int)min((int64_t)kSlice, k_end - (int64_t)s * kSlice);
                 unsigned char* at = ring + (size_t)stage * G::STAGE;
-                const int left = (int)min((int64_t)kSlice, k_end - (int64_t)s * kSlice);
-                if (A_ACROSS && B_ACROSS && left < kSlice && k_end < p.k) {
-                    // stored rows past the counted ones may hold anything, and must not reach a sum, not even times zero
-                    for (int u = lane; u < (kSlice - left) * 8 * (kBM + BN) / 64; u += 32) {
-                        const int c = u / ((kSlice - left) * 8), r = u - c * (kSlice - left) * 8;
+                // stored rows past the counted ones may hold anything, and must not reach a sum, not even times zero
+                const bool clear = A_ACROSS && B_ACROSS && left < kSlice && k_end < p.k;
+                if (rank == 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], (sent / G::STAGES) & 1u, abort_flag));
+                else if (clear) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ctl.ragged, ragged, abort_flag));
+                if (!ok) break;
+                if (clear) {
+                    if (CG == 2 && rank == 0 && lane == 0) mbar_arrive_at(of_rank(&ctl.ragged, 1));
+                    const int per = (kSlice - left) * 8;
+                    for (int q = lane; q < per * (kBM + G::ROWS_B) / 64; q += 32) {
+                        const int c = q / per, r = q - c * per;
                         *reinterpret_cast<uint4*>(at + c * 8192 + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                }
-                tc_fence_after_sync();
-                if (lane == 0) {
-                    const uint32_t a = smem_u32(at), b = a + G::A;
-#pragma unroll
-                    for (int k = 0; k < kSlice / 16; ++k) {
-                        const uint64_t ad = A_ACROSS ? umma_smem_desc(a + k * 2048, 8192, 1024) : umma_smem_desc(a + k * 32, 16, 1024);
-                        const uint64_t bd = B_ACROSS ? umma_smem_desc(b + k * 2048, 8192, 1024) : umma_smem_desc(b + k * 32, 16, 1024);
-                        umma_bf16(d, ad, bd, idesc, (s | k) != 0);
+                    if (CG == 2) {
+                        if (rank == 1 && lane == 0) mbar_release_at(of_rank(&ctl.cleared, 0));
+                        if (rank == 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.cleared, ragged, abort_flag))) {
+                            ok = false;
+                            break;
+                        }
+                        ragged ^= 1u;
                     }
-                    umma_commit(&ctl.empty[stage]);
-                    if (s == slices - 1) umma_commit(&ctl.acc_full[buf]);
                 }
-                __syncwarp();
-                if (++stage == G::STAGES) {
-                    stage = 0;
-                    phase ^= 1u;
+                if (rank == 0) {
+                    tc_fence_after_sync();
+                    if (lane == 0) {
+                        const uint32_t a = smem_u32(at), b = a + G::A;
+#pragma unroll
+                        for (int k = 0; k < kSlice / 16; ++k) {
+                            const uint64_t ad = A_ACROSS ? umma_smem_desc(a + k * 2048, 8192, 1024) : umma_smem_desc(a + k * 32, 16, 1024);
+                            const uint64_t bd = B_ACROSS ? umma_smem_desc(b + k * 2048, 8192, 1024) : umma_smem_desc(b + k * 32, 16, 1024);
+                            mma<CG>(d, ad, bd, idesc, s > u.s0 || k > 0);
+                        }
+                        commit<CG>(&ctl.empty[stage]);
+                        if (s == u.s1 - 1) commit<CG>(&ctl.acc_full[buf]);
+                    }
+                    __syncwarp();
                 }
             }
         }
-        if (lane == 0) umma_commit(&ctl.drain);
-        __syncwarp();
+        if (rank == 0) {
+            if (lane == 0) commit<CG>(&ctl.drain);
+            __syncwarp();
+        }
+        // both CTAs' memory is read until the last product is done
         const long long t0 = clock64();
         while (!mbar_try_wait(&ctl.drain, 0) && clock64() - t0 < kWaitCycles) {
         }
-    }
-    if (warp >= 4) {
+    } else if (warp >= 4) {
         // ---- epilogue
         const int quad = warp & 3, half = (warp - 4) >> 2;
         float* mine = stage_f + (warp - 4) * kStageFloats;
@@ -191,67 +303,89 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         uint16_t* pre = static_cast<uint16_t*>(const_cast<void*>(p.pre.data));
         const uint16_t* res = static_cast<const uint16_t*>(p.residual.data);
         int it = 0;
-        for (int i = blockIdx.x; i < tiles.n && ok; i += gridDim.x, ++it) {
-            int m, n;
-            tile_at(tiles, i, m, n);
+        for (int i = first; i < units && ok; i += step) {
+            const Unit u = unit_at(plan, mt, slices, i);
+            const bool some = u.s0 < u.s1;   // else no term at all
             const int buf = it & 1;
-            if (slices > 0) {
+            if (some) {
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_full[buf], (uint32_t)((it >> 1) & 1), abort_flag))) {
                     ok = false;
                     break;
                 }
                 tc_fence_after_sync();
+                ++it;
             }
-            const int64_t row0 = (int64_t)m * kBM + quad * 32;
+            const int64_t row0 = ((int64_t)u.m * CG + rank) * kBM + quad * 32 + r8;
+            const bool rows_in = row0 - r8 + 32 <= m_end;
 #pragma unroll 1
             for (int c = 0; c < BN / 64; ++c) {
-                const int64_t col = (int64_t)n * BN + half * (BN / 2) + c * 32 + sub * 4;
-                const bool whole = vec && col + 4 <= p.n;
+                const int64_t col = (int64_t)u.n * BN + half * (BN / 2) + c * 32 + sub * 4;
+                const bool whole = vec && rows_in && col + 4 <= p.n;
+                uint2 add[8];
+                if (res && whole && u.part < 0) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) add[q] = *reinterpret_cast<const uint2*>(res + (row0 + q * 4) * p.residual.stride + col);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) add[q] = make_uint2(0, 0);
+                }
                 float bias[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) bias[e] = p.bias && col + e < p.n ? p.bias[col + e] : 0.0f;
                 uint32_t v[32];
-                if (slices > 0) {
+                if (some) {
                     tmem_ld_32cols(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2) + c * 32), v);
                     tmem_ld_wait();
+                    if (c == BN / 64 - 1) {
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (CG == 1) mbar_arrive(&ctl.acc_empty[buf]);
+                            else mbar_arrive_at(of_rank(&ctl.acc_empty[buf], 0));
+                        }
+                    }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0u;
                 }
-                if (c == BN / 64 - 1 && slices > 0) {
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&ctl.acc_empty[buf]);
-                }
                 __syncwarp();                // the stage's readers of the chunk before are done
 #pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    *reinterpret_cast<uint4*>(mine + lane * 32 + ((u ^ (lane & 7)) << 2)) = make_uint4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+                for (int w = 0; w < 8; ++w)
+                    *reinterpret_cast<uint4*>(mine + lane * 32 + ((w ^ (lane & 7)) << 2)) = make_uint4(v[4 * w], v[4 * w + 1], v[4 * w + 2], v[4 * w + 3]);
                 __syncwarp();
+                if (u.part >= 0) {
+                    float* to = plan.parts + ((int64_t)u.part * CG + rank) * kBM * BN + (int64_t)(quad * 32 + r8) * BN + half * (BN / 2) + c * 32 + sub * 4;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int r = q * 4 + r8;
-                    const int64_t row = row0 + r;
-                    const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
-                    float z[4] = {f.x + bias[0], f.y + bias[1], f.z + bias[2], f.w + bias[3]};
-                    if (row >= m_end) continue;
-                    if (whole) {
-                        if (pre) *reinterpret_cast<uint2*>(pre + row * p.pre.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
+                    for (int q = 0; q < 8; ++q)
+                        *reinterpret_cast<float4*>(to + q * 4 * BN) = *reinterpret_cast<const float4*>(mine + (q * 4 + r8) * 32 + ((sub ^ ((q * 4 + r8) & 7)) << 2));
+                    continue;
+                }
+                if (whole) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const int r = q * 4 + r8;
+                        const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
+                        float z[4] = {f.x + bias[0], f.y + bias[1], f.z + bias[2], f.w + bias[3]};
+                        if (pre) *reinterpret_cast<uint2*>(pre + (row0 + q * 4) * p.pre.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) z[e] = activate(z[e], p.act);
-                        if (res) {
-                            const uint2 w = *reinterpret_cast<const uint2*>(res + row * p.residual.stride + col);
-                            z[0] += bf16_lo(w.x);
-                            z[1] += bf16_hi(w.x);
-                            z[2] += bf16_lo(w.y);
-                            z[3] += bf16_hi(w.y);
-                        }
-                        *reinterpret_cast<uint2*>(out + row * p.out.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
-                    } else {
-                        for (int e = 0; e < 4; ++e) {
-                            if (col + e >= p.n) break;
-                            if (pre) store1(pre + row * p.pre.stride + col + e, z[e]);
-                            float y = activate(z[e], p.act);
+                        z[0] += bf16_lo(add[q].x);
+                        z[1] += bf16_hi(add[q].x);
+                        z[2] += bf16_lo(add[q].y);
+                        z[3] += bf16_hi(add[q].y);
+                        *reinterpret_cast<uint2*>(out + (row0 + q * 4) * p.out.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
+                    }
+                } else {
+#pragma unroll 1
+                    for (int q = 0; q < 8; ++q) {
+                        const int r = q * 4 + r8;
+                        const int64_t row = row0 + q * 4;
+                        if (row >= m_end) break;
+#pragma unroll 1
+                        for (int e = 0; e < 4 && col + e < p.n; ++e) {
+                            const float z = mine[r * 32 + ((sub ^ (r & 7)) << 2) + e] + (p.bias ? p.bias[col + e] : 0.0f);
+                            if (pre) store1(pre + row * p.pre.stride + col + e, z);
+                            float y = activate(z, p.act);
                             if (res) y += load1(res + row * p.residual.stride + col + e);
                             store1(out + row * p.out.stride + col + e, y);
                         }
@@ -266,34 +400,114 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     }
     tc_fence_before_sync();
     __syncthreads();
+    if (CG == 2) cluster_sync_all();         // nothing of the other CTA is on its way here any more
     tc_fence_after_sync();
-    if (warp == 2) tmem_dealloc(tmem, G::TMEM);
+    if (warp == 2) dealloc<CG>(tmem, G::TMEM);
 }
 
-template <int BN, bool AA, bool BA>
+// Adds the parts of the cut tiles up in order and finishes them.  A thread takes four columns of a row.
+template <int CG, int BN>
+__global__ void __launch_bounds__(256) product_join_kernel(const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan, bool vec) {
+    grid_dependency_wait();
+    grid_dependency_release();
+    const int64_t live = live_rows(p.live, p.ctl, false);
+    const int64_t m_end = p.live_k ? p.m : min(p.m, live);
+    const int mt = (int)((m_end + CG * kBM - 1) / (CG * kBM)), tail = mt * plan.nt - plan.whole;
+    constexpr int kPerTile = CG * kBM * BN / 4;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, t = at / kPerTile;
+    if (t >= tail) return;
+    const int in = (int)(at - t * kPerTile), r = in / (BN / 4), q = in - r * (BN / 4);
+    int m, n;
+    tile_at(mt, plan.nt, plan.whole + (int)t, m, n);
+    const int64_t row = (int64_t)m * CG * kBM + r, col = (int64_t)n * BN + q * 4;
+    if (row >= m_end || col >= p.n) return;
+    float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float4* from = reinterpret_cast<const float4*>(plan.parts + t * plan.splits * CG * kBM * BN) + in;
+    for (int s = 0; s < plan.splits; ++s) {
+        const float4 f = from[(int64_t)s * kPerTile];
+        z[0] += f.x;
+        z[1] += f.y;
+        z[2] += f.z;
+        z[3] += f.w;
+    }
+    uint16_t* out = static_cast<uint16_t*>(const_cast<void*>(p.out.data)) + row * p.out.stride + col;
+    const uint16_t* res = p.residual.data ? static_cast<const uint16_t*>(p.residual.data) + row * p.residual.stride + col : nullptr;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (res && col + e < p.n) z[e] += load1(res + e);
+    if (vec && col + 4 <= p.n) {
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < p.n) store1(out + e, z[e]);
+    }
+}
+
+// Splits of the tiles that do not fill a round of `teams`: the fewest slices one after the other, counting the parts' way through memory.
+Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats) {
+    Plan plan{nt, (int)tiles, 1, p.parts};
+    const int64_t slices = (p.k + kSlice - 1) / kSlice, whole = tiles / teams * teams, tail = tiles - whole;
+    if (!p.parts || tail == 0) return plan;
+    double best = (double)slices;
+    for (int s = 2; s <= 16 && slices / s >= 8; ++s) {
+        const int64_t parts = tail * s;
+        if (parts * tile_floats > p.part_floats) break;
+        // a slice takes about 0.3 us; the parts are written and read at about 5 TB/s, behind a launch of about 4 us
+        const double cost = (double)((parts + teams - 1) / teams) * (double)((slices + s - 1) / s) + (4.0 + (double)(parts * tile_floats) * 8.0 / 5e6) / 0.3;
+        if (cost < best) {
+            best = cost;
+            plan.whole = (int)whole;
+            plan.splits = s;
+        }
+    }
+    return plan;
+}
+
+template <int CG, int BN, bool AA, bool BA>
 aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
-    using G = Geo<BN>;
+    using G = Geo<CG, BN>;
     ProductParams p = in;
     alignas(64) CUtensorMap map_a, map_b;
     const int64_t a_rows = AA ? p.k : p.m, a_cols = AA ? p.m : p.k, b_rows = BA ? p.k : p.n, b_cols = BA ? p.n : p.k;
     if (!encode_bf16_tile_map(&map_a, p.a.data, a_rows, a_cols, p.a.stride, AA ? kSlice : kBM) ||
-        !encode_bf16_tile_map(&map_b, p.b.data, b_rows, b_cols, p.b.stride, BA ? kSlice : BN))
+        !encode_bf16_tile_map(&map_b, p.b.data, b_rows, b_cols, p.b.stride, BA ? kSlice : G::ROWS_B))
         return AA_ERR_CUDA;
-    int mt = (int)((p.m + kBM - 1) / kBM), nt = (int)((p.n + BN - 1) / BN);
-    const void* kernel = (const void*)product_tc_kernel<BN, AA, BA>;
+    const int64_t mt = (p.m + CG * kBM - 1) / (CG * kBM), nt = (p.n + BN - 1) / BN, tiles = mt * nt;
+    const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA>;
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
-    const int64_t n = (int64_t)mt * nt;
-    const int grid = (int)(n < c->sm_count ? n : c->sm_count);
-    void* args[] = {&map_a, &map_b, &p, &mt, &nt, &vec};
-    if (launch_overlapped(c, kernel, dim3(grid), dim3(kTcThreads), args, G::SMEM, false) != cudaSuccess) return AA_ERR_CUDA;
+    const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kTcThreads, G::SMEM, CG);
+    if (teams < 1) return AA_ERR_CUDA;
+    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN);
+    const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
+    void* args[] = {&map_a, &map_b, &p, &plan, &vec};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((units < teams ? units : teams) * CG));
+    cfg.blockDim = dim3(kTcThreads);
+    cfg.dynamicSmemBytes = G::SMEM;
+    cfg.stream = c->stream;
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = CG;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = CG == 1 ? 1 : 2;
+    if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) return AA_ERR_CUDA;
+    ++c->launches;
+    if (tail == 0) return AA_OK;
+    void* join[] = {&p, &plan, &vec};
+    const int64_t threads = tail * CG * kBM * BN / 4;
+    if (launch_overlapped(c, (const void*)product_join_kernel<CG, BN>, dim3((unsigned)(threads / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     return AA_OK;
 }
 
-template <int BN>
+template <int CG, int BN>
 aa_status launch_majors(aa_ctx_impl* c, const ProductParams& p, bool vec) {
-    if (p.a_across) return launch_tc<BN, true, true>(c, p, vec);
-    return p.b_across ? launch_tc<BN, false, true>(c, p, vec) : launch_tc<BN, false, false>(c, p, vec);
+    if (p.a_across) return launch_tc<CG, BN, true, true>(c, p, vec);
+    return p.b_across ? launch_tc<CG, BN, false, true>(c, p, vec) : launch_tc<CG, BN, false, false>(c, p, vec);
 }
 
 }  // namespace
@@ -301,18 +515,18 @@ aa_status launch_majors(aa_ctx_impl* c, const ProductParams& p, bool vec) {
 bool product_tc_fits(const ProductParams& p) {
     const auto tma = [](const MatArg& a) { return (uintptr_t)a.data % 16 == 0 && a.stride % 8 == 0; };
     const int64_t tiles = ((p.m + kBM - 1) / kBM) * ((p.n + 63) / 64);
-    return tma(p.a) && tma(p.b) && p.m <= 0x3FFFFFFF && p.n <= 0x3FFFFFFF && p.k <= 0x3FFFFFFF && tiles < 0x3FFFFFFF;
+    return tma(p.a) && tma(p.b) && p.m <= 0x3FFFFFFF && p.n <= 0x3FFFFFFF && p.k <= 0x3FFFFFFF && tiles < 0x3FFFFFF;
 }
 
 aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p) {
     const auto quad = [](const MatArg& a) { return !a.data || ((uintptr_t)a.data % 8 == 0 && a.stride % 4 == 0); };
     const bool vec = quad(p.out) && quad(p.pre) && quad(p.residual);
     // the widest tile moves the fewest bytes a product; narrower ones where it would leave SMs idle
-    const int64_t mt = (p.m + kBM - 1) / kBM;
-    const auto waves = [&](int bn) { return (double)((mt * ((p.n + bn - 1) / bn) + c->sm_count - 1) / c->sm_count) * bn; };
-    if (p.n > 128 && waves(256) <= waves(128)) return launch_majors<256>(c, p, vec);
-    if (p.n > 64 && waves(128) <= waves(64)) return launch_majors<128>(c, p, vec);
-    return launch_majors<64>(c, p, vec);
+    const int64_t mt = (p.m + kBM - 1) / kBM, sms = c->sm_count;
+    const auto tiles = [&](int bn) { return mt * ((p.n + bn - 1) / bn); };
+    if (tiles(256) >= sms || (p.parts && p.k >= 16 * kSlice && tiles(256) * (p.k / (8 * kSlice)) >= sms)) return launch_majors<2, 256>(c, p, vec);
+    if (tiles(128) >= sms) return launch_majors<1, 128>(c, p, vec);
+    return launch_majors<1, 64>(c, p, vec);
 }
 
 }  // namespace aa
