@@ -141,6 +141,26 @@ __device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_flo
 __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void store1(uint16_t* p, float x) { *p = (uint16_t)pack_bf16(x, 0.0f); }
 
+// V consecutive elements: one, or a vector of 16 bytes (16-byte aligned pointers).
+template <typename T, int V>
+__device__ __forceinline__ void load_elems(const T* p, float* out) {
+    if constexpr (V == 1) {
+        out[0] = load1(p);
+    } else {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        float t[V];
+        Vec<T>::unpack(u, t);
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = t[e];
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_elems(T* p, const float* x) {
+    if constexpr (V == 1) store1(p, x[0]);
+    else if constexpr (V == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    else *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
 #endif  // __CUDACC__
 
 }  // namespace aa

@@ -126,49 +126,52 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
         if (zero == AA_OK && dbias) zero = cuda_ok(cudaMemsetAsync(dbias, 0, (size_t)w->rows * sizeof(float), c->stream));
         return zero;
     }
-    MatArg g = mat(dout);
-    if (activation != AA_ACT_NONE) g = MatArg{scratch, (w->rows + 7) / 8 * 8};
-    if (activation != AA_ACT_NONE || dbias) {
+    const bool act = activation != AA_ACT_NONE;
+    const MatArg g = act ? MatArg{scratch, (w->rows + 7) / 8 * 8} : mat(dout);
+    float* parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + need.g);
+    ProductParams grad_x = {}, grad_w = {};
+    grad_x.ctl = grad_w.ctl = c->ctl;
+    grad_x.live = grad_w.live = live;
+    grad_x.a = grad_w.a = g;
+    grad_x.parts = grad_w.parts = parts;
+    grad_x.part_floats = grad_w.part_floats = (int64_t)(need.parts / sizeof(float));
+    if (dw) {
+        grad_w.b = mat(x);
+        grad_w.a_across = grad_w.b_across = grad_w.live_k = true;
+        grad_w.m = w->rows;
+        grad_w.n = x->cols;
+        grad_w.k = x->rows;
+        grad_w.out = mat(dw);
+        // the sums come with the product where its kernel has them and there is no other pass over dout
+        if (!act && dbias && x->dtype == AA_BF16 && product_tc_fits(grad_w)) grad_w.a_sums = dbias;
+    }
+    if (act || (dbias && !grad_w.a_sums)) {
         SlopeParams s = {};
         s.dout = mat(dout);
         s.pre = mat(pre);
-        if (activation != AA_ACT_NONE && (dx || dw)) s.g = g;
+        if (act && (dx || dw)) s.g = g;
         s.rows = x->rows;
         s.cols = w->rows;
         s.live = live;
         s.act = activation;
-        s.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + need.g);
+        s.parts = parts;
         s.dbias = dbias;
         s.ctl = c->ctl;
         const aa_status done = launch_slope(c, s, x->dtype);
         if (done != AA_OK) return done;
     }
-    ProductParams p = {};
-    p.ctl = c->ctl;
-    p.live = live;
-    p.a = g;
-    p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + need.g);
-    p.part_floats = (int64_t)(need.parts / sizeof(float));
     if (dx) {
-        p.b = mat(w);
-        p.b_across = true;
-        p.m = x->rows;
-        p.n = x->cols;
-        p.k = w->rows;
-        p.residual = mat(residual);
-        p.out = mat(dx);
-        const aa_status done = launch_product(c, p, x->dtype);
+        grad_x.b = mat(w);
+        grad_x.b_across = true;
+        grad_x.m = x->rows;
+        grad_x.n = x->cols;
+        grad_x.k = w->rows;
+        grad_x.residual = mat(residual);
+        grad_x.out = mat(dx);
+        const aa_status done = launch_product(c, grad_x, x->dtype);
         if (done != AA_OK) return done;
     }
-    if (!dw) return AA_OK;
-    p.b = mat(x);
-    p.a_across = p.b_across = p.live_k = true;
-    p.m = w->rows;
-    p.n = x->cols;
-    p.k = x->rows;
-    p.residual = MatArg{nullptr, 0};
-    p.out = mat(dw);
-    return launch_product(c, p, x->dtype);
+    return dw ? launch_product(c, grad_w, x->dtype) : AA_OK;
 }
 
 aa_status aa_layer_norm(aa_ctx* ctx, const aa_rows* x, const float* gamma, const float* beta, float eps, const int32_t* offsets, int64_t n_seg,

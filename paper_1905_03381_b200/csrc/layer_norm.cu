@@ -19,25 +19,6 @@ namespace {
 
 constexpr int kEach = 16;                // columns a thread
 
-template <typename T, int V>
-__device__ __forceinline__ void load_vec(const T* p, float* out) {
-    if constexpr (V == 1) {
-        out[0] = load1(p);
-    } else {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        float t[V];
-        Vec<T>::unpack(u, t);
-#pragma unroll
-        for (int e = 0; e < V; ++e) out[e] = t[e];
-    }
-}
-template <typename T, int V>
-__device__ __forceinline__ void store_vec(T* p, const float* x) {
-    if constexpr (V == 1) store1(p, x[0]);
-    else if constexpr (V == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    else *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-}
-
 // Sums of two values over a group of G lanes of a warp, or over the CTA (G > 32; `buf` is not used again before another barrier).
 template <int G>
 __device__ __forceinline__ float2 group_sum(float2 s, float2* buf) {
@@ -84,7 +65,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>) norm_kernel(NormParams p) {
             const int c = (i * G + l) * V;
 #pragma unroll
             for (int e = 0; e < V; ++e) v[i * V + e] = 0.0f;
-            if (c < cols) load_vec<T, V>(x + c, v + i * V);
+            if (c < cols) load_elems<T, V>(x + c, v + i * V);
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) s.x += v[i];
@@ -106,7 +87,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>) norm_kernel(NormParams p) {
             if (c >= cols || !on) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) v[i * V + e] = fmaf(v[i * V + e] * r, p.gamma ? p.gamma[c + e] : 1.0f, p.beta ? p.beta[c + e] : 0.0f);
-            store_vec<T, V>(out + c, v + i * V);
+            store_elems<T, V>(out + c, v + i * V);
         }
     }
 }
@@ -144,8 +125,8 @@ __global__ void __launch_bounds__(kThreadsOf<G>) norm_grad_kernel(NormParams p) 
 #pragma unroll
             for (int e = 0; e < V; ++e) v[i * V + e] = u[i * V + e] = 0.0f;
             if (c < cols) {
-                load_vec<T, V>(x + c, v + i * V);
-                load_vec<T, V>(d + c, u + i * V);
+                load_elems<T, V>(x + c, v + i * V);
+                load_elems<T, V>(d + c, u + i * V);
             }
         }
 #pragma unroll
@@ -174,7 +155,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>) norm_grad_kernel(NormParams p) 
             const int c = (i * G + l) * V;
             if (c >= cols || !on) continue;
             float y[V], add[V];
-            if (res) load_vec<T, V>(res + c, add);
+            if (res) load_elems<T, V>(res + c, add);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const int j = i * V + e;
@@ -184,7 +165,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>) norm_grad_kernel(NormParams p) 
                 y[e] = r * (fmaf(u[j], gm[j], -mg) - h * k);
                 if (res) y[e] += add[e];
             }
-            store_vec<T, V>(out + c, y);
+            store_elems<T, V>(out + c, y);
         }
     }
     if (!p.parts) return;

@@ -34,6 +34,7 @@ struct ProductParams {
     MatArg residual, pre, out;   // nullable but out
     float* parts;            // scratch for tiles cut along the contraction, nullable (then bias, act and pre are empty)
     int64_t part_floats;
+    float* a_sums;           // [m] sums of A over the contraction, nullable (a_across)
     Control* ctl;
 };
 
@@ -41,7 +42,7 @@ aa_status launch_product(aa_ctx_impl* c, const ProductParams& p, int dtype);
 // bf16 operands that TMA can fetch (16-byte aligned bases and rows).
 bool product_tc_fits(const ProductParams& p);
 aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p);
-// g = dout * act'(pre), rounded to the matrices' type; column sums of the unrounded g (or of dout alone where act is AA_ACT_NONE and g null) into dbias.
+// g = dout * act'(pre), rounded to the matrices' type (null: not written); column sums of the unrounded g into dbias.
 struct SlopeParams {
     MatArg dout, pre, g;
     int64_t rows, cols;
@@ -67,20 +68,62 @@ __device__ __forceinline__ int64_t live_rows(const LiveRows& l, Control* ctl, bo
     return 0;
 }
 
-__device__ __forceinline__ float activate(float z, int act) {
-    if (act == AA_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (act == AA_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if (act == AA_ACT_SILU) return z / (1.0f + expf(-z));
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Normal distribution at z and its density's exponential e = exp(-z^2 / 2), which the gradient needs too.  The tail is Hastings' rational approximation
+// (Abramowitz and Stegun, 7.1.26): erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), within 1.5e-7; it shares e.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = rcp_approx(fmaf(0.3275911f, x, 1.0f));
+    e = ex2_approx(z * z * -0.72134752044448170f);
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f);
+    q = 0.5f * t * q * e;
+    return z > 0.0f ? 1.0f - q : q;
+}
+__device__ __forceinline__ float logistic(float z) { return rcp_approx(1.0f + ex2_approx(z * -1.4426950408889634f)); }
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    if (ACT == AA_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    float e;
+    if (ACT == AA_ACT_GELU) return z * normal_cdf(z, e);
+    if (ACT == AA_ACT_SILU) return z * logistic(z);
     return z;
+}
+// The same where the activation is known at run time: one branch for N values.
+template <int N>
+__device__ __forceinline__ void activate_all(float (&z)[N], int act) {
+    if (act == AA_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_RELU>(z[i]);
+    } else if (act == AA_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_GELU>(z[i]);
+    } else if (act == AA_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_SILU>(z[i]);
+    }
 }
 
 // act'(z); relu'(0) = 0.
-__device__ __forceinline__ float activation_slope(float z, int act) {
-    if (act == AA_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == AA_ACT_GELU) return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-    if (act == AA_ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-z));
-        return s * (1.0f + z * (1.0f - s));
+template <int ACT>
+__device__ __forceinline__ float activation_slope(float z) {
+    if (ACT == AA_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (ACT == AA_ACT_GELU) {
+        float e;
+        const float cdf = normal_cdf(z, e);
+        return fmaf(z * 0.39894228040143268f, e, cdf);
+    }
+    if (ACT == AA_ACT_SILU) {
+        const float s = logistic(z);
+        return s * fmaf(z, 1.0f - s, 1.0f);
     }
     return 1.0f;
 }

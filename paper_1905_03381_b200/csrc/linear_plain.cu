@@ -52,42 +52,83 @@ __global__ void __launch_bounds__(256) product_plain_kernel(ProductParams p) {
             if (n >= p.n) break;
             float z = acc[i][j] + (p.bias ? p.bias[n] : 0.0f);
             if (p.pre.data) store1(static_cast<T*>(const_cast<void*>(p.pre.data)) + m * p.pre.stride + n, z);
-            z = activate(z, p.act);
+            float y[1] = {z};
+            activate_all(y, p.act);
+            z = y[0];
             if (p.residual.data) z += load1(static_cast<const T*>(p.residual.data) + m * p.residual.stride + n);
             store1(static_cast<T*>(const_cast<void*>(p.out.data)) + m * p.out.stride + n, z);
         }
     }
 }
 
-// Rows are shared out in kSlopeParts runs whose column sums stay apart until the join.
-template <typename T>
+// Bound by memory: two values read and one written an element (one read where only the sums are wanted).  A CTA takes 32 x V columns of a run of rows, a
+// warp every eighth row, a lane V columns; rows are shared out in kSlopeParts runs whose column sums stay apart until the join.
+template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(256) slope_kernel(SlopeParams p) {
+    __shared__ float sums[8][32 * V];
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0);
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col >= p.cols) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t col = ((int64_t)blockIdx.x * 32 + lane) * V;
     const int64_t run = (p.rows + kSlopeParts - 1) / kSlopeParts, r0 = run * blockIdx.y, r1 = min(live, r0 + run);
     const T *d = static_cast<const T*>(p.dout.data), *z = static_cast<const T*>(p.pre.data);
     T* g = static_cast<T*>(const_cast<void*>(p.g.data));
-    float sum = 0.0f;
-    for (int64_t r = r0; r < r1; ++r) {
-        float x = load1(d + r * p.dout.stride + col);
-        if (p.act != AA_ACT_NONE) x *= activation_slope(load1(z + r * p.pre.stride + col), p.act);
-        if (g) store1(g + r * p.g.stride + col, x);
-        sum += x;
+    float sum[V] = {};
+    if (col < p.cols) {
+#pragma unroll 4
+        for (int64_t r = r0 + warp; r < r1; r += 8) {
+            float x[V], y[V];
+            load_elems<T, V>(d + r * p.dout.stride + col, x);
+            if (ACT != AA_ACT_NONE) {
+                load_elems<T, V>(z + r * p.pre.stride + col, y);
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[e] *= activation_slope<ACT>(y[e]);
+                if (g) store_elems<T, V>(g + r * p.g.stride + col, x);
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += x[e];
+        }
     }
-    if (p.dbias) p.parts[(int64_t)blockIdx.y * p.cols + col] = sum;
+    if (!p.dbias) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[warp][lane * V + e] = sum[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * V; i += 256) {
+        const int64_t c = (int64_t)blockIdx.x * 32 * V + i;
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) s += sums[w][i];
+        if (c < p.cols) p.parts[(int64_t)blockIdx.y * p.cols + c] = s;
+    }
 }
 
+// 32 columns a CTA; each of 8 warps adds up every eighth part.
 __global__ void __launch_bounds__(256) slope_join_kernel(const float* parts, float* dbias, int64_t cols) {
+    __shared__ float sums[8][32];
     grid_dependency_wait();
     grid_dependency_release();
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col >= cols) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t col = (int64_t)blockIdx.x * 32 + lane;
     float sum = 0.0f;
-    for (int i = 0; i < kSlopeParts; ++i) sum += parts[(int64_t)i * cols + col];
-    dbias[col] = sum;
+    if (col < cols)
+#pragma unroll 4
+        for (int i = warp; i < kSlopeParts; i += 8) sum += parts[(int64_t)i * cols + col];
+    sums[warp][lane] = sum;
+    __syncthreads();
+    if (warp == 0 && col < cols) {
+#pragma unroll
+        for (int w = 1; w < 8; ++w) sum += sums[w][lane];
+        dbias[col] = sum;
+    }
+}
+
+template <typename T, int V>
+const void* slope_of(int act) {
+    if (act == AA_ACT_RELU) return (const void*)slope_kernel<T, V, AA_ACT_RELU>;
+    if (act == AA_ACT_GELU) return (const void*)slope_kernel<T, V, AA_ACT_GELU>;
+    if (act == AA_ACT_SILU) return (const void*)slope_kernel<T, V, AA_ACT_SILU>;
+    return (const void*)slope_kernel<T, V, AA_ACT_NONE>;
 }
 
 }  // namespace
@@ -106,14 +147,17 @@ aa_status launch_product(aa_ctx_impl* c, const ProductParams& in, int dtype) {
 
 aa_status launch_slope(aa_ctx_impl* c, const SlopeParams& in, int dtype) {
     SlopeParams p = in;
-    const unsigned ct = (unsigned)((p.cols + 255) / 256);
-    const void* kernel = dtype == AA_BF16 ? (const void*)slope_kernel<uint16_t> : (const void*)slope_kernel<float>;
+    const int es = dtype == AA_BF16 ? 2 : 4, wide = 16 / es;
+    const auto aligned = [&](const MatArg& a) { return !a.data || ((uintptr_t)a.data % 16 == 0 && (a.stride * es) % 16 == 0); };
+    const bool vec = p.cols % wide == 0 && aligned(p.dout) && aligned(p.pre) && aligned(p.g);
+    const int v = vec ? wide : 1;
+    const void* kernel = dtype == AA_BF16 ? (vec ? slope_of<uint16_t, 8>(p.act) : slope_of<uint16_t, 1>(p.act)) : (vec ? slope_of<float, 4>(p.act) : slope_of<float, 1>(p.act));
     void* args[] = {&p};
-    if (launch_overlapped(c, kernel, dim3(ct, kSlopeParts), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+    if (launch_overlapped(c, kernel, dim3((unsigned)((p.cols + 32 * v - 1) / (32 * v)), kSlopeParts), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     if (!p.dbias) return AA_OK;
     void* join[] = {&p.parts, &p.dbias, &p.cols};
-    if (launch_overlapped(c, (const void*)slope_join_kernel, dim3(ct), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+    if (launch_overlapped(c, (const void*)slope_join_kernel, dim3((unsigned)((p.cols + 31) / 32)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     return AA_OK;
 }

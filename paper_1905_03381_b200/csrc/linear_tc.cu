@@ -19,7 +19,7 @@ namespace aa {
 namespace {
 
 constexpr int kBM = 128, kSlice = 64, kGroupM = 16;
-constexpr int kTcThreads = 384;          // producer, issuer, allocator, one idle warp, eight epilogue warps
+constexpr int kTcThreads = 384;          // producer, issuer, two for column sums (the first of them allocates), eight for the epilogue
 constexpr int kEpilogue = 8;
 constexpr int kStageFloats = 32 * 32;    // per epilogue warp
 constexpr int kMaxStages = 8;
@@ -34,7 +34,7 @@ struct Geo {
 };
 
 struct Ctl {
-    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+    uint64_t full[kMaxStages], empty[kMaxStages], done[kMaxStages], acc_full[2], acc_empty[2], drain;
     uint64_t ragged, cleared;            // the last slice of tokens: it has arrived (second CTA), its rest is zero there (first CTA)
     uint32_t tmem;
     int abort_flag;
@@ -44,6 +44,7 @@ struct Ctl {
 struct Plan {
     int nt, whole, splits;
     float* parts;                        // [part][CG 128][BN]
+    float* sum_parts;                    // [part][CG 128]
 };
 
 struct Unit {
@@ -133,7 +134,9 @@ __device__ __forceinline__ void dealloc(uint32_t addr, uint32_t cols) {
     else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
 }
 
-template <int CG, int BN, bool A_ACROSS, bool B_ACROSS>
+// SUMS: the sums of A over the contraction, too (A's slices are in shared memory already; another pass over A would cost as much as reading it).  Two warps,
+// idle otherwise, add up the slice's 128 columns once the products have read it and hand the stage back with them.
+template <int CG, int BN, bool A_ACROSS, bool B_ACROSS, bool SUMS>
 __global__ void __launch_bounds__(kTcThreads, 1)
 product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan,
                   bool vec) {
@@ -148,7 +151,8 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (threadIdx.x == 0) {
         for (int s = 0; s < G::STAGES; ++s) {
             mbar_init(&ctl.full[s], 1);      // both CTAs' copies count on the first one's
-            mbar_init(&ctl.empty[s], 1);
+            mbar_init(&ctl.empty[s], SUMS ? 3 : 1);
+            mbar_init(&ctl.done[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&ctl.acc_full[b], 1);
@@ -280,6 +284,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                             mma<CG>(d, ad, bd, idesc, s > u.s0 || k > 0);
                         }
                         commit<CG>(&ctl.empty[stage]);
+                        if (SUMS) commit<CG>(&ctl.done[stage]);
                         if (s == u.s1 - 1) commit<CG>(&ctl.acc_full[buf]);
                     }
                     __syncwarp();
@@ -293,6 +298,52 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         // both CTAs' memory is read until the last product is done
         const long long t0 = clock64();
         while (!mbar_try_wait(&ctl.drain, 0) && clock64() - t0 < kWaitCycles) {
+        }
+    } else if (SUMS && warp < 4) {
+        // ---- column sums: warp 2 the first 64 columns of the CTA's 128, warp 3 the others; a lane takes 8 columns of every fourth token
+        const int chunk = warp - 2, unit = lane & 7, r4 = lane >> 3;
+        uint32_t sent = 0;
+        for (int i = first; i < units && ok; i += step) {
+            const Unit u = unit_at(plan, mt, slices, i);
+            float sum[8] = {};
+            for (int s = u.s0; s < u.s1; ++s, ++sent) {
+                const int stage = (int)(sent % G::STAGES);
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.done[stage], (sent / G::STAGES) & 1u, abort_flag))) {
+                    ok = false;
+                    break;
+                }
+                if (u.n == 0) {              // the tiles of a row of tiles share A
+                    const unsigned char* at = ring + (size_t)stage * G::STAGE + chunk * 8192;
+                    float part[8] = {};
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        const int r = q * 4 + r4;
+                        float x[8];
+                        Vec<uint16_t>::unpack(*reinterpret_cast<const uint4*>(at + r * 128 + ((unit ^ (r & 7)) << 4)), x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) part[e] += x[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += part[e];
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.empty[stage]);
+            }
+            if (!ok || u.n != 0) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 8);
+                sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 16);
+            }
+            if (r4 == 0) {
+                const int at = chunk * 64 + unit * 8;
+                const int64_t row = ((int64_t)u.m * CG + rank) * kBM + at;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (u.part >= 0) plan.sum_parts[((int64_t)u.part * CG + rank) * kBM + at + e] = sum[e];
+                    else if (row + e < p.m) p.a_sums[row + e] = sum[e];
+                }
+            }
         }
     } else if (warp >= 4) {
         // ---- epilogue
@@ -367,8 +418,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
                         float z[4] = {f.x + bias[0], f.y + bias[1], f.z + bias[2], f.w + bias[3]};
                         if (pre) *reinterpret_cast<uint2*>(pre + (row0 + q * 4) * p.pre.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) z[e] = activate(z[e], p.act);
+                        activate_all(z, p.act);
                         z[0] += bf16_lo(add[q].x);
                         z[1] += bf16_hi(add[q].x);
                         z[2] += bf16_lo(add[q].y);
@@ -385,7 +435,9 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         for (int e = 0; e < 4 && col + e < p.n; ++e) {
                             const float z = mine[r * 32 + ((sub ^ (r & 7)) << 2) + e] + (p.bias ? p.bias[col + e] : 0.0f);
                             if (pre) store1(pre + row * p.pre.stride + col + e, z);
-                            float y = activate(z, p.act);
+                            float one[1] = {z};
+                            activate_all(one, p.act);
+                            float y = one[0];
                             if (res) y += load1(res + row * p.residual.stride + col + e);
                             store1(out + row * p.out.stride + col + e, y);
                         }
@@ -421,6 +473,11 @@ __global__ void __launch_bounds__(256) product_join_kernel(const __grid_constant
     tile_at(mt, plan.nt, plan.whole + (int)t, m, n);
     const int64_t row = (int64_t)m * CG * kBM + r, col = (int64_t)n * BN + q * 4;
     if (row >= m_end || col >= p.n) return;
+    if (p.a_sums && col == 0) {
+        float sum = 0.0f;
+        for (int s = 0; s < plan.splits; ++s) sum += plan.sum_parts[(t * plan.splits + s) * CG * kBM + r];
+        p.a_sums[row] = sum;
+    }
     float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const float4* from = reinterpret_cast<const float4*>(plan.parts + t * plan.splits * CG * kBM * BN) + in;
     for (int s = 0; s < plan.splits; ++s) {
@@ -445,26 +502,27 @@ __global__ void __launch_bounds__(256) product_join_kernel(const __grid_constant
 }
 
 // Splits of the tiles that do not fill a round of `teams`: the fewest slices one after the other, counting the parts' way through memory.
-Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats) {
-    Plan plan{nt, (int)tiles, 1, p.parts};
+Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats, int tile_rows) {
+    Plan plan{nt, (int)tiles, 1, p.parts, nullptr};
     const int64_t slices = (p.k + kSlice - 1) / kSlice, whole = tiles / teams * teams, tail = tiles - whole;
     if (!p.parts || tail == 0) return plan;
     double best = (double)slices;
     for (int s = 2; s <= 16 && slices / s >= 8; ++s) {
         const int64_t parts = tail * s;
-        if (parts * tile_floats > p.part_floats) break;
+        if (parts * (tile_floats + tile_rows) > p.part_floats) break;
         // a slice takes about 0.3 us; the parts are written and read at about 5 TB/s, behind a launch of about 4 us
         const double cost = (double)((parts + teams - 1) / teams) * (double)((slices + s - 1) / s) + (4.0 + (double)(parts * tile_floats) * 8.0 / 5e6) / 0.3;
         if (cost < best) {
             best = cost;
             plan.whole = (int)whole;
             plan.splits = s;
+            plan.sum_parts = p.parts + parts * tile_floats;
         }
     }
     return plan;
 }
 
-template <int CG, int BN, bool AA, bool BA>
+template <int CG, int BN, bool AA, bool BA, bool SUMS>
 aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     using G = Geo<CG, BN>;
     ProductParams p = in;
@@ -474,11 +532,11 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
         !encode_bf16_tile_map(&map_b, p.b.data, b_rows, b_cols, p.b.stride, BA ? kSlice : G::ROWS_B))
         return AA_ERR_CUDA;
     const int64_t mt = (p.m + CG * kBM - 1) / (CG * kBM), nt = (p.n + BN - 1) / BN, tiles = mt * nt;
-    const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA>;
+    const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA, SUMS>;
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
     const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kTcThreads, G::SMEM, CG);
     if (teams < 1) return AA_ERR_CUDA;
-    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN);
+    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     void* args[] = {&map_a, &map_b, &p, &plan, &vec};
     cudaLaunchConfig_t cfg = {};
@@ -506,8 +564,8 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
 
 template <int CG, int BN>
 aa_status launch_majors(aa_ctx_impl* c, const ProductParams& p, bool vec) {
-    if (p.a_across) return launch_tc<CG, BN, true, true>(c, p, vec);
-    return p.b_across ? launch_tc<CG, BN, false, true>(c, p, vec) : launch_tc<CG, BN, false, false>(c, p, vec);
+    if (p.a_across) return p.a_sums ? launch_tc<CG, BN, true, true, true>(c, p, vec) : launch_tc<CG, BN, true, true, false>(c, p, vec);
+    return p.b_across ? launch_tc<CG, BN, false, true, false>(c, p, vec) : launch_tc<CG, BN, false, false, false>(c, p, vec);
 }
 
 }  // namespace
