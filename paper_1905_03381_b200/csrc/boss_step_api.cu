@@ -46,7 +46,7 @@ LinearScratch linear_scratch(int64_t rows, int64_t cols, int dtype, int act) {
     LinearScratch s;
     s.g = act == AA_ACT_NONE ? 0 : up((size_t)rows * (size_t)((cols + 7) / 8 * 8) * (dtype == AA_BF16 ? 2 : 4));
     const size_t sums = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));
-    s.parts = dtype == AA_BF16 && sums < kProductParts ? kProductParts : sums;
+    s.parts = sums < kProductParts ? kProductParts : sums;
     s.total = s.g + s.parts;
     return s;
 }

@@ -1,0 +1,376 @@
+// Products of linear layers on the tensor cores for operands that TMA cannot feed to them: fp32, and bf16 rows that start at any alignment.
+//
+// The matrix unit takes bf16 factors.  An fp32 number is the sum of three of them, x = h + m + l with h = bf16(x), m = bf16(x - h), l = bf16(x - h - m): 24 bits in
+// all, each difference exact.  Of the nine products of two numbers the six largest are summed - h h', h m', m h', m m', h l', l h' - the others are
+// below 2^-22 of the product.  h h' has an accumulator of its own in TMEM, so that the large sum is rounded once for 16 terms.  The matrix unit rounds
+// towards zero there (one part in 2^24 a step of 16 terms, all in one direction: 1.4e-5 of a sum of 4,096 positive terms), so that every 256 terms
+// the accumulators go to registers, where the runs are added with ordinary rounding.
+// Six products of bf16 at 1.6 PFLOP/s are 0.27 PFLOP/s of fp32, against 0.07 of the ordinary lanes.
+//
+// A persistent CTA takes 128 x 128 tiles.  Eight warps fetch 64-wide slices with ordinary loads a slice ahead, take them apart and store the terms in the
+// layout that TMA would have left (128-byte swizzle); elements out of range are zeros, so strides, alignment and counted rows need nothing
+// else.  One warp issues the products, eight add the runs up and finish a tile, as in the kernel for bf16.
+#include "linear_plan.cuh"
+#include "tensor_core.cuh"
+
+namespace aa {
+
+namespace {
+
+constexpr int kTile = 128, kStages = 2;
+constexpr int kLoaders = 8, kEpilogue = 8;
+constexpr int kSplitThreads = 544;       // warps 0..7 load, 8 issues, 9..16 finish
+constexpr int kRun = 4;                  // slices summed in TMEM
+constexpr int kTermBytes = kTile * 128;
+
+template <int TERMS>
+struct Split {
+    static constexpr int OPERAND = TERMS * kTermBytes, STAGE = 2 * OPERAND;
+    static constexpr int ACC = TERMS == 1 ? kTile : 2 * kTile, TMEM = 2 * ACC;
+    static constexpr size_t SMEM = 1024 + (size_t)kStages * STAGE + kEpilogue * 32 * 32 * sizeof(float);
+};
+
+struct SplitCtl {
+    uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drain;
+    uint32_t tmem;
+    int abort_flag;
+};
+
+// Stored rows and columns of an operand that count.
+struct Box {
+    const void* data;
+    int64_t stride, rows, cols;
+    bool vec;                            // 16-byte aligned base and rows
+};
+
+// Elements 2 lane and 2 lane + 1 of 64 at (row, col), or with vectors: lanes 0..7 hold eight each of this row (see load_batch).
+template <typename T>
+__device__ __forceinline__ float element(const Box& b, int64_t row, int64_t col) {
+    return row < b.rows && col < b.cols ? load1(static_cast<const T*>(b.data) + row * b.stride + col) : 0.0f;
+}
+
+// The 16 floats a lane fetches of a batch of 8 rows of 64 elements.  Vectors: lane l takes elements 8 (l % 8) .. + 7 of rows l / 8 and l / 8 + 4.
+// Otherwise elements 2 l and 2 l + 1 of every row.
+template <typename T>
+__device__ __forceinline__ void load_batch(const Box& b, int64_t row0, int64_t col0, float (&x)[16]) {
+    const int lane = threadIdx.x & 31;
+    if (b.vec) {
+        const int64_t col = col0 + (lane & 7) * 8;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t row = row0 + (lane >> 3) + 4 * h;
+            const T* at = static_cast<const T*>(b.data) + row * b.stride + col;
+            if (row < b.rows && col + 8 <= b.cols) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 16 / (int)sizeof(T)) load_elems<T, 16 / (int)sizeof(T)>(at + e, x + 8 * h + e);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[8 * h + e] = row < b.rows && col + e < b.cols ? load1(at + e) : 0.0f;
+            }
+        }
+    } else {
+        const int64_t col = col0 + 2 * lane;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            x[2 * r] = element<T>(b, row0 + r, col);
+            x[2 * r + 1] = element<T>(b, row0 + r, col + 1);
+        }
+    }
+}
+
+// Two numbers' terms, packed.
+template <int TERMS>
+__device__ __forceinline__ void take_apart(float a, float b, uint32_t (&t)[TERMS]) {
+    t[0] = pack_bf16(a, b);
+    if (TERMS == 3) {
+        a -= bf16_lo(t[0]);
+        b -= bf16_hi(t[0]);
+        t[1] = pack_bf16(a, b);
+        a -= bf16_lo(t[1]);
+        b -= bf16_hi(t[1]);
+        t[2] = pack_bf16(a, b);
+    }
+}
+
+// The batch into rows r0 .. r0 + 7 of a [rows x 128 bytes] swizzled block; r0 a multiple of 8.
+template <int TERMS>
+__device__ __forceinline__ void store_batch(unsigned char* block, int r0, bool vec, const float (&x)[16]) {
+    const int lane = threadIdx.x & 31;
+    if (vec) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = (lane >> 3) + 4 * h;
+            uint32_t t[4][TERMS];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) take_apart<TERMS>(x[8 * h + 2 * q], x[8 * h + 2 * q + 1], t[q]);
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k)
+                *reinterpret_cast<uint4*>(block + k * kTermBytes + (r0 + r) * 128 + (((lane & 7) ^ r) << 4)) = make_uint4(t[0][k], t[1][k], t[2][k], t[3][k]);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            uint32_t t[TERMS];
+            take_apart<TERMS>(x[2 * r], x[2 * r + 1], t);
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) *reinterpret_cast<uint32_t*>(block + k * kTermBytes + (r0 + r) * 128 + (((lane >> 2) ^ r) << 4) + (lane & 3) * 4) = t[k];
+        }
+    }
+}
+
+template <typename T, int TERMS, bool A_ACROSS, bool B_ACROSS>
+__global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan, bool a_vec, bool b_vec, bool out_vec) {
+    using S = Split<TERMS>;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ SplitCtl ctl;
+    unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    float* stage_f = reinterpret_cast<float*>(ring + (size_t)kStages * S::STAGE);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* abort_flag = &ctl.abort_flag;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&ctl.full[s], kLoaders);
+            mbar_init(&ctl.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&ctl.acc_full[b], 1);
+            mbar_init(&ctl.acc_empty[b], kEpilogue);
+        }
+        mbar_init(&ctl.drain, 1);
+        ctl.abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 8) tmem_alloc(&ctl.tmem, S::TMEM);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *(volatile uint32_t*)&ctl.tmem;
+    grid_dependency_wait();
+    grid_dependency_release();
+    const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
+    const int64_t m_end = p.live_k ? p.m : min(p.m, live), k_end = p.live_k ? min(p.k, live) : p.k;
+    const int mt = (int)((m_end + kTile - 1) / kTile), units = units_of(plan, mt), slices = (int)((k_end + kSlice - 1) / kSlice);
+    bool ok = true;
+    if (warp < kLoaders) {
+        // ---- loaders: a slice is 16 batches of 8 rows of each operand, two a warp; the next batch is under way while this one is stored
+        const Box a{p.a.data, p.a.stride, A_ACROSS ? k_end : m_end, A_ACROSS ? m_end : k_end, a_vec}, b{p.b.data, p.b.stride, B_ACROSS ? k_end : p.n, B_ACROSS ? p.n : k_end, b_vec};
+        int i = blockIdx.x, s = 0;
+        Unit u = {};
+        // the first slice from here on, over the units without one
+        const auto settle = [&]() {
+            for (; i < units; i += gridDim.x) {
+                u = unit_at(plan, mt, slices, i);
+                s = u.s0;
+                if (u.s0 < u.s1) return;
+            }
+        };
+        const auto fetch = [&](int q, float (&x)[16]) {
+            const int batch = warp * 2 + (q & 1);
+            const bool of_a = q < 2, across = of_a ? A_ACROSS : B_ACROSS;
+            const int64_t tile0 = (int64_t)(of_a ? u.m : u.n) * kTile;
+            // across: the first 64 rows of the block are tokens against columns 0..63 of the tile, the others against 64..127
+            const int64_t row = across ? (int64_t)s * kSlice + (batch & 7) * 8 : tile0 + batch * 8, col = across ? tile0 + (batch >> 3) * 64 : (int64_t)s * kSlice;
+            load_batch<T>(of_a ? a : b, row, col, x);
+        };
+        float x[4][16];
+        uint32_t sent = 0;
+        settle();
+        if (i < units)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) fetch(q, x[q]);
+        while (i < units) {
+            const int stage = (int)(sent % kStages);
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.empty[stage], ((sent / kStages) & 1u) ^ 1u, abort_flag))) {
+                ok = false;
+                break;
+            }
+            if (++s >= u.s1) {
+                i += gridDim.x;
+                settle();
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                unsigned char* block = ring + (size_t)stage * S::STAGE + (q < 2 ? 0 : S::OPERAND);
+                store_batch<TERMS>(block, (warp * 2 + (q & 1)) * 8, q < 2 ? a_vec : b_vec, x[q]);
+                if (i < units) fetch(q, x[q]);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.full[stage]);
+            ++sent;
+        }
+    } else if (warp == 8) {
+        // ---- issuer
+        constexpr uint32_t idesc = umma_idesc_bf16(kTile, kTile, A_ACROSS, B_ACROSS);
+        uint32_t sent = 0;
+        int it = 0;
+        for (int i = blockIdx.x; i < units && ok; i += gridDim.x) {
+            const Unit u = unit_at(plan, mt, slices, i);
+            uint32_t d = 0;
+            for (int s = u.s0; s < u.s1; ++s, ++sent) {
+                const int in_run = (s - u.s0) % kRun;
+                if (in_run == 0) {
+                    if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_empty[it & 1], (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag))) {
+                        ok = false;
+                        break;
+                    }
+                    d = tmem + (uint32_t)((it & 1) * S::ACC);
+                }
+                const int stage = (int)(sent % kStages);
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], (sent / kStages) & 1u, abort_flag))) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after_sync();
+                const bool last = in_run == kRun - 1 || s == u.s1 - 1;
+                if (lane == 0) {
+                    const uint32_t a = smem_u32(ring + (size_t)stage * S::STAGE), b = a + S::OPERAND;
+#pragma unroll
+                    for (int k = 0; k < kSlice / 16; ++k) {
+                        const auto ad = [&](int t) { return A_ACROSS ? umma_smem_desc(a + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(a + t * kTermBytes + k * 32, 16, 1024); };
+                        const auto bd = [&](int t) { return B_ACROSS ? umma_smem_desc(b + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(b + t * kTermBytes + k * 32, 16, 1024); };
+                        const bool more = (in_run | k) != 0;
+                        umma_bf16(d, ad(0), bd(0), idesc, more);
+                        if (TERMS == 3) {
+                            umma_bf16(d + kTile, ad(0), bd(2), idesc, more);
+                            umma_bf16(d + kTile, ad(2), bd(0), idesc, true);
+                            umma_bf16(d + kTile, ad(1), bd(1), idesc, true);
+                            umma_bf16(d + kTile, ad(0), bd(1), idesc, true);
+                            umma_bf16(d + kTile, ad(1), bd(0), idesc, true);
+                        }
+                    }
+                    umma_commit(&ctl.empty[stage]);
+                    if (last) umma_commit(&ctl.acc_full[it & 1]);
+                }
+                __syncwarp();
+                if (last) ++it;
+            }
+        }
+        if (lane == 0) umma_commit(&ctl.drain);
+        __syncwarp();
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&ctl.drain, 0) && clock64() - t0 < kWaitCycles) {
+        }
+    } else {
+        // ---- epilogue: a warp has 32 rows and 64 columns
+        const int quad = warp & 3, half = (warp - 9) >> 2;
+        float* mine = stage_f + (warp - 9) * 32 * 32;
+        const int sub = lane & 7, r8 = lane >> 3;
+        T* out = static_cast<T*>(const_cast<void*>(p.out.data));
+        T* pre = static_cast<T*>(const_cast<void*>(p.pre.data));
+        const T* res = static_cast<const T*>(p.residual.data);
+        int it = 0;
+        for (int i = blockIdx.x; i < units && ok; i += gridDim.x) {
+            const Unit u = unit_at(plan, mt, slices, i);
+            float sum[64];
+#pragma unroll
+            for (int e = 0; e < 64; ++e) sum[e] = 0.0f;
+            for (int s = u.s0; s < u.s1; s += kRun, ++it) {
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_full[it & 1], (uint32_t)((it >> 1) & 1), abort_flag))) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after_sync();
+                const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)((it & 1) * S::ACC + half * 64);
+#pragma unroll
+                for (int t = 0; t < (TERMS == 3 ? 2 : 1); ++t)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t v[32];
+                        tmem_ld_32cols(at + (uint32_t)(t * kTile + c * 32), v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) sum[c * 32 + e] += __uint_as_float(v[e]);
+                    }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl.acc_empty[it & 1]);
+            }
+            if (!ok) break;
+            const int64_t row0 = (int64_t)u.m * kTile + quad * 32 + r8;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                __syncwarp();                // the stage's readers of the chunk before are done
+#pragma unroll
+                for (int w = 0; w < 8; ++w)
+                    *reinterpret_cast<float4*>(mine + lane * 32 + ((w ^ (lane & 7)) << 2)) =
+                        make_float4(sum[c * 32 + 4 * w], sum[c * 32 + 4 * w + 1], sum[c * 32 + 4 * w + 2], sum[c * 32 + 4 * w + 3]);
+                __syncwarp();
+                const int in_tile = half * 64 + c * 32 + sub * 4;
+                const int64_t col = (int64_t)u.n * kTile + in_tile;
+                const int cols = (int)max((int64_t)0, min((int64_t)4, p.n - col));
+                float bias[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bias[e] = p.bias && e < cols ? p.bias[col + e] : 0.0f;
+#pragma unroll 2
+                for (int q = 0; q < 8; ++q) {
+                    const int64_t row = row0 + q * 4;
+                    const int r = q * 4 + r8;
+                    const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
+                    if (u.part >= 0) {
+                        *reinterpret_cast<float4*>(plan.parts + ((int64_t)u.part * kTile + quad * 32 + r) * kTile + in_tile) = f;
+                        continue;
+                    }
+                    float z[4] = {f.x + bias[0], f.y + bias[1], f.z + bias[2], f.w + bias[3]};
+                    if (row >= m_end) continue;
+                    if (out_vec && cols == 4) {
+                        if (pre) store_quad(pre + row * p.pre.stride + col, z);
+                        activate_all(z, p.act);
+                        if (res) {
+                            float y[4];
+                            load_quad(res + row * p.residual.stride + col, y);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) z[e] += y[e];
+                        }
+                        store_quad(out + row * p.out.stride + col, z);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (pre && e < cols) store1(pre + row * p.pre.stride + col + e, z[e]);
+                        activate_all(z, p.act);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e < cols) store1(out + row * p.out.stride + col + e, res ? z[e] + load1(res + row * p.residual.stride + col + e) : z[e]);
+                    }
+                }
+            }
+        }
+    }
+    if (!ok) {
+        *abort_flag = 1;
+        if (lane == 0) latch(p.ctl, AA_ERR_SCAN_TIMEOUT);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 8) tmem_dealloc(tmem, S::TMEM);
+}
+
+template <typename T, int TERMS>
+aa_status launch_split(aa_ctx_impl* c, const ProductParams& in) {
+    ProductParams p = in;
+    constexpr int es = (int)sizeof(T);
+    const auto lies = [](const MatArg& a, int64_t bytes) { return !a.data || ((uintptr_t)a.data % bytes == 0 && a.stride * es % bytes == 0); };
+    bool a_vec = lies(p.a, 16), b_vec = lies(p.b, 16), out_vec = lies(p.out, 4 * es) && lies(p.pre, 4 * es) && lies(p.residual, 4 * es);
+    const int64_t mt = (p.m + kTile - 1) / kTile, nt = (p.n + kTile - 1) / kTile, tiles = mt * nt;
+    if (tiles > 0x3FFFFFF) return AA_ERR_UNSUPPORTED;
+    Plan plan = make_plan(p, tiles, (int)nt, c->sm_count, kTile * kTile, kTile, TERMS == 3 ? 1.2 : 0.6);
+    const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
+    const void* kernel = p.a_across ? (const void*)product_split_kernel<T, TERMS, true, true>
+                                    : (p.b_across ? (const void*)product_split_kernel<T, TERMS, false, true> : (const void*)product_split_kernel<T, TERMS, false, false>);
+    if (allow_smem(c, kernel, Split<TERMS>::SMEM) != AA_OK) return AA_ERR_CUDA;
+    void* args[] = {&p, &plan, &a_vec, &b_vec, &out_vec};
+    if (launch_overlapped(c, kernel, dim3((unsigned)(units < c->sm_count ? units : c->sm_count)), dim3(kSplitThreads), args, Split<TERMS>::SMEM, false) != cudaSuccess) return AA_ERR_CUDA;
+    ++c->launches;
+    if (tail == 0) return AA_OK;
+    void* join[] = {&p, &plan, &out_vec};
+    if (launch_overlapped(c, (const void*)product_join_kernel<T, kTile, kTile>, dim3((unsigned)(tail * kTile * kTile / 4 / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+    ++c->launches;
+    return AA_OK;
+}
+
+}  // namespace
+
+aa_status launch_product_split(aa_ctx_impl* c, const ProductParams& p, int dtype) { return dtype == AA_BF16 ? launch_split<uint16_t, 1>(c, p) : launch_split<float, 3>(c, p); }
+
+}  // namespace aa

@@ -11,14 +11,14 @@
 //
 // Tiles that do not fill the last round of SMs can be cut along the contraction (the backward call has scratch memory): their parts go to
 // scratch in fp32 and a second kernel adds them up in order and finishes them.
-#include "linear.cuh"
+#include "linear_plan.cuh"
 #include "tensor_core.cuh"
 
 namespace aa {
 
 namespace {
 
-constexpr int kBM = 128, kSlice = 64, kGroupM = 16;
+constexpr int kBM = 128;
 constexpr int kTcThreads = 384;          // producer, issuer, two for column sums (the first of them allocates), eight for the epilogue
 constexpr int kEpilogue = 8;
 constexpr int kStageFloats = 32 * 32;    // per epilogue warp
@@ -39,43 +39,6 @@ struct Ctl {
     uint32_t tmem;
     int abort_flag;
 };
-
-// What a launch does in which order: the first `whole` tiles at once, the others in `splits` parts each.
-struct Plan {
-    int nt, whole, splits;
-    float* parts;                        // [part][CG 128][BN]
-    float* sum_parts;                    // [part][CG 128]
-};
-
-struct Unit {
-    int m, n, s0, s1, part;              // slices [s0, s1); part < 0: the whole tile
-};
-
-__device__ __forceinline__ void tile_at(int mt, int nt, int i, int& m, int& n) {
-    const int per = kGroupM * nt, g = i / per, in = i - g * per, rows = min(kGroupM, mt - g * kGroupM);
-    n = in / rows;
-    m = g * kGroupM + (in - n * rows);
-}
-__device__ __forceinline__ int units_of(const Plan& p, int mt) {
-    const int tiles = mt * p.nt;
-    return tiles <= p.whole ? tiles : p.whole + (tiles - p.whole) * p.splits;
-}
-__device__ __forceinline__ Unit unit_at(const Plan& p, int mt, int slices, int i) {
-    Unit u;
-    if (i < p.whole) {
-        tile_at(mt, p.nt, i, u.m, u.n);
-        u.s0 = 0;
-        u.s1 = slices;
-        u.part = -1;
-    } else {
-        const int j = i - p.whole, t = j / p.splits, q = j - t * p.splits;
-        tile_at(mt, p.nt, p.whole + t, u.m, u.n);
-        u.s0 = (int)((int64_t)slices * q / p.splits);
-        u.s1 = (int)((int64_t)slices * (q + 1) / p.splits);
-        u.part = j;
-    }
-    return u;
-}
 
 // ---- a pair of CTAs
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -457,71 +420,6 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (warp == 2) dealloc<CG>(tmem, G::TMEM);
 }
 
-// Adds the parts of the cut tiles up in order and finishes them.  A thread takes four columns of a row.
-template <int CG, int BN>
-__global__ void __launch_bounds__(256) product_join_kernel(const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan, bool vec) {
-    grid_dependency_wait();
-    grid_dependency_release();
-    const int64_t live = live_rows(p.live, p.ctl, false);
-    const int64_t m_end = p.live_k ? p.m : min(p.m, live);
-    const int mt = (int)((m_end + CG * kBM - 1) / (CG * kBM)), tail = mt * plan.nt - plan.whole;
-    constexpr int kPerTile = CG * kBM * BN / 4;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, t = at / kPerTile;
-    if (t >= tail) return;
-    const int in = (int)(at - t * kPerTile), r = in / (BN / 4), q = in - r * (BN / 4);
-    int m, n;
-    tile_at(mt, plan.nt, plan.whole + (int)t, m, n);
-    const int64_t row = (int64_t)m * CG * kBM + r, col = (int64_t)n * BN + q * 4;
-    if (row >= m_end || col >= p.n) return;
-    if (p.a_sums && col == 0) {
-        float sum = 0.0f;
-        for (int s = 0; s < plan.splits; ++s) sum += plan.sum_parts[(t * plan.splits + s) * CG * kBM + r];
-        p.a_sums[row] = sum;
-    }
-    float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const float4* from = reinterpret_cast<const float4*>(plan.parts + t * plan.splits * CG * kBM * BN) + in;
-    for (int s = 0; s < plan.splits; ++s) {
-        const float4 f = from[(int64_t)s * kPerTile];
-        z[0] += f.x;
-        z[1] += f.y;
-        z[2] += f.z;
-        z[3] += f.w;
-    }
-    uint16_t* out = static_cast<uint16_t*>(const_cast<void*>(p.out.data)) + row * p.out.stride + col;
-    const uint16_t* res = p.residual.data ? static_cast<const uint16_t*>(p.residual.data) + row * p.residual.stride + col : nullptr;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (res && col + e < p.n) z[e] += load1(res + e);
-    if (vec && col + 4 <= p.n) {
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < p.n) store1(out + e, z[e]);
-    }
-}
-
-// Splits of the tiles that do not fill a round of `teams`: the fewest slices one after the other, counting the parts' way through memory.
-Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats, int tile_rows) {
-    Plan plan{nt, (int)tiles, 1, p.parts, nullptr};
-    const int64_t slices = (p.k + kSlice - 1) / kSlice, whole = tiles / teams * teams, tail = tiles - whole;
-    if (!p.parts || tail == 0) return plan;
-    double best = (double)slices;
-    for (int s = 2; s <= 16 && slices / s >= 8; ++s) {
-        const int64_t parts = tail * s;
-        if (parts * (tile_floats + tile_rows) > p.part_floats) break;
-        // a slice takes about 0.3 us; the parts are written and read at about 5 TB/s, behind a launch of about 4 us
-        const double cost = (double)((parts + teams - 1) / teams) * (double)((slices + s - 1) / s) + (4.0 + (double)(parts * tile_floats) * 8.0 / 5e6) / 0.3;
-        if (cost < best) {
-            best = cost;
-            plan.whole = (int)whole;
-            plan.splits = s;
-            plan.sum_parts = p.parts + parts * tile_floats;
-        }
-    }
-    return plan;
-}
-
 template <int CG, int BN, bool AA, bool BA, bool SUMS>
 aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     using G = Geo<CG, BN>;
@@ -536,7 +434,7 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
     const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kTcThreads, G::SMEM, CG);
     if (teams < 1) return AA_ERR_CUDA;
-    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM);
+    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     void* args[] = {&map_a, &map_b, &p, &plan, &vec};
     cudaLaunchConfig_t cfg = {};
@@ -557,7 +455,7 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     if (tail == 0) return AA_OK;
     void* join[] = {&p, &plan, &vec};
     const int64_t threads = tail * CG * kBM * BN / 4;
-    if (launch_overlapped(c, (const void*)product_join_kernel<CG, BN>, dim3((unsigned)(threads / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+    if (launch_overlapped(c, (const void*)product_join_kernel<uint16_t, CG * kBM, BN>, dim3((unsigned)(threads / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     return AA_OK;
 }
