@@ -9,7 +9,7 @@
 //
 // A persistent CTA takes 128 x 128 tiles.  Eight warps fetch 64-wide slices with ordinary loads a slice ahead, take them apart and store the terms in the
 // layout that TMA would have left (128-byte swizzle); elements out of range are zeros, so strides, alignment and counted rows need nothing
-// else.  One warp issues the products, eight add the runs up and finish a tile, as in the kernel for bf16.
+// else.  The first of them issues the products as soon as all have stored a slice, eight other warps add the runs up and finish a tile, as in the kernel for bf16.
 #include "linear_plan.cuh"
 #include "tensor_core.cuh"
 
@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kTile = 128, kStages = 2;
 constexpr int kLoaders = 8, kEpilogue = 8;
-constexpr int kSplitThreads = 544;       // warps 0..7 load, 8 issues, 9..16 finish
+constexpr int kSplitThreads = 512;       // warps 0..7 load (the first of them issues, too), 8..15 finish: 128 registers a thread
 constexpr int kRun = 4;                  // slices summed in TMEM
 constexpr int kTermBytes = kTile * 128;
 
@@ -40,40 +40,36 @@ struct SplitCtl {
 struct Box {
     const void* data;
     int64_t stride, rows, cols;
-    bool vec;                            // 16-byte aligned base and rows
 };
 
-// Elements 2 lane and 2 lane + 1 of 64 at (row, col), or with vectors: lanes 0..7 hold eight each of this row (see load_batch).
-template <typename T>
-__device__ __forceinline__ float element(const Box& b, int64_t row, int64_t col) {
-    return row < b.rows && col < b.cols ? load1(static_cast<const T*>(b.data) + row * b.stride + col) : 0.0f;
-}
-
-// The 16 floats a lane fetches of a batch of 8 rows of 64 elements.  Vectors: lane l takes elements 8 (l % 8) .. + 7 of rows l / 8 and l / 8 + 4.
-// Otherwise elements 2 l and 2 l + 1 of every row.
-template <typename T>
-__device__ __forceinline__ void load_batch(const Box& b, int64_t row0, int64_t col0, float (&x)[16]) {
+// The 16 numbers a lane fetches of a batch of 8 rows of 64 elements.  VEC (16-byte aligned base and rows, columns in eights): lane l takes elements 8 (l % 8) .. + 7 of
+// rows l / 8 and l / 8 + 4, of a stand-in where they do not count (there is a row and a column at least; `in` says which numbers count); otherwise
+// elements 2 l and 2 l + 1 of every row, zeros where they do not count.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_batch(const Box& b, int64_t row0, int64_t col0, float (&x)[16], uint32_t& in) {
     const int lane = threadIdx.x & 31;
-    if (b.vec) {
+    if (VEC) {
+        asm volatile("" : "+l"(row0));   // the addresses are worked out here, not held in registers from slice to slice
         const int64_t col = col0 + (lane & 7) * 8;
+        const bool c = col < b.cols;
+        in = 0;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t row = row0 + (lane >> 3) + 4 * h;
-            const T* at = static_cast<const T*>(b.data) + row * b.stride + col;
-            if (row < b.rows && col + 8 <= b.cols) {
+            const T* at = static_cast<const T*>(b.data) + min(row, b.rows - 1) * b.stride + (c ? col : 0);
 #pragma unroll
-                for (int e = 0; e < 8; e += 16 / (int)sizeof(T)) load_elems<T, 16 / (int)sizeof(T)>(at + e, x + 8 * h + e);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[8 * h + e] = row < b.rows && col + e < b.cols ? load1(at + e) : 0.0f;
-            }
+            for (int e = 0; e < 8; e += 16 / (int)sizeof(T)) load_elems<T, 16 / (int)sizeof(T)>(at + e, x + 8 * h + e);
+            if (c && row < b.rows) in |= 0xFFu << (8 * h);
         }
     } else {
         const int64_t col = col0 + 2 * lane;
+        in = 0;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            x[2 * r] = element<T>(b, row0 + r, col);
-            x[2 * r + 1] = element<T>(b, row0 + r, col + 1);
+            const T* at = static_cast<const T*>(b.data) + (row0 + r) * b.stride + col;
+            const bool row = row0 + r < b.rows, one = row && col < b.cols, two = row && col + 1 < b.cols;
+            x[2 * r] = one ? load1(at) : 0.0f;
+            x[2 * r + 1] = two ? load1(at + 1) : 0.0f;
         }
     }
 }
@@ -93,10 +89,14 @@ __device__ __forceinline__ void take_apart(float a, float b, uint32_t (&t)[TERMS
 }
 
 // The batch into rows r0 .. r0 + 7 of a [rows x 128 bytes] swizzled block; r0 a multiple of 8.
-template <int TERMS>
-__device__ __forceinline__ void store_batch(unsigned char* block, int r0, bool vec, const float (&x)[16]) {
+template <int TERMS, bool VEC>
+__device__ __forceinline__ void store_batch(unsigned char* block, int r0, float (&x)[16], uint32_t in) {
     const int lane = threadIdx.x & 31;
-    if (vec) {
+    if (VEC && !__all_sync(0xFFFFFFFFu, in == 0xFFFFu)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = (in >> e) & 1u ? x[e] : 0.0f;
+    }
+    if (VEC) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = (lane >> 3) + 4 * h;
@@ -118,8 +118,8 @@ __device__ __forceinline__ void store_batch(unsigned char* block, int r0, bool v
     }
 }
 
-template <typename T, int TERMS, bool A_ACROSS, bool B_ACROSS>
-__global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan, bool a_vec, bool b_vec, bool out_vec) {
+template <typename T, int TERMS, bool VEC, bool A_ACROSS, bool B_ACROSS>
+__global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan, bool out_vec) {
     using S = Split<TERMS>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ SplitCtl ctl;
@@ -153,108 +153,110 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
     bool ok = true;
     if (warp < kLoaders) {
         // ---- loaders: a slice is 16 batches of 8 rows of each operand, two a warp; the next batch is under way while this one is stored
-        const Box a{p.a.data, p.a.stride, A_ACROSS ? k_end : m_end, A_ACROSS ? m_end : k_end, a_vec}, b{p.b.data, p.b.stride, B_ACROSS ? k_end : p.n, B_ACROSS ? p.n : k_end, b_vec};
+        const Box a{p.a.data, p.a.stride, A_ACROSS ? k_end : m_end, A_ACROSS ? m_end : k_end}, b{p.b.data, p.b.stride, B_ACROSS ? k_end : p.n, B_ACROSS ? p.n : k_end};
         int i = blockIdx.x, s = 0;
         Unit u = {};
         // the first slice from here on, over the units without one
         const auto settle = [&]() {
             for (; i < units; i += gridDim.x) {
-                u = unit_at(plan, mt, slices, i);
-                s = u.s0;
-                if (u.s0 < u.s1) return;
+                const Unit next = unit_at(plan, mt, slices, i);
+                if (next.s0 == next.s1) continue;
+                u = next;
+                s = next.s0;
+                return;
             }
         };
-        const auto fetch = [&](int q, float (&x)[16]) {
+        const auto fetch = [&](int q, float (&x)[16], uint32_t& in) {
             const int batch = warp * 2 + (q & 1);
             const bool of_a = q < 2, across = of_a ? A_ACROSS : B_ACROSS;
             const int64_t tile0 = (int64_t)(of_a ? u.m : u.n) * kTile;
             // across: the first 64 rows of the block are tokens against columns 0..63 of the tile, the others against 64..127
             const int64_t row = across ? (int64_t)s * kSlice + (batch & 7) * 8 : tile0 + batch * 8, col = across ? tile0 + (batch >> 3) * 64 : (int64_t)s * kSlice;
-            load_batch<T>(of_a ? a : b, row, col, x);
+            load_batch<T, VEC>(of_a ? a : b, row, col, x, in);
+        };
+        // products of slice number `issued` of this CTA, by the first warp
+        constexpr uint32_t idesc = umma_idesc_bf16(kTile, kTile, A_ACROSS, B_ACROSS);
+        uint32_t issued = 0;
+        int in_run = 0, it = 0, of = blockIdx.x, togo = 0;
+        const auto issue = [&]() -> bool {
+            while (togo == 0) {
+                const Unit v = unit_at(plan, mt, slices, of);
+                of += gridDim.x;
+                togo = v.s1 - v.s0;
+            }
+            if (in_run == 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_empty[it & 1], (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag))) return false;
+            const int stage = (int)(issued % kStages);
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], (issued / kStages) & 1u, abort_flag))) return false;
+            tc_fence_after_sync();
+            const bool last = in_run == kRun - 1 || togo == 1;
+            if (lane == 0) {
+                const uint32_t d = tmem + (uint32_t)((it & 1) * S::ACC), a = smem_u32(ring + (size_t)stage * S::STAGE), b = a + S::OPERAND;
+#pragma unroll
+                for (int k = 0; k < kSlice / 16; ++k) {
+                    const auto ad = [&](int t) { return A_ACROSS ? umma_smem_desc(a + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(a + t * kTermBytes + k * 32, 16, 1024); };
+                    const auto bd = [&](int t) { return B_ACROSS ? umma_smem_desc(b + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(b + t * kTermBytes + k * 32, 16, 1024); };
+                    const bool more = (in_run | k) != 0;
+                    umma_bf16(d, ad(0), bd(0), idesc, more);
+                    if (TERMS == 3) {
+                        umma_bf16(d + kTile, ad(0), bd(2), idesc, more);
+                        umma_bf16(d + kTile, ad(2), bd(0), idesc, true);
+                        umma_bf16(d + kTile, ad(1), bd(1), idesc, true);
+                        umma_bf16(d + kTile, ad(0), bd(1), idesc, true);
+                        umma_bf16(d + kTile, ad(1), bd(0), idesc, true);
+                    }
+                }
+                umma_commit(&ctl.empty[stage]);
+                if (last) umma_commit(&ctl.acc_full[it & 1]);
+            }
+            __syncwarp();
+            ++issued;
+            --togo;
+            in_run = last ? 0 : in_run + 1;
+            if (last) ++it;
+            return true;
         };
         float x[4][16];
+        uint32_t in[4];
         uint32_t sent = 0;
         settle();
         if (i < units)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) fetch(q, x[q]);
-        while (i < units) {
+            for (int q = 0; q < 4; ++q) fetch(q, x[q], in[q]);
+        while (i < units && ok) {
             const int stage = (int)(sent % kStages);
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.empty[stage], ((sent / kStages) & 1u) ^ 1u, abort_flag))) {
                 ok = false;
                 break;
             }
+            // the last slice of all is fetched once more and not stored, rather than have the loads behind a branch
             if (++s >= u.s1) {
                 i += gridDim.x;
                 settle();
+                if (i >= units) --s;
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 unsigned char* block = ring + (size_t)stage * S::STAGE + (q < 2 ? 0 : S::OPERAND);
-                store_batch<TERMS>(block, (warp * 2 + (q & 1)) * 8, q < 2 ? a_vec : b_vec, x[q]);
-                if (i < units) fetch(q, x[q]);
+                store_batch<TERMS, VEC>(block, (warp * 2 + (q & 1)) * 8, x[q], in[q]);
+                fetch(q, x[q], in[q]);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(&ctl.full[stage]);
             ++sent;
+            if (warp == 0) ok = issue();
         }
-    } else if (warp == 8) {
-        // ---- issuer
-        constexpr uint32_t idesc = umma_idesc_bf16(kTile, kTile, A_ACROSS, B_ACROSS);
-        uint32_t sent = 0;
-        int it = 0;
-        for (int i = blockIdx.x; i < units && ok; i += gridDim.x) {
-            const Unit u = unit_at(plan, mt, slices, i);
-            uint32_t d = 0;
-            for (int s = u.s0; s < u.s1; ++s, ++sent) {
-                const int in_run = (s - u.s0) % kRun;
-                if (in_run == 0) {
-                    if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_empty[it & 1], (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag))) {
-                        ok = false;
-                        break;
-                    }
-                    d = tmem + (uint32_t)((it & 1) * S::ACC);
-                }
-                const int stage = (int)(sent % kStages);
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], (sent / kStages) & 1u, abort_flag))) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after_sync();
-                const bool last = in_run == kRun - 1 || s == u.s1 - 1;
-                if (lane == 0) {
-                    const uint32_t a = smem_u32(ring + (size_t)stage * S::STAGE), b = a + S::OPERAND;
-#pragma unroll
-                    for (int k = 0; k < kSlice / 16; ++k) {
-                        const auto ad = [&](int t) { return A_ACROSS ? umma_smem_desc(a + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(a + t * kTermBytes + k * 32, 16, 1024); };
-                        const auto bd = [&](int t) { return B_ACROSS ? umma_smem_desc(b + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(b + t * kTermBytes + k * 32, 16, 1024); };
-                        const bool more = (in_run | k) != 0;
-                        umma_bf16(d, ad(0), bd(0), idesc, more);
-                        if (TERMS == 3) {
-                            umma_bf16(d + kTile, ad(0), bd(2), idesc, more);
-                            umma_bf16(d + kTile, ad(2), bd(0), idesc, true);
-                            umma_bf16(d + kTile, ad(1), bd(1), idesc, true);
-                            umma_bf16(d + kTile, ad(0), bd(1), idesc, true);
-                            umma_bf16(d + kTile, ad(1), bd(0), idesc, true);
-                        }
-                    }
-                    umma_commit(&ctl.empty[stage]);
-                    if (last) umma_commit(&ctl.acc_full[it & 1]);
-                }
-                __syncwarp();
-                if (last) ++it;
+        if (warp == 0) {
+            if (lane == 0) umma_commit(&ctl.drain);
+            __syncwarp();
+            const long long t0 = clock64();
+            while (!mbar_try_wait(&ctl.drain, 0) && clock64() - t0 < kWaitCycles) {
             }
-        }
-        if (lane == 0) umma_commit(&ctl.drain);
-        __syncwarp();
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&ctl.drain, 0) && clock64() - t0 < kWaitCycles) {
         }
     } else {
         // ---- epilogue: a warp has 32 rows and 64 columns
-        const int quad = warp & 3, half = (warp - 9) >> 2;
-        float* mine = stage_f + (warp - 9) * 32 * 32;
+        const int quad = warp & 3, half = (warp - 8) >> 2;
+        float* mine = stage_f + (warp - 8) * 32 * 32;
         const int sub = lane & 7, r8 = lane >> 3;
         T* out = static_cast<T*>(const_cast<void*>(p.out.data));
         T* pre = static_cast<T*>(const_cast<void*>(p.pre.data));
@@ -275,12 +277,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
 #pragma unroll
                 for (int t = 0; t < (TERMS == 3 ? 2 : 1); ++t)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t v[32];
-                        tmem_ld_32cols(at + (uint32_t)(t * kTile + c * 32), v);
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[16];
+                        tmem_ld_16cols(at + (uint32_t)(t * kTile + c * 16), v);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) sum[c * 32 + e] += __uint_as_float(v[e]);
+                        for (int e = 0; e < 16; ++e) sum[c * 16 + e] += __uint_as_float(v[e]);
                     }
                 tc_fence_before_sync();
                 __syncwarp();
@@ -346,20 +348,17 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
     if (warp == 8) tmem_dealloc(tmem, S::TMEM);
 }
 
-template <typename T, int TERMS>
-aa_status launch_split(aa_ctx_impl* c, const ProductParams& in) {
+template <typename T, int TERMS, bool VEC>
+aa_status launch_split(aa_ctx_impl* c, const ProductParams& in, bool out_vec) {
     ProductParams p = in;
-    constexpr int es = (int)sizeof(T);
-    const auto lies = [](const MatArg& a, int64_t bytes) { return !a.data || ((uintptr_t)a.data % bytes == 0 && a.stride * es % bytes == 0); };
-    bool a_vec = lies(p.a, 16), b_vec = lies(p.b, 16), out_vec = lies(p.out, 4 * es) && lies(p.pre, 4 * es) && lies(p.residual, 4 * es);
     const int64_t mt = (p.m + kTile - 1) / kTile, nt = (p.n + kTile - 1) / kTile, tiles = mt * nt;
     if (tiles > 0x3FFFFFF) return AA_ERR_UNSUPPORTED;
     Plan plan = make_plan(p, tiles, (int)nt, c->sm_count, kTile * kTile, kTile, TERMS == 3 ? 1.2 : 0.6);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
-    const void* kernel = p.a_across ? (const void*)product_split_kernel<T, TERMS, true, true>
-                                    : (p.b_across ? (const void*)product_split_kernel<T, TERMS, false, true> : (const void*)product_split_kernel<T, TERMS, false, false>);
+    const void* kernel = p.a_across ? (const void*)product_split_kernel<T, TERMS, VEC, true, true>
+                                    : (p.b_across ? (const void*)product_split_kernel<T, TERMS, VEC, false, true> : (const void*)product_split_kernel<T, TERMS, VEC, false, false>);
     if (allow_smem(c, kernel, Split<TERMS>::SMEM) != AA_OK) return AA_ERR_CUDA;
-    void* args[] = {&p, &plan, &a_vec, &b_vec, &out_vec};
+    void* args[] = {&p, &plan, &out_vec};
     if (launch_overlapped(c, kernel, dim3((unsigned)(units < c->sm_count ? units : c->sm_count)), dim3(kSplitThreads), args, Split<TERMS>::SMEM, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     if (tail == 0) return AA_OK;
@@ -371,6 +370,13 @@ aa_status launch_split(aa_ctx_impl* c, const ProductParams& in) {
 
 }  // namespace
 
-aa_status launch_product_split(aa_ctx_impl* c, const ProductParams& p, int dtype) { return dtype == AA_BF16 ? launch_split<uint16_t, 1>(c, p) : launch_split<float, 3>(c, p); }
+aa_status launch_product_split(aa_ctx_impl* c, const ProductParams& p, int dtype) {
+    const int64_t es = dtype == AA_BF16 ? 2 : 4;
+    const auto lies = [&](const MatArg& a, int64_t bytes) { return !a.data || ((uintptr_t)a.data % bytes == 0 && a.stride * es % bytes == 0); };
+    const bool vec = lies(p.a, 16) && lies(p.b, 16) && (p.a_across ? p.m : p.k) % 8 == 0 && (p.b_across ? p.n : p.k) % 8 == 0;
+    const bool out_vec = lies(p.out, 4 * es) && lies(p.pre, 4 * es) && lies(p.residual, 4 * es);
+    if (dtype == AA_BF16) return vec ? launch_split<uint16_t, 1, true>(c, p, out_vec) : launch_split<uint16_t, 1, false>(c, p, out_vec);
+    return vec ? launch_split<float, 3, true>(c, p, out_vec) : launch_split<float, 3, false>(c, p, out_vec);
+}
 
 }  // namespace aa
