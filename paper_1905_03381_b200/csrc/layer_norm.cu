@@ -11,6 +11,7 @@
 // Rows too long for registers are swept three times, and their columns are summed by a kernel of their own.
 #include <type_traits>
 
+#include "async_copy.cuh"
 #include "layer_norm.cuh"
 
 namespace aa {
@@ -126,135 +127,174 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_kerne
     }
 }
 
-// AHEAD: the next row's loads are under way while a row is worked on; otherwise more CTAs share the SM (loads of single elements, which a thread has many of,
-// wait for one another).  gamma and the thread's column sums lie in shared memory, [quad][thread], a private float4 each.
-template <typename T, int V, int E, int G, bool AHEAD>
-__global__ void __launch_bounds__(kThreadsOf<G>, (AHEAD || E == 16 ? 512 : 1024) / kThreadsOf<G>) norm_grad_kernel(NormParams p) {
-    constexpr int TH = kThreadsOf<G>, N = E / V, Q = E / 4;
+// A row's columns of this thread in shared memory, fetched by asynchronous copies that only this thread waits for: [word][thread], so that the threads of a
+// warp read neighbouring words.
+template <typename T, int V, int E, int TH>
+struct Slot {
+    using Word = typename Raw<T, V, E>::Word;
+    static constexpr int N = E / V, BYTES = N * TH * (int)sizeof(Word);
+    __device__ static __forceinline__ void clear(char* at) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) reinterpret_cast<Word*>(at)[i * TH + threadIdx.x] = Word{};
+    }
+    __device__ static __forceinline__ void fetch(char* at, const T* row, int first, int step, int cols) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t to = smem_u32(reinterpret_cast<Word*>(at) + i * TH + threadIdx.x);
+            if (first + i * step >= cols) continue;
+            if constexpr (sizeof(Word) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + first + i * step) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(row + first + i * step) : "memory");
+        }
+    }
+    __device__ static __forceinline__ void read(const char* at, Raw<T, V, E>& x) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x.w[i] = reinterpret_cast<const Word*>(at)[i * TH + threadIdx.x];
+    }
+};
+
+// AHEAD rows of a group are under way while one is worked on, 150 KB an SM at three (a row's worth of registers would be half of that and too little at
+// the latency of a busy memory).  0: single bf16 numbers, which asynchronous copies cannot fetch; they are loaded when they are needed.
+template <typename T, int V, int E, int G, int AHEAD>
+__global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_kernel(NormParams p) {
+    constexpr int TH = kThreadsOf<G>, N = E / V, RING = AHEAD + 1;
+    using S = Slot<T, V, E, TH>;
     __shared__ float2 buf[2][32];
-    extern __shared__ float4 quads[];        // gamma[Q][TH], dgamma[Q][TH], dbeta[Q][TH]
-    float4 *gm4 = quads + threadIdx.x, *dg4 = gm4 + Q * TH, *db4 = dg4 + Q * TH;
+    extern __shared__ __align__(16) char ring[];     // [RING][x, dout, residual]; at the end the column sums
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
     const int l = threadIdx.x % G, groups = TH / G;
     const int cols = (int)p.cols, first = l * V, step = G * V;
     const float inv = 1.0f / (float)cols;
+    float gm[E], dg[E], db[E];
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        float g[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int j = q * 4 + e, c = first + j / V * step + j % V;
-            g[e] = c < cols ? (p.gamma ? p.gamma[c] : 1.0f) : 0.0f;
-        }
-        gm4[q * TH] = make_float4(g[0], g[1], g[2], g[3]);
-        dg4[q * TH] = db4[q * TH] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int j = 0; j < E; ++j) {
+        const int c = first + j / V * step + j % V;
+        gm[j] = c < cols ? (p.gamma ? p.gamma[c] : 1.0f) : 0.0f;
+        dg[j] = db[j] = 0.0f;
     }
-    Raw<T, V, E> x, d, res;
-    // the lanes of a warp keep step: rows past the end are looked at as the last one and not written
-    const auto fetch = [&](int64_t r0) {
-        const int64_t row = min(r0 + threadIdx.x / G, live - 1);
-        x.fetch(static_cast<const T*>(p.x.data) + row * p.x.stride, first, step, cols);
-        d.fetch(static_cast<const T*>(p.dout.data) + row * p.dout.stride, first, step, cols);
-        if (p.residual.data) res.fetch(static_cast<const T*>(p.residual.data) + row * p.residual.stride, first, step, cols);
-    };
     const int64_t jump = (int64_t)gridDim.x * groups;
-    int64_t r0 = (int64_t)blockIdx.x * groups;
-    if (AHEAD && r0 < live) fetch(r0);
-    for (; r0 < live; r0 += jump) {
-        const int64_t row = r0 + threadIdx.x / G;
-        const bool on = row < live;
-        if (!AHEAD) fetch(r0);
+    // the lanes of a warp keep step: rows past the end are looked at as the last one and not written
+    const int64_t mine = (int64_t)blockIdx.x * groups + threadIdx.x / G;
+    Raw<T, V, E> x, d, res;
+    const auto fetch = [&](int64_t r, int slot) {
+        const int64_t row = min(r, live - 1);
+        const T *px = static_cast<const T*>(p.x.data) + row * p.x.stride, *pd = static_cast<const T*>(p.dout.data) + row * p.dout.stride;
+        const T* pr = p.residual.data ? static_cast<const T*>(p.residual.data) + row * p.residual.stride : nullptr;
+        if constexpr (AHEAD > 0) {
+            char* at = ring + slot * 3 * S::BYTES;
+            S::fetch(at, px, first, step, cols);
+            S::fetch(at + S::BYTES, pd, first, step, cols);
+            if (pr) S::fetch(at + 2 * S::BYTES, pr, first, step, cols);
+        } else {
+            x.fetch(px, first, step, cols);
+            d.fetch(pd, first, step, cols);
+            if (pr) res.fetch(pr, first, step, cols);
+        }
+    };
+    // a group goes on while the first of its warp's rows does
+    const int64_t lead = G >= 32 ? mine : (int64_t)blockIdx.x * groups + (threadIdx.x & ~31) / G;
+    int slot = 0;
+    if constexpr (AHEAD > 0) {
+#pragma unroll
+        for (int a = 0; a < RING; ++a)
+#pragma unroll
+            for (int o = 0; o < 3; ++o) S::clear(ring + (3 * a + o) * S::BYTES);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (lead + a * jump < live) fetch(mine + a * jump, a);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    }
+    for (int64_t r = 0; lead + r < live; r += jump) {
+        const int64_t row = mine + r;
+        const bool on = G >= 32 || row < live;
+        if constexpr (AHEAD > 0) {
+            if (lead + r + AHEAD * jump < live) fetch(row + AHEAD * jump, slot >= 1 ? slot - 1 : AHEAD);
+            asm volatile("cp.async.commit_group;\n\tcp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+            const char* at = ring + slot * 3 * S::BYTES;
+            S::read(at, x);
+            S::read(at + S::BYTES, d);
+            if (p.residual.data) S::read(at + 2 * S::BYTES, res);
+            slot = slot == AHEAD ? 0 : slot + 1;
+        } else {
+            fetch(row, 0);
+        }
         float v[E], u[E];
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const bool has = first + i * step < cols;
             x.values(i, v + i * V);
             d.values(i, u + i * V);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                v[i * V + e] = has ? v[i * V + e] : 0.0f;
-                u[i * V + e] = has ? u[i * V + e] : 0.0f;
+            if constexpr (AHEAD == 0) {
+                const bool has = first + i * step < cols;
+                v[i] = has ? v[i] : 0.0f;
+                u[i] = has ? u[i] : 0.0f;
             }
         }
-        const Raw<T, V, E> add = res;
-        if (AHEAD && r0 + jump < live) fetch(r0 + jump);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const float4 g = gm4[q * TH];
-            s.x += (v[4 * q] + v[4 * q + 1]) + (v[4 * q + 2] + v[4 * q + 3]);
-            s.y = fmaf(u[4 * q], g.x, s.y);
-            s.y = fmaf(u[4 * q + 1], g.y, s.y);
-            s.y = fmaf(u[4 * q + 2], g.z, s.y);
-            s.y = fmaf(u[4 * q + 3], g.w, s.y);
+        for (int j = 0; j < E; ++j) {
+            s.x += v[j];
+            s.y = fmaf(u[j], gm[j], s.y);
         }
         s = group_sum<G>(s, buf[0]);
         const float mean = __fdiv_rn(s.x, (float)cols), mg = s.y * inv;
         s = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const float4 g4 = gm4[q * TH];
-            const float g[4] = {g4.x, g4.y, g4.z, g4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = 4 * q + e;
-                v[j] = first + j / V * step < cols ? v[j] - mean : 0.0f;
-                s.x = fmaf(v[j], v[j], s.x);
-                s.y = fmaf(v[j], u[j] * g[e], s.y);
-            }
+        for (int j = 0; j < E; ++j) {
+            v[j] = first + j / V * step < cols ? v[j] - mean : 0.0f;
+            s.x = fmaf(v[j], v[j], s.x);
+            s.y = fmaf(v[j], u[j] * gm[j], s.y);
         }
         s = group_sum<G>(s, buf[1]);
-        const float r = 1.0f / sqrtf(s.x * inv + p.eps), k = s.y * inv * r;
+        const float rs = 1.0f / sqrtf(s.x * inv + p.eps), k = s.y * inv * rs;
         T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
-        float y[E];
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const float4 g4 = gm4[q * TH];
-            const float g[4] = {g4.x, g4.y, g4.z, g4.w};
-            float h[4], w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = 4 * q + e;
-                h[e] = v[j] * r;
-                w[e] = on ? u[j] : 0.0f;
-                y[j] = r * (fmaf(u[j], g[e], -mg) - h[e] * k);
-            }
-            float4 a = dg4[q * TH], b = db4[q * TH];
-            a.x = fmaf(w[0], h[0], a.x), a.y = fmaf(w[1], h[1], a.y), a.z = fmaf(w[2], h[2], a.z), a.w = fmaf(w[3], h[3], a.w);
-            b.x += w[0], b.y += w[1], b.z += w[2], b.w += w[3];
-            dg4[q * TH] = a;
-            db4[q * TH] = b;
-        }
-        if (!on) continue;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = first + i * step;
-            if (c >= cols) continue;
-            if (p.residual.data) {
-                float z[V];
-                add.values(i, z);
+            float y[V];
+            if (p.residual.data) res.values(i, y);
 #pragma unroll
-                for (int e = 0; e < V; ++e) y[i * V + e] += z[e];
+            for (int e = 0; e < V; ++e) {
+                const int j = i * V + e;
+                const float h = v[j] * rs, w = on ? u[j] : 0.0f;
+                dg[j] = fmaf(w, h, dg[j]);
+                db[j] += w;
+                const float z = rs * (fmaf(u[j], gm[j], -mg) - h * k);
+                y[e] = p.residual.data ? z + y[e] : z;
             }
-            store_elems<T, V>(out + c, y + i * V);
+            if (c < cols && on) store_elems<T, V>(out + c, y);
         }
     }
     if (!p.parts) return;
-    __syncthreads();
     float* to = p.parts + (int64_t)blockIdx.x * 2 * cols;
-    const float *dg = reinterpret_cast<const float*>(quads + Q * TH), *db = dg + 4 * Q * TH;
-    for (int c = threadIdx.x; c < cols; c += TH) {
-        const int j = c / step * V + c % V, owner = c % step / V;      // element j of the group's thread `owner`
-        float a = 0.0f, b = 0.0f;
-        for (int w = 0; w < groups; ++w) {                             // one group after the other
-            const int at = ((j >> 2) * TH + w * G + owner) * 4 + (j & 3);
-            a += dg[at];
-            b += db[at];
+    if constexpr (TH == G) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int c = first + j / V * step + j % V;
+            if (c < cols) {
+                to[c] = dg[j];
+                to[cols + c] = db[j];
+            }
         }
-        to[c] = a;
-        to[cols + c] = b;
+    } else {
+        // [group][2][columns]: a CTA's groups one after the other
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        float* sums = reinterpret_cast<float*>(ring) + (threadIdx.x / G) * 2 * G * E;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const int c = first + j / V * step + j % V;
+            sums[c] = dg[j];
+            sums[G * E + c] = db[j];
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * cols; c += TH) {
+            const int at = c < cols ? c : G * E + c - cols;
+            float t = 0.0f;
+            for (int w = 0; w < groups; ++w) t += reinterpret_cast<const float*>(ring)[w * 2 * G * E + at];
+            to[c] = t;
+        }
     }
 }
 
@@ -262,98 +302,131 @@ __global__ void __launch_bounds__(kThreadsOf<G>, (AHEAD || E == 16 ? 512 : 1024)
 
 constexpr int kSweep = 512;
 
-template <typename T>
+// f(first column, its V values) over a row by the CTA.
+template <typename T, int V, typename F>
+__device__ __forceinline__ void sweep(const T* row, int64_t cols, F f) {
+#pragma unroll 4
+    for (int64_t c = threadIdx.x * V; c < cols; c += kSweep * V) {
+        float x[V];
+        load_elems<T, V>(row + c, x);
+        f(c, x);
+    }
+}
+
+// Mean and 1 / sqrt(var + eps) of a row.
+template <typename T, int V>
+__device__ __forceinline__ float2 row_stats(const NormParams& p, const T* x, float2 (*buf)[32]) {
+    float2 s = make_float2(0.0f, 0.0f);
+    sweep<T, V>(x, p.cols, [&](int64_t, const float* v) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) s.x += v[e];
+    });
+    const float mean = __fdiv_rn(group_sum<kSweep>(s, buf[0]).x, (float)p.cols);
+    s = make_float2(0.0f, 0.0f);
+    sweep<T, V>(x, p.cols, [&](int64_t, const float* v) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) s.x = fmaf(v[e] - mean, v[e] - mean, s.x);
+    });
+    return make_float2(mean, 1.0f / sqrtf(group_sum<kSweep>(s, buf[1]).x / (float)p.cols + p.eps));
+}
+
+template <typename T, int V>
 __global__ void __launch_bounds__(kSweep) norm_sweep_kernel(NormParams p) {
     __shared__ float2 buf[2][32];
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
-    const float inv = 1.0f / (float)p.cols;
     for (int64_t row = blockIdx.x; row < live; row += gridDim.x) {
         const T* x = static_cast<const T*>(p.x.data) + row * p.x.stride;
-        float2 s = make_float2(0.0f, 0.0f);
-        for (int64_t c = threadIdx.x; c < p.cols; c += kSweep) s.x += load1(x + c);
-        const float mean = __fdiv_rn(group_sum<kSweep>(s, buf[0]).x, (float)p.cols);
-        s = make_float2(0.0f, 0.0f);
-        for (int64_t c = threadIdx.x; c < p.cols; c += kSweep) {
-            const float d = load1(x + c) - mean;
-            s.x = fmaf(d, d, s.x);
-        }
-        const float r = 1.0f / sqrtf(group_sum<kSweep>(s, buf[1]).x * inv + p.eps);
         T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
-        for (int64_t c = threadIdx.x; c < p.cols; c += kSweep)
-            store1(out + c, fmaf((load1(x + c) - mean) * r, p.gamma ? p.gamma[c] : 1.0f, p.beta ? p.beta[c] : 0.0f));
+        const float2 st = row_stats<T, V>(p, x, buf);
+        sweep<T, V>(x, p.cols, [&](int64_t c, float* v) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = fmaf((v[e] - st.x) * st.y, p.gamma ? p.gamma[c + e] : 1.0f, p.beta ? p.beta[c + e] : 0.0f);
+            store_elems<T, V>(out + c, v);
+        });
     }
 }
 
 // Sums of dout h and dout over runs of rows, before the rows' own kernel may overwrite x or dout.  stats: mean and r of each row.
-template <typename T>
-__global__ void __launch_bounds__(256) norm_columns_kernel(NormParams p) {
+template <typename T, int V>
+__global__ void __launch_bounds__(128) norm_columns_kernel(NormParams p) {
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, false);
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t c = ((int64_t)blockIdx.x * 128 + threadIdx.x) * V;
     if (c >= p.cols) return;
     const int64_t run = (p.live.rows + kSweepParts - 1) / kSweepParts, r0 = run * blockIdx.y, r1 = min(live, r0 + run);
-    float a = 0.0f, b = 0.0f;
+    float a[V] = {}, b[V] = {};
+#pragma unroll 4
     for (int64_t row = r0; row < r1; ++row) {
         const float2 st = p.stats[row];
-        const float d = load1(static_cast<const T*>(p.dout.data) + row * p.dout.stride + c);
-        a = fmaf(d, (load1(static_cast<const T*>(p.x.data) + row * p.x.stride + c) - st.x) * st.y, a);
-        b += d;
+        float d[V], x[V];
+        load_elems<T, V>(static_cast<const T*>(p.dout.data) + row * p.dout.stride + c, d);
+        load_elems<T, V>(static_cast<const T*>(p.x.data) + row * p.x.stride + c, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            a[e] = fmaf(d[e], (x[e] - st.x) * st.y, a[e]);
+            b[e] += d[e];
+        }
     }
     float* to = p.parts + (int64_t)blockIdx.y * 2 * p.cols;
-    to[c] = a;
-    to[p.cols + c] = b;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        to[c + e] = a[e];
+        to[p.cols + c + e] = b[e];
+    }
 }
 
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(kSweep) norm_stats_kernel(NormParams p) {
     __shared__ float2 buf[2][32];
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
-    const float inv = 1.0f / (float)p.cols;
     for (int64_t row = blockIdx.x; row < live; row += gridDim.x) {
-        const T* x = static_cast<const T*>(p.x.data) + row * p.x.stride;
-        float2 s = make_float2(0.0f, 0.0f);
-        for (int64_t c = threadIdx.x; c < p.cols; c += kSweep) s.x += load1(x + c);
-        const float mean = __fdiv_rn(group_sum<kSweep>(s, buf[0]).x, (float)p.cols);
-        s = make_float2(0.0f, 0.0f);
-        for (int64_t c = threadIdx.x; c < p.cols; c += kSweep) {
-            const float d = load1(x + c) - mean;
-            s.x = fmaf(d, d, s.x);
-        }
-        const float r = 1.0f / sqrtf(group_sum<kSweep>(s, buf[1]).x * inv + p.eps);
-        if (threadIdx.x == 0) p.stats[row] = make_float2(mean, r);
+        const float2 st = row_stats<T, V>(p, static_cast<const T*>(p.x.data) + row * p.x.stride, buf);
+        if (threadIdx.x == 0) p.stats[row] = st;
     }
 }
 
-template <typename T>
+template <typename T, int V>
 __global__ void __launch_bounds__(kSweep) norm_grad_sweep_kernel(NormParams p) {
-    __shared__ float2 buf[2][32];
+    __shared__ float2 buf[32];
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, false);
     const float inv = 1.0f / (float)p.cols;
     for (int64_t row = blockIdx.x; row < live; row += gridDim.x) {
         const T *x = static_cast<const T*>(p.x.data) + row * p.x.stride, *d = static_cast<const T*>(p.dout.data) + row * p.dout.stride;
+        const T* res = p.residual.data ? static_cast<const T*>(p.residual.data) + row * p.residual.stride : nullptr;
+        T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
         const float2 st = p.stats[row];
         float2 s = make_float2(0.0f, 0.0f);
-        for (int64_t c = threadIdx.x; c < p.cols; c += kSweep) {
-            const float g = load1(d + c) * (p.gamma ? p.gamma[c] : 1.0f);
-            s.x += g;
-            s.y = fmaf(g, load1(x + c) - st.x, s.y);
-        }
-        s = group_sum<kSweep>(s, buf[0]);
+        sweep<T, V>(d, p.cols, [&](int64_t c, const float* u) {
+            float v[V];
+            load_elems<T, V>(x + c, v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float g = u[e] * (p.gamma ? p.gamma[c + e] : 1.0f);
+                s.x += g;
+                s.y = fmaf(g, v[e] - st.x, s.y);
+            }
+        });
+        s = group_sum<kSweep>(s, buf);
         const float mg = s.x * inv, k = s.y * inv * st.y;
-        T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
-        for (int64_t c = threadIdx.x; c < p.cols; c += kSweep) {
-            float y = st.y * (load1(d + c) * (p.gamma ? p.gamma[c] : 1.0f) - mg - (load1(x + c) - st.x) * st.y * k);
-            if (p.residual.data) y += load1(static_cast<const T*>(p.residual.data) + row * p.residual.stride + c);
-            store1(out + c, y);
-        }
-        __syncthreads();                     // buf[0] is read by all before the next row writes it
+        sweep<T, V>(d, p.cols, [&](int64_t c, const float* u) {
+            float v[V], y[V];
+            load_elems<T, V>(x + c, v);
+            if (res) load_elems<T, V>(res + c, y);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float z = st.y * (u[e] * (p.gamma ? p.gamma[c + e] : 1.0f) - mg - (v[e] - st.x) * st.y * k);
+                y[e] = res ? z + y[e] : z;
+            }
+            store_elems<T, V>(out + c, y);
+        });
+        __syncthreads();                     // buf is read by all before the next row writes it
     }
 }
 
@@ -384,8 +457,11 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, int 
 template <typename T, int V, int E, int G>
 aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
     constexpr int TH = kThreadsOf<G>, groups = TH / G;
-    const void* kernel = grad ? (const void*)norm_grad_kernel<T, V, E, G, (V > 1)> : (const void*)norm_kernel<T, V, E, G>;
-    const size_t smem = grad ? 3 * sizeof(float) * E * TH : 0;
+    // as many rows ahead as an SM's shared memory holds
+    constexpr int AHEAD = V == 1 && sizeof(T) == 2 ? 0 : (E * sizeof(T) <= 32 ? 3 : 1);
+    const void* kernel = grad ? (const void*)norm_grad_kernel<T, V, E, G, AHEAD> : (const void*)norm_kernel<T, V, E, G>;
+    const size_t sums = TH == G ? 0 : 2 * sizeof(float) * E * TH, slots = AHEAD ? (AHEAD + 1) * 3 * (size_t)Slot<T, V, E, TH>::BYTES : 0;
+    const size_t smem = !grad ? 0 : (sums > slots ? sums : slots);
     if (smem && allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     int ctas = resident_ctas(c, kernel, TH, smem);
     if (ctas < 1) return AA_ERR_CUDA;
@@ -399,43 +475,53 @@ aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
     return AA_OK;
 }
 
-// The smallest group whose threads have 8 columns each at most (narrow rows of packed bf16: 16, which are two words).
+// The smallest group whose threads have 16 columns of packed bf16 each, or 8 others (more where no group is that wide).
 template <typename T, int V>
 aa_status launch_width(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
     if constexpr (V == 8) {
         if (p.cols <= 128) return launch_rows<T, V, 16, 8>(c, p, grad, n);
         if (p.cols <= 256) return launch_rows<T, V, 16, 16>(c, p, grad, n);
         if (p.cols <= 512) return launch_rows<T, V, 16, 32>(c, p, grad, n);
+        if (p.cols <= 1024) return launch_rows<T, V, 16, 64>(c, p, grad, n);
+        if (p.cols <= 2048) return launch_rows<T, V, 16, 128>(c, p, grad, n);
+        if (p.cols <= 4096) return launch_rows<T, V, 16, 256>(c, p, grad, n);
+        return launch_rows<T, V, 16, 512>(c, p, grad, n);
     } else {
         if (p.cols <= 128) return launch_rows<T, V, 8, 16>(c, p, grad, n);
         if (p.cols <= 256) return launch_rows<T, V, 8, 32>(c, p, grad, n);
         if (p.cols <= 512) return launch_rows<T, V, 8, 64>(c, p, grad, n);
+        if (p.cols <= 1024) return launch_rows<T, V, 8, 128>(c, p, grad, n);
+        if (p.cols <= 2048) return launch_rows<T, V, 8, 256>(c, p, grad, n);
+        if (p.cols <= 4096) return launch_rows<T, V, 8, 512>(c, p, grad, n);
+        if constexpr (sizeof(T) == 4)
+            if (p.cols <= 6144) return launch_rows<T, V, 12, 512>(c, p, grad, n);
+        return launch_rows<T, V, 16, 512>(c, p, grad, n);
     }
-    if (p.cols <= 1024) return launch_rows<T, V, 8, 128>(c, p, grad, n);
-    if (p.cols <= 2048) return launch_rows<T, V, 8, 256>(c, p, grad, n);
-    if (p.cols <= 4096) return launch_rows<T, V, 8, 512>(c, p, grad, n);
-    if constexpr (V != 8)
-        if (p.cols <= 6144) return launch_rows<T, V, 12, 512>(c, p, grad, n);
-    return launch_rows<T, V, 16, 512>(c, p, grad, n);
 }
 
-template <typename T>
+
+template <typename T, int V>
 aa_status launch_sweeps(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
-    const int grid = (int)(p.live.rows < 2 * c->sm_count ? p.live.rows : 2 * c->sm_count);
+    const int grid = (int)(p.live.rows < 4 * c->sm_count ? p.live.rows : 4 * c->sm_count);
     void* args[] = {&p};
-    const void* first = grad ? (const void*)norm_stats_kernel<T> : (const void*)norm_sweep_kernel<T>;
+    const void* first = grad ? (const void*)norm_stats_kernel<T, V> : (const void*)norm_sweep_kernel<T, V>;
     if (launch_overlapped(c, first, dim3(grid), dim3(kSweep), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     if (!grad) return AA_OK;
     if (p.parts) {
-        if (launch_overlapped(c, (const void*)norm_columns_kernel<T>, dim3((unsigned)((p.cols + 255) / 256), kSweepParts), dim3(256), args, 0, false) != cudaSuccess)
+        if (launch_overlapped(c, (const void*)norm_columns_kernel<T, V>, dim3((unsigned)((p.cols + 128 * V - 1) / (128 * V)), kSweepParts), dim3(128), args, 0, false) != cudaSuccess)
             return AA_ERR_CUDA;
         ++c->launches;
     }
-    if (launch_overlapped(c, (const void*)norm_grad_sweep_kernel<T>, dim3(grid), dim3(kSweep), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+    if (launch_overlapped(c, (const void*)norm_grad_sweep_kernel<T, V>, dim3(grid), dim3(kSweep), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     *n_parts = kSweepParts;
     return AA_OK;
+}
+
+template <typename T, int V>
+aa_status launch_norm(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
+    return p.cols > kNormInRegisters ? launch_sweeps<T, V>(c, p, grad, n) : launch_width<T, V>(c, p, grad, n);
 }
 
 }  // namespace
@@ -451,9 +537,8 @@ aa_status launch_layer_norm(aa_ctx_impl* c, const NormParams& p, int dtype, bool
     const bool vec = p.cols % wide == 0 && aligned(p.x) && aligned(p.out) && aligned(p.dout) && aligned(p.residual);
     int n_parts = 0;
     aa_status st;
-    if (p.cols > kNormInRegisters) st = dtype == AA_BF16 ? launch_sweeps<uint16_t>(c, p, grad, &n_parts) : launch_sweeps<float>(c, p, grad, &n_parts);
-    else if (dtype == AA_BF16) st = vec ? launch_width<uint16_t, 8>(c, p, grad, &n_parts) : launch_width<uint16_t, 1>(c, p, grad, &n_parts);
-    else st = vec ? launch_width<float, 4>(c, p, grad, &n_parts) : launch_width<float, 1>(c, p, grad, &n_parts);
+    if (dtype == AA_BF16) st = vec ? launch_norm<uint16_t, 8>(c, p, grad, &n_parts) : launch_norm<uint16_t, 1>(c, p, grad, &n_parts);
+    else st = vec ? launch_norm<float, 4>(c, p, grad, &n_parts) : launch_norm<float, 1>(c, p, grad, &n_parts);
     if (st != AA_OK || !grad || !p.parts) return st;
     float* parts = p.parts;
     int64_t cols = p.cols;
