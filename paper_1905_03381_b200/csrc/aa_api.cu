@@ -148,6 +148,23 @@ cudaError_t launch_overlapped(aa_ctx_impl* c, const void* kernel, dim3 grid, dim
     return cudaLaunchKernelExC(&cfg, kernel, args);
 }
 
+cudaError_t launch_clusters(aa_ctx_impl* c, const void* kernel, unsigned grid, unsigned threads, void** args, size_t smem, int cluster) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = c->stream;
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = (unsigned)cluster;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelExC(&cfg, kernel, args);
+}
+
 namespace {
 
 bool valid_mix(float mix) { return mix >= 0.0f && mix <= 1.0f; }

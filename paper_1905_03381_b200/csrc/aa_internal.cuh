@@ -290,6 +290,9 @@ aa_status launch_assistant_step_csr(aa_ctx_impl* c, const CsrFeat& f, const int3
 // cooperative = the CTAs wait for one another (the grid must be resident at once).
 cudaError_t launch_overlapped(aa_ctx_impl* c, const void* kernel, dim3 grid, dim3 block, void** args, size_t smem, bool cooperative);
 
+// launch_overlapped for a kernel of clusters of `cluster` CTAs (1: none).
+cudaError_t launch_clusters(aa_ctx_impl* c, const void* kernel, unsigned grid, unsigned threads, void** args, size_t smem, int cluster);
+
 // Convolution + rectifier + average pooling of every stored image row (the convolutional Assistant's feature map).
 aa_status launch_conv_pool_features(aa_ctx_impl* c, const void* x, int dtype, int64_t n, int64_t row_stride, const aa_conv& cv,
                                     float* phi, int64_t phi_stride);

@@ -1,6 +1,7 @@
 // Tiles of the tensor-core products: in which order a launch takes them, and which it cuts along the contraction so that the last round of SMs is full.
 #pragma once
 
+#include "async_copy.cuh"
 #include "linear.cuh"
 
 namespace aa {
@@ -12,14 +13,22 @@ struct Plan {
     int nt, whole, splits;
     float* parts;                        // [part][rows of a tile][columns of a tile]
     float* sum_parts;                    // [part][rows of a tile]
+    int cluster;                         // above 1: the parts of a tile are the CTAs of a cluster, which join them themselves (no scratch memory)
 };
 
 // Splits of the tiles that do not fill a round of `teams`: the fewest slices one after the other, counting the parts' way through memory.
 // slice_us: what a slice of a tile takes.
-inline Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats, int tile_rows, double slice_us) {
-    Plan plan{nt, (int)tiles, 1, p.parts, nullptr};
+inline Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats, int tile_rows, double slice_us, bool may_cluster) {
+    Plan plan{nt, (int)tiles, 1, p.parts, nullptr, 1};
     const int64_t slices = (p.k + kSlice - 1) / kSlice, whole = tiles / teams * teams, tail = tiles - whole;
-    if (!p.parts || tail == 0) return plan;
+    if (!p.parts) {
+        // few tiles and no scratch memory: as many CTAs on each as the SMs give, with four slices or more apiece
+        int c = 8;
+        while (c > 1 && (tiles * c > teams || slices < 4 * c)) c /= 2;
+        if (may_cluster && c > 1) plan.whole = 0, plan.splits = plan.cluster = c;
+        return plan;
+    }
+    if (tail == 0) return plan;
     double best = (double)slices;
     for (int s = 2; s <= 16 && slices / s >= 4; ++s) {
         const int64_t parts = tail * s;
@@ -37,6 +46,24 @@ inline Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, 
 }
 
 #ifdef __CUDACC__
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same place in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t of_rank(const void* shared, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(shared)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ void store_remote(uint32_t at, float4 x) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
+}
 
 struct Unit {
     int m, n, s0, s1, part;              // slices [s0, s1); part < 0: the whole tile
@@ -66,6 +93,58 @@ __device__ __forceinline__ Unit unit_at(const Plan& p, int mt, int slices, int i
         u.part = j;
     }
     return u;
+}
+
+// Bias, pre, activation, residual and the rounding of four neighbouring columns (cols of them count; vec: pointers allow vectors).
+template <typename T>
+__device__ __forceinline__ void finish_quad(const ProductParams& p, float (&z)[4], int64_t row, int64_t col, int cols, bool vec) {
+    T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride + col;
+    T* pre = p.pre.data ? static_cast<T*>(const_cast<void*>(p.pre.data)) + row * p.pre.stride + col : nullptr;
+    const T* res = p.residual.data ? static_cast<const T*>(p.residual.data) + row * p.residual.stride + col : nullptr;
+    if (p.bias) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] += e < cols ? p.bias[col + e] : 0.0f;
+    }
+    if (vec && cols == 4) {
+        if (pre) store_quad(pre, z);
+        activate_all(z, p.act);
+        if (res) {
+            float y[4];
+            load_quad(res, y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] += y[e];
+        }
+        store_quad(out, z);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (pre && e < cols) store1(pre + e, z[e]);
+        activate_all(z, p.act);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < cols) store1(out + e, res ? z[e] + load1(res + e) : z[e]);
+    }
+}
+
+// The CTAs of a cluster have the parts of a tile of 128 rows in [CTA][128 / cluster rows][BN] of everybody's `parts` (shared memory): this CTA finishes its rows.
+// `threads` threads from `tid` on; after a cluster barrier.
+template <typename T, int BN>
+__device__ __forceinline__ void finish_cluster(const ProductParams& p, const Plan& plan, const Unit& u, const float* parts, int64_t m_end, bool vec, int tid, int threads) {
+    const int rows = 128 / plan.cluster, rank = (int)cluster_rank();
+    for (int i = tid; i < rows * (BN / 4); i += threads) {
+        const int r = i / (BN / 4), c = (i - r * (BN / 4)) * 4;
+        const int64_t row = (int64_t)u.m * 128 + rank * rows + r, col = (int64_t)u.n * BN + c;
+        if (row >= m_end || col >= p.n) continue;
+        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < plan.cluster; ++s) {
+            const float4 f = *reinterpret_cast<const float4*>(parts + ((int64_t)s * rows + r) * BN + c);
+            z[0] += f.x;
+            z[1] += f.y;
+            z[2] += f.z;
+            z[3] += f.w;
+        }
+        finish_quad<T>(p, z, row, col, (int)min((int64_t)4, p.n - col), vec);
+    }
 }
 
 // Adds the parts of the cut tiles up in order and finishes them.  A thread takes four columns of a row.

@@ -10,6 +10,8 @@
 // A persistent CTA takes 128 x 128 tiles.  Eight warps fetch 64-wide slices with ordinary loads a slice ahead, take them apart and store the terms in the
 // layout that TMA would have left (128-byte swizzle); elements out of range are zeros, so strides, alignment and counted rows need nothing
 // else.  The first of them issues the products as soon as all have stored a slice, eight other warps add the runs up and finish a tile, as in the kernel for bf16.
+#include <type_traits>
+
 #include "linear_plan.cuh"
 #include "tensor_core.cuh"
 
@@ -42,43 +44,66 @@ struct Box {
     int64_t stride, rows, cols;
 };
 
-// The 16 numbers a lane fetches of a batch of 8 rows of 64 elements.  VEC (16-byte aligned base and rows, columns in eights): lane l takes elements 8 (l % 8) .. + 7 of
-// rows l / 8 and l / 8 + 4, of a stand-in where they do not count (there is a row and a column at least; `in` says which numbers count); otherwise
-// elements 2 l and 2 l + 1 of every row, zeros where they do not count.
+// The 16 numbers a lane fetches of a batch of 8 rows of 64 elements, as they lie in memory.  VEC (16-byte aligned base and rows, columns in eights): lane l takes elements
+// 8 (l % 8) .. + 7 of rows l / 8 and l / 8 + 4, otherwise elements 2 l and 2 l + 1 of every row.  The loads are straight code, of a stand-in where the
+// element does not count (there is a row and a column at least), and nothing touches what they bring before it is stored, so that they
+// stay under way; `in` says which numbers count.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_batch(const Box& b, int64_t row0, int64_t col0, float (&x)[16], uint32_t& in) {
-    const int lane = threadIdx.x & 31;
-    if (VEC) {
-        asm volatile("" : "+l"(row0));   // the addresses are worked out here, not held in registers from slice to slice
-        const int64_t col = col0 + (lane & 7) * 8;
-        const bool c = col < b.cols;
+struct Batch {
+    using Word = typename std::conditional<VEC, uint4, T>::type;
+    static constexpr int N = VEC ? 16 * (int)sizeof(T) / 16 : 16;
+    Word w[N];
+    uint32_t in;
+
+    __device__ __forceinline__ void load(const Box& b, int64_t row0, int64_t col0) {
+        const int lane = threadIdx.x & 31;
+        asm volatile("" : "+l"(row0));       // the addresses are worked out here, not held in registers from slice to slice
         in = 0;
+        if constexpr (VEC) {
+            const int64_t col = col0 + (lane & 7) * 8;
+            const bool c = col < b.cols;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t row = row0 + (lane >> 3) + 4 * h;
-            const T* at = static_cast<const T*>(b.data) + min(row, b.rows - 1) * b.stride + (c ? col : 0);
+            for (int h = 0; h < 2; ++h) {
+                const int64_t row = row0 + (lane >> 3) + 4 * h;
+                const T* at = static_cast<const T*>(b.data) + min(row, b.rows - 1) * b.stride + (c ? col : 0);
 #pragma unroll
-            for (int e = 0; e < 8; e += 16 / (int)sizeof(T)) load_elems<T, 16 / (int)sizeof(T)>(at + e, x + 8 * h + e);
-            if (c && row < b.rows) in |= 0xFFu << (8 * h);
-        }
-    } else {
-        const int64_t col = col0 + 2 * lane;
-        in = 0;
+                for (int e = 0; e < N / 2; ++e) w[h * (N / 2) + e] = reinterpret_cast<const uint4*>(at)[e];
+                if (c && row < b.rows) in |= 0xFFu << (8 * h);
+            }
+        } else {
+            const int64_t col = col0 + 2 * lane;
+            const int64_t c0 = min(col, b.cols - 1), c1 = min(col + 1, b.cols - 1);
+            const uint32_t two = (col < b.cols ? 1u : 0u) | (col + 1 < b.cols ? 2u : 0u);
+            const T* base = static_cast<const T*>(b.data);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const T* at = static_cast<const T*>(b.data) + (row0 + r) * b.stride + col;
-            const bool row = row0 + r < b.rows, one = row && col < b.cols, two = row && col + 1 < b.cols;
-            x[2 * r] = one ? load1(at) : 0.0f;
-            x[2 * r + 1] = two ? load1(at + 1) : 0.0f;
+            for (int r = 0; r < 8; ++r) {
+                const int64_t at = min(row0 + r, b.rows - 1) * b.stride;
+                w[2 * r] = base[at + c0];
+                w[2 * r + 1] = base[at + c1];
+                if (row0 + r < b.rows) in |= two << (2 * r);
+            }
         }
     }
-}
+    __device__ __forceinline__ void values(float (&x)[16]) const {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if constexpr (VEC && sizeof(T) == 4) x[e] = __uint_as_float((&w[e / 4].x)[e % 4]);
+            else if constexpr (VEC) x[e] = e % 2 ? bf16_hi((&w[e / 8].x)[e / 2 % 4]) : bf16_lo((&w[e / 8].x)[e / 2 % 4]);
+            else if constexpr (sizeof(T) == 4) x[e] = w[e];
+            else x[e] = __uint_as_float((uint32_t)w[e] << 16);
+        }
+        if (!__all_sync(0xFFFFFFFFu, in == 0xFFFFu)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = (in >> e) & 1u ? x[e] : 0.0f;
+        }
+    }
+};
 
 // Two numbers' terms, packed.
 template <int TERMS>
 __device__ __forceinline__ void take_apart(float a, float b, uint32_t (&t)[TERMS]) {
     t[0] = pack_bf16(a, b);
-    if (TERMS == 3) {
+    if constexpr (TERMS == 3) {
         a -= bf16_lo(t[0]);
         b -= bf16_hi(t[0]);
         t[1] = pack_bf16(a, b);
@@ -90,12 +115,8 @@ __device__ __forceinline__ void take_apart(float a, float b, uint32_t (&t)[TERMS
 
 // The batch into rows r0 .. r0 + 7 of a [rows x 128 bytes] swizzled block; r0 a multiple of 8.
 template <int TERMS, bool VEC>
-__device__ __forceinline__ void store_batch(unsigned char* block, int r0, float (&x)[16], uint32_t in) {
+__device__ __forceinline__ void store_batch(unsigned char* block, int r0, const float (&x)[16]) {
     const int lane = threadIdx.x & 31;
-    if (VEC && !__all_sync(0xFFFFFFFFu, in == 0xFFFFu)) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = (in >> e) & 1u ? x[e] : 0.0f;
-    }
     if (VEC) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -127,6 +148,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
     float* stage_f = reinterpret_cast<float*>(ring + (size_t)kStages * S::STAGE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort_flag = &ctl.abort_flag;
+    Unit last = {};                      // of a cluster: the tile, and whether there is one
+    bool has = false;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(&ctl.full[s], kLoaders);
@@ -166,13 +189,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
                 return;
             }
         };
-        const auto fetch = [&](int q, float (&x)[16], uint32_t& in) {
+        const auto fetch = [&](int q, Batch<T, VEC>& x) {
             const int batch = warp * 2 + (q & 1);
             const bool of_a = q < 2, across = of_a ? A_ACROSS : B_ACROSS;
             const int64_t tile0 = (int64_t)(of_a ? u.m : u.n) * kTile;
             // across: the first 64 rows of the block are tokens against columns 0..63 of the tile, the others against 64..127
             const int64_t row = across ? (int64_t)s * kSlice + (batch & 7) * 8 : tile0 + batch * 8, col = across ? tile0 + (batch >> 3) * 64 : (int64_t)s * kSlice;
-            load_batch<T, VEC>(of_a ? a : b, row, col, x, in);
+            x.load(of_a ? a : b, row, col);
         };
         // products of slice number `issued` of this CTA, by the first warp
         constexpr uint32_t idesc = umma_idesc_bf16(kTile, kTile, A_ACROSS, B_ACROSS);
@@ -215,35 +238,38 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
             if (last) ++it;
             return true;
         };
-        float x[4][16];
-        uint32_t in[4];
+        Batch<T, VEC> x[4];
         uint32_t sent = 0;
         settle();
         if (i < units)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) fetch(q, x[q], in[q]);
+            for (int q = 0; q < 4; ++q) fetch(q, x[q]);
         while (i < units && ok) {
             const int stage = (int)(sent % kStages);
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.empty[stage], ((sent / kStages) & 1u) ^ 1u, abort_flag))) {
                 ok = false;
                 break;
             }
-            // the last slice of all is fetched once more and not stored, rather than have the loads behind a branch
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                unsigned char* block = ring + (size_t)stage * S::STAGE + (q < 2 ? 0 : S::OPERAND);
+                float v[16];
+                x[q].values(v);
+                store_batch<TERMS, VEC>(block, (warp * 2 + (q & 1)) * 8, v);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl.full[stage]);
+            ++sent;
+            // only now the next slice's loads: the fence waits for every load under way.  The last slice of all is fetched once more and not stored, rather than
+            // have the loads behind a branch.
             if (++s >= u.s1) {
                 i += gridDim.x;
                 settle();
                 if (i >= units) --s;
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                unsigned char* block = ring + (size_t)stage * S::STAGE + (q < 2 ? 0 : S::OPERAND);
-                store_batch<TERMS, VEC>(block, (warp * 2 + (q & 1)) * 8, x[q], in[q]);
-                fetch(q, x[q], in[q]);
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl.full[stage]);
-            ++sent;
+            for (int q = 0; q < 4; ++q) fetch(q, x[q]);
             if (warp == 0) ok = issue();
         }
         if (warp == 0) {
@@ -258,9 +284,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
         const int quad = warp & 3, half = (warp - 8) >> 2;
         float* mine = stage_f + (warp - 8) * 32 * 32;
         const int sub = lane & 7, r8 = lane >> 3;
-        T* out = static_cast<T*>(const_cast<void*>(p.out.data));
-        T* pre = static_cast<T*>(const_cast<void*>(p.pre.data));
-        const T* res = static_cast<const T*>(p.residual.data);
         int it = 0;
         for (int i = blockIdx.x; i < units && ok; i += gridDim.x) {
             const Unit u = unit_at(plan, mt, slices, i);
@@ -289,6 +312,17 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
                 if (lane == 0) mbar_arrive(&ctl.acc_empty[it & 1]);
             }
             if (!ok) break;
+            if (plan.cluster > 1) {
+                // every CTA of the cluster is through with its ring: its shared memory takes the parts of 128 / cluster rows
+                last = u;
+                has = true;
+                cluster_sync_all();
+                const int rows = kTile / plan.cluster, r = quad * 32 + lane;
+                const uint32_t to = of_rank(ring, (uint32_t)(r / rows)) + (uint32_t)((((int)cluster_rank() * rows + r % rows) * kTile + half * 64) * 4);
+#pragma unroll
+                for (int e = 0; e < 64; e += 4) store_remote(to + (uint32_t)(e * 4), make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]));
+                break;
+            }
             const int64_t row0 = (int64_t)u.m * kTile + quad * 32 + r8;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -301,9 +335,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
                 const int in_tile = half * 64 + c * 32 + sub * 4;
                 const int64_t col = (int64_t)u.n * kTile + in_tile;
                 const int cols = (int)max((int64_t)0, min((int64_t)4, p.n - col));
-                float bias[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) bias[e] = p.bias && e < cols ? p.bias[col + e] : 0.0f;
 #pragma unroll 2
                 for (int q = 0; q < 8; ++q) {
                     const int64_t row = row0 + q * 4;
@@ -313,30 +344,17 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
                         *reinterpret_cast<float4*>(plan.parts + ((int64_t)u.part * kTile + quad * 32 + r) * kTile + in_tile) = f;
                         continue;
                     }
-                    float z[4] = {f.x + bias[0], f.y + bias[1], f.z + bias[2], f.w + bias[3]};
-                    if (row >= m_end) continue;
-                    if (out_vec && cols == 4) {
-                        if (pre) store_quad(pre + row * p.pre.stride + col, z);
-                        activate_all(z, p.act);
-                        if (res) {
-                            float y[4];
-                            load_quad(res + row * p.residual.stride + col, y);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) z[e] += y[e];
-                        }
-                        store_quad(out + row * p.out.stride + col, z);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (pre && e < cols) store1(pre + row * p.pre.stride + col + e, z[e]);
-                        activate_all(z, p.act);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (e < cols) store1(out + row * p.out.stride + col + e, res ? z[e] + load1(res + row * p.residual.stride + col + e) : z[e]);
-                    }
+                    float z[4] = {f.x, f.y, f.z, f.w};
+                    if (row < m_end && cols > 0) finish_quad<T>(p, z, row, col, cols, out_vec);
                 }
             }
         }
+    }
+    if (plan.cluster > 1) {
+        // once before the parts are sent (the senders have done it) and once after
+        if (!has) cluster_sync_all();
+        cluster_sync_all();
+        if (has) finish_cluster<T, kTile>(p, plan, last, reinterpret_cast<const float*>(ring), m_end, out_vec, (int)threadIdx.x - kLoaders * 32, kEpilogue * 32);
     }
     if (!ok) {
         *abort_flag = 1;
@@ -353,15 +371,16 @@ aa_status launch_split(aa_ctx_impl* c, const ProductParams& in, bool out_vec) {
     ProductParams p = in;
     const int64_t mt = (p.m + kTile - 1) / kTile, nt = (p.n + kTile - 1) / kTile, tiles = mt * nt;
     if (tiles > 0x3FFFFFF) return AA_ERR_UNSUPPORTED;
-    Plan plan = make_plan(p, tiles, (int)nt, c->sm_count, kTile * kTile, kTile, TERMS == 3 ? 1.2 : 0.6);
+    Plan plan = make_plan(p, tiles, (int)nt, c->sm_count, kTile * kTile, kTile, TERMS == 3 ? 2.6 : 1.5, true);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     const void* kernel = p.a_across ? (const void*)product_split_kernel<T, TERMS, VEC, true, true>
                                     : (p.b_across ? (const void*)product_split_kernel<T, TERMS, VEC, false, true> : (const void*)product_split_kernel<T, TERMS, VEC, false, false>);
     if (allow_smem(c, kernel, Split<TERMS>::SMEM) != AA_OK) return AA_ERR_CUDA;
     void* args[] = {&p, &plan, &out_vec};
-    if (launch_overlapped(c, kernel, dim3((unsigned)(units < c->sm_count ? units : c->sm_count)), dim3(kSplitThreads), args, Split<TERMS>::SMEM, false) != cudaSuccess) return AA_ERR_CUDA;
+    const unsigned grid = (unsigned)(units < c->sm_count || plan.cluster > 1 ? units : c->sm_count);
+    if (launch_clusters(c, kernel, grid, kSplitThreads, args, Split<TERMS>::SMEM, plan.cluster) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
-    if (tail == 0) return AA_OK;
+    if (tail == 0 || plan.cluster > 1) return AA_OK;
     void* join[] = {&p, &plan, &out_vec};
     if (launch_overlapped(c, (const void*)product_join_kernel<T, kTile, kTile>, dim3((unsigned)(tail * kTile * kTile / 4 / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;

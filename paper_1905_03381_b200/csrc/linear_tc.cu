@@ -40,21 +40,6 @@ struct Ctl {
     int abort_flag;
 };
 
-// ---- a pair of CTAs
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The same barrier of CTA `rank` of the pair.
-__device__ __forceinline__ uint32_t of_rank(const void* shared, uint32_t rank) {
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(shared)), "r"(rank));
-    return a;
-}
 // Orders the reads of TMEM and shared memory by tcgen05 only, which the barriers of a pair do at their default scope.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // Orders ordinary writes before it too, over the pair (dear: not for every slice).
@@ -99,7 +84,8 @@ __device__ __forceinline__ void dealloc(uint32_t addr, uint32_t cols) {
 
 // SUMS: the sums of A over the contraction, too (A's slices are in shared memory already; another pass over A would cost as much as reading it).  Two warps,
 // idle otherwise, add up the slice's 128 columns once the products have read it and hand the stage back with them.
-template <int CG, int BN, bool A_ACROSS, bool B_ACROSS, bool SUMS>
+// JOIN (single CTAs): the parts of a tile are the CTAs of a cluster, as in linear_plan.cuh; a CTA has one unit then.
+template <int CG, int BN, bool A_ACROSS, bool B_ACROSS, bool SUMS, bool JOIN>
 __global__ void __launch_bounds__(kTcThreads, 1)
 product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan,
                   bool vec) {
@@ -110,6 +96,8 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     float* stage_f = reinterpret_cast<float*>(ring + (size_t)G::STAGES * G::STAGE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CG == 1 ? 0 : (int)cluster_rank();
+    Unit last = {};                      // JOIN: the tile, and whether there is one
+    bool has = false;
     volatile int* abort_flag = &ctl.abort_flag;
     if (threadIdx.x == 0) {
         for (int s = 0; s < G::STAGES; ++s) {
@@ -329,6 +317,12 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 tc_fence_after_sync();
                 ++it;
             }
+            if (JOIN) {
+                // every CTA of the cluster is through with its ring: its shared memory takes the parts of 128 / cluster rows
+                last = u;
+                has = true;
+                cluster_sync_all();
+            }
             const int64_t row0 = ((int64_t)u.m * CG + rank) * kBM + quad * 32 + r8;
             const bool rows_in = row0 - r8 + 32 <= m_end;
 #pragma unroll 1
@@ -361,6 +355,14 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0u;
+                }
+                if (JOIN) {
+                    const int rows = kBM / plan.cluster, r = quad * 32 + lane;
+                    const uint32_t to = of_rank(ring, (uint32_t)(r / rows)) + (uint32_t)((((int)cluster_rank() * rows + r % rows) * BN + half * (BN / 2) + c * 32) * 4);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        store_remote(to + (uint32_t)(e * 4), make_float4(__uint_as_float(v[e]), __uint_as_float(v[e + 1]), __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])));
+                    continue;
                 }
                 __syncwarp();                // the stage's readers of the chunk before are done
 #pragma unroll
@@ -409,6 +411,12 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
         }
     }
+    if (JOIN) {
+        // once before the parts are sent (the senders have done it) and once after
+        if (!has) cluster_sync_all();
+        cluster_sync_all();
+        if (has) finish_cluster<uint16_t, BN>(p, plan, last, reinterpret_cast<const float*>(ring), m_end, vec, (int)threadIdx.x - 128, kEpilogue * 32);
+    }
     if (!ok) {
         *abort_flag = 1;
         if (lane == 0) latch(p.ctl, AA_ERR_SCAN_TIMEOUT);
@@ -420,7 +428,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (warp == 2) dealloc<CG>(tmem, G::TMEM);
 }
 
-template <int CG, int BN, bool AA, bool BA, bool SUMS>
+template <int CG, int BN, bool AA, bool BA, bool SUMS, bool JOIN>
 aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     using G = Geo<CG, BN>;
     ProductParams p = in;
@@ -430,29 +438,17 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
         !encode_bf16_tile_map(&map_b, p.b.data, b_rows, b_cols, p.b.stride, BA ? kSlice : G::ROWS_B))
         return AA_ERR_CUDA;
     const int64_t mt = (p.m + CG * kBM - 1) / (CG * kBM), nt = (p.n + BN - 1) / BN, tiles = mt * nt;
-    const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA, SUMS>;
+    const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA, SUMS, JOIN>;
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
     const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kTcThreads, G::SMEM, CG);
     if (teams < 1) return AA_ERR_CUDA;
-    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2);
+    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2, JOIN);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     void* args[] = {&map_a, &map_b, &p, &plan, &vec};
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((units < teams ? units : teams) * CG));
-    cfg.blockDim = dim3(kTcThreads);
-    cfg.dynamicSmemBytes = G::SMEM;
-    cfg.stream = c->stream;
-    cudaLaunchAttribute attrs[2];
-    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attrs[0].val.programmaticStreamSerializationAllowed = 1;
-    attrs[1].id = cudaLaunchAttributeClusterDimension;
-    attrs[1].val.clusterDim.x = CG;
-    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
-    cfg.attrs = attrs;
-    cfg.numAttrs = CG == 1 ? 1 : 2;
-    if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) return AA_ERR_CUDA;
+    const int cluster = JOIN ? plan.cluster : CG;
+    if (launch_clusters(c, kernel, (unsigned)(JOIN ? units : (units < teams ? units : teams) * CG), kTcThreads, args, G::SMEM, cluster) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
-    if (tail == 0) return AA_OK;
+    if (tail == 0 || JOIN) return AA_OK;
     void* join[] = {&p, &plan, &vec};
     const int64_t threads = tail * CG * kBM * BN / 4;
     if (launch_overlapped(c, (const void*)product_join_kernel<uint16_t, CG * kBM, BN>, dim3((unsigned)(threads / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
@@ -462,8 +458,13 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
 
 template <int CG, int BN>
 aa_status launch_majors(aa_ctx_impl* c, const ProductParams& p, bool vec) {
-    if (p.a_across) return p.a_sums ? launch_tc<CG, BN, true, true, true>(c, p, vec) : launch_tc<CG, BN, true, true, false>(c, p, vec);
-    return p.b_across ? launch_tc<CG, BN, false, true, false>(c, p, vec) : launch_tc<CG, BN, false, false, false>(c, p, vec);
+    if (p.a_across) return p.a_sums ? launch_tc<CG, BN, true, true, true, false>(c, p, vec) : launch_tc<CG, BN, true, true, false, false>(c, p, vec);
+    if (p.b_across) return launch_tc<CG, BN, false, true, false, false>(c, p, vec);
+    if constexpr (CG == 1) {
+        const int64_t tiles = (p.m + kBM - 1) / kBM * ((p.n + BN - 1) / BN);
+        if (!p.parts && make_plan(p, tiles, 1, c->sm_count, 1, 1, 1.0, true).cluster > 1) return launch_tc<CG, BN, false, false, false, true>(c, p, vec);
+    }
+    return launch_tc<CG, BN, false, false, false, false>(c, p, vec);
 }
 
 }  // namespace

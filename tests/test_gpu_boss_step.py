@@ -552,3 +552,20 @@ def test_adamw_refusals(aa):
     aa.aa_adamw(B.adamw_list([B.adamw_tensor(p, g, m, v), B.adamw_tensor(other[0], g, other[1], other[2]), B.adamw_tensor(none, none, none, none)]), rule)
     aa.aa_adamw(B.adamw_list([]), rule)
     assert rule.t == 2
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,k,n", [(20, 4096, 64), (130, 1024, 200), (33, 8192, 130), (70, 2056, 24), (300, 513, 65), (17, 1001, 333), (200, 600, 1000)])
+def test_linear_of_few_tiles_and_long_sums(aa, dtype, m, k, n):
+    """Products that a few tiles cover and whose sums are long enough to be shared out."""
+    out, p, want, z, bar, pre_bar = check_linear(aa, dtype, m, k, n, "silu", True, True, True)
+    close(out, want, bar)
+    close(p, z, pre_bar)
+    check_grad(aa, dtype, m, k, n, "silu", True)
+    x, w = mat(m, k, 1, dtype), mat(n, k, 2, dtype, std=k ** -0.5)
+    x[m // 2:] = float("nan")
+    out = like((m, n), dtype)
+    aa.aa_linear(x, w, out, count_dev=i32([m // 2]))
+    want, z, size = S.linear(f64(x)[:m // 2], f64(w), None, None, None)
+    close(out[:m // 2], want, c(k) * size + HALF[dtype] * np.abs(want))
+    assert torch.all(out[m // 2:] == 7.0)
