@@ -42,6 +42,9 @@ aa_status launch_product(aa_ctx_impl* c, const ProductParams& p, int dtype);
 // bf16 operands that TMA can fetch (16-byte aligned bases and rows).
 bool product_tc_fits(const ProductParams& p);
 aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p);
+// At most 16 rows, forward.
+bool product_few_fits(const ProductParams& p);
+aa_status launch_product_few(aa_ctx_impl* c, const ProductParams& p, int dtype);
 aa_status launch_product_split(aa_ctx_impl* c, const ProductParams& p, int dtype);
 // g = dout * act'(pre), rounded to the matrices' type (null: not written); column sums of the unrounded g into dbias.
 struct SlopeParams {

@@ -135,6 +135,7 @@ const void* slope_of(int act) {
 
 aa_status launch_product(aa_ctx_impl* c, const ProductParams& in, int dtype) {
     ProductParams p = in;
+    if (product_few_fits(p)) return launch_product_few(c, p, dtype);
     if (dtype == AA_BF16 && product_tc_fits(p)) return launch_product_tc(c, p);
     return launch_product_split(c, p, dtype);
     const int64_t mt = (p.m + kT - 1) / kT, nt = (p.n + kT - 1) / kT;

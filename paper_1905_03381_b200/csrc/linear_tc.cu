@@ -324,15 +324,15 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 cluster_sync_all();
             }
             const int64_t row0 = ((int64_t)u.m * CG + rank) * kBM + quad * 32 + r8;
-            const bool rows_in = row0 - r8 + 32 <= m_end;
+            const int rows = (int)max((int64_t)0, min((int64_t)32, m_end - row0 + r8));      // of the warp's 32 that count
 #pragma unroll 1
             for (int c = 0; c < BN / 64; ++c) {
                 const int64_t col = (int64_t)u.n * BN + half * (BN / 2) + c * 32 + sub * 4;
-                const bool whole = vec && rows_in && col + 4 <= p.n;
+                const bool whole = vec && col + 4 <= p.n;
                 uint2 add[8];
                 if (res && whole && u.part < 0) {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) add[q] = *reinterpret_cast<const uint2*>(res + (row0 + q * 4) * p.residual.stride + col);
+                    for (int q = 0; q < 8; ++q) add[q] = r8 + q * 4 < rows ? *reinterpret_cast<const uint2*>(res + (row0 + q * 4) * p.residual.stride + col) : make_uint2(0, 0);
                 } else {
 #pragma unroll
                     for (int q = 0; q < 8; ++q) add[q] = make_uint2(0, 0);
@@ -382,6 +382,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         const int r = q * 4 + r8;
                         const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
                         float z[4] = {f.x + bias[0], f.y + bias[1], f.z + bias[2], f.w + bias[3]};
+                        if (r >= rows) continue;
                         if (pre) *reinterpret_cast<uint2*>(pre + (row0 + q * 4) * p.pre.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
                         activate_all(z, p.act);
                         z[0] += bf16_lo(add[q].x);

@@ -569,3 +569,19 @@ def test_linear_of_few_tiles_and_long_sums(aa, dtype, m, k, n):
     want, z, size = S.linear(f64(x)[:m // 2], f64(w), None, None, None)
     close(out[:m // 2], want, c(k) * size + HALF[dtype] * np.abs(want))
     assert torch.all(out[m // 2:] == 7.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m", [1, 2, 7, 8, 9, 15, 16])
+@pytest.mark.parametrize("k,n", [(512, 4000), (96, 33), (33, 17), (1000, 1030), (2049, 70), (8, 15), (4096, 16)])
+def test_linear_of_few_rows(aa, dtype, m, k, n):
+    out, p, want, z, bar, pre_bar = check_linear(aa, dtype, m, k, n, "gelu", True, True, True)
+    close(out, want, bar)
+    close(p, z, pre_bar)
+    out, _, want, _, bar, _ = check_linear(aa, dtype, m, k, n, None, False, False, False, (1, 3, 5), 1)
+    close(out, want, bar)
+    x, w = mat(m, k, 1, dtype), mat(n, k, 2, dtype)
+    x[m // 2:] = float("nan")
+    out = like((m, n), dtype)
+    aa.aa_linear(x, w, out, count_dev=i32([m // 2]))
+    assert torch.all(torch.isfinite(out[:m // 2])) and torch.all(out[m // 2:] == 7.0)
