@@ -35,19 +35,34 @@ bool same_or_clear(const aa_rows* out, const aa_rows* in) {
 bool floats_ok(const float* p) { return (uintptr_t)p % 4 == 0; }
 bool act_ok(int32_t a) { return a >= AA_ACT_NONE && a <= AA_ACT_SILU; }
 
-// G, then the column sums' parts or (later in the call) the products' parts.
+// Operands are copied into scratch memory where that pays: fp32 numbers as three planes of bf16 terms, bf16 rows that TMA cannot fetch with an alignment
+// that it can.  The copies cost a pass over the operands; the products by TMA run two to three times as fast as those that take their
+// operands apart on the way (1,001 -> 8,001 at 130 rows: see launch_product_split), which outweighs it from about 0.5 GFLOP on.
+constexpr double kCopyFlops = 5e8;
+
+bool by_tma(const aa_rows* m) { return (uintptr_t)m->data % 16 == 0 && m->row_stride % 8 == 0; }
+
+// G, x and w as far as they are copied, then the column sums' parts or (later in the call) the products' parts.
 struct LinearScratch {
-    size_t g, parts, total;
+    size_t g, x, w, parts, total;            // bytes
+    bool copies;
 };
 // The parts of a cut tile are 256 KB in fp32 on each pair of SMs; three rounds of them (58 MB) leave little to balance.
 constexpr size_t kProductParts = 3ull * 74 * 256 * 256 * sizeof(float);
-LinearScratch linear_scratch(int64_t rows, int64_t cols, int dtype, int act) {
+int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
+LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-    LinearScratch s;
-    s.g = act == AA_ACT_NONE ? 0 : up((size_t)rows * (size_t)((cols + 7) / 8 * 8) * (dtype == AA_BF16 ? 2 : 4));
+    LinearScratch s = {};
+    const bool wide = x->dtype == AA_F32;
+    const int64_t rows = x->rows, inner = x->cols, cols = w->rows;
+    s.copies = rows > 16 && 2.0 * (double)rows * (double)inner * (double)cols >= kCopyFlops;
+    const size_t each = s.copies && wide ? 6 : (wide ? 4 : 2);
+    if (act != AA_ACT_NONE || (s.copies && (wide || cols % 8))) s.g = up((size_t)rows * (size_t)padded(cols) * each);
+    if (s.copies && (wide || !by_tma(x))) s.x = up((size_t)rows * (size_t)padded(inner) * each);
+    if (s.copies && (wide || !by_tma(w))) s.w = up((size_t)cols * (size_t)padded(inner) * each);
     const size_t sums = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));
     s.parts = sums < kProductParts ? kProductParts : sums;
-    s.total = s.g + s.parts;
+    s.total = s.g + s.x + s.w + s.parts;
     return s;
 }
 
@@ -95,7 +110,7 @@ aa_status aa_linear_grad_scratch_bytes(const aa_rows* x, const aa_rows* w, int32
     if (!bytes || !act_ok(activation)) return AA_ERR_INVALID_ARG;
     const aa_status st = check_linear(x, w);
     if (st != AA_OK) return st;
-    *bytes = linear_scratch(x->rows, w->rows, x->dtype, activation).total;
+    *bytes = linear_scratch(x, w, activation).total;
     return AA_OK;
 }
 
@@ -115,7 +130,7 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
     if (!same_or_clear(dx, residual) || !clear_of(dw, residual) || !clear_of(dw, dx) || !clear_of(dx, dbias, w->rows) || !clear_of(dw, dbias, w->rows) ||
         !clear_of(residual, dbias, w->rows))
         return AA_ERR_INVALID_ARG;
-    const LinearScratch need = linear_scratch(x->rows, w->rows, x->dtype, activation);
+    const LinearScratch need = linear_scratch(x, w, activation);
     if (!scratch || (uintptr_t)scratch % 256) return AA_ERR_INVALID_ARG;
     if (scratch_bytes < need.total) return AA_ERR_WORKSPACE;
     aa_ctx_impl* c = reinterpret_cast<aa_ctx_impl*>(ctx);
@@ -126,52 +141,80 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
         if (zero == AA_OK && dbias) zero = cuda_ok(cudaMemsetAsync(dbias, 0, (size_t)w->rows * sizeof(float), c->stream));
         return zero;
     }
-    const bool act = activation != AA_ACT_NONE;
-    const MatArg g = act ? MatArg{scratch, (w->rows + 7) / 8 * 8} : mat(dout);
-    float* parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + need.g);
+    const bool act = activation != AA_ACT_NONE, wide = x->dtype == AA_F32, planes = wide && need.copies;
+    char* at = static_cast<char*>(scratch);
+    float* parts = reinterpret_cast<float*>(at + need.g + need.x + need.w);
     ProductParams grad_x = {}, grad_w = {};
     grad_x.ctl = grad_w.ctl = c->ctl;
     grad_x.live = grad_w.live = live;
-    grad_x.a = grad_w.a = g;
     grad_x.parts = grad_w.parts = parts;
     grad_x.part_floats = grad_w.part_floats = (int64_t)(need.parts / sizeof(float));
+    // G is a matrix of its own where there is an activation, or where dout is copied
+    const bool copy_g = need.g > 0 && (act || planes || !by_tma(dout));
+    const MatArg g = copy_g ? MatArg{at, padded(w->rows)} : mat(dout);
+    const MatArg xs = need.x ? MatArg{at + need.g, padded(x->cols)} : mat(x), ws = need.w ? MatArg{at + need.g + need.x, padded(x->cols)} : mat(w);
+    grad_x.a = grad_w.a = g;
+    grad_x.b = ws;
+    grad_w.b = xs;
+    if (planes) {
+        grad_x.plane_a = grad_w.plane_a = x->rows * g.stride;
+        grad_x.plane_b = w->rows * ws.stride;
+        grad_w.plane_b = x->rows * xs.stride;
+    }
     if (dw) {
-        grad_w.b = mat(x);
         grad_w.a_across = grad_w.b_across = grad_w.live_k = true;
         grad_w.m = w->rows;
         grad_w.n = x->cols;
         grad_w.k = x->rows;
         grad_w.out = mat(dw);
         // the sums come with the product where its kernel has them and there is no other pass over dout
-        if (!act && dbias && x->dtype == AA_BF16 && product_tc_fits(grad_w)) grad_w.a_sums = dbias;
+        if (!copy_g && dbias && !wide && product_tc_fits(grad_w)) grad_w.a_sums = dbias;
     }
-    if (act || (dbias && !grad_w.a_sums)) {
-        SlopeParams s = {};
+    aa_status done = AA_OK;
+    SlopeParams s = {};
+    s.rows = x->rows;
+    s.live = live;
+    s.ctl = c->ctl;
+    if ((copy_g && (dx || dw)) || (dbias && !grad_w.a_sums)) {
         s.dout = mat(dout);
         s.pre = mat(pre);
-        if (act && (dx || dw)) s.g = g;
-        s.rows = x->rows;
+        if (copy_g && (dx || dw)) s.g = g;
+        if (s.g.data && need.copies) s.plane = x->rows * g.stride;
         s.cols = w->rows;
-        s.live = live;
         s.act = activation;
         s.parts = parts;
-        s.dbias = dbias;
-        s.ctl = c->ctl;
-        const aa_status done = launch_slope(c, s, x->dtype);
-        if (done != AA_OK) return done;
+        s.dbias = grad_w.a_sums ? nullptr : dbias;
+        if ((done = launch_slope(c, s, x->dtype)) != AA_OK) return done;
+    }
+    s.pre = MatArg{nullptr, 0};
+    s.act = AA_ACT_NONE;
+    s.dbias = nullptr;
+    s.cols = x->cols;
+    if (dw && need.x) {
+        s.dout = mat(x);
+        s.g = xs;
+        s.plane = x->rows * xs.stride;
+        if ((done = launch_slope(c, s, x->dtype)) != AA_OK) return done;
+    }
+    if (dx && need.w) {
+        s.dout = mat(w);
+        s.g = ws;
+        s.plane = w->rows * ws.stride;
+        s.rows = w->rows;
+        s.live = live_arg(nullptr, 0, nullptr, w->rows);
+        if ((done = launch_slope(c, s, x->dtype)) != AA_OK) return done;
     }
     if (dx) {
-        grad_x.b = mat(w);
         grad_x.b_across = true;
         grad_x.m = x->rows;
         grad_x.n = x->cols;
         grad_x.k = w->rows;
         grad_x.residual = mat(residual);
         grad_x.out = mat(dx);
-        const aa_status done = launch_product(c, grad_x, x->dtype);
-        if (done != AA_OK) return done;
+        if ((done = planes ? launch_product_planes(c, grad_x) : launch_product(c, grad_x, x->dtype)) != AA_OK) return done;
     }
-    return dw ? launch_product(c, grad_w, x->dtype) : AA_OK;
+    if (!dw) return AA_OK;
+    return planes ? launch_product_planes(c, grad_w) : launch_product(c, grad_w, x->dtype);
 }
 
 aa_status aa_layer_norm(aa_ctx* ctx, const aa_rows* x, const float* gamma, const float* beta, float eps, const int32_t* offsets, int64_t n_seg,

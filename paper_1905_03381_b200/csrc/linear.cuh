@@ -34,6 +34,7 @@ struct ProductParams {
     MatArg residual, pre, out;   // nullable but out
     float* parts;            // scratch for tiles cut along the contraction, nullable (then bias, act and pre are empty)
     int64_t part_floats;
+    int64_t plane_a, plane_b;    // above 0: A and B are three planes of bf16 terms of fp32 numbers, so many elements apart
     float* a_sums;           // [m] sums of A over the contraction, nullable (a_across)
     Control* ctl;
 };
@@ -45,10 +46,13 @@ aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p);
 // At most 16 rows, forward.
 bool product_few_fits(const ProductParams& p);
 aa_status launch_product_few(aa_ctx_impl* c, const ProductParams& p, int dtype);
+// fp32 operands taken apart beforehand (plane_a, plane_b).
+aa_status launch_product_planes(aa_ctx_impl* c, const ProductParams& p);
 aa_status launch_product_split(aa_ctx_impl* c, const ProductParams& p, int dtype);
 // g = dout * act'(pre), rounded to the matrices' type (null: not written); column sums of the unrounded g into dbias.
 struct SlopeParams {
     MatArg dout, pre, g;
+    int64_t plane;           // above 0: g is bf16 terms (three of fp32, one of bf16) in planes so many elements apart, rows padded to a multiple of 8 elements
     int64_t rows, cols;
     LiveRows live;
     int act;

@@ -1,7 +1,7 @@
 // Tiles of the tensor-core products: in which order a launch takes them, and which it cuts along the contraction so that the last round of SMs is full.
 #pragma once
 
-#include "async_copy.cuh"
+#include "cta_pair.cuh"
 #include "linear.cuh"
 
 namespace aa {
@@ -46,24 +46,6 @@ inline Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, 
 }
 
 #ifdef __CUDACC__
-
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The same place in the shared memory of CTA `rank` of the cluster.
-__device__ __forceinline__ uint32_t of_rank(const void* shared, uint32_t rank) {
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(shared)), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ void store_remote(uint32_t at, float4 x) {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
-}
 
 struct Unit {
     int m, n, s0, s1, part;              // slices [s0, s1); part < 0: the whole tile

@@ -11,8 +11,8 @@
 //
 // Tiles that do not fill the last round of SMs can be cut along the contraction (the backward call has scratch memory): their parts go to
 // scratch in fp32 and a second kernel adds them up in order and finishes them.
+#include "cta_pair.cuh"
 #include "linear_plan.cuh"
-#include "tensor_core.cuh"
 
 namespace aa {
 
@@ -39,48 +39,6 @@ struct Ctl {
     uint32_t tmem;
     int abort_flag;
 };
-
-// Orders the reads of TMEM and shared memory by tcgen05 only, which the barriers of a pair do at their default scope.
-__device__ __forceinline__ void mbar_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// Orders ordinary writes before it too, over the pair (dear: not for every slice).
-__device__ __forceinline__ void mbar_release_at(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// A box into this CTA's shared memory whose bytes count on a barrier of either CTA.
-template <int CG>
-__device__ __forceinline__ void load_box(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar, uint32_t first_bar) {
-    if (CG == 1) tma_load_2d(dst, map, x, y, bar);
-    else
-        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_u32(dst)), "l"(map),
-                     "r"(first_bar), "r"(x), "r"(y)
-                     : "memory");
-}
-template <int CG>
-__device__ __forceinline__ void commit(uint64_t* bar) {
-    if (CG == 1) umma_commit(bar);
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((uint16_t)3) : "memory");
-}
-template <int CG>
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    if (CG == 1) umma_bf16(d, a, b, idesc, accumulate);
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                     "r"((uint32_t)accumulate)
-                     : "memory");
-}
-template <int CG>
-__device__ __forceinline__ void alloc(uint32_t* dst, uint32_t cols) {
-    if (CG == 1) {
-        tmem_alloc(dst, cols);
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(cols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    }
-}
-template <int CG>
-__device__ __forceinline__ void dealloc(uint32_t addr, uint32_t cols) {
-    if (CG == 1) tmem_dealloc(addr, cols);
-    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
-}
 
 // SUMS: the sums of A over the contraction, too (A's slices are in shared memory already; another pass over A would cost as much as reading it).  Two warps,
 // idle otherwise, add up the slice's 128 columns once the products have read it and hand the stage back with them.

@@ -19,6 +19,9 @@ namespace aa {
 bool encode_bf16_tile_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t row_stride,
                           uint32_t box_rows);
 
+// The same for `planes` such matrices, `plane_stride` elements apart (three dimensions, box [1 x box_rows x 64]).
+bool encode_bf16_planes_map(CUtensorMap* map, const void* base, uint64_t planes, uint64_t rows, uint64_t cols, uint64_t row_stride, uint64_t plane_stride, uint32_t box_rows);
+
 #ifdef __CUDACC__
 
 // ---------------------------------------------------------------- TMA (tiled)

@@ -585,3 +585,24 @@ def test_linear_of_few_rows(aa, dtype, m, k, n):
     out = like((m, n), dtype)
     aa.aa_linear(x, w, out, count_dev=i32([m // 2]))
     assert torch.all(torch.isfinite(out[:m // 2])) and torch.all(out[m // 2:] == 7.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,k,n,pads,shift", [(700, 515, 1001, (0, 0, 0), 0), (300, 1000, 1100, (0, 0, 0), 0), (520, 777, 700, (3, 1, 5), 1), (1100, 512, 640, (0, 0, 0), 0), (130, 1001, 2051, (0, 0, 0), 0)])
+def test_linear_gradients_of_operands_that_are_copied(aa, dtype, m, k, n, pads, shift):
+    """Large enough for copies of the operands in scratch memory; counted rows, whose successors hold NaN."""
+    for act, residual in (("gelu", True), (None, False)):
+        check_grad(aa, dtype, m, k, n, act, residual, pads, shift)
+    rows = m - 37
+    x, w, dout = mat(m, k, 1, dtype, pads[0], shift), mat(n, k, 2, dtype, pads[1], shift), mat(m, n, 3, dtype, pads[2], shift)
+    x[rows:] = float("nan")
+    dout[rows:] = float("nan")
+    dx, dw, db = like((m, k), dtype), like((n, k), dtype), torch.full((n,), 7.0, device=DEV)
+    scratch = aa.linear_grad_scratch(x, w)
+    scratch.fill_(255)                      # NaN in every type
+    aa.aa_linear_grad(x, w, dout, scratch, dx=dx, dw=dw, dbias=db, count_dev=i32([rows]))
+    got, size, _ = S.linear_grad(f64(x)[:rows], f64(w), f64(dout)[:rows], None, None, None)
+    close(dx[:rows], got["dx"], c(n) * size["dx"] + HALF[dtype] * np.abs(got["dx"]))
+    assert torch.all(dx[rows:] == 7.0)
+    close(dw, got["dw"], c(rows) * size["dw"] + HALF[dtype] * np.abs(got["dw"]))
+    close(db, got["dbias"], c(rows) * size["dbias"])
