@@ -36,9 +36,9 @@ bool floats_ok(const float* p) { return (uintptr_t)p % 4 == 0; }
 bool act_ok(int32_t a) { return a >= AA_ACT_NONE && a <= AA_ACT_SILU; }
 
 // Operands are copied into scratch memory where that pays: fp32 numbers as three planes of bf16 terms, bf16 rows that TMA cannot fetch with an alignment
-// that it can.  The copies cost a pass over the operands; the products by TMA run two to three times as fast as those that take their
-// operands apart on the way (1,001 -> 8,001 at 130 rows: see launch_product_split), which outweighs it from about 0.5 GFLOP on.
-constexpr double kCopyFlops = 5e8;
+// that it can.  The products by TMA run two to three times as fast as those that take their operands apart on the way, but the copies are a
+// pass over memory: each copied number has to serve 64 multiply-adds, and the call 0.5 GFLOP.
+constexpr double kCopyFlops = 5e8, kCopyReuse = 64.0;
 
 bool by_tma(const aa_rows* m) { return (uintptr_t)m->data % 16 == 0 && m->row_stride % 8 == 0; }
 
@@ -55,7 +55,8 @@ LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     LinearScratch s = {};
     const bool wide = x->dtype == AA_F32;
     const int64_t rows = x->rows, inner = x->cols, cols = w->rows;
-    s.copies = rows > 16 && 2.0 * (double)rows * (double)inner * (double)cols >= kCopyFlops;
+    const double products = (double)rows * (double)inner * (double)cols, numbers = (double)rows * (double)(inner + cols) + (double)inner * (double)cols;
+    s.copies = 2.0 * products >= kCopyFlops && products >= kCopyReuse * numbers;
     const size_t each = s.copies && wide ? 6 : (wide ? 4 : 2);
     if (act != AA_ACT_NONE || (s.copies && (wide || cols % 8))) s.g = up((size_t)rows * (size_t)padded(cols) * each);
     if (s.copies && (wide || !by_tma(x))) s.x = up((size_t)rows * (size_t)padded(inner) * each);

@@ -62,28 +62,38 @@ __global__ void __launch_bounds__(256) product_plain_kernel(ProductParams p) {
 }
 
 // Bound by memory: two values read and one written an element (one read where only the sums are wanted).  A CTA takes 32 x V columns of a run of rows, a
-// warp every eighth row, a lane V columns; rows are shared out in kSlopeParts runs whose column sums stay apart until the join.
+// warp every eighth row, a lane V neighbouring columns (VEC: as one word); rows are shared out in kSlopeParts runs whose column sums stay apart until the join.
 // TERMS 0: g in the matrices' type.  1 or 3: bf16 terms of g in planes, rows up to a multiple of 64 behind the counted ones zero (the products that read them take 64 at a time).
-template <typename T, int V, int ACT, int TERMS>
+template <typename T, bool VEC, int ACT, int TERMS>
 __global__ void __launch_bounds__(256) slope_kernel(SlopeParams p) {
+    constexpr int V = 16 / (int)sizeof(T);
     __shared__ float sums[8][32 * V];
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t col = ((int64_t)blockIdx.x * 32 + lane) * V;
+    const int n = (int)max((int64_t)0, min((int64_t)V, p.cols - col));          // columns of this lane
     const int64_t run = (p.rows + kSlopeParts - 1) / kSlopeParts, r0 = run * blockIdx.y, r1 = min(r0 + run, TERMS ? min(p.rows, (live + 63) / 64 * 64) : live);
     const T *d = static_cast<const T*>(p.dout.data), *z = static_cast<const T*>(p.pre.data);
     T* g = static_cast<T*>(const_cast<void*>(p.g.data));
+    const auto load = [&](const T* at, float* x) {
+        if constexpr (VEC) {
+            load_elems<T, V>(at, x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = e < n ? load1(at + e) : 0.0f;
+        }
+    };
     float sum[V] = {};
-    if (col < p.cols) {
+    if (n > 0) {
 #pragma unroll 4
         for (int64_t r = r0 + warp; r < r1; r += 8) {
             float x[V], y[V];
             if (TERMS == 0 || r < live) {
-                load_elems<T, V>(d + r * p.dout.stride + col, x);
+                load(d + r * p.dout.stride + col, x);
                 if (ACT != AA_ACT_NONE) {
-                    load_elems<T, V>(z + r * p.pre.stride + col, y);
+                    load(z + r * p.pre.stride + col, y);
 #pragma unroll
                     for (int e = 0; e < V; ++e) x[e] *= activation_slope<ACT>(y[e]);
                 }
@@ -92,23 +102,31 @@ __global__ void __launch_bounds__(256) slope_kernel(SlopeParams p) {
                 for (int e = 0; e < V; ++e) x[e] = 0.0f;
             }
             if constexpr (TERMS > 0) {
+                // padded rows: the columns behind the last are written too, and not read
                 uint16_t* to = static_cast<uint16_t*>(const_cast<void*>(p.g.data)) + r * p.g.stride + col;
 #pragma unroll
                 for (int e = 0; e < V; ++e) y[e] = x[e];
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t) {
-                    uint32_t w[(V + 1) / 2];
+                    uint32_t w[V / 2];
 #pragma unroll
-                    for (int e = 0; e < V; e += 2) w[e / 2] = pack_bf16(y[e], e + 1 < V ? y[e + 1] : 0.0f);
+                    for (int e = 0; e < V; e += 2) {
+                        w[e / 2] = pack_bf16(y[e], y[e + 1]);
+                        y[e] -= bf16_lo(w[e / 2]);
+                        y[e + 1] -= bf16_hi(w[e / 2]);
+                    }
                     if constexpr (V == 8) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else if constexpr (V == 4) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-                    else *to = (uint16_t)w[0];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) y[e] -= e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+                    else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
                     to += p.plane;
                 }
             } else if (ACT != AA_ACT_NONE && g) {
-                store_elems<T, V>(g + r * p.g.stride + col, x);
+                if constexpr (VEC) {
+                    store_elems<T, V>(g + r * p.g.stride + col, x);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (e < n) store1(g + r * p.g.stride + col + e, x[e]);
+                }
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[e] += x[e];
@@ -147,16 +165,16 @@ __global__ void __launch_bounds__(256) slope_join_kernel(const float* parts, flo
     }
 }
 
-template <typename T, int V, int TERMS>
+template <typename T, bool VEC, int TERMS>
 const void* slope_of(int act) {
-    if (act == AA_ACT_RELU) return (const void*)slope_kernel<T, V, AA_ACT_RELU, TERMS>;
-    if (act == AA_ACT_GELU) return (const void*)slope_kernel<T, V, AA_ACT_GELU, TERMS>;
-    if (act == AA_ACT_SILU) return (const void*)slope_kernel<T, V, AA_ACT_SILU, TERMS>;
-    return (const void*)slope_kernel<T, V, AA_ACT_NONE, TERMS>;
+    if (act == AA_ACT_RELU) return (const void*)slope_kernel<T, VEC, AA_ACT_RELU, TERMS>;
+    if (act == AA_ACT_GELU) return (const void*)slope_kernel<T, VEC, AA_ACT_GELU, TERMS>;
+    if (act == AA_ACT_SILU) return (const void*)slope_kernel<T, VEC, AA_ACT_SILU, TERMS>;
+    return (const void*)slope_kernel<T, VEC, AA_ACT_NONE, TERMS>;
 }
 
-template <typename T, int V>
-const void* slope_of(int act, bool planes) { return planes ? slope_of<T, V, sizeof(T) == 4 ? 3 : 1>(act) : slope_of<T, V, 0>(act); }
+template <typename T, bool VEC>
+const void* slope_of(int act, bool planes) { return planes ? slope_of<T, VEC, sizeof(T) == 4 ? 3 : 1>(act) : slope_of<T, VEC, 0>(act); }
 
 }  // namespace
 
@@ -179,12 +197,11 @@ aa_status launch_slope(aa_ctx_impl* c, const SlopeParams& in, int dtype) {
     const int es = dtype == AA_BF16 ? 2 : 4, wide = 16 / es;
     const auto aligned = [&](const MatArg& a) { return !a.data || ((uintptr_t)a.data % 16 == 0 && (a.stride * es) % 16 == 0); };
     const bool vec = p.cols % wide == 0 && aligned(p.dout) && aligned(p.pre) && (p.plane > 0 || aligned(p.g));
-    const int v = vec ? wide : 1;
     const bool planes = p.plane > 0;
-    const void* kernel = dtype == AA_BF16 ? (vec ? slope_of<uint16_t, 8>(p.act, planes) : slope_of<uint16_t, 1>(p.act, planes))
-                                          : (vec ? slope_of<float, 4>(p.act, planes) : slope_of<float, 1>(p.act, planes));
+    const void* kernel = dtype == AA_BF16 ? (vec ? slope_of<uint16_t, true>(p.act, planes) : slope_of<uint16_t, false>(p.act, planes))
+                                          : (vec ? slope_of<float, true>(p.act, planes) : slope_of<float, false>(p.act, planes));
     void* args[] = {&p};
-    if (launch_overlapped(c, kernel, dim3((unsigned)((p.cols + 32 * v - 1) / (32 * v)), kSlopeParts), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+    if (launch_overlapped(c, kernel, dim3((unsigned)((p.cols + 32 * wide - 1) / (32 * wide)), kSlopeParts), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     if (!p.dbias) return AA_OK;
     void* join[] = {&p.parts, &p.dbias, &p.cols};
