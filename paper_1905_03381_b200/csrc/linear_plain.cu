@@ -1,4 +1,6 @@
 // Products of linear layers in fp32 arithmetic on the ordinary lanes: any type, stride and alignment.
+#include <type_traits>
+
 #include "linear.cuh"
 
 namespace aa {
@@ -77,59 +79,86 @@ __global__ void __launch_bounds__(256) slope_kernel(SlopeParams p) {
     const int64_t run = (p.rows + kSlopeParts - 1) / kSlopeParts, r0 = run * blockIdx.y, r1 = min(r0 + run, TERMS ? min(p.rows, (live + 63) / 64 * 64) : live);
     const T *d = static_cast<const T*>(p.dout.data), *z = static_cast<const T*>(p.pre.data);
     T* g = static_cast<T*>(const_cast<void*>(p.g.data));
-    const auto load = [&](const T* at, float* x) {
+    float sum[V] = {};
+    // ROWS rows' loads, all before the first store: nothing tells the compiler that g is apart from dout and pre
+    using Word = typename std::conditional<VEC, uint4, T>::type;
+    constexpr int N = VEC ? 1 : V, ROWS = VEC ? 4 : 2;
+    const auto fetch = [&](const T* at, Word (&w)[N]) {
         if constexpr (VEC) {
-            load_elems<T, V>(at, x);
+            w[0] = *reinterpret_cast<const uint4*>(at);
         } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) x[e] = e < n ? load1(at + e) : 0.0f;
+            for (int e = 0; e < V; ++e) w[e] = at[min(e, n - 1)];
         }
     };
-    float sum[V] = {};
+    const auto values = [&](const Word (&w)[N], float (&x)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if constexpr (VEC && sizeof(T) == 4) x[e] = __uint_as_float((&w[0].x)[e]);
+            else if constexpr (VEC) x[e] = e % 2 ? bf16_hi((&w[0].x)[e / 2]) : bf16_lo((&w[0].x)[e / 2]);
+            else if constexpr (sizeof(T) == 4) x[e] = e < n ? (float)w[e] : 0.0f;
+            else x[e] = e < n ? __uint_as_float((uint32_t)w[e] << 16) : 0.0f;
+        }
+    };
+    const auto put = [&](int64_t r, const float (&x)[V]) {
+        if constexpr (TERMS > 0) {
+            // padded rows: the columns behind the last are written too, and not read
+            uint16_t* to = static_cast<uint16_t*>(const_cast<void*>(p.g.data)) + r * p.g.stride + col;
+            float y[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = x[e];
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) {
+                uint32_t w[V / 2];
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    w[e / 2] = pack_bf16(y[e], y[e + 1]);
+                    y[e] -= bf16_lo(w[e / 2]);
+                    y[e + 1] -= bf16_hi(w[e / 2]);
+                }
+                if constexpr (V == 8) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+                else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+                to += p.plane;
+            }
+        } else if (ACT != AA_ACT_NONE && g) {
+            if constexpr (VEC) {
+                store_elems<T, V>(g + r * p.g.stride + col, x);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (e < n) store1(g + r * p.g.stride + col + e, x[e]);
+            }
+        }
+    };
     if (n > 0) {
-#pragma unroll 4
-        for (int64_t r = r0 + warp; r < r1; r += 8) {
-            float x[V], y[V];
-            if (TERMS == 0 || r < live) {
-                load(d + r * p.dout.stride + col, x);
+        const int64_t last = min(r1, live) - 1;
+        for (int64_t r = r0 + warp; r <= last; r += 8 * ROWS) {
+            Word dw[ROWS][N], zw[ROWS][N];
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                const int64_t at = min(r + 8 * i, last);
+                fetch(d + at * p.dout.stride + col, dw[i]);
+                if (ACT != AA_ACT_NONE) fetch(z + at * p.pre.stride + col, zw[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (r + 8 * i > last) break;
+                float x[V];
+                values(dw[i], x);
                 if (ACT != AA_ACT_NONE) {
-                    load(z + r * p.pre.stride + col, y);
+                    float y[V];
+                    values(zw[i], y);
 #pragma unroll
                     for (int e = 0; e < V; ++e) x[e] *= activation_slope<ACT>(y[e]);
                 }
-            } else {
+                put(r + 8 * i, x);
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = 0.0f;
+                for (int e = 0; e < V; ++e) sum[e] += x[e];
             }
-            if constexpr (TERMS > 0) {
-                // padded rows: the columns behind the last are written too, and not read
-                uint16_t* to = static_cast<uint16_t*>(const_cast<void*>(p.g.data)) + r * p.g.stride + col;
-#pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = x[e];
-#pragma unroll
-                for (int t = 0; t < TERMS; ++t) {
-                    uint32_t w[V / 2];
-#pragma unroll
-                    for (int e = 0; e < V; e += 2) {
-                        w[e / 2] = pack_bf16(y[e], y[e + 1]);
-                        y[e] -= bf16_lo(w[e / 2]);
-                        y[e + 1] -= bf16_hi(w[e / 2]);
-                    }
-                    if constexpr (V == 8) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-                    to += p.plane;
-                }
-            } else if (ACT != AA_ACT_NONE && g) {
-                if constexpr (VEC) {
-                    store_elems<T, V>(g + r * p.g.stride + col, x);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < V; ++e)
-                        if (e < n) store1(g + r * p.g.stride + col + e, x[e]);
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] += x[e];
+        }
+        if (TERMS > 0) {
+            const float zero[V] = {};
+            for (int64_t r = max(r0, live) + warp; r < r1; r += 8) put(r, zero);
         }
     }
     if (!p.dbias) return;
