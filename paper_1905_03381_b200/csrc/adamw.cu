@@ -5,7 +5,7 @@
 // copied to the device; a CTA finds its tensor by bisection over the running number of chunks.  A warp owns 256 consecutive elements, which is
 // one block of the 8-bit states: two runs of 128, four elements a lane in each, so that every access is contiguous over the warp, a lane's
 // four elements share one block of random words and the block's largest magnitude is a warp reduction.
-// Products, sums, roots and quotients are each rounded by themselves: a code's rounding depends on the last bits of what is rounded.
+// What is rounded to a code comes of products, sums and roots that are each rounded by themselves: the code depends on its last bits.
 #include <math.h>
 
 #include "boss_common.cuh"
@@ -14,7 +14,7 @@ namespace aa {
 
 namespace {
 
-constexpr int kWarpsPerCta = 8, kPerCta = kWarpsPerCta * 256 * 2;      // a warp takes two blocks, one after the other
+constexpr int kWarpsPerCta = 8, kPerCta = kWarpsPerCta * 256 * 4;      // a warp takes four blocks, one after the other
 
 struct Entry {
     float* param;
@@ -34,7 +34,7 @@ struct Table {
     Entry e[N];
     int n;
     float b1, c1, b2, c2;    // betas and 1 - beta
-    float rate, root, eps;   // lr / (1 - beta1^t), 1 / (1 - beta2^t)
+    float rate, root, eps;   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
     uint32_t t_lo, t_hi, seed_lo, seed_hi;
     const float* grad_scale;
 };
@@ -55,14 +55,14 @@ __device__ __forceinline__ uint32_t encode4(const float (&y)[4]) {
     return w;
 }
 
-// x in units, |x| < 256 -> a neighbouring e4m3 number, by 16 random bits.  What is not finite becomes NaN.
+// x in units, |x| < 256 -> a neighbouring e4m3 number, by 16 random bits.
 __device__ __forceinline__ float to_e4m3(float x, uint32_t u) {
     const float a = fabsf(x);
     const bool low = a < 0.015625f;                        // below the normal numbers: the equal steps of [2^-6, 2^-5)
     float y = low ? __fadd_rn(a, 0.015625f) : a;
     y = __uint_as_float((__float_as_uint(y) + (u << 4)) & 0xFFF00000u);
     y = low ? __fadd_rn(y, -0.015625f) : y;
-    return a < 512.0f ? copysignf(y, x) : __uint_as_float(0x7FFFFFFFu);
+    return copysignf(y, x);
 }
 // The same for a root x >= 0 whose square is to keep its mean.
 __device__ __forceinline__ float root_to_e4m3(float x, uint32_t u) {
@@ -73,17 +73,17 @@ __device__ __forceinline__ float root_to_e4m3(float x, uint32_t u) {
     z = low ? __fadd_rn(z, -0.015625f) : z;
     const float part = __fmul_rn(__fmul_rn((float)u, 1.52587890625e-5f), __fmul_rn(__fadd_rn(z, -y), __fadd_rn(z, y)));
     y = __fmul_rn(__fadd_rn(x, -y), __fadd_rn(x, y)) > part ? z : y;
-    return x < 512.0f ? y : __uint_as_float(0x7FFFFFFFu);
+    return x > 0.0f ? fmaxf(y, 0.001953125f) : y;          // 2^-9 at least
 }
 
-__device__ __forceinline__ uint32_t scale_byte(float top) {
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    return top > 0.0f ? (uint32_t)max((int)(__float_as_uint(top) >> 23) - 7, 1) : 0u;
+__device__ __forceinline__ float sqrt_approx(float x) {
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
+
+// Scale of a block from the bits of its largest magnitude (those of an infinity or NaN are larger than any number's).
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) { return top ? (uint32_t)max((int)(top >> 23) - 7, 1) : 0u; }
 
 template <bool VEC>
 __device__ __forceinline__ void load4(const float* p, int64_t left, float (&x)[4]) {
@@ -170,7 +170,7 @@ __device__ __forceinline__ void update(const Table<N>& tab, const Entry& e, int6
             vc[h] = load_codes<VEC>(static_cast<const uint8_t*>(e.v) + at[h], left);
         }
     }
-    float m_top = 0.0f, v_top = 0.0f;
+    uint32_t m_top = 0, v_top = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if (BITS == 8) {
@@ -183,13 +183,17 @@ __device__ __forceinline__ void update(const Table<N>& tab, const Entry& e, int6
             if (BITS == 8) v[h][i] = __fmul_rn(v[h][i], v[h][i]);
             m[h][i] = __fadd_rn(__fmul_rn(m[h][i], tab.b1), __fmul_rn(x, tab.c1));
             v[h][i] = __fadd_rn(__fmul_rn(v[h][i], tab.b2), __fmul_rn(__fmul_rn(x, x), tab.c2));
-            const float den = __fadd_rn(__fsqrt_rn(__fmul_rn(v[h][i], tab.root)), tab.eps);
-            p[h][i] = __fadd_rn(__fmul_rn(p[h][i], e.keep), -__fmul_rn(__fdiv_rn(m[h][i], den), tab.rate));
+            // the step itself is nobody's border: quotient and root to two units of the last place
+            float den;
             if (BITS == 8) {
                 v[h][i] = __fsqrt_rn(v[h][i]);
-                m_top = fmaxf(m_top, fabsf(m[h][i]));
-                v_top = fmaxf(v_top, v[h][i]);
+                m_top = max(m_top, __float_as_uint(m[h][i]) & 0x7FFFFFFFu);
+                v_top = max(v_top, __float_as_uint(v[h][i]) & 0x7FFFFFFFu);
+                den = fmaf(v[h][i], tab.root, tab.eps);
+            } else {
+                den = fmaf(sqrt_approx(v[h][i]), tab.root, tab.eps);
             }
+            p[h][i] = fmaf(-tab.rate, __fdividef(m[h][i], den), __fmul_rn(p[h][i], e.keep));
         }
         const int64_t left = e.n - at[h];
         store4<VEC>(e.param + at[h], left, p[h]);
@@ -200,22 +204,24 @@ __device__ __forceinline__ void update(const Table<N>& tab, const Entry& e, int6
         }
     }
     if (BITS == 32) return;
+    m_top = __reduce_max_sync(0xFFFFFFFFu, m_top);
+    v_top = __reduce_max_sync(0xFFFFFFFFu, v_top);
     mb = scale_byte(m_top);
     vb = scale_byte(v_top);
     const float mi = mb ? __uint_as_float((254u - mb) << 23) : 1.0f, vi = vb ? __uint_as_float((254u - vb) << 23) : 1.0f;
+    const bool numbers = max(m_top, v_top) < 0x7F800000u;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const Words4 w = philox4x32_10((uint32_t)(at[h] >> 2), e.index, tab.t_lo, tab.t_hi, tab.seed_lo, tab.seed_hi);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bool some = v[h][i] > 0.0f;
             m[h][i] = to_e4m3(__fmul_rn(m[h][i], mi), w.w[i] & 0xFFFFu);
             v[h][i] = root_to_e4m3(__fmul_rn(v[h][i], vi), w.w[i] >> 16);
-            if (some && v[h][i] == 0.0f) v[h][i] = 0.001953125f;      // 2^-9
         }
+        // the codes of a block with an infinity or NaN are no numbers
         const int64_t left = e.n - at[h];
-        store_codes<VEC>(static_cast<uint8_t*>(e.m) + at[h], left, encode4(m[h]));
-        store_codes<VEC>(static_cast<uint8_t*>(e.v) + at[h], left, encode4(v[h]));
+        store_codes<VEC>(static_cast<uint8_t*>(e.m) + at[h], left, numbers ? encode4(m[h]) : 0x7F7F7F7Fu);
+        store_codes<VEC>(static_cast<uint8_t*>(e.v) + at[h], left, numbers ? encode4(v[h]) : 0x7F7F7F7Fu);
     }
     if (lane == 0) {
         e.m_scale[block] = (uint8_t)mb;
@@ -258,7 +264,7 @@ aa_status launch_some(aa_ctx_impl* c, const aa_adamw_tensor* t, int64_t count, c
     tab.b2 = (float)r->beta2;
     tab.c2 = (float)(1.0 - r->beta2);
     tab.rate = (float)(r->lr / (1.0 - pow(r->beta1, step)));
-    tab.root = (float)(1.0 / (1.0 - pow(r->beta2, step)));
+    tab.root = (float)sqrt(1.0 / (1.0 - pow(r->beta2, step)));
     tab.eps = (float)r->eps;
     tab.t_lo = (uint32_t)(r->t + 1);
     tab.t_hi = (uint32_t)((uint64_t)(r->t + 1) >> 32);
