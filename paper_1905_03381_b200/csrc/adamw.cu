@@ -35,9 +35,24 @@ struct Table {
     int n;
     float b1, c1, b2, c2;    // betas and 1 - beta
     float rate, root, eps;   // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-    uint32_t t_lo, t_hi, seed_lo, seed_hi;
+    uint32_t t_lo, t_hi, keys[20];   // round keys of the draws
     const float* grad_scale;
 };
+
+// Philox4x32-10 of counter (c0, c1, t) under keys that the host has laid out round by round.
+template <int N>
+__device__ __forceinline__ Words4 draw(const Table<N>& tab, uint32_t c0, uint32_t c1) {
+    uint32_t c2 = tab.t_lo, c3 = tab.t_hi;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ tab.keys[2 * r];
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ tab.keys[2 * r + 1];
+        c3 = (uint32_t)a;
+    }
+    return Words4{{c0, c1, c2, c3}};
+}
 
 __device__ __forceinline__ void decode4(uint32_t w, float unit, float (&x)[4]) {
     uint32_t a, b;
@@ -55,25 +70,26 @@ __device__ __forceinline__ uint32_t encode4(const float (&y)[4]) {
     return w;
 }
 
-// x in units, |x| < 256 -> a neighbouring e4m3 number, by 16 random bits.
-__device__ __forceinline__ float to_e4m3(float x, uint32_t u) {
-    const float a = fabsf(x);
-    const bool low = a < 0.015625f;                        // below the normal numbers: the equal steps of [2^-6, 2^-5)
-    float y = low ? __fadd_rn(a, 0.015625f) : a;
-    y = __uint_as_float((__float_as_uint(y) + (u << 4)) & 0xFFF00000u);
-    y = low ? __fadd_rn(y, -0.015625f) : y;
-    return copysignf(y, x);
+// x in units, |x| < 256 -> a neighbouring e4m3 number, by the low 16 bits of w.  Below 2^-6 the steps are those of [2^-6, 2^-5).
+__device__ __forceinline__ float to_e4m3(float x, uint32_t w) {
+    const float lift = fabsf(x) < 0.015625f ? 0.015625f : 0.0f;
+    const float y = __uint_as_float((__float_as_uint(__fadd_rn(fabsf(x), lift)) + ((w & 0xFFFFu) << 4)) & 0xFFF00000u);
+    return copysignf(__fadd_rn(y, -lift), x);
 }
-// The same for a root x >= 0 whose square is to keep its mean.
-__device__ __forceinline__ float root_to_e4m3(float x, uint32_t u) {
-    const bool low = x < 0.015625f;
-    const uint32_t bits = __float_as_uint(low ? __fadd_rn(x, 0.015625f) : x) & 0xFFF00000u;
+// The same for a root x >= 0 whose square is to keep its mean, by the high 16 bits of w.  (z - y)(z + y) of two neighbours has few bits and is exact in any
+// order.  LOW: x may be below 2^-6.
+template <bool LOW>
+__device__ __forceinline__ float root_to_e4m3(float x, uint32_t w) {
+    const float lift = LOW && x < 0.015625f ? 0.015625f : 0.0f;
+    const uint32_t bits = __float_as_uint(LOW ? __fadd_rn(x, lift) : x) & 0xFFF00000u;
     float y = __uint_as_float(bits), z = __uint_as_float(bits + 0x100000u);
-    y = low ? __fadd_rn(y, -0.015625f) : y;
-    z = low ? __fadd_rn(z, -0.015625f) : z;
-    const float part = __fmul_rn(__fmul_rn((float)u, 1.52587890625e-5f), __fmul_rn(__fadd_rn(z, -y), __fadd_rn(z, y)));
-    y = __fmul_rn(__fadd_rn(x, -y), __fadd_rn(x, y)) > part ? z : y;
-    return x > 0.0f ? fmaxf(y, 0.001953125f) : y;          // 2^-9 at least
+    if (LOW) {
+        y = __fadd_rn(y, -lift);
+        z = __fadd_rn(z, -lift);
+    }
+    const float u = __fadd_rn(__uint_as_float((w >> 9 & 0x7FFF80u) | 0x3F800000u), -1.0f);      // the 16 bits over 65,536
+    y = __fmul_rn(__fadd_rn(x, -y), __fadd_rn(x, y)) > __fmul_rn(u, __fmaf_rn(z, z, -__fmul_rn(y, y))) ? z : y;
+    return LOW && x > 0.0f ? fmaxf(y, 0.001953125f) : y;   // 2^-9 at least
 }
 
 __device__ __forceinline__ float sqrt_approx(float x) {
@@ -93,16 +109,6 @@ __device__ __forceinline__ void load4(const float* p, int64_t left, float (&x)[4
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = i < left ? p[i] : 0.0f;
-    }
-}
-template <bool VEC>
-__device__ __forceinline__ void load4(const uint16_t* p, int64_t left, float (&x)[4]) {
-    if (VEC && left >= 4) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = i < left ? load1(p + i) : 0.0f;
     }
 }
 template <bool VEC>
@@ -145,83 +151,123 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int64_t left, uint32_t w
     }
 }
 
-template <int N, int BITS, bool VEC>
-__device__ __forceinline__ void update(const Table<N>& tab, const Entry& e, int64_t block, float gs) {
+// A lane's eight elements of a block as they lie in memory.
+template <int BITS>
+struct Fetched {
+    float p[2][4], g[2][4];                  // g: the words of a bf16 gradient until `widen`
+    float m[2][4], v[2][4];                  // BITS 32
+    uint32_t mc[2], vc[2], mb, vb;           // BITS 8
+};
+
+template <int BITS, bool VEC>
+__device__ __forceinline__ void fetch(const Entry& e, int64_t block, Fetched<BITS>& f) {
     const int lane = threadIdx.x & 31;
-    const int64_t at[2] = {block * 256 + lane * 4, block * 256 + 128 + lane * 4};
-    float p[2][4], g[2][4], m[2][4], v[2][4];
-    uint32_t mc[2], vc[2];
-    uint32_t mb = 0, vb = 0;
     if (BITS == 8) {
-        mb = e.m_scale[block];
-        vb = e.v_scale[block];
+        f.mb = e.m_scale[block];
+        f.vb = e.v_scale[block];
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int64_t left = e.n - at[h];
-        load4<VEC>(e.param + at[h], left, p[h]);
-        if (e.flags & 1) load4<VEC>(static_cast<const uint16_t*>(e.grad) + at[h], left, g[h]);
-        else load4<VEC>(static_cast<const float*>(e.grad) + at[h], left, g[h]);
-        if (BITS == 32) {
-            load4<VEC>(static_cast<const float*>(e.m) + at[h], left, m[h]);
-            load4<VEC>(static_cast<const float*>(e.v) + at[h], left, v[h]);
+        const int64_t at = block * 256 + h * 128 + lane * 4, left = e.n - at;
+        load4<VEC>(e.param + at, left, f.p[h]);
+        if (!(e.flags & 1)) {
+            load4<VEC>(static_cast<const float*>(e.grad) + at, left, f.g[h]);
+        } else if (VEC && left >= 4) {
+            const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(e.grad) + at);
+            f.g[h][0] = __uint_as_float(w.x);
+            f.g[h][1] = __uint_as_float(w.y);
         } else {
-            mc[h] = load_codes<VEC>(static_cast<const uint8_t*>(e.m) + at[h], left);
-            vc[h] = load_codes<VEC>(static_cast<const uint8_t*>(e.v) + at[h], left);
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = i < left ? static_cast<const uint16_t*>(e.grad)[at + i] : 0u;
+            f.g[h][0] = __uint_as_float(w[0] | w[1] << 16);
+            f.g[h][1] = __uint_as_float(w[2] | w[3] << 16);
+        }
+        if (BITS == 32) {
+            load4<VEC>(static_cast<const float*>(e.m) + at, left, f.m[h]);
+            load4<VEC>(static_cast<const float*>(e.v) + at, left, f.v[h]);
+        } else {
+            f.mc[h] = load_codes<VEC>(static_cast<const uint8_t*>(e.m) + at, left);
+            f.vc[h] = load_codes<VEC>(static_cast<const uint8_t*>(e.v) + at, left);
         }
     }
+}
+
+template <int N, int BITS, bool VEC>
+__device__ __forceinline__ void update(const Table<N>& tab, const Entry& e, int64_t block, float gs, Fetched<BITS>& f) {
+    const int lane = threadIdx.x & 31;
     uint32_t m_top = 0, v_top = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if (BITS == 8) {
-            decode4(mc[h], __uint_as_float(mb << 23), m[h]);
-            decode4(vc[h], __uint_as_float(vb << 23), v[h]);
+            decode4(f.mc[h], __uint_as_float(f.mb << 23), f.m[h]);
+            decode4(f.vc[h], __uint_as_float(f.vb << 23), f.v[h]);
+        }
+        if (e.flags & 1) {
+            const uint32_t a = __float_as_uint(f.g[h][0]), b = __float_as_uint(f.g[h][1]);
+            f.g[h][0] = bf16_lo(a), f.g[h][1] = bf16_hi(a), f.g[h][2] = bf16_lo(b), f.g[h][3] = bf16_hi(b);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float x = tab.grad_scale ? __fmul_rn(g[h][i], gs) : g[h][i];
-            if (BITS == 8) v[h][i] = __fmul_rn(v[h][i], v[h][i]);
-            m[h][i] = __fadd_rn(__fmul_rn(m[h][i], tab.b1), __fmul_rn(x, tab.c1));
-            v[h][i] = __fadd_rn(__fmul_rn(v[h][i], tab.b2), __fmul_rn(__fmul_rn(x, x), tab.c2));
+            float &p = f.p[h][i], &m = f.m[h][i], &v = f.v[h][i];
+            const float x = tab.grad_scale ? __fmul_rn(f.g[h][i], gs) : f.g[h][i];
+            if (BITS == 8) v = __fmul_rn(v, v);
+            m = __fadd_rn(__fmul_rn(m, tab.b1), __fmul_rn(x, tab.c1));
+            v = __fadd_rn(__fmul_rn(v, tab.b2), __fmul_rn(__fmul_rn(x, x), tab.c2));
             // the step itself is nobody's border: quotient and root to two units of the last place
             float den;
             if (BITS == 8) {
-                v[h][i] = __fsqrt_rn(v[h][i]);
-                m_top = max(m_top, __float_as_uint(m[h][i]) & 0x7FFFFFFFu);
-                v_top = max(v_top, __float_as_uint(v[h][i]) & 0x7FFFFFFFu);
-                den = fmaf(v[h][i], tab.root, tab.eps);
+                v = __fsqrt_rn(v);
+                m_top = max(m_top, __float_as_uint(m) & 0x7FFFFFFFu);
+                v_top = max(v_top, __float_as_uint(v) & 0x7FFFFFFFu);
+                den = fmaf(v, tab.root, tab.eps);
             } else {
-                den = fmaf(sqrt_approx(v[h][i]), tab.root, tab.eps);
+                den = fmaf(sqrt_approx(v), tab.root, tab.eps);
             }
-            p[h][i] = fmaf(-tab.rate, __fdividef(m[h][i], den), __fmul_rn(p[h][i], e.keep));
+            p = fmaf(-tab.rate, __fdividef(m, den), __fmul_rn(p, e.keep));
         }
-        const int64_t left = e.n - at[h];
-        store4<VEC>(e.param + at[h], left, p[h]);
-        if (e.copy) store4<VEC>(e.copy + at[h], left, p[h]);
+        const int64_t at = block * 256 + h * 128 + lane * 4, left = e.n - at;
+        store4<VEC>(e.param + at, left, f.p[h]);
+        if (e.copy) store4<VEC>(e.copy + at, left, f.p[h]);
         if (BITS == 32) {
-            store4<VEC>(static_cast<float*>(e.m) + at[h], left, m[h]);
-            store4<VEC>(static_cast<float*>(e.v) + at[h], left, v[h]);
+            store4<VEC>(static_cast<float*>(e.m) + at, left, f.m[h]);
+            store4<VEC>(static_cast<float*>(e.v) + at, left, f.v[h]);
         }
     }
     if (BITS == 32) return;
     m_top = __reduce_max_sync(0xFFFFFFFFu, m_top);
     v_top = __reduce_max_sync(0xFFFFFFFFu, v_top);
-    mb = scale_byte(m_top);
-    vb = scale_byte(v_top);
+    const uint32_t mb = scale_byte(m_top), vb = scale_byte(v_top);
     const float mi = mb ? __uint_as_float((254u - mb) << 23) : 1.0f, vi = vb ? __uint_as_float((254u - vb) << 23) : 1.0f;
+    float least = 256.0f;                    // root: moments that nothing moved for long are rare
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f.v[h][i] = __fmul_rn(f.v[h][i], vi);
+            least = fminf(least, f.v[h][i]);
+        }
+    const bool low = __any_sync(0xFFFFFFFFu, !(least >= 0.015625f));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const Words4 w = draw(tab, (uint32_t)((block * 256 + h * 128) >> 2) + lane, e.index);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.m[h][i] = to_e4m3(__fmul_rn(f.m[h][i], mi), w.w[i]);
+        if (low) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.v[h][i] = root_to_e4m3<true>(f.v[h][i], w.w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.v[h][i] = root_to_e4m3<false>(f.v[h][i], w.w[i]);
+        }
+    }
+    // the codes of a block with an infinity or NaN are no numbers
     const bool numbers = max(m_top, v_top) < 0x7F800000u;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const Words4 w = philox4x32_10((uint32_t)(at[h] >> 2), e.index, tab.t_lo, tab.t_hi, tab.seed_lo, tab.seed_hi);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            m[h][i] = to_e4m3(__fmul_rn(m[h][i], mi), w.w[i] & 0xFFFFu);
-            v[h][i] = root_to_e4m3(__fmul_rn(v[h][i], vi), w.w[i] >> 16);
-        }
-        // the codes of a block with an infinity or NaN are no numbers
-        const int64_t left = e.n - at[h];
-        store_codes<VEC>(static_cast<uint8_t*>(e.m) + at[h], left, numbers ? encode4(m[h]) : 0x7F7F7F7Fu);
-        store_codes<VEC>(static_cast<uint8_t*>(e.v) + at[h], left, numbers ? encode4(v[h]) : 0x7F7F7F7Fu);
+        const int64_t at = block * 256 + h * 128 + lane * 4, left = e.n - at;
+        store_codes<VEC>(static_cast<uint8_t*>(e.m) + at, left, numbers ? encode4(f.m[h]) : 0x7F7F7F7Fu);
+        store_codes<VEC>(static_cast<uint8_t*>(e.v) + at, left, numbers ? encode4(f.v[h]) : 0x7F7F7F7Fu);
     }
     if (lane == 0) {
         e.m_scale[block] = (uint8_t)mb;
@@ -229,14 +275,40 @@ __device__ __forceinline__ void update(const Table<N>& tab, const Entry& e, int6
     }
 }
 
-template <int N, int BITS>
-__global__ void __launch_bounds__(kWarpsPerCta * 32) adamw_kernel(const __grid_constant__ Table<N> tab) {
-    int lo = 0, hi = tab.n;                  // the last entry with first <= blockIdx.x
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tab.e[mid].first <= blockIdx.x) lo = mid; else hi = mid;
+// A warp's blocks.  With fp32 moments the next one's loads are under way while one is worked on; with e4m3 ones, which take four times the arithmetic, the
+// registers are better spent on more warps.
+template <int N, int BITS, bool VEC>
+__device__ __forceinline__ void run(const Table<N>& tab, const Entry& e, int64_t block, float gs) {
+    constexpr int kBlocks = kPerCta / 256 / kWarpsPerCta;
+    Fetched<BITS> now, next;
+    if (block * 256 >= e.n) return;
+    if (BITS == 32) fetch<BITS, VEC>(e, block, now);
+#pragma unroll 1
+    for (int i = 0; i < kBlocks; ++i, block += kWarpsPerCta) {
+        const int64_t after = block + kWarpsPerCta;
+        const bool more = i + 1 < kBlocks && after * 256 < e.n;
+        if (BITS == 8) fetch<BITS, VEC>(e, block, now);
+        else if (more) fetch<BITS, VEC>(e, after, next);
+        update<N, BITS, VEC>(tab, e, block, gs, now);
+        if (!more) return;
+        if (BITS == 32) now = next;
     }
-    const Entry& e = tab.e[lo];
+}
+
+template <int N, int BITS>
+__global__ void __launch_bounds__(kWarpsPerCta * 32, BITS == 8 ? 5 : 3) adamw_kernel(const __grid_constant__ Table<N> tab) {
+    __shared__ Entry entry;                  // out of the parameters, where every access by a computed index would be a trip of its own
+    if (threadIdx.x < 32) {
+        int lo = 0, hi = tab.n;              // the last entry with first <= blockIdx.x
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (tab.e[mid].first <= blockIdx.x) lo = mid; else hi = mid;
+        }
+        const uint32_t* from = reinterpret_cast<const uint32_t*>(&tab.e[lo]);
+        if (threadIdx.x < sizeof(Entry) / 4) reinterpret_cast<uint32_t*>(&entry)[threadIdx.x] = from[threadIdx.x];
+    }
+    __syncthreads();
+    const Entry& e = entry;
     const int64_t block = (int64_t)(blockIdx.x - e.first) * (kPerCta / 256) + (threadIdx.x >> 5);
     grid_dependency_wait();
     grid_dependency_release();
@@ -245,13 +317,8 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) adamw_kernel(const __grid_c
         gs = *tab.grad_scale;
         if (!(fabsf(gs) < INFINITY)) return;
     }
-#pragma unroll 1
-    for (int i = 0; i < kPerCta / 256 / kWarpsPerCta; ++i) {
-        const int64_t b = block + i * kWarpsPerCta;
-        if (b * 256 >= e.n) return;
-        if (e.flags & 2) update<N, BITS, true>(tab, e, b, gs);
-        else update<N, BITS, false>(tab, e, b, gs);
-    }
+    if (e.flags & 2) run<N, BITS, true>(tab, e, block, gs);
+    else run<N, BITS, false>(tab, e, block, gs);
 }
 
 template <int N, int BITS>
@@ -268,8 +335,10 @@ aa_status launch_some(aa_ctx_impl* c, const aa_adamw_tensor* t, int64_t count, c
     tab.eps = (float)r->eps;
     tab.t_lo = (uint32_t)(r->t + 1);
     tab.t_hi = (uint32_t)((uint64_t)(r->t + 1) >> 32);
-    tab.seed_lo = (uint32_t)r->seed;
-    tab.seed_hi = (uint32_t)(r->seed >> 32);
+    for (int i = 0; i < 10; ++i) {
+        tab.keys[2 * i] = (uint32_t)r->seed + (uint32_t)i * 0x9E3779B9u;
+        tab.keys[2 * i + 1] = (uint32_t)(r->seed >> 32) + (uint32_t)i * 0xBB67AE85u;
+    }
     tab.grad_scale = grad_scale;
     int64_t at = 0;
     while (at < count) {
