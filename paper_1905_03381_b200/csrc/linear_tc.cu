@@ -40,6 +40,36 @@ struct Ctl {
     int abort_flag;
 };
 
+// A lane's part of a 32 x 32 chunk out of the warp's stage: four columns of rows r8, r8 + 4, ... below `rows`.  Steps are four rows, in elements.
+template <int ACT>
+__device__ __forceinline__ void put_chunk(uint32_t stage, int sub, int r8, int rows, const float (&bias)[4], bool some, const uint2 (&add)[8], uint16_t* to, int64_t step,
+                                          uint16_t* raw, int64_t raw_step) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        float z[4];
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(z[0]), "=f"(z[1]), "=f"(z[2]), "=f"(z[3])
+                     : "r"(stage + (uint32_t)(q * 512 + ((sub ^ ((q * 4 + r8) & 7)) << 4)))
+                     : "memory");
+        if (q * 4 + r8 < rows) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] += bias[e];
+            if (raw) *reinterpret_cast<uint2*>(raw) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = activate<ACT>(z[e]);
+            if (some) {
+                z[0] += bf16_lo(add[q].x);
+                z[1] += bf16_hi(add[q].x);
+                z[2] += bf16_lo(add[q].y);
+                z[3] += bf16_hi(add[q].y);
+            }
+            *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
+        }
+        to += step;
+        if (raw) raw += raw_step;
+    }
+}
+
 // SUMS: the sums of A over the contraction, too (A's slices are in shared memory already; another pass over A would cost as much as reading it).  Two warps,
 // idle otherwise, add up the slice's 128 columns once the products have read it and hand the stage back with them.
 // JOIN (single CTAs): the parts of a tile are the CTAs of a cluster, as in linear_plan.cuh; a CTA has one unit then.
@@ -295,9 +325,11 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 #pragma unroll
                     for (int q = 0; q < 8; ++q) add[q] = make_uint2(0, 0);
                 }
-                float bias[4];
+                float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (p.bias) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) bias[e] = p.bias && col + e < p.n ? p.bias[col + e] : 0.0f;
+                    for (int e = 0; e < 4; ++e) bias[e] = col + e < p.n ? p.bias[col + e] : 0.0f;
+                }
                 uint32_t v[32];
                 if (some) {
                     tmem_ld_32cols(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2) + c * 32), v);
@@ -335,20 +367,13 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     continue;
                 }
                 if (whole) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const int r = q * 4 + r8;
-                        const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
-                        float z[4] = {f.x + bias[0], f.y + bias[1], f.z + bias[2], f.w + bias[3]};
-                        if (r >= rows) continue;
-                        if (pre) *reinterpret_cast<uint2*>(pre + (row0 + q * 4) * p.pre.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
-                        activate_all(z, p.act);
-                        z[0] += bf16_lo(add[q].x);
-                        z[1] += bf16_hi(add[q].x);
-                        z[2] += bf16_lo(add[q].y);
-                        z[3] += bf16_hi(add[q].y);
-                        *reinterpret_cast<uint2*>(out + (row0 + q * 4) * p.out.stride + col) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
-                    }
+                    const uint32_t at = smem_u32(mine + r8 * 32);
+                    uint16_t* to = out + row0 * p.out.stride + col;
+                    uint16_t* raw = pre ? pre + row0 * p.pre.stride + col : nullptr;
+                    if (p.act == AA_ACT_NONE) put_chunk<AA_ACT_NONE>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
+                    else if (p.act == AA_ACT_RELU) put_chunk<AA_ACT_RELU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
+                    else if (p.act == AA_ACT_GELU) put_chunk<AA_ACT_GELU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
+                    else put_chunk<AA_ACT_SILU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
                 } else {
 #pragma unroll 1
                     for (int q = 0; q < 8; ++q) {
