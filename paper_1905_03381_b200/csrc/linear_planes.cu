@@ -73,7 +73,7 @@ product_planes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                     ok = false;
                     break;
                 }
-                if (lane == 0) {
+                if (elect_one()) {
                     unsigned char* a = ring + (size_t)stage * kStage;
                     unsigned char* b = a + kTerms * kPlaneA;
                     const uint32_t bar = of_rank(&ctl.full[stage], 0);
@@ -106,6 +106,7 @@ product_planes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
     } else if (warp == 1) {
         // ---- issuer
         constexpr uint32_t idesc = umma_idesc_bf16(2 * kM, kBN, A_ACROSS, B_ACROSS);
+        const uint64_t a_desc = umma_smem_desc(smem_u32(ring), A_ACROSS ? 8192 : 16, 1024), b_desc = umma_smem_desc(smem_u32(ring) + kTerms * kPlaneA, B_ACROSS ? 8192 : 16, 1024);
         uint32_t sent = 0;
         int it = 0;
         for (int i = first; i < units && ok && rank == 0; i += step) {
@@ -122,12 +123,14 @@ product_planes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 }
                 tc_fence_after_sync();
                 const bool end = in_run == kRun - 1 || s == u.s1 - 1;
-                if (lane == 0) {
-                    const uint32_t d = tmem + (uint32_t)((it & 1) * kAcc), a = smem_u32(ring + (size_t)stage * kStage), b = a + kTerms * kPlaneA;
+                if (elect_one()) {
+                    const uint32_t d = tmem + (uint32_t)((it & 1) * kAcc);
+                    // the address is the descriptor's low field, in units of 16 bytes
+                    const uint64_t at = (uint64_t)(uint32_t)(stage * (kStage >> 4));
 #pragma unroll
                     for (int k = 0; k < kSlice / 16; ++k) {
-                        const auto ad = [&](int t) { return A_ACROSS ? umma_smem_desc(a + t * kPlaneA + k * 2048, 8192, 1024) : umma_smem_desc(a + t * kPlaneA + k * 32, 16, 1024); };
-                        const auto bd = [&](int t) { return B_ACROSS ? umma_smem_desc(b + t * kPlaneB + k * 2048, 8192, 1024) : umma_smem_desc(b + t * kPlaneB + k * 32, 16, 1024); };
+                        const auto ad = [&](int t) { return a_desc + at + (uint64_t)(t * (kPlaneA >> 4) + (A_ACROSS ? k * 128 : k * 2)); };
+                        const auto bd = [&](int t) { return b_desc + at + (uint64_t)(t * (kPlaneB >> 4) + (B_ACROSS ? k * 128 : k * 2)); };
                         const bool more = (in_run | k) != 0;
                         mma<2>(d, ad(0), bd(0), idesc, more);
                         mma<2>(d + kBN, ad(0), bd(2), idesc, more);
@@ -144,7 +147,7 @@ product_planes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
             }
         }
         if (rank == 0) {
-            if (lane == 0) commit<2>(&ctl.drain);
+            if (elect_one()) commit<2>(&ctl.drain);
             __syncwarp();
         }
         // both CTAs' memory is read until the last product is done

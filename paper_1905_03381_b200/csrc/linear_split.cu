@@ -199,6 +199,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
         };
         // products of slice number `issued` of this CTA, by the first warp
         constexpr uint32_t idesc = umma_idesc_bf16(kTile, kTile, A_ACROSS, B_ACROSS);
+        const uint64_t a_desc = umma_smem_desc(smem_u32(ring), A_ACROSS ? 8192 : 16, 1024), b_desc = umma_smem_desc(smem_u32(ring) + S::OPERAND, B_ACROSS ? 8192 : 16, 1024);
         uint32_t issued = 0;
         int in_run = 0, it = 0, of = blockIdx.x, togo = 0;
         const auto issue = [&]() -> bool {
@@ -212,12 +213,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], (issued / kStages) & 1u, abort_flag))) return false;
             tc_fence_after_sync();
             const bool last = in_run == kRun - 1 || togo == 1;
-            if (lane == 0) {
-                const uint32_t d = tmem + (uint32_t)((it & 1) * S::ACC), a = smem_u32(ring + (size_t)stage * S::STAGE), b = a + S::OPERAND;
+            if (elect_one()) {
+                const uint32_t d = tmem + (uint32_t)((it & 1) * S::ACC);
+                // the address is the descriptor's low field, in units of 16 bytes
+                const uint64_t at = (uint64_t)(uint32_t)(stage * (S::STAGE >> 4));
 #pragma unroll
                 for (int k = 0; k < kSlice / 16; ++k) {
-                    const auto ad = [&](int t) { return A_ACROSS ? umma_smem_desc(a + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(a + t * kTermBytes + k * 32, 16, 1024); };
-                    const auto bd = [&](int t) { return B_ACROSS ? umma_smem_desc(b + t * kTermBytes + k * 2048, 8192, 1024) : umma_smem_desc(b + t * kTermBytes + k * 32, 16, 1024); };
+                    const auto ad = [&](int t) { return a_desc + at + (uint64_t)(t * (kTermBytes >> 4) + (A_ACROSS ? k * 128 : k * 2)); };
+                    const auto bd = [&](int t) { return b_desc + at + (uint64_t)(t * (kTermBytes >> 4) + (B_ACROSS ? k * 128 : k * 2)); };
                     const bool more = (in_run | k) != 0;
                     umma_bf16(d, ad(0), bd(0), idesc, more);
                     if (TERMS == 3) {
@@ -273,7 +276,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
             if (warp == 0) ok = issue();
         }
         if (warp == 0) {
-            if (lane == 0) umma_commit(&ctl.drain);
+            if (elect_one()) umma_commit(&ctl.drain);
             __syncwarp();
             const long long t0 = clock64();
             while (!mbar_try_wait(&ctl.drain, 0) && clock64() - t0 < kWaitCycles) {

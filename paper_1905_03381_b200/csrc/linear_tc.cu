@@ -131,7 +131,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     ok = false;
                     break;
                 }
-                if (lane == 0) {
+                if (elect_one()) {
                     unsigned char* a = ring + (size_t)stage * G::STAGE;
                     unsigned char* b = a + G::A;
                     uint64_t* bar = &ctl.full[stage];
@@ -171,6 +171,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     } else if (warp == 1) {
         // ---- issuer; in the second CTA it only clears what lies behind the last token
         constexpr uint32_t idesc = umma_idesc_bf16(CG * kBM, BN, A_ACROSS, B_ACROSS);
+        const uint64_t a_desc = umma_smem_desc(smem_u32(ring), A_ACROSS ? 8192 : 16, 1024), b_desc = umma_smem_desc(smem_u32(ring) + G::A, B_ACROSS ? 8192 : 16, 1024);
         int it = 0;
         uint32_t sent = 0, ragged = 0;
         for (int i = first; i < units && ok; i += step) {
@@ -214,14 +215,11 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 }
                 if (rank == 0) {
                     tc_fence_after_sync();
-                    if (lane == 0) {
-                        const uint32_t a = smem_u32(at), b = a + G::A;
+                    if (elect_one()) {
+                        // the address is the descriptor's low field, in units of 16 bytes
+                        const uint64_t ad = a_desc + (uint64_t)(uint32_t)(stage * (G::STAGE >> 4)), bd = b_desc + (uint64_t)(uint32_t)(stage * (G::STAGE >> 4));
 #pragma unroll
-                        for (int k = 0; k < kSlice / 16; ++k) {
-                            const uint64_t ad = A_ACROSS ? umma_smem_desc(a + k * 2048, 8192, 1024) : umma_smem_desc(a + k * 32, 16, 1024);
-                            const uint64_t bd = B_ACROSS ? umma_smem_desc(b + k * 2048, 8192, 1024) : umma_smem_desc(b + k * 32, 16, 1024);
-                            mma<CG>(d, ad, bd, idesc, s > u.s0 || k > 0);
-                        }
+                        for (int k = 0; k < kSlice / 16; ++k) mma<CG>(d, ad + (A_ACROSS ? k * 128 : k * 2), bd + (B_ACROSS ? k * 128 : k * 2), idesc, s > u.s0 || k > 0);
                         commit<CG>(&ctl.empty[stage]);
                         if (SUMS) commit<CG>(&ctl.done[stage]);
                         if (s == u.s1 - 1) commit<CG>(&ctl.acc_full[buf]);
@@ -231,7 +229,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             }
         }
         if (rank == 0) {
-            if (lane == 0) commit<CG>(&ctl.drain);
+            if (elect_one()) commit<CG>(&ctl.drain);
             __syncwarp();
         }
         // both CTAs' memory is read until the last product is done
