@@ -19,7 +19,8 @@ namespace aa {
 namespace {
 
 constexpr int kBM = 128;
-constexpr int kTcThreads = 384;          // producer, issuer, two for column sums (the first of them allocates), eight for the epilogue
+constexpr int kTcThreads = 384;          // producer, issuer, allocator, an idle warp, eight for the epilogue
+constexpr int kSumThreads = 512;         // and four for column sums
 constexpr int kEpilogue = 8;
 constexpr int kStageFloats = 32 * 32;    // per epilogue warp
 constexpr int kMaxStages = 8;
@@ -70,11 +71,11 @@ __device__ __forceinline__ void put_chunk(uint32_t stage, int sub, int r8, int r
     }
 }
 
-// SUMS: the sums of A over the contraction, too (A's slices are in shared memory already; another pass over A would cost as much as reading it).  Two warps,
-// idle otherwise, add up the slice's 128 columns once the products have read it and hand the stage back with them.
+// SUMS: the sums of A over the contraction, too (A's slices are in shared memory already; another pass over A would cost as much as reading it).  Four
+// warps add up the slice's 128 columns once the products have read it and hand the stage back with them (two warps took longer than the products).
 // JOIN (single CTAs): the parts of a tile are the CTAs of a cluster, as in linear_plan.cuh; a CTA has one unit then.
 template <int CG, int BN, bool A_ACROSS, bool B_ACROSS, bool SUMS, bool JOIN>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(SUMS ? kSumThreads : kTcThreads, 1)
 product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan,
                   bool vec) {
     using G = Geo<CG, BN>;
@@ -90,7 +91,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (threadIdx.x == 0) {
         for (int s = 0; s < G::STAGES; ++s) {
             mbar_init(&ctl.full[s], 1);      // both CTAs' copies count on the first one's
-            mbar_init(&ctl.empty[s], SUMS ? 3 : 1);
+            mbar_init(&ctl.empty[s], SUMS ? 5 : 1);
             mbar_init(&ctl.done[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -236,53 +237,52 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const long long t0 = clock64();
         while (!mbar_try_wait(&ctl.drain, 0) && clock64() - t0 < kWaitCycles) {
         }
-    } else if (SUMS && warp < 4) {
-        // ---- column sums: warp 2 the first 64 columns of the CTA's 128, warp 3 the others; a lane takes 8 columns of every fourth token
-        const int chunk = warp - 2, unit = lane & 7, r4 = lane >> 3;
+    } else if (SUMS && warp >= 12) {
+        // ---- column sums: 64 of the CTA's 128 columns and half of the tokens a warp; a lane takes 8 columns of every fourth token
+        const int chunk = warp & 1, part = (warp >> 1) & 1, unit = lane & 7, r4 = lane >> 3;
+        __shared__ float halves[2][kBM];
         uint32_t sent = 0;
-        for (int i = first; i < units && ok; i += step) {
+        // a warp that gave up still meets the others at their barriers
+        for (int i = first; i < units; i += step) {
             const Unit u = unit_at(plan, mt, slices, i);
             float sum[8] = {};
-            for (int s = u.s0; s < u.s1; ++s, ++sent) {
+            for (int s = u.s0; s < u.s1 && ok; ++s, ++sent) {
                 const int stage = (int)(sent % G::STAGES);
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.done[stage], (sent / G::STAGES) & 1u, abort_flag))) {
-                    ok = false;
-                    break;
-                }
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ctl.done[stage], (sent / G::STAGES) & 1u, abort_flag));
+                if (!ok) break;
                 if (u.n == 0) {              // the tiles of a row of tiles share A
-                    const unsigned char* at = ring + (size_t)stage * G::STAGE + chunk * 8192;
-                    float part[8] = {};
+                    const unsigned char* at = ring + (size_t)stage * G::STAGE + chunk * 8192 + part * 4096;
+                    float some[8] = {};
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) {
+                    for (int q = 0; q < 8; ++q) {
                         const int r = q * 4 + r4;
                         float x[8];
                         Vec<uint16_t>::unpack(*reinterpret_cast<const uint4*>(at + r * 128 + ((unit ^ (r & 7)) << 4)), x);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) part[e] += x[e];
+                        for (int e = 0; e < 8; ++e) some[e] += x[e];
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] += part[e];
+                    for (int e = 0; e < 8; ++e) sum[e] += some[e];
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl.empty[stage]);
             }
-            if (!ok || u.n != 0) continue;
+            if (u.n != 0) continue;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 8);
                 sum[e] += __shfl_xor_sync(0xFFFFFFFFu, sum[e], 16);
+                if (r4 == 0) halves[part][chunk * 64 + unit * 8 + e] = sum[e];
             }
-            if (r4 == 0) {
-                const int at = chunk * 64 + unit * 8;
-                const int64_t row = ((int64_t)u.m * CG + rank) * kBM + at;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (u.part >= 0) plan.sum_parts[((int64_t)u.part * CG + rank) * kBM + at + e] = sum[e];
-                    else if (row + e < p.m) p.a_sums[row + e] = sum[e];
-                }
-            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            const int at = (int)threadIdx.x - 384;
+            const int64_t row = ((int64_t)u.m * CG + rank) * kBM + at;
+            const float total = halves[0][at] + halves[1][at];
+            if (u.part >= 0) plan.sum_parts[((int64_t)u.part * CG + rank) * kBM + at] = total;
+            else if (row < p.m) p.a_sums[row] = total;
+            asm volatile("bar.sync 1, 128;" ::: "memory");
         }
-    } else if (warp >= 4) {
+    } else if (warp >= 4 && warp < 12) {
         // ---- epilogue
         const int quad = warp & 3, half = (warp - 4) >> 2;
         float* mine = stage_f + (warp - 4) * kStageFloats;
@@ -413,6 +413,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 template <int CG, int BN, bool AA, bool BA, bool SUMS, bool JOIN>
 aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     using G = Geo<CG, BN>;
+    constexpr int kThreads = SUMS ? kSumThreads : kTcThreads;
     ProductParams p = in;
     alignas(64) CUtensorMap map_a, map_b;
     const int64_t a_rows = AA ? p.k : p.m, a_cols = AA ? p.m : p.k, b_rows = BA ? p.k : p.n, b_cols = BA ? p.n : p.k;
@@ -422,13 +423,13 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     const int64_t mt = (p.m + CG * kBM - 1) / (CG * kBM), nt = (p.n + BN - 1) / BN, tiles = mt * nt;
     const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA, SUMS, JOIN>;
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
-    const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kTcThreads, G::SMEM, CG);
+    const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kThreads, G::SMEM, CG);
     if (teams < 1) return AA_ERR_CUDA;
     Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2, JOIN);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     void* args[] = {&map_a, &map_b, &p, &plan, &vec};
     const int cluster = JOIN ? plan.cluster : CG;
-    if (launch_clusters(c, kernel, (unsigned)(JOIN ? units : (units < teams ? units : teams) * CG), kTcThreads, args, G::SMEM, cluster) != cudaSuccess) return AA_ERR_CUDA;
+    if (launch_clusters(c, kernel, (unsigned)(JOIN ? units : (units < teams ? units : teams) * CG), kThreads, args, G::SMEM, cluster) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     if (tail == 0 || JOIN) return AA_OK;
     void* join[] = {&p, &plan, &vec};
