@@ -75,6 +75,17 @@ aa_status check_linear(const aa_rows* x, const aa_rows* w) {
 }  // namespace
 }  // namespace aa
 
+namespace aa {
+
+// Up to 16 rows of a forward call straight from memory; bf16 operands that TMA can fetch by TMA; the others by the kernel that takes its operands apart on the way.
+aa_status launch_product(aa_ctx_impl* c, const ProductParams& p, int dtype) {
+    if (product_few_fits(p)) return launch_product_few(c, p, dtype);
+    if (dtype == AA_BF16 && product_tc_fits(p)) return launch_product_tc(c, p);
+    return launch_product_split(c, p, dtype);
+}
+
+}  // namespace aa
+
 using namespace aa;
 
 extern "C" {
