@@ -152,19 +152,51 @@ struct Slot {
     }
 };
 
+// The same for rows that start anywhere (V = 1, groups of whole warps): a warp has 32 E neighbouring columns, lane l those numbered l, l + 32, ...; it fetches
+// the 16-byte words that cover them and finds its elements behind a shift.  Words that reach beyond the row lie in the matrix all the same
+// (`lo`, `hi`: its ends); the few that do not are fetched element by element.
+template <typename T, int E, int TH>
+struct Shifted {
+    static constexpr int WARP = 32 * E * (int)sizeof(T) + 16, BYTES = TH / 32 * WARP;
+    __device__ static __forceinline__ void fetch(char* at, const T* seg, int n, const char* lo, const char* hi) {
+        if (n <= 0) return;
+        const uint32_t shift = (uint32_t)(uintptr_t)seg & 15u;
+        const char* from = reinterpret_cast<const char*>(seg) - shift;
+        char* to = at + (threadIdx.x >> 5) * WARP;
+        const int words = ((n < 32 * E ? n : 32 * E) * (int)sizeof(T) + (int)shift + 15) / 16;
+        for (int j = threadIdx.x & 31; j < words; j += 32) {
+            const char* src = from + j * 16;
+            if (src >= lo && src + 16 <= hi) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + j * 16)), "l"(src) : "memory");
+            } else {
+                for (int e = 0; e < 16; e += (int)sizeof(T))
+                    if (src + e >= lo && src + e + (int)sizeof(T) <= hi) *reinterpret_cast<T*>(to + j * 16 + e) = *reinterpret_cast<const T*>(src + e);
+            }
+        }
+    }
+    __device__ static __forceinline__ void read(const char* at, const T* seg, Raw<T, 1, E>& x) {
+        const T* from = reinterpret_cast<const T*>(at + (threadIdx.x >> 5) * WARP + ((uint32_t)(uintptr_t)seg & 15u)) + (threadIdx.x & 31);
+#pragma unroll
+        for (int i = 0; i < E; ++i) x.w[i] = from[32 * i];
+    }
+};
+
 // AHEAD rows of a group are under way while one is worked on, 150 KB an SM at three (a row's worth of registers would be half of that and too little at
-// the latency of a busy memory).  0: single bf16 numbers, which asynchronous copies cannot fetch; they are loaded when they are needed.
+// the latency of a busy memory).
 template <typename T, int V, int E, int G, int AHEAD>
 __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_kernel(NormParams p) {
     constexpr int TH = kThreadsOf<G>, N = E / V, RING = AHEAD + 1;
+    constexpr bool SHIFT = V == 1;
     using S = Slot<T, V, E, TH>;
+    using U = Shifted<T, E, TH>;
+    constexpr int BYTES = SHIFT ? U::BYTES : S::BYTES;
     __shared__ float2 buf[2][32];
     extern __shared__ __align__(16) char ring[];     // [RING][x, dout, residual]; at the end the column sums
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
     const int l = threadIdx.x % G, groups = TH / G;
-    const int cols = (int)p.cols, first = l * V, step = G * V;
+    const int cols = (int)p.cols, seg = (l & ~31) * E, first = SHIFT ? seg + (l & 31) : l * V, step = SHIFT ? 32 : G * V;
     const float inv = 1.0f / (float)cols;
     float gm[E], dg[E], db[E];
 #pragma unroll
@@ -177,56 +209,54 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_
     // the lanes of a warp keep step: rows past the end are looked at as the last one and not written
     const int64_t mine = (int64_t)blockIdx.x * groups + threadIdx.x / G;
     Raw<T, V, E> x, d, res;
+    const auto row_of = [&](const MatArg& m, int64_t row) { return static_cast<const T*>(m.data) + row * m.stride; };
+    const auto end_of = [&](const MatArg& m) { return reinterpret_cast<const char*>(row_of(m, live - 1) + cols); };
+    const auto fetch_one = [&](char* at, const MatArg& m, int64_t row) {
+        if constexpr (SHIFT) U::fetch(at, row_of(m, row) + seg, cols - seg, static_cast<const char*>(m.data), end_of(m));
+        else S::fetch(at, row_of(m, row), first, step, cols);
+    };
     const auto fetch = [&](int64_t r, int slot) {
         const int64_t row = min(r, live - 1);
-        const T *px = static_cast<const T*>(p.x.data) + row * p.x.stride, *pd = static_cast<const T*>(p.dout.data) + row * p.dout.stride;
-        const T* pr = p.residual.data ? static_cast<const T*>(p.residual.data) + row * p.residual.stride : nullptr;
-        if constexpr (AHEAD > 0) {
-            char* at = ring + slot * 3 * S::BYTES;
-            S::fetch(at, px, first, step, cols);
-            S::fetch(at + S::BYTES, pd, first, step, cols);
-            if (pr) S::fetch(at + 2 * S::BYTES, pr, first, step, cols);
-        } else {
-            x.fetch(px, first, step, cols);
-            d.fetch(pd, first, step, cols);
-            if (pr) res.fetch(pr, first, step, cols);
-        }
+        char* at = ring + slot * 3 * BYTES;
+        fetch_one(at, p.x, row);
+        fetch_one(at + BYTES, p.dout, row);
+        if (p.residual.data) fetch_one(at + 2 * BYTES, p.residual, row);
+    };
+    const auto read_one = [&](const char* at, const MatArg& m, int64_t row, Raw<T, V, E>& w) {
+        if constexpr (SHIFT) U::read(at, row_of(m, row) + seg, w);
+        else S::read(at, w);
     };
     // a group goes on while the first of its warp's rows does
     const int64_t lead = G >= 32 ? mine : (int64_t)blockIdx.x * groups + (threadIdx.x & ~31) / G;
     int slot = 0;
-    if constexpr (AHEAD > 0) {
+    if constexpr (!SHIFT) {
 #pragma unroll
-        for (int a = 0; a < RING; ++a)
+        for (int a = 0; a < 3 * RING; ++a) S::clear(ring + a * BYTES);
+    }
 #pragma unroll
-            for (int o = 0; o < 3; ++o) S::clear(ring + (3 * a + o) * S::BYTES);
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            if (lead + a * jump < live) fetch(mine + a * jump, a);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
+    for (int a = 0; a < AHEAD; ++a) {
+        if (lead + a * jump < live) fetch(mine + a * jump, a);
+        asm volatile("cp.async.commit_group;" ::: "memory");
     }
     for (int64_t r = 0; lead + r < live; r += jump) {
         const int64_t row = mine + r;
         const bool on = G >= 32 || row < live;
-        if constexpr (AHEAD > 0) {
-            if (lead + r + AHEAD * jump < live) fetch(row + AHEAD * jump, slot >= 1 ? slot - 1 : AHEAD);
-            asm volatile("cp.async.commit_group;\n\tcp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
-            const char* at = ring + slot * 3 * S::BYTES;
-            S::read(at, x);
-            S::read(at + S::BYTES, d);
-            if (p.residual.data) S::read(at + 2 * S::BYTES, res);
-            slot = slot == AHEAD ? 0 : slot + 1;
-        } else {
-            fetch(row, 0);
-        }
+        if (SHIFT) __syncwarp();             // the slot's readers are done
+        if (lead + r + AHEAD * jump < live) fetch(row + AHEAD * jump, slot >= 1 ? slot - 1 : AHEAD);
+        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+        if (SHIFT) __syncwarp();
+        const char* at = ring + slot * 3 * BYTES;
+        read_one(at, p.x, row, x);
+        read_one(at + BYTES, p.dout, row, d);
+        if (p.residual.data) read_one(at + 2 * BYTES, p.residual, row, res);
+        slot = slot == AHEAD ? 0 : slot + 1;
         float v[E], u[E];
         float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             x.values(i, v + i * V);
             d.values(i, u + i * V);
-            if constexpr (AHEAD == 0) {
+            if constexpr (SHIFT) {
                 const bool has = first + i * step < cols;
                 v[i] = has ? v[i] : 0.0f;
                 u[i] = has ? u[i] : 0.0f;
@@ -458,9 +488,9 @@ template <typename T, int V, int E, int G>
 aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
     constexpr int TH = kThreadsOf<G>, groups = TH / G;
     // as many rows ahead as an SM's shared memory holds
-    constexpr int AHEAD = V == 1 && sizeof(T) == 2 ? 0 : (E * sizeof(T) <= 32 ? 3 : 1);
+    constexpr int AHEAD = E * sizeof(T) <= 32 ? 3 : (E == 12 ? 2 : 1);
     const void* kernel = grad ? (const void*)norm_grad_kernel<T, V, E, G, AHEAD> : (const void*)norm_kernel<T, V, E, G>;
-    const size_t sums = TH == G ? 0 : 2 * sizeof(float) * E * TH, slots = AHEAD ? (AHEAD + 1) * 3 * (size_t)Slot<T, V, E, TH>::BYTES : 0;
+    const size_t sums = TH == G ? 0 : 2 * sizeof(float) * E * TH, slots = (AHEAD + 1) * 3 * (size_t)(V == 1 ? Shifted<T, E, TH>::BYTES : Slot<T, V, E, TH>::BYTES);
     const size_t smem = !grad ? 0 : (sums > slots ? sums : slots);
     if (smem && allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     int ctas = resident_ctas(c, kernel, TH, smem);
@@ -475,30 +505,33 @@ aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
     return AA_OK;
 }
 
-// The smallest group whose threads have 16 columns of packed bf16 each, or 8 others (more where no group is that wide).
+// The smallest group whose threads have 16 columns of bf16 each, or 8 of fp32 (more where no group is that wide).
 template <typename T, int V>
 aa_status launch_width(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
-    if constexpr (V == 8) {
+    if constexpr (V == 1) {                  // whole warps, see Shifted
+        if (p.cols <= 128) return launch_rows<T, V, 4, 32>(c, p, grad, n);
+        if (p.cols <= 256) return launch_rows<T, V, 8, 32>(c, p, grad, n);
+    } else if constexpr (V == 8) {
         if (p.cols <= 128) return launch_rows<T, V, 16, 8>(c, p, grad, n);
         if (p.cols <= 256) return launch_rows<T, V, 16, 16>(c, p, grad, n);
+    } else {
+        if (p.cols <= 128) return launch_rows<T, V, 8, 16>(c, p, grad, n);
+        if (p.cols <= 256) return launch_rows<T, V, 8, 32>(c, p, grad, n);
+    }
+    if constexpr (sizeof(T) == 2) {
         if (p.cols <= 512) return launch_rows<T, V, 16, 32>(c, p, grad, n);
         if (p.cols <= 1024) return launch_rows<T, V, 16, 64>(c, p, grad, n);
         if (p.cols <= 2048) return launch_rows<T, V, 16, 128>(c, p, grad, n);
         if (p.cols <= 4096) return launch_rows<T, V, 16, 256>(c, p, grad, n);
-        return launch_rows<T, V, 16, 512>(c, p, grad, n);
     } else {
-        if (p.cols <= 128) return launch_rows<T, V, 8, 16>(c, p, grad, n);
-        if (p.cols <= 256) return launch_rows<T, V, 8, 32>(c, p, grad, n);
         if (p.cols <= 512) return launch_rows<T, V, 8, 64>(c, p, grad, n);
         if (p.cols <= 1024) return launch_rows<T, V, 8, 128>(c, p, grad, n);
         if (p.cols <= 2048) return launch_rows<T, V, 8, 256>(c, p, grad, n);
         if (p.cols <= 4096) return launch_rows<T, V, 8, 512>(c, p, grad, n);
-        if constexpr (sizeof(T) == 4)
-            if (p.cols <= 6144) return launch_rows<T, V, 12, 512>(c, p, grad, n);
-        return launch_rows<T, V, 16, 512>(c, p, grad, n);
+        if (p.cols <= 6144) return launch_rows<T, V, 12, 512>(c, p, grad, n);
     }
+    return launch_rows<T, V, 16, 512>(c, p, grad, n);
 }
-
 
 template <typename T, int V>
 aa_status launch_sweeps(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
