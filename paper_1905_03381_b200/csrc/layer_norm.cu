@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_kerne
         }
         if (r0 + jump < live) fetch(r0 + jump);
 #pragma unroll
-        for (int j = 0; j < E; j += 4) s.x += (v[j] + v[j + 1]) + (v[j + 2] + v[j + 3]);
+        for (int j = 0; j < E; ++j) s.x += v[j];
         const float mean = __fdiv_rn(group_sum<G>(s, buf[0]).x, (float)cols);     // exact for constant rows
         s = make_float2(0.0f, 0.0f);
 #pragma unroll
@@ -164,9 +164,10 @@ struct Shifted {
         const char* from = reinterpret_cast<const char*>(seg) - shift;
         char* to = at + (threadIdx.x >> 5) * WARP;
         const int words = ((n < 32 * E ? n : 32 * E) * (int)sizeof(T) + (int)shift + 15) / 16;
+        const bool inside = from >= lo && from + words * 16 <= hi;
         for (int j = threadIdx.x & 31; j < words; j += 32) {
             const char* src = from + j * 16;
-            if (src >= lo && src + 16 <= hi) {
+            if (inside || (src >= lo && src + 16 <= hi)) {
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + j * 16)), "l"(src) : "memory");
             } else {
                 for (int e = 0; e < 16; e += (int)sizeof(T))
@@ -488,7 +489,7 @@ template <typename T, int V, int E, int G>
 aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
     constexpr int TH = kThreadsOf<G>, groups = TH / G;
     // as many rows ahead as an SM's shared memory holds
-    constexpr int AHEAD = E * sizeof(T) <= 32 ? 3 : (E == 12 ? 2 : 1);
+    constexpr int AHEAD = E * sizeof(T) <= 36 ? 3 : (E * sizeof(T) <= 48 ? 2 : 1);
     const void* kernel = grad ? (const void*)norm_grad_kernel<T, V, E, G, AHEAD> : (const void*)norm_kernel<T, V, E, G>;
     const size_t sums = TH == G ? 0 : 2 * sizeof(float) * E * TH, slots = (AHEAD + 1) * 3 * (size_t)(V == 1 ? Shifted<T, E, TH>::BYTES : Slot<T, V, E, TH>::BYTES);
     const size_t smem = !grad ? 0 : (sums > slots ? sums : slots);
@@ -528,8 +529,11 @@ aa_status launch_width(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
         if (p.cols <= 1024) return launch_rows<T, V, 8, 128>(c, p, grad, n);
         if (p.cols <= 2048) return launch_rows<T, V, 8, 256>(c, p, grad, n);
         if (p.cols <= 4096) return launch_rows<T, V, 8, 512>(c, p, grad, n);
-        if (p.cols <= 6144) return launch_rows<T, V, 12, 512>(c, p, grad, n);
     }
+    if constexpr (V == 1)
+        if (p.cols <= 4608) return launch_rows<T, V, 9, 512>(c, p, grad, n);
+    if constexpr (V != 8)
+        if (p.cols <= 6144) return launch_rows<T, V, 12, 512>(c, p, grad, n);
     return launch_rows<T, V, 16, 512>(c, p, grad, n);
 }
 
