@@ -44,43 +44,50 @@ struct Box {
     int64_t stride, rows, cols;
 };
 
-// The 16 numbers a lane fetches of a batch of 8 rows of 64 elements, as they lie in memory.  VEC (16-byte aligned base and rows, columns in eights): lane l takes elements
-// 8 (l % 8) .. + 7 of rows l / 8 and l / 8 + 4, otherwise elements 2 l and 2 l + 1 of every row.  The loads are straight code, of a stand-in where the
-// element does not count (there is a row and a column at least), and nothing touches what they bring before it is stored, so that they
-// stay under way; `in` says which numbers count.
+// The 16 numbers a lane fetches of a batch of 8 rows of 64 elements, as they lie in memory: runs of RUN elements at column RUN (l % LANES) of rows l / LANES, l / LANES + 32 /
+// LANES, ...  VEC (16-byte aligned base and rows, columns in eights): a run is 16 bytes; otherwise it is two elements.  Neighbouring lanes read neighbouring runs.
+// Nothing touches what the loads bring before it is stored, so that they stay under way.  Where an element does not count a stand-in is loaded (there is a
+// row and a column at least); `in` says which numbers count.
 template <typename T, bool VEC>
 struct Batch {
     using Word = typename std::conditional<VEC, uint4, T>::type;
-    static constexpr int N = VEC ? 16 * (int)sizeof(T) / 16 : 16;
-    Word w[N];
+    static constexpr int RUN = VEC ? 16 / (int)sizeof(T) : 2, LANES = 64 / RUN, RUNS = 16 / RUN, ROWS = 32 / LANES;   // ROWS: between a lane's runs
+    static constexpr int PER = VEC ? 1 : RUN;
+    Word w[RUNS * PER];
     uint32_t in;
 
     __device__ __forceinline__ void load(const Box& b, int64_t row0, int64_t col0) {
         const int lane = threadIdx.x & 31;
-        asm volatile("" : "+l"(row0));       // the addresses are worked out here, not held in registers from slice to slice
-        in = 0;
+        const int64_t col = col0 + (lane % LANES) * RUN;
         if constexpr (VEC) {
-            const int64_t col = col0 + (lane & 7) * 8;
-            const bool c = col < b.cols;
+            asm volatile("" : "+l"(row0));   // the addresses are worked out here, not held in registers from slice to slice
+            in = 0;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int64_t row = row0 + (lane >> 3) + 4 * h;
-                const T* at = static_cast<const T*>(b.data) + min(row, b.rows - 1) * b.stride + (c ? col : 0);
+            for (int h = 0; h < RUNS; ++h) {
+                const int64_t row = row0 + lane / LANES + ROWS * h;
+                w[h] = *reinterpret_cast<const Word*>(static_cast<const T*>(b.data) + min(row, b.rows - 1) * b.stride + (col < b.cols ? col : 0));
+                if (row < b.rows && col < b.cols) in |= ((1u << RUN) - 1) << (h * RUN);
+            }
+        } else if (row0 + 8 <= b.rows && col0 + 64 <= b.cols) {
+            const T* at = static_cast<const T*>(b.data) + (row0 + lane / LANES) * b.stride + col;
+            in = 0xFFFFu;
 #pragma unroll
-                for (int e = 0; e < N / 2; ++e) w[h * (N / 2) + e] = reinterpret_cast<const uint4*>(at)[e];
-                if (c && row < b.rows) in |= 0xFFu << (8 * h);
+            for (int h = 0; h < RUNS; ++h) {
+                w[2 * h] = at[0];
+                w[2 * h + 1] = at[1];
+                at += ROWS * b.stride;
             }
         } else {
-            const int64_t col = col0 + 2 * lane;
-            const int64_t c0 = min(col, b.cols - 1), c1 = min(col + 1, b.cols - 1);
-            const uint32_t two = (col < b.cols ? 1u : 0u) | (col + 1 < b.cols ? 2u : 0u);
-            const T* base = static_cast<const T*>(b.data);
+            in = 0;
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const int64_t at = min(row0 + r, b.rows - 1) * b.stride;
-                w[2 * r] = base[at + c0];
-                w[2 * r + 1] = base[at + c1];
-                if (row0 + r < b.rows) in |= two << (2 * r);
+            for (int h = 0; h < RUNS; ++h) {
+                const int64_t row = row0 + lane / LANES + ROWS * h;
+                const T* at = static_cast<const T*>(b.data) + min(row, b.rows - 1) * b.stride;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    w[2 * h + e] = at[col + e < b.cols ? col + e : 0];
+                    if (row < b.rows && col + e < b.cols) in |= 1u << (2 * h + e);
+                }
             }
         }
     }
@@ -114,27 +121,22 @@ __device__ __forceinline__ void take_apart(float a, float b, uint32_t (&t)[TERMS
 }
 
 // The batch into rows r0 .. r0 + 7 of a [rows x 128 bytes] swizzled block; r0 a multiple of 8.
-template <int TERMS, bool VEC>
+template <typename T, int TERMS, bool VEC>
 __device__ __forceinline__ void store_batch(unsigned char* block, int r0, const float (&x)[16]) {
-    const int lane = threadIdx.x & 31;
-    if (VEC) {
+    using B = Batch<T, VEC>;
+    const int lane = threadIdx.x & 31, byte = (lane % B::LANES) * B::RUN * 2;        // of the row's 128
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = (lane >> 3) + 4 * h;
-            uint32_t t[4][TERMS];
+    for (int h = 0; h < B::RUNS; ++h) {
+        const int r = lane / B::LANES + B::ROWS * h;
+        uint32_t t[B::RUN / 2][TERMS];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) take_apart<TERMS>(x[8 * h + 2 * q], x[8 * h + 2 * q + 1], t[q]);
+        for (int q = 0; q < B::RUN / 2; ++q) take_apart<TERMS>(x[h * B::RUN + 2 * q], x[h * B::RUN + 2 * q + 1], t[q]);
+        unsigned char* to = block + (r0 + r) * 128 + (((byte >> 4) ^ r) << 4) + (byte & 15);
 #pragma unroll
-            for (int k = 0; k < TERMS; ++k)
-                *reinterpret_cast<uint4*>(block + k * kTermBytes + (r0 + r) * 128 + (((lane & 7) ^ r) << 4)) = make_uint4(t[0][k], t[1][k], t[2][k], t[3][k]);
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            uint32_t t[TERMS];
-            take_apart<TERMS>(x[2 * r], x[2 * r + 1], t);
-#pragma unroll
-            for (int k = 0; k < TERMS; ++k) *reinterpret_cast<uint32_t*>(block + k * kTermBytes + (r0 + r) * 128 + (((lane >> 2) ^ r) << 4) + (lane & 3) * 4) = t[k];
+        for (int k = 0; k < TERMS; ++k) {
+            if constexpr (B::RUN == 8) *reinterpret_cast<uint4*>(to + k * kTermBytes) = make_uint4(t[0][k], t[1][k], t[2][k], t[3][k]);
+            else if constexpr (B::RUN == 4) *reinterpret_cast<uint2*>(to + k * kTermBytes) = make_uint2(t[0][k], t[1][k]);
+            else *reinterpret_cast<uint32_t*>(to + k * kTermBytes) = t[0][k];
         }
     }
 }
@@ -258,7 +260,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) product_split_kernel(const _
                 unsigned char* block = ring + (size_t)stage * S::STAGE + (q < 2 ? 0 : S::OPERAND);
                 float v[16];
                 x[q].values(v);
-                store_batch<TERMS, VEC>(block, (warp * 2 + (q & 1)) * 8, v);
+                store_batch<T, TERMS, VEC>(block, (warp * 2 + (q & 1)) * 8, v);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
