@@ -91,9 +91,10 @@ int resident_ctas(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_sm
 
 int resident_clusters(aa_ctx_impl* c, const void* kernel, int threads, size_t dyn_smem, int cluster) {
     aa_ctx* ctx = reinterpret_cast<aa_ctx*>(c);
+    const int key = -(threads * 16 + cluster);               // beside the grids' entries, which have no clusters
     for (int i = 0; i < ctx->occ_used; ++i) {
         const OccEntry& e = ctx->occ[i];
-        if (e.kernel == kernel && e.threads == -threads && e.smem == dyn_smem) return e.ctas;
+        if (e.kernel == kernel && e.threads == key && e.smem == dyn_smem) return e.ctas;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(c->sm_count / cluster * cluster));
@@ -107,7 +108,7 @@ int resident_clusters(aa_ctx_impl* c, const void* kernel, int threads, size_t dy
     cfg.numAttrs = 1;
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) return -1;
-    if (ctx->occ_used < kOccSlots) ctx->occ[ctx->occ_used++] = OccEntry{kernel, -threads, dyn_smem, n};
+    if (ctx->occ_used < kOccSlots) ctx->occ[ctx->occ_used++] = OccEntry{kernel, key, dyn_smem, n};
     return n;
 }
 

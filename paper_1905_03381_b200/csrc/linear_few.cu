@@ -149,7 +149,9 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 || sizeof(T) == 2 ? 2 
             z[2] += f.z;
             z[3] += f.w;
         }
-        finish_quad<T>(p, z, row, col, (int)min((int64_t)4, p.n - col), out_vec);
+        float bias[4];
+        load_bias(p, col, bias);
+        finish_quads<T, 1>(p, z, bias, row, 1, p.m, col, out_vec);
     }
 }
 

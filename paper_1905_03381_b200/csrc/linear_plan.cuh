@@ -16,18 +16,22 @@ struct Plan {
     int cluster;                         // above 1: the parts of a tile are the CTAs of a cluster, which join them themselves (no scratch memory)
 };
 
+// CTAs that share a tile as a cluster, where there are few tiles and no scratch memory: as many as run at once, up to eight, with a
+// slice or more apiece (fp32, 200 x 300 -> 700 from a flushed L2: 33 us with four slices at least, 28 with two, 25 with one; bf16, 24 x 512 -> 512: 12, 10, 10).
+inline int tile_cluster(aa_ctx_impl* c, const void* kernel, int threads, size_t smem, const ProductParams& p, int64_t tiles) {
+    const int64_t slices = (p.k + kSlice - 1) / kSlice;
+    int n = 8;
+    while (n > 1 && (tiles * n > c->sm_count || slices < n || resident_clusters(c, kernel, threads, smem, n) < tiles)) n /= 2;
+    return p.parts ? 1 : n;
+}
+
 // Splits of the tiles that do not fill a round of `teams`: the fewest slices one after the other, counting the parts' way through memory.
 // slice_us: what a slice of a tile takes.
-inline Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats, int tile_rows, double slice_us, bool may_cluster) {
-    Plan plan{nt, (int)tiles, 1, p.parts, nullptr, 1};
+inline Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats, int tile_rows, double slice_us, int cluster) {
+    Plan plan{nt, (int)tiles, 1, p.parts, nullptr, cluster};
     const int64_t slices = (p.k + kSlice - 1) / kSlice, whole = tiles / teams * teams, tail = tiles - whole;
-    if (!p.parts) {
-        // few tiles and no scratch memory: as many CTAs on each as the SMs give, with four slices or more apiece
-        int c = 8;
-        while (c > 1 && (tiles * c > teams || slices < 4 * c)) c /= 2;
-        if (may_cluster && c > 1) plan.whole = 0, plan.splits = plan.cluster = c;
-        return plan;
-    }
+    if (cluster > 1) plan.whole = 0, plan.splits = cluster;
+    if (!p.parts) return plan;
     if (tail == 0) return plan;
     double best = (double)slices;
     for (int s = 2; s <= 16 && slices / s >= 4; ++s) {
@@ -70,62 +74,116 @@ __device__ __forceinline__ Unit unit_at(const Plan& p, int mt, int slices, int i
     } else {
         const int j = i - p.whole, t = j / p.splits, q = j - t * p.splits;
         tile_at(mt, p.nt, p.whole + t, u.m, u.n);
-        u.s0 = (int)((int64_t)slices * q / p.splits);
-        u.s1 = (int)((int64_t)slices * (q + 1) / p.splits);
+        u.s0 = (int)((uint32_t)slices * (uint32_t)q / (uint32_t)p.splits);       // 2^25 slices in 16 parts at most
+        u.s1 = (int)((uint32_t)slices * (uint32_t)(q + 1) / (uint32_t)p.splits);
         u.part = j;
     }
     return u;
 }
 
-// Bias, pre, activation, residual and the rounding of four neighbouring columns (cols of them count; vec: pointers allow vectors).
-template <typename T>
-__device__ __forceinline__ void finish_quad(const ProductParams& p, float (&z)[4], int64_t row, int64_t col, int cols, bool vec) {
+// The bias of the columns from `col` on that count.
+__device__ __forceinline__ void load_bias(const ProductParams& p, int64_t col, float (&bias)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[e] = p.bias && col + e < p.n ? p.bias[col + e] : 0.0f;
+}
+
+// Bias, pre, activation, residual and the rounding of four neighbouring columns (those below p.n count) of N rows `step` apart (those below `end`).
+// vec: pointers allow vectors.  The residuals are loaded first, so that the rows' loads are under way together.
+template <typename T, int N>
+__device__ __forceinline__ void finish_quads(const ProductParams& p, float (&z)[N * 4], const float (&bias)[4], int64_t row, int64_t step, int64_t end, int64_t col, bool vec) {
     T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride + col;
     T* pre = p.pre.data ? static_cast<T*>(const_cast<void*>(p.pre.data)) + row * p.pre.stride + col : nullptr;
     const T* res = p.residual.data ? static_cast<const T*>(p.residual.data) + row * p.residual.stride + col : nullptr;
-    if (p.bias) {
+    const int rows = (int)min((int64_t)N, (end - row + step - 1) / step), cols = (int)min((int64_t)4, p.n - col);
+    if (rows <= 0 || cols <= 0) return;
+    float y[N * 4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] += e < cols ? p.bias[col + e] : 0.0f;
-    }
+    for (int i = 0; i < N * 4; ++i) y[i] = 0.0f;
     if (vec && cols == 4) {
-        if (pre) store_quad(pre, z);
-        activate_all(z, p.act);
         if (res) {
-            float y[4];
-            load_quad(res, y);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] += y[e];
+            for (int q = 0; q < N; ++q) {
+                float v[4];
+                load_quad(res + (int64_t)min(q, rows - 1) * step * p.residual.stride, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[q * 4 + e] = v[e];
+            }
         }
-        store_quad(out, z);
-    } else {
+    } else if (res) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (pre && e < cols) store1(pre + e, z[e]);
-        activate_all(z, p.act);
+        for (int i = 0; i < N * 4; ++i) y[i] = load1(res + (int64_t)min(i / 4, rows - 1) * step * p.residual.stride + min(i % 4, cols - 1));
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < cols) store1(out + e, res ? z[e] + load1(res + e) : z[e]);
+    for (int i = 0; i < N * 4; ++i) z[i] += bias[i % 4];
+    const auto put = [&](T* to, int64_t stride) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            if (q >= rows) continue;
+            T* at = to + (int64_t)q * step * stride;
+            if (vec && cols == 4) {
+                const float v[4] = {z[q * 4], z[q * 4 + 1], z[q * 4 + 2], z[q * 4 + 3]};
+                store_quad(at, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < cols) store1(at + e, z[q * 4 + e]);
+            }
+        }
+    };
+    if (pre) put(pre, p.pre.stride);
+    activate_all(z, p.act);
+#pragma unroll
+    for (int i = 0; i < N * 4; ++i) z[i] += y[i];
+    put(out, p.out.stride);
+}
+
+// A warp's 32 rows of 32 columns (a lane has 32 columns of row `lane` of them in sum[32 C..]) through its stage, so that eight lanes write a row's 128 bytes
+// together: as a part (`part`: its first row and column, BN apart) or finished.  row0, col: of the warp's first row and of this lane's four columns.
+template <typename T, int C, int BN>
+__device__ __forceinline__ void finish_chunk(const ProductParams& p, float* part, float* stage, const float (&sum)[64], const float (&bias)[4], int64_t row0, int64_t end, int64_t col, bool vec) {
+    constexpr int kAtOnce = 4;
+    const int lane = threadIdx.x & 31, sub = lane & 7, r8 = lane >> 3;
+    __syncwarp();                            // the stage's readers of the chunk before are done
+#pragma unroll
+    for (int w = 0; w < 8; ++w)
+        *reinterpret_cast<float4*>(stage + lane * 32 + ((w ^ (lane & 7)) << 2)) =
+            make_float4(sum[C * 32 + 4 * w], sum[C * 32 + 4 * w + 1], sum[C * 32 + 4 * w + 2], sum[C * 32 + 4 * w + 3]);
+    __syncwarp();
+#pragma unroll 1
+    for (int q0 = 0; q0 < 8; q0 += kAtOnce) {
+        float z[kAtOnce * 4];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int r = (q0 + q) * 4 + r8;
+            const float4 f = *reinterpret_cast<const float4*>(stage + r * 32 + ((sub ^ (r & 7)) << 2));
+            z[q * 4] = f.x, z[q * 4 + 1] = f.y, z[q * 4 + 2] = f.z, z[q * 4 + 3] = f.w;
+            if (part) *reinterpret_cast<float4*>(part + r * BN + sub * 4) = f;
+        }
+        if (!part) finish_quads<T, kAtOnce>(p, z, bias, row0 + q0 * 4 + r8, 4, end, col, vec);
     }
 }
 
 // The CTAs of a cluster have the parts of a tile of 128 rows in [CTA][128 / cluster rows][BN] of everybody's `parts` (shared memory): this CTA finishes its rows.
-// `threads` threads from `tid` on; after a cluster barrier.
+// `threads` threads (a multiple of BN / 4) from `tid` on; after a cluster barrier.
 template <typename T, int BN>
 __device__ __forceinline__ void finish_cluster(const ProductParams& p, const Plan& plan, const Unit& u, const float* parts, int64_t m_end, bool vec, int tid, int threads) {
-    const int rows = 128 / plan.cluster, rank = (int)cluster_rank();
-    for (int i = tid; i < rows * (BN / 4); i += threads) {
-        const int r = i / (BN / 4), c = (i - r * (BN / 4)) * 4;
-        const int64_t row = (int64_t)u.m * 128 + rank * rows + r, col = (int64_t)u.n * BN + c;
-        if (row >= m_end || col >= p.n) continue;
-        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < plan.cluster; ++s) {
-            const float4 f = *reinterpret_cast<const float4*>(parts + ((int64_t)s * rows + r) * BN + c);
-            z[0] += f.x;
-            z[1] += f.y;
-            z[2] += f.z;
-            z[3] += f.w;
-        }
-        finish_quad<T>(p, z, row, col, (int)min((int64_t)4, p.n - col), vec);
+    constexpr int kAtOnce = 2, kQuads = BN / 4;
+    const int rows = 128 / plan.cluster, rank = (int)cluster_rank(), step = threads / kQuads, c = tid % kQuads * 4;
+    const int64_t row0 = (int64_t)u.m * 128 + rank * rows, end = min(m_end, row0 + rows), col = (int64_t)u.n * BN + c;
+    float bias[4];
+    load_bias(p, col, bias);
+    for (int r = tid / kQuads; r < rows; r += kAtOnce * step) {
+        float z[kAtOnce * 4] = {};
+        for (int s = 0; s < plan.cluster; ++s)
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) {
+                const float4 f = *reinterpret_cast<const float4*>(parts + ((int64_t)s * rows + min(r + q * step, rows - 1)) * BN + c);
+                z[q * 4] += f.x;
+                z[q * 4 + 1] += f.y;
+                z[q * 4 + 2] += f.z;
+                z[q * 4 + 3] += f.w;
+            }
+        finish_quads<T, kAtOnce>(p, z, bias, row0 + r, step, end, col, vec);
     }
 }
 

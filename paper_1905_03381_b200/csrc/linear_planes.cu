@@ -186,31 +186,11 @@ product_planes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
                 if (lane == 0) mbar_arrive_at(of_rank(&ctl.acc_empty[it & 1], 0));
             }
             if (!ok) break;
-            const int64_t row0 = ((int64_t)u.m * 2 + rank) * kM + quad * 32 + r8;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                __syncwarp();                // the stage's readers of the chunk before are done
-#pragma unroll
-                for (int w = 0; w < 8; ++w)
-                    *reinterpret_cast<float4*>(mine + lane * 32 + ((w ^ (lane & 7)) << 2)) =
-                        make_float4(sum[c * 32 + 4 * w], sum[c * 32 + 4 * w + 1], sum[c * 32 + 4 * w + 2], sum[c * 32 + 4 * w + 3]);
-                __syncwarp();
-                const int in_tile = half * 64 + c * 32 + sub * 4;
-                const int64_t col = (int64_t)u.n * kBN + in_tile;
-                const int cols = (int)max((int64_t)0, min((int64_t)4, p.n - col));
-#pragma unroll 2
-                for (int q = 0; q < 8; ++q) {
-                    const int r = q * 4 + r8;
-                    const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
-                    if (u.part >= 0) {
-                        *reinterpret_cast<float4*>(plan.parts + (((int64_t)u.part * 2 + rank) * kM + quad * 32 + r) * kBN + in_tile) = f;
-                        continue;
-                    }
-                    float z[4] = {f.x, f.y, f.z, f.w};
-                    const int64_t row = row0 + q * 4;
-                    if (row < m_end && cols > 0) finish_quad<float>(p, z, row, col, cols, vec);
-                }
-            }
+            const int64_t row0 = ((int64_t)u.m * 2 + rank) * kM + quad * 32, col = (int64_t)u.n * kBN + half * 64 + sub * 4;
+            float* part = u.part >= 0 ? plan.parts + (((int64_t)u.part * 2 + rank) * kM + quad * 32) * kBN + half * 64 : nullptr;
+            constexpr float none[4] = {};                        // these products have no bias
+            finish_chunk<float, 0, kBN>(p, part, mine, sum, none, row0, m_end, col, vec);
+            finish_chunk<float, 1, kBN>(p, part ? part + 32 : nullptr, mine, sum, none, row0, m_end, col + 32, vec);
         }
     }
     if (!ok) {
@@ -238,7 +218,7 @@ aa_status launch_planes(aa_ctx_impl* c, const ProductParams& in) {
     if (allow_smem(c, kernel, kPlaneSmem) != AA_OK) return AA_ERR_CUDA;
     const int teams = resident_clusters(c, kernel, kPlaneThreads, kPlaneSmem, 2);
     if (teams < 1) return AA_ERR_CUDA;
-    Plan plan = make_plan(p, tiles, (int)nt, teams, 2 * kM * kBN, 2 * kM, 1.2, false);
+    Plan plan = make_plan(p, tiles, (int)nt, teams, 2 * kM * kBN, 2 * kM, 1.2, 1);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     bool vec = true;
     for (const MatArg* m : {&p.out, &p.residual}) vec = vec && (!m->data || ((uintptr_t)m->data % 16 == 0 && m->stride % 4 == 0));

@@ -411,7 +411,7 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 }
 
 template <int CG, int BN, bool AA, bool BA, bool SUMS, bool JOIN>
-aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
+aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec, int cluster = 1) {
     using G = Geo<CG, BN>;
     constexpr int kThreads = SUMS ? kSumThreads : kTcThreads;
     ProductParams p = in;
@@ -425,14 +425,13 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec) {
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
     const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kThreads, G::SMEM, CG);
     if (teams < 1) return AA_ERR_CUDA;
-    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2, JOIN);
+    const Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2, cluster);
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
-    void* args[] = {&map_a, &map_b, &p, &plan, &vec};
-    const int cluster = JOIN ? plan.cluster : CG;
-    if (launch_clusters(c, kernel, (unsigned)(JOIN ? units : (units < teams ? units : teams) * CG), kThreads, args, G::SMEM, cluster) != cudaSuccess) return AA_ERR_CUDA;
+    void* args[] = {&map_a, &map_b, &p, const_cast<Plan*>(&plan), &vec};
+    if (launch_clusters(c, kernel, (unsigned)(JOIN ? units : (units < teams ? units : teams) * CG), kThreads, args, G::SMEM, JOIN ? cluster : CG) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     if (tail == 0 || JOIN) return AA_OK;
-    void* join[] = {&p, &plan, &vec};
+    void* join[] = {&p, const_cast<Plan*>(&plan), &vec};
     const int64_t threads = tail * CG * kBM * BN / 4;
     if (launch_overlapped(c, (const void*)product_join_kernel<uint16_t, CG * kBM, BN>, dim3((unsigned)(threads / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
@@ -445,7 +444,10 @@ aa_status launch_majors(aa_ctx_impl* c, const ProductParams& p, bool vec) {
     if (p.b_across) return launch_tc<CG, BN, false, true, false, false>(c, p, vec);
     if constexpr (CG == 1) {
         const int64_t tiles = (p.m + kBM - 1) / kBM * ((p.n + BN - 1) / BN);
-        if (!p.parts && make_plan(p, tiles, 1, c->sm_count, 1, 1, 1.0, true).cluster > 1) return launch_tc<CG, BN, false, false, false, true>(c, p, vec);
+        const void* kernel = (const void*)product_tc_kernel<CG, BN, false, false, false, true>;
+        if (allow_smem(c, kernel, Geo<CG, BN>::SMEM) != AA_OK) return AA_ERR_CUDA;
+        const int cluster = tile_cluster(c, kernel, kTcThreads, Geo<CG, BN>::SMEM, p, tiles);
+        if (cluster > 1) return launch_tc<CG, BN, false, false, false, true>(c, p, vec, cluster);
     }
     return launch_tc<CG, BN, false, false, false, false>(c, p, vec);
 }
