@@ -516,9 +516,10 @@ aa_status aa_rel_attention_grad(aa_ctx* ctx, const aa_attn* attn, const aa_rel_b
  *   bias, residual and pre are nullable; pre is what aa_linear_grad needs of a layer with an activation.
  *   AA_ACT_RELU max(z, 0); AA_ACT_GELU z (1 + erf(z / sqrt 2)) / 2; AA_ACT_SILU z / (1 + exp(-z)).
  * Products are summed in fp32, bias, activation and residual are applied in fp32, and the result is rounded once.  fp32 operands enter
- * the products with all their bits.  A factor of zero against an infinity or NaN gives NaN, as in the formula.
+ * the products as sums of three bf16 terms: with all their 24 bits from 2^-110 up, with an error of at most 2^-134 below it.  A factor of zero against an infinity or
+ * NaN gives NaN, as in the formula; an infinite fp32 factor, or one above 3.38e38, gives infinities or NaN in the outputs that it enters.
  * out may be residual itself (same pointer and stride); what is written has otherwise no element in common with another operand.
- * rows may be 0 (dw and dbias of no rows are 0); cols and inner are 1 to 2^30.
+ * rows may be 0 (dw and dbias of no rows are 0) and at most 2^31 - 1; cols and inner are 1 to 2^30.
  */
 typedef enum { AA_ACT_NONE = 0, AA_ACT_RELU = 1, AA_ACT_GELU = 2, AA_ACT_SILU = 3 } aa_activation;
 
@@ -531,7 +532,8 @@ aa_status aa_linear(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, const float
  * dx, dw, dbias are nullable (not computed), written and not added to; residual (nullable, needs dx) is a gradient that reaches x past the layer, dx may
  * be residual itself.  dx and dw have the dtype of x and w, dbias is fp32.  With an activation and bf16 operands G is rounded to bf16 before the
  * two products (dbias sums it unrounded).  Sums run in an order that depends on the sizes alone, so equal calls give equal bits.
- * scratch: DEVICE memory of at least aa_linear_grad_scratch_bytes(...) bytes, 256-byte aligned.
+ * scratch: DEVICE memory of at least aa_linear_grad_scratch_bytes(...) bytes for these operands (strides and alignment count, too), 256-byte aligned; it holds nothing
+ * between calls, and calls that may run at the same time need one each.
  */
 aa_status aa_linear_grad_scratch_bytes(const aa_rows* x, const aa_rows* w, int32_t activation, size_t* bytes);
 aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_t activation, const aa_rows* pre, const aa_rows* dout,

@@ -662,6 +662,8 @@ class AutoAssist:
 
     def _live(self, rows: int, offsets, n_seg, count_dev):
         """offsets, n_seg and count_dev as the C calls take them."""
+        if offsets is None and count_dev is None:
+            return None, 0, None
         _check(offsets, torch.int32, "offsets")
         _check(count_dev, torch.int32, "count_dev")
         if offsets is None:
@@ -674,6 +676,13 @@ class AutoAssist:
         if count_dev is not None and count_dev.numel() < 1:
             _short(count_dev, 1, "count_dev")
         return _ptr(offsets), n_seg, _ptr(count_dev)
+
+    def _here(self, *tensors):
+        """Raises unless the tensors (those that are given) are on the context's device."""
+        here = self.workspace.device
+        for t in tensors:
+            if t is not None and t.device != here:
+                raise TypeError(f"expected tensors on {here}, got one on {t.device}")
 
     def _scratch(self, nbytes: int) -> torch.Tensor:
         return torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
@@ -702,12 +711,13 @@ class AutoAssist:
                   count_dev=None, n_seg=None):
         """out = activation(x w^T + bias) + residual; pre receives x w^T + bias.  w is [out, in], bias fp32, activation None, "relu", "gelu" or "silu".
         offsets / count_dev: only the token rows of the counted sentences (without offsets: of the counted rows) are evaluated."""
+        self._here(x, w, out, bias, residual, pre, offsets, count_dev)
         xm = rows_desc(x)
         self._ok(self._L.aa_linear(self._ctx, byref(xm), byref(rows_desc(w)), self._vector(bias, w.shape[0], "bias"), self._activation(activation),
                                    _rows_or_none(residual), *self._live(xm.rows, offsets, n_seg, count_dev), _rows_or_none(pre), byref(rows_desc(out))), "aa_linear")
 
     def linear_grad_scratch(self, x: torch.Tensor, w: torch.Tensor, activation=None) -> torch.Tensor:
-        """Device scratch for aa_linear_grad on operands of these shapes."""
+        """Device scratch for aa_linear_grad on these operands (their shapes, strides and alignment decide what is copied)."""
         nbytes = c_size_t(0)
         self._ok(self._L.aa_linear_grad_scratch_bytes(byref(rows_desc(x)), byref(rows_desc(w)), self._activation(activation), byref(nbytes)),
                  "aa_linear_grad_scratch_bytes")
@@ -717,6 +727,7 @@ class AutoAssist:
                        pre=None, residual=None, offsets=None, count_dev=None, n_seg=None):
         """Gradients of aa_linear from dout; those that are None are not computed.  residual is added to dx.  pre: as aa_linear left it (layers with an
         activation)."""
+        self._here(x, w, dout, scratch, dx, dw, dbias, pre, residual, offsets, count_dev)
         xm = rows_desc(x)
         self._ok(self._L.aa_linear_grad(self._ctx, byref(xm), byref(rows_desc(w)), self._activation(activation), _rows_or_none(pre), byref(rows_desc(dout)),
                                         _rows_or_none(residual), *self._live(xm.rows, offsets, n_seg, count_dev), _rows_or_none(dx), _rows_or_none(dw),
@@ -724,6 +735,7 @@ class AutoAssist:
 
     def aa_layer_norm(self, x: torch.Tensor, out: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, offsets=None, count_dev=None, n_seg=None):
         """out = (x - mean) / sqrt(var + eps) * gamma + beta, row by row; gamma and beta fp32.  out may be x."""
+        self._here(x, out, gamma, beta, offsets, count_dev)
         xm = rows_desc(x)
         self._ok(self._L.aa_layer_norm(self._ctx, byref(xm), self._vector(gamma, xm.cols, "gamma"), self._vector(beta, xm.cols, "beta"), eps,
                                        *self._live(xm.rows, offsets, n_seg, count_dev), byref(rows_desc(out))), "aa_layer_norm")
@@ -737,6 +749,7 @@ class AutoAssist:
     def aa_layer_norm_grad(self, x: torch.Tensor, dout: torch.Tensor, dx: torch.Tensor, scratch: torch.Tensor, gamma=None, eps: float = 1e-5, residual=None,
                            dgamma=None, dbeta=None, offsets=None, count_dev=None, n_seg=None):
         """Gradients of aa_layer_norm from dout; residual is added to dx.  dx may be x, dout or residual."""
+        self._here(x, dout, dx, scratch, gamma, residual, dgamma, dbeta, offsets, count_dev)
         xm = rows_desc(x)
         self._ok(self._L.aa_layer_norm_grad(self._ctx, byref(xm), self._vector(gamma, xm.cols, "gamma"), eps, byref(rows_desc(dout)), _rows_or_none(residual),
                                             *self._live(xm.rows, offsets, n_seg, count_dev), byref(rows_desc(dx)), self._vector(dgamma, xm.cols, "dgamma"),
@@ -745,6 +758,7 @@ class AutoAssist:
     def aa_adamw(self, tensors: ctypes.Array, rule: aa_adamw_rule, grad_scale=None):
         """One AdamW step on an adamw_list; rule.t advances.  grad_scale: fp32 device scalar that multiplies the gradients; if it is not finite the step
         writes nothing."""
+        self._here(grad_scale, *([tensors._keep[0][0]] if len(tensors) and hasattr(tensors, "_keep") else []))
         self._ok(self._L.aa_adamw(self._ctx, tensors, len(tensors), byref(rule), self._vector(grad_scale, 1, "grad_scale")), "aa_adamw")
 
     def host_step_plan(self, x_host: torch.Tensor, logits_host: torch.Tensor):

@@ -9,7 +9,7 @@ namespace aa {
 
 namespace {
 
-constexpr int64_t kMaxWidth = 1ll << 30;
+constexpr int64_t kMaxWidth = 1ll << 30, kMaxRows = (1ll << 31) - 1;
 
 MatArg mat(const aa_rows* m) { return m ? MatArg{m->data, m->row_stride} : MatArg{nullptr, 0}; }
 
@@ -69,7 +69,7 @@ LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
 
 aa_status check_linear(const aa_rows* x, const aa_rows* w) {
     if (check_rows(x) != AA_OK || check_rows(w) != AA_OK || x->dtype != w->dtype || x->cols != w->cols || w->rows < 1) return AA_ERR_INVALID_ARG;
-    return x->cols > kMaxWidth || w->rows > kMaxWidth ? AA_ERR_UNSUPPORTED : AA_OK;
+    return x->cols > kMaxWidth || w->rows > kMaxWidth || x->rows > kMaxRows ? AA_ERR_UNSUPPORTED : AA_OK;
 }
 
 }  // namespace

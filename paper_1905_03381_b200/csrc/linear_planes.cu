@@ -158,7 +158,7 @@ product_planes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_co
         // ---- epilogue: a warp has 32 rows and 64 columns
         const int quad = warp & 3, half = (warp - 4) >> 2;
         float* mine = stage_f + (warp - 4) * 32 * 32;
-        const int sub = lane & 7, r8 = lane >> 3;
+        const int sub = lane & 7;
         int it = 0;
         for (int i = first; i < units && ok; i += step) {
             const Unit u = unit_at(plan, mt, slices, i);
