@@ -3,11 +3,13 @@
 //   c = x - mean(x),  r = 1 / sqrt(mean(c^2) + eps),  h = c r,  out = h gamma + beta
 //   g = dout gamma,   dx = r (g - mean(g) - h mean(g h)) + residual,   dgamma = sum_rows dout h,  dbeta = sum_rows dout
 //
-// Bound by memory: 2 values a column pass forward, 3 or 4 backward, against about 10 and 20 instructions.  A row stays in the registers of a group of
-// threads (8 or 16 columns each) between its sums and its result, so that memory is touched once; mean and variance are two rounds over registers, so that
-// nothing cancels.  Backward the rounds carry (sum x, sum g) and (sum c^2, sum g c): mean(g h) = r mean(g c), and no statistics are kept from the
-// forward pass (two floats a row would save one round of shuffles and no memory).  A group walks over rows of its own and adds up dout h and dout of its
-// columns; the sums of a CTA's groups are joined in shared memory, those of the CTAs by a second kernel, both in a fixed order.
+// Bound by memory where rows are short or fp32 (25,000 x 512 fp32: forward 18.8 us, 5.4 TB/s, backward 29 us, 5.3 TB/s; bf16 with residual 23 us, 4.5 TB/s), by
+// instructions and the latency of sums where an SM's warps share a row (3,001 x 4,099 fp32 backward: 39 us with both launches, the floor is 22).
+// 2 values a column pass forward, 3 or 4 backward.  A row stays in the registers of a group of threads (8 or 16 columns each) between its sums and its
+// result, so that memory is touched once; mean and variance are two rounds over registers, so that nothing cancels.  Backward the rounds carry
+// (sum x, sum g) and (sum c^2, sum g c): mean(g h) = r mean(g c), and no statistics are kept from the forward pass (two floats a row would save one round of
+// shuffles and no memory).  A group walks over rows of its own and adds up dout h and dout of its columns; the sums of a CTA's groups are joined in
+// shared memory, those of the CTAs by a second kernel, both in a fixed order.
 // Rows too long for registers are swept three times, and their columns are summed by a kernel of their own.
 #include <type_traits>
 
@@ -36,14 +38,65 @@ __device__ __forceinline__ float2 group_sum(float2 s, float2* buf) {
         if ((threadIdx.x & 31) == 0) mine[threadIdx.x % G >> 5] = s;
         if constexpr (kThreadsOf<G> == G) __syncthreads();
         else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(G) : "memory");
-        s = mine[0];
+        if constexpr (G >= 256) {            // a number a lane and a tree: a third of the instructions of 16 loads
+            s = mine[threadIdx.x % (G / 32)];
 #pragma unroll
-        for (int w = 1; w < G / 32; ++w) {
-            s.x += mine[w].x;
-            s.y += mine[w].y;
+            for (int o = G / 64; o > 0; o >>= 1) {
+                s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, o);
+                s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, o);
+            }
+        } else {
+            s = mine[0];
+#pragma unroll
+            for (int w = 1; w < G / 32; ++w) {
+                s.x += mine[w].x;
+                s.y += mine[w].y;
+            }
         }
     }
     return s;
+}
+
+// The same for K values.
+template <int G, int K>
+__device__ __forceinline__ void group_sums(float (&s)[K], float* buf) {
+    static_assert(K == 2 || K == 4, "");
+    if constexpr (K == 2 && G > 32) {        // the shorter chain of steps
+        const float2 t = group_sum<G>(make_float2(s[0], s[1]), reinterpret_cast<float2*>(buf));
+        s[0] = t.x;
+        s[1] = t.y;
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    // a warp halves the number of values a lane has with the first steps: value q ends up in the lanes with q = lane % K
+    float t;
+    if constexpr (K == 4) {
+        const bool up = lane & 2;
+        const float a = up ? s[2] : s[0], b = up ? s[3] : s[1];
+        const float c = __shfl_xor_sync(0xFFFFFFFFu, up ? s[0] : s[2], 2), d = __shfl_xor_sync(0xFFFFFFFFu, up ? s[1] : s[3], 2);
+        const bool odd = lane & 1;
+        t = (odd ? b + d : a + c) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a + c : b + d, 1);
+    } else {
+        const bool odd = lane & 1;
+        t = (odd ? s[1] : s[0]) + __shfl_xor_sync(0xFFFFFFFFu, odd ? s[0] : s[1], 1);
+    }
+#pragma unroll
+    for (int o = K; o < (G < 32 ? G : 32); o *= 2) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+    if constexpr (G > 32) {
+        constexpr int WARPS = G / 32, ALL = WARPS * K;
+        const int group = threadIdx.x / G;
+        float* mine = buf + group * ALL;
+        if (lane < K) mine[(threadIdx.x % G >> 5) * K + lane] = t;
+        if constexpr (kThreadsOf<G> == G) __syncthreads();
+        else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(G) : "memory");
+        t = mine[lane % ALL];
+#pragma unroll
+        for (int i = 32; i < ALL; i += 32) t += mine[lane + i];
+#pragma unroll
+        for (int o = K; o < (ALL < 32 ? ALL : 32); o *= 2) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+    }
+#pragma unroll
+    for (int q = 0; q < K; ++q) s[q] = __shfl_sync(0xFFFFFFFFu, t, G < 32 ? (lane & ~(G - 1)) | q : q);
 }
 
 // What a thread fetches of a row, as it lies in memory.
@@ -114,7 +167,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_kerne
             v[j] = first + j / V * step < cols ? v[j] - mean : 0.0f;
             s.x = fmaf(v[j], v[j], s.x);
         }
-        const float r = 1.0f / sqrtf(group_sum<G>(s, buf[1]).x * inv + p.eps);
+        const float r = rsqrtf(group_sum<G>(s, buf[1]).x * inv + p.eps);
         T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -157,17 +210,26 @@ struct Slot {
 // (`lo`, `hi`: its ends); the few that do not are fetched element by element.
 template <typename T, int E, int TH>
 struct Shifted {
-    static constexpr int WARP = 32 * E * (int)sizeof(T) + 16, BYTES = TH / 32 * WARP;
+    static constexpr int WARP = 32 * E * (int)sizeof(T) + 16, BYTES = TH / 32 * WARP, TRIPS = (WARP / 16 + 31) / 32;
+    // n: columns of the warp that count, 32 E at most
     __device__ static __forceinline__ void fetch(char* at, const T* seg, int n, const char* lo, const char* hi) {
         if (n <= 0) return;
+        const int lane = threadIdx.x & 31;
         const uint32_t shift = (uint32_t)(uintptr_t)seg & 15u;
         const char* from = reinterpret_cast<const char*>(seg) - shift;
         char* to = at + (threadIdx.x >> 5) * WARP;
-        const int words = ((n < 32 * E ? n : 32 * E) * (int)sizeof(T) + (int)shift + 15) / 16;
-        const bool inside = from >= lo && from + words * 16 <= hi;
-        for (int j = threadIdx.x & 31; j < words; j += 32) {
+        const int words = (n * (int)sizeof(T) + (int)shift + 15) / 16;
+        if (from >= lo && from + words * 16 <= hi) {
+            const uint32_t at32 = smem_u32(to) + lane * 16;
+            const char* src = from + lane * 16;
+#pragma unroll
+            for (int q = 0; q < TRIPS; ++q)
+                if (lane + 32 * q < words) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at32 + 512 * q), "l"(src + 512 * q) : "memory");
+            return;
+        }
+        for (int j = lane; j < words; j += 32) {
             const char* src = from + j * 16;
-            if (inside || (src >= lo && src + 16 <= hi)) {
+            if (src >= lo && src + 16 <= hi) {
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + j * 16)), "l"(src) : "memory");
             } else {
                 for (int e = 0; e < 16; e += (int)sizeof(T))
@@ -175,29 +237,36 @@ struct Shifted {
             }
         }
     }
-    __device__ static __forceinline__ void read(const char* at, const T* seg, Raw<T, 1, E>& x) {
-        const T* from = reinterpret_cast<const T*>(at + (threadIdx.x >> 5) * WARP + ((uint32_t)(uintptr_t)seg & 15u)) + (threadIdx.x & 31);
+    // seg: the low bits of the address
+    __device__ static __forceinline__ void read(const char* at, uint32_t seg, Raw<T, 1, E>& x) {
+        const T* from = reinterpret_cast<const T*>(at + (threadIdx.x >> 5) * WARP + (seg & 15u)) + (threadIdx.x & 31);
 #pragma unroll
         for (int i = 0; i < E; ++i) x.w[i] = from[32 * i];
     }
 };
 
-// AHEAD rows of a group are under way while one is worked on, 150 KB an SM at three (a row's worth of registers would be half of that and too little at
-// the latency of a busy memory).
-template <typename T, int V, int E, int G, int AHEAD>
-__global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_kernel(NormParams p) {
-    constexpr int TH = kThreadsOf<G>, N = E / V, RING = AHEAD + 1;
+// R rows of a group are worked on at a time - two where all warps of an SM are one group and registers allow: barriers and the latency of sums come once for
+// both (3,001 x 4,099 fp32: 41.7 us one by one, 39.4 in twos; groups of 256 threads gain nothing).  `steps` times R rows are under way; a step's place is
+// filled again as soon as its numbers are in registers.
+template <typename T, int V, int E, int G, int R>
+__global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_kernel(NormParams p, int steps) {
+    constexpr int TH = kThreadsOf<G>, N = E / V;
     constexpr bool SHIFT = V == 1;
+    static_assert(R == 1 || G >= 32, "a group's second row is skipped by whole warps");
     using S = Slot<T, V, E, TH>;
     using U = Shifted<T, E, TH>;
     constexpr int BYTES = SHIFT ? U::BYTES : S::BYTES;
-    __shared__ float2 buf[2][32];
-    extern __shared__ __align__(16) char ring[];     // [RING][x, dout, residual]; at the end the column sums
+    __shared__ __align__(8) float buf[2][TH / 32 * 2 * R];
+    extern __shared__ __align__(16) char ring[];     // [steps][R][x, dout, residual if there is one]; at the end the column sums
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
     const int l = threadIdx.x % G, groups = TH / G;
     const int cols = (int)p.cols, seg = (l & ~31) * E, first = SHIFT ? seg + (l & 31) : l * V, step = SHIFT ? 32 : G * V;
+    const int n_warp = min(cols - seg, 32 * E);
+    // every column of the warp (of the row, where lanes hold vectors) is one: no tests on the way
+    const bool full = SHIFT ? n_warp == 32 * E : N * step <= cols, extra = p.residual.data != nullptr;
+    const int row_bytes = (extra ? 3 : 2) * BYTES;
     const float inv = 1.0f / (float)cols;
     float gm[E], dg[E], db[E];
 #pragma unroll
@@ -209,92 +278,120 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_
     const int64_t jump = (int64_t)gridDim.x * groups;
     // the lanes of a warp keep step: rows past the end are looked at as the last one and not written
     const int64_t mine = (int64_t)blockIdx.x * groups + threadIdx.x / G;
-    Raw<T, V, E> x, d, res;
     const auto row_of = [&](const MatArg& m, int64_t row) { return static_cast<const T*>(m.data) + row * m.stride; };
     const auto end_of = [&](const MatArg& m) { return reinterpret_cast<const char*>(row_of(m, live - 1) + cols); };
     const auto fetch_one = [&](char* at, const MatArg& m, int64_t row) {
-        if constexpr (SHIFT) U::fetch(at, row_of(m, row) + seg, cols - seg, static_cast<const char*>(m.data), end_of(m));
+        if constexpr (SHIFT) U::fetch(at, row_of(m, row) + seg, n_warp, static_cast<const char*>(m.data), end_of(m));
         else S::fetch(at, row_of(m, row), first, step, cols);
     };
-    const auto fetch = [&](int64_t r, int slot) {
-        const int64_t row = min(r, live - 1);
-        char* at = ring + slot * 3 * BYTES;
-        fetch_one(at, p.x, row);
-        fetch_one(at + BYTES, p.dout, row);
-        if (p.residual.data) fetch_one(at + 2 * BYTES, p.residual, row);
-    };
     const auto read_one = [&](const char* at, const MatArg& m, int64_t row, Raw<T, V, E>& w) {
-        if constexpr (SHIFT) U::read(at, row_of(m, row) + seg, w);
+        if constexpr (SHIFT) U::read(at, (uint32_t)(uintptr_t)m.data + ((uint32_t)row * (uint32_t)m.stride + (uint32_t)seg) * (uint32_t)sizeof(T), w);
         else S::read(at, w);
     };
     // a group goes on while the first of its warp's rows does
     const int64_t lead = G >= 32 ? mine : (int64_t)blockIdx.x * groups + (threadIdx.x & ~31) / G;
-    int slot = 0;
-    if constexpr (!SHIFT) {
+    const auto fetch = [&](int64_t r, int slot) {
 #pragma unroll
-        for (int a = 0; a < 3 * RING; ++a) S::clear(ring + a * BYTES);
-    }
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-        if (lead + a * jump < live) fetch(mine + a * jump, a);
+        for (int q = 0; q < R; ++q) {
+            if (lead + r + q * jump >= live) continue;
+            const int64_t row = G >= 32 ? mine + r + q * jump : min(mine + r, live - 1);
+            char* at = ring + (slot * R + q) * row_bytes;
+            fetch_one(at, p.x, row);
+            fetch_one(at + BYTES, p.dout, row);
+            if (extra) fetch_one(at + 2 * BYTES, p.residual, row);
+        }
         asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    for (int64_t r = 0; lead + r < live; r += jump) {
-        const int64_t row = mine + r;
-        const bool on = G >= 32 || row < live;
-        if (SHIFT) __syncwarp();             // the slot's readers are done
-        if (lead + r + AHEAD * jump < live) fetch(row + AHEAD * jump, slot >= 1 ? slot - 1 : AHEAD);
-        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+    };
+    if constexpr (!SHIFT)
+        for (int a = 0; a < steps * row_bytes / BYTES * R; ++a) S::clear(ring + a * BYTES);
+    for (int a = 0; a < steps; ++a) fetch(a * R * jump, a);
+    int slot = 0;
+    for (int64_t r = 0; lead + r < live; r += R * jump) {
+        if (steps >= 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else if (steps == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        else if (steps == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
         if (SHIFT) __syncwarp();
-        const char* at = ring + slot * 3 * BYTES;
-        read_one(at, p.x, row, x);
-        read_one(at + BYTES, p.dout, row, d);
-        if (p.residual.data) read_one(at + 2 * BYTES, p.residual, row, res);
-        slot = slot == AHEAD ? 0 : slot + 1;
-        float v[E], u[E];
-        float2 s = make_float2(0.0f, 0.0f);
+        Raw<T, V, E> res[R];
+        float v[R][E], u[R][E], s[2 * R] = {};
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            x.values(i, v + i * V);
-            d.values(i, u + i * V);
-            if constexpr (SHIFT) {
-                const bool has = first + i * step < cols;
-                v[i] = has ? v[i] : 0.0f;
-                u[i] = has ? u[i] : 0.0f;
-            }
+        for (int q = 0; q < R; ++q) {
+            const int64_t row = mine + r + q * jump;
+            const char* at = ring + (slot * R + q) * row_bytes;
+            Raw<T, V, E> x, d;
+            read_one(at, p.x, row, x);
+            read_one(at + BYTES, p.dout, row, d);
+            if (extra) read_one(at + 2 * BYTES, p.residual, row, res[q]);
+            // (the values of vectors behind the end are zeros already)
+            const auto first_sums = [&](auto all) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    x.values(i, v[q] + i * V);
+                    d.values(i, u[q] + i * V);
+                    if constexpr (SHIFT && !all.value) {
+                        const bool has = first + i * step < cols;
+                        v[q][i] = has ? v[q][i] : 0.0f;
+                        u[q][i] = has ? u[q][i] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    s[2 * q] += v[q][j];
+                    s[2 * q + 1] = fmaf(u[q][j], gm[j], s[2 * q + 1]);
+                }
+            };
+            if (full) first_sums(std::true_type{});
+            else first_sums(std::false_type{});
         }
+        if (SHIFT) __syncwarp();             // the slot's readers are done
+        fetch(r + steps * R * jump, slot);
+        slot = slot + 1 == steps ? 0 : slot + 1;
+        group_sums<G>(s, buf[0]);
+        float mg[R];
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            s.x += v[j];
-            s.y = fmaf(u[j], gm[j], s.y);
+        for (int q = 0; q < R; ++q) {
+            const float mean = __fdiv_rn(s[2 * q], (float)cols);
+            mg[q] = s[2 * q + 1] * inv;
+            s[2 * q] = s[2 * q + 1] = 0.0f;
+            const auto second_sums = [&](auto all) {
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    v[q][j] = all.value || first + j / V * step < cols ? v[q][j] - mean : 0.0f;
+                    s[2 * q] = fmaf(v[q][j], v[q][j], s[2 * q]);
+                    s[2 * q + 1] = fmaf(v[q][j], u[q][j] * gm[j], s[2 * q + 1]);
+                }
+            };
+            if (full) second_sums(std::true_type{});
+            else second_sums(std::false_type{});
         }
-        s = group_sum<G>(s, buf[0]);
-        const float mean = __fdiv_rn(s.x, (float)cols), mg = s.y * inv;
-        s = make_float2(0.0f, 0.0f);
+        group_sums<G>(s, buf[1]);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            v[j] = first + j / V * step < cols ? v[j] - mean : 0.0f;
-            s.x = fmaf(v[j], v[j], s.x);
-            s.y = fmaf(v[j], u[j] * gm[j], s.y);
-        }
-        s = group_sum<G>(s, buf[1]);
-        const float rs = 1.0f / sqrtf(s.x * inv + p.eps), k = s.y * inv * rs;
-        T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
+        for (int q = 0; q < R; ++q) {
+            const int64_t row = mine + r + q * jump;
+            const bool on = (G >= 32 && q == 0) || row < live;
+            if (q > 0 && !on) continue;
+            const float rs = rsqrtf(s[2 * q] * inv + p.eps), k = s[2 * q + 1] * inv * rs;
+            T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
+            const auto finish = [&](auto all) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = first + i * step;
-            float y[V];
-            if (p.residual.data) res.values(i, y);
+                for (int i = 0; i < N; ++i) {
+                    const int c = first + i * step;
+                    float y[V];
+                    if (extra) res[q].values(i, y);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int j = i * V + e;
-                const float h = v[j] * rs, w = on ? u[j] : 0.0f;
-                dg[j] = fmaf(w, h, dg[j]);
-                db[j] += w;
-                const float z = rs * (fmaf(u[j], gm[j], -mg) - h * k);
-                y[e] = p.residual.data ? z + y[e] : z;
-            }
-            if (c < cols && on) store_elems<T, V>(out + c, y);
+                    for (int e = 0; e < V; ++e) {
+                        const int j = i * V + e;
+                        const float h = v[q][j] * rs, w = on ? u[q][j] : 0.0f;
+                        dg[j] = fmaf(w, h, dg[j]);
+                        db[j] += w;
+                        const float z = rs * (fmaf(u[q][j], gm[j], -mg[q]) - h * k);
+                        y[e] = extra ? z + y[e] : z;
+                    }
+                    if ((all.value || c < cols) && on) store_elems<T, V>(out + c, y);
+                }
+            };
+            if (full) finish(std::true_type{});
+            else finish(std::false_type{});
         }
     }
     if (!p.parts) return;
@@ -487,26 +584,29 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, int 
 
 template <typename T, int V, int E, int G>
 aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
-    constexpr int TH = kThreadsOf<G>, groups = TH / G;
-    // as many rows ahead as an SM's shared memory holds
-    constexpr int AHEAD = E * sizeof(T) <= 36 ? 3 : (E * sizeof(T) <= 48 ? 2 : 1);
-    const void* kernel = grad ? (const void*)norm_grad_kernel<T, V, E, G, AHEAD> : (const void*)norm_kernel<T, V, E, G>;
-    const size_t sums = TH == G ? 0 : 2 * sizeof(float) * E * TH, slots = (AHEAD + 1) * 3 * (size_t)(V == 1 ? Shifted<T, E, TH>::BYTES : Slot<T, V, E, TH>::BYTES);
-    const size_t smem = !grad ? 0 : (sums > slots ? sums : slots);
+    constexpr int TH = kThreadsOf<G>, groups = TH / G, R = G >= 512 && E <= 9 ? 2 : 1;
+    const void* kernel = grad ? (const void*)norm_grad_kernel<T, V, E, G, R> : (const void*)norm_kernel<T, V, E, G>;
+    // two steps, one where two would hold more than 150 KB an SM: more are slower (25,000 x 512 fp32: 29.1 us with two, 29.9 with three, 32.1 with four, 33.3 with
+    // one; 6,000 x 2,048 with residual, 98 KB a step: 38.8 with one, 42.6 with two)
+    const size_t sums = TH == G ? 1 : 2 * sizeof(float) * E * TH, room = (size_t)150 * 1024 * TH / 512;
+    const size_t one = (size_t)R * (p.residual.data ? 3 : 2) * (V == 1 ? Shifted<T, E, TH>::BYTES : Slot<T, V, E, TH>::BYTES);
+    int steps = (int)(room / one);
+    steps = steps > 2 ? 2 : (steps < 1 ? 1 : steps);
+    const size_t smem = !grad ? 0 : (sums > steps * one ? sums : steps * one);
     if (smem && allow_smem(c, kernel, smem) != AA_OK) return AA_ERR_CUDA;
     int ctas = resident_ctas(c, kernel, TH, smem);
     if (ctas < 1) return AA_ERR_CUDA;
     const int64_t wanted = (p.live.rows + groups - 1) / groups;
     if (grad && ctas > kNormParts) ctas = kNormParts;
     if (ctas > wanted) ctas = (int)wanted;
-    void* args[] = {&p};
+    void* args[] = {&p, &steps};             // (the forward kernel takes the first alone)
     if (launch_overlapped(c, kernel, dim3(ctas), dim3(TH), args, smem, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     *n_parts = ctas;
     return AA_OK;
 }
 
-// The smallest group whose threads have 16 columns of bf16 each, or 8 of fp32 (more where no group is that wide).
+// The smallest group whose threads have 16 columns of bf16 each, or 8 of fp32 (more where no group is that wide, 8 where rows go in twos).
 template <typename T, int V>
 aa_status launch_width(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
     if constexpr (V == 1) {                  // whole warps, see Shifted
@@ -523,7 +623,8 @@ aa_status launch_width(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
         if (p.cols <= 512) return launch_rows<T, V, 16, 32>(c, p, grad, n);
         if (p.cols <= 1024) return launch_rows<T, V, 16, 64>(c, p, grad, n);
         if (p.cols <= 2048) return launch_rows<T, V, 16, 128>(c, p, grad, n);
-        if (p.cols <= 4096) return launch_rows<T, V, 16, 256>(c, p, grad, n);
+        // backward, rows in twos: 3,000 x 4,096 takes 30 us, 32 with 16 columns a thread
+        if (p.cols <= 4096) return grad && V == 8 ? launch_rows<T, V, 8, 512>(c, p, grad, n) : launch_rows<T, V, 16, 256>(c, p, grad, n);
     } else {
         if (p.cols <= 512) return launch_rows<T, V, 8, 64>(c, p, grad, n);
         if (p.cols <= 1024) return launch_rows<T, V, 8, 128>(c, p, grad, n);

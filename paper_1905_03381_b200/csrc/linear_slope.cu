@@ -127,8 +127,9 @@ __global__ void __launch_bounds__(256) slope_join_kernel(const float* parts, flo
     const int64_t col = (int64_t)blockIdx.x * 32 + lane;
     float sum = 0.0f;
     if (col < cols)
-#pragma unroll 4
-        for (int i = warp; i < kSlopeParts; i += 8) sum += parts[(int64_t)i * cols + col];
+#pragma unroll
+        for (int i = 0; i < kSlopeParts; i += 8)             // all loads at once
+            if (i + warp < kSlopeParts) sum += parts[(int64_t)(i + warp) * cols + col];
     sums[warp][lane] = sum;
     __syncthreads();
     if (warp == 0 && col < cols) {
