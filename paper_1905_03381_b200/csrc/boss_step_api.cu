@@ -183,39 +183,38 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
         if (!copy_g && dbias && !wide && product_tc_fits(grad_w)) grad_w.a_sums = dbias;
     }
     aa_status done = AA_OK;
-    SlopeParams s = {};
-    s.rows = x->rows;
-    s.live = live;
-    s.ctl = c->ctl;
-    if ((copy_g && (dx || dw)) || (dbias && !grad_w.a_sums)) {
-        s.dout = mat(dout);
+    // the pass over dout, then the copies of x and w
+    SlopeParams jobs[kSlopeJobs];
+    int n_jobs = 0;
+    const auto pass = [&](const aa_rows* from, const MatArg& to, const LiveRows& rows) -> SlopeParams& {
+        SlopeParams& s = jobs[n_jobs++];
+        s = {};
+        s.dout = mat(from);
+        s.g = to;
+        if (to.data && need.copies) s.plane = from->rows * to.stride;
+        s.rows = from->rows;
+        s.cols = from->cols;
+        s.live = rows;
+        s.act = AA_ACT_NONE;
+        s.ctl = c->ctl;
+        return s;
+    };
+    const bool want_g = copy_g && (dx || dw);
+    if (want_g || (dbias && !grad_w.a_sums)) {
+        SlopeParams& s = pass(dout, want_g ? g : MatArg{nullptr, 0}, live);
         s.pre = mat(pre);
-        if (copy_g && (dx || dw)) s.g = g;
-        if (s.g.data && need.copies) s.plane = x->rows * g.stride;
-        s.cols = w->rows;
         s.act = activation;
         s.parts = parts;
         s.dbias = grad_w.a_sums ? nullptr : dbias;
-        if ((done = launch_slope(c, s, x->dtype)) != AA_OK) return done;
+        // a pass that copies nothing is of another kind
+        if (s.plane == 0) {
+            if ((done = launch_slopes(c, jobs, 1, x->dtype)) != AA_OK) return done;
+            n_jobs = 0;
+        }
     }
-    s.pre = MatArg{nullptr, 0};
-    s.act = AA_ACT_NONE;
-    s.dbias = nullptr;
-    s.cols = x->cols;
-    if (dw && need.x) {
-        s.dout = mat(x);
-        s.g = xs;
-        s.plane = x->rows * xs.stride;
-        if ((done = launch_slope(c, s, x->dtype)) != AA_OK) return done;
-    }
-    if (dx && need.w) {
-        s.dout = mat(w);
-        s.g = ws;
-        s.plane = w->rows * ws.stride;
-        s.rows = w->rows;
-        s.live = live_arg(nullptr, 0, nullptr, w->rows);
-        if ((done = launch_slope(c, s, x->dtype)) != AA_OK) return done;
-    }
+    if (dw && need.x) pass(x, xs, live);
+    if (dx && need.w) pass(w, ws, live_arg(nullptr, 0, nullptr, w->rows));
+    if (n_jobs > 0 && (done = launch_slopes(c, jobs, n_jobs, x->dtype)) != AA_OK) return done;
     if (dx) {
         grad_x.b_across = true;
         grad_x.m = x->rows;

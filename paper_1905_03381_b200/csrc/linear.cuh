@@ -61,7 +61,9 @@ struct SlopeParams {
     Control* ctl;
 };
 constexpr int kSlopeParts = 148;
-aa_status launch_slope(aa_ctx_impl* c, const SlopeParams& p, int dtype);
+// n passes, one or up to kSlopeJobs copies (plane above 0), of which the first may have an activation and dbias.
+constexpr int kSlopeJobs = 3;
+aa_status launch_slopes(aa_ctx_impl* c, const SlopeParams* p, int n, int dtype);
 
 #ifdef __CUDACC__
 

@@ -11,11 +11,8 @@ namespace {
 // warp every eighth row, a lane V neighbouring columns (VEC: as one word); rows are shared out in kSlopeParts runs whose column sums stay apart until the join.
 // TERMS 0: g in the matrices' type.  1 or 3: bf16 terms of g in planes, rows up to a multiple of 64 behind the counted ones zero (the products that read them take 64 at a time).
 template <typename T, bool VEC, int ACT, int TERMS>
-__global__ void __launch_bounds__(256) slope_kernel(SlopeParams p) {
+__device__ __forceinline__ void slope(const SlopeParams& p, float (*sums)[32 * (16 / (int)sizeof(T))]) {
     constexpr int V = 16 / (int)sizeof(T);
-    __shared__ float sums[8][32 * V];
-    grid_dependency_wait();
-    grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t col = ((int64_t)blockIdx.x * 32 + lane) * V;
@@ -118,6 +115,19 @@ __global__ void __launch_bounds__(256) slope_kernel(SlopeParams p) {
     }
 }
 
+// The copies of a call are one launch (blockIdx.z): 4,099 x 515 x 1,001 fp32 takes 24 us as three and 18 as one.
+struct Slopes {
+    SlopeParams of[kSlopeJobs];
+};
+template <typename T, bool VEC, int ACT, int TERMS>
+__global__ void __launch_bounds__(256) slope_kernel(const __grid_constant__ Slopes jobs) {
+    __shared__ float sums[8][32 * (16 / (int)sizeof(T))];
+    grid_dependency_wait();
+    grid_dependency_release();
+    if (TERMS == 0 || blockIdx.z == 0) slope<T, VEC, ACT, TERMS>(jobs.of[0], sums);
+    else slope<T, VEC, AA_ACT_NONE, TERMS>(jobs.of[blockIdx.z], sums);
+}
+
 // 32 columns a CTA; each of 8 warps adds up every eighth part.
 __global__ void __launch_bounds__(256) slope_join_kernel(const float* parts, float* dbias, int64_t cols) {
     __shared__ float sums[8][32];
@@ -152,18 +162,27 @@ const void* slope_of(int act, bool planes) { return planes ? slope_of<T, VEC, si
 
 }  // namespace
 
-aa_status launch_slope(aa_ctx_impl* c, const SlopeParams& in, int dtype) {
-    SlopeParams p = in;
+aa_status launch_slopes(aa_ctx_impl* c, const SlopeParams* in, int n, int dtype) {
     const int es = dtype == AA_BF16 ? 2 : 4, wide = 16 / es;
     const auto aligned = [&](const MatArg& a) { return !a.data || ((uintptr_t)a.data % 16 == 0 && (a.stride * es) % 16 == 0); };
-    const bool vec = p.cols % wide == 0 && aligned(p.dout) && aligned(p.pre) && (p.plane > 0 || aligned(p.g));
-    const bool planes = p.plane > 0;
-    const void* kernel = dtype == AA_BF16 ? (vec ? slope_of<uint16_t, true>(p.act, planes) : slope_of<uint16_t, false>(p.act, planes))
-                                          : (vec ? slope_of<float, true>(p.act, planes) : slope_of<float, false>(p.act, planes));
-    void* args[] = {&p};
-    if (launch_overlapped(c, kernel, dim3((unsigned)((p.cols + 32 * wide - 1) / (32 * wide)), kSlopeParts), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
-    ++c->launches;
-    if (!p.dbias) return AA_OK;
+    const auto vectors = [&](const SlopeParams& p) { return p.cols % wide == 0 && aligned(p.dout) && aligned(p.pre) && (p.plane > 0 || aligned(p.g)); };
+    // neighbours whose rows are read in the same way go together
+    for (int i = 0, j; i < n; i = j) {
+        Slopes jobs = {};
+        const bool vec = vectors(in[i]), planes = in[i].plane > 0;
+        int64_t cols = 0;
+        for (j = i; j < n && vectors(in[j]) == vec; ++j) {
+            jobs.of[j - i] = in[j];
+            cols = cols < in[j].cols ? in[j].cols : cols;
+        }
+        const void* kernel = dtype == AA_BF16 ? (vec ? slope_of<uint16_t, true>(in[i].act, planes) : slope_of<uint16_t, false>(in[i].act, planes))
+                                              : (vec ? slope_of<float, true>(in[i].act, planes) : slope_of<float, false>(in[i].act, planes));
+        void* args[] = {&jobs};
+        if (launch_overlapped(c, kernel, dim3((unsigned)((cols + 32 * wide - 1) / (32 * wide)), kSlopeParts, (unsigned)(j - i)), dim3(256), args, 0, false) != cudaSuccess) return AA_ERR_CUDA;
+        ++c->launches;
+    }
+    if (!in[0].dbias) return AA_OK;
+    SlopeParams p = in[0];
     void* join[] = {&p.parts, &p.dbias, &p.cols};
     if (launch_overlapped(c, (const void*)slope_join_kernel, dim3((unsigned)((p.cols + 31) / 32)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
