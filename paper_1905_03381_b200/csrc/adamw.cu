@@ -5,6 +5,8 @@
 // copied to the device; a CTA finds its tensor by bisection over the running number of chunks.  A warp owns 256 consecutive elements, which is
 // one block of the 8-bit states: two runs of 128, four elements a lane in each, so that every access is contiguous over the warp, a lane's
 // four elements share one block of random words and the block's largest magnitude is a warp reduction.
+// 51.7 M parameters, bf16 gradients and copies: fp32 moments 219 us (1.44 GB, 6.5 TB/s: the copy rate); e4m3 moments 258 us (0.83 GB, 3.2 TB/s), bound by
+// 111 instructions an element, of which the draws, the decoding and the rounding to codes are most (64 % of the issue slots in use).
 // What is rounded to a code comes of products, sums and roots that are each rounded by themselves: the code depends on its last bits.
 #include <math.h>
 

