@@ -9,7 +9,7 @@ import torch
 import boss_step_reference as S
 from paper_1905_03381_b200 import binding as B
 from paper_1905_03381_b200 import build
-from test_gpu_boss_step import BF16, DEV, F32, HALF, c, check_linear, close, entry, f64, i32, like, mat, norm_bars
+from test_gpu_boss_step import BF16, DEV, F32, HALF, c, check_grad, check_linear, close, entry, f64, i32, like, mat, norm_bars
 
 pytestmark = pytest.mark.gpu
 
@@ -33,6 +33,26 @@ def test_linear_with_every_operand_on_ragged_tiles(aa, dtype, m, k, n):
         close(p, z, pre_bar)
     out, _, want, _, bar, _ = check_linear(aa, dtype, m, k, n, "relu", True, True, False, (1, 3, 5), 1)
     close(out, want, bar)
+
+
+@pytest.mark.parametrize("m,k,n,pads,shift", [(70, 1024, 2056, (0, 0, 0), 0), (40, 1025, 2049, (0, 0, 0), 0), (5, 1500, 1501, (1, 3, 5), 1), (300, 1032, 2064, (0, 0, 0), 0)])
+def test_gradients_of_large_fp32_weights_and_few_rows(aa, m, k, n, pads, shift):
+    """Not worth copies of the weights: taken apart on the way."""
+    check_grad(aa, F32, m, k, n, "silu", True, pads, shift)
+    check_grad(aa, F32, m, k, n, None, False, pads, shift)
+
+
+@pytest.mark.parametrize("m,k,n", [(3, 64, 40), (200, 512, 512), (700, 264, 1000)])
+def test_gradients_where_dout_alone_starts_anywhere(aa, m, k, n):
+    x, w, dout = mat(m, k, 1, BF16), mat(n, k, 2, BF16, std=k ** -0.5), mat(m, n, 3, BF16, 3, 1)
+    for rows in (m, m // 2):
+        dx, dw, db = like((m, k), BF16), like((n, k), BF16), torch.full((n,), 7.0, device=DEV)
+        aa.aa_linear_grad(x, w, dout, aa.linear_grad_scratch(x, w), dx=dx, dw=dw, dbias=db, count_dev=i32([rows]))
+        got, size, _ = S.linear_grad(f64(x)[:rows], f64(w), f64(dout)[:rows], None, None, None)
+        close(dx[:rows], got["dx"], c(n) * size["dx"] + HALF[BF16] * np.abs(got["dx"]))
+        assert torch.all(dx[rows:] == 7.0)
+        close(dw, got["dw"], c(rows) * size["dw"] + HALF[BF16] * np.abs(got["dw"]))
+        close(db, got["dbias"], c(rows) * size["dbias"])
 
 
 class Layer:
