@@ -1,6 +1,8 @@
 // C entry points of linear layers and layer normalisation: argument checks and dispatch.
 #include <string.h>
 
+#include <algorithm>
+
 #include "boss_args.cuh"
 #include "layer_norm.cuh"
 #include "linear.cuh"
@@ -43,13 +45,15 @@ constexpr int64_t kFewRowsOfCopies = 512, kWeightsOfCopies = 1 << 21;
 
 bool by_tma(const aa_rows* m) { return (uintptr_t)m->data % 16 == 0 && m->row_stride % 8 == 0; }
 
-// G, x and w as far as they are copied, then the column sums' parts or (later in the call) the products' parts.
+// G, x and w as far as they are copied, then the column sums' parts or (later in the call) the products' parts, and the runs of long bf16 products.
 struct LinearScratch {
-    size_t g, x, w, parts, total;            // bytes
+    size_t g, x, w, parts, runs, total;      // bytes
     bool copies;
 };
 // The parts of a cut tile are 256 KB in fp32 on each pair of SMs; three rounds of them (58 MB) leave little to balance.
 constexpr size_t kProductParts = 3ull * 74 * 256 * 256 * sizeof(float);
+// One tile a pair of SMs.
+constexpr size_t kProductRuns = 74ull * 256 * 256 * sizeof(float);
 int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
 LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
@@ -63,7 +67,8 @@ LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     if (s.copies && (wide || !by_tma(w))) s.w = up((size_t)cols * (size_t)padded(inner) * each);
     const size_t sums = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));
     s.parts = sums < kProductParts ? kProductParts : sums;
-    s.total = s.g + s.x + s.w + s.parts;
+    s.runs = !wide && std::max(rows, cols) > (int64_t)kTcRun * 64 ? kProductRuns : 0;
+    s.total = s.g + s.x + s.w + s.parts + s.runs;
     return s;
 }
 
@@ -161,6 +166,8 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
     grad_x.live = grad_w.live = live;
     grad_x.parts = grad_w.parts = parts;
     grad_x.part_floats = grad_w.part_floats = (int64_t)(need.parts / sizeof(float));
+    grad_x.runs = grad_w.runs = need.runs ? parts + need.parts / sizeof(float) : nullptr;
+    grad_x.run_floats = grad_w.run_floats = (int64_t)(need.runs / sizeof(float));
     // G is a matrix of its own where there is an activation, or where dout is copied
     const bool copy_g = need.g > 0 && (act || planes || !by_tma(dout));
     const MatArg g = copy_g ? MatArg{at, padded(w->rows)} : mat(dout);

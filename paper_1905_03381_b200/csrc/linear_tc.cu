@@ -12,8 +12,16 @@
 // 8,192^3 takes 690 us (1.59 PFLOP/s, of 1.62 that a library's plain product reaches in a burst); 25,000 x 2,048 -> 512 44 us behind other launches (1.19 PFLOP/s):
 // 196 tiles are 2.65 rounds of 74 pairs, which a forward call, without scratch memory, takes as three.  Few rows are bound by latency: 64 x 512 -> 2,048 takes 10 us.
 //
+// The matrix unit rounds a sum towards zero, by a step of it (a part in 2^23 at most) once in 16 terms, all in one direction: a million terms of one sign lose more than the
+// rounding to bf16 does.  So backward a run of 16,384 terms (a part in 2^13 at most, 2^-16 measured) goes to the epilogue, which adds the runs up in fp32 with ordinary rounding, in
+// scratch memory that stays in L2, while the next run's products go on.  The vocabulary gradients take 1,510 us without runs, 1,535 with these, 1,610 and 1,670 with runs of
+// 8,192 and 4,096 terms.  A forward call has no scratch memory: 32,768 terms in one run at most (a part in 2^12, an eighth of what the rounding to bf16 may take), longer
+// contractions by linear_split.cu.
+//
 // Tiles that do not fill the last round of SMs can be cut along the contraction (the backward call has scratch memory): their parts go to
 // scratch in fp32 and a second kernel adds them up in order and finishes them.
+#include <algorithm>
+
 #include "cta_pair.cuh"
 #include "linear_plan.cuh"
 
@@ -82,6 +90,7 @@ __global__ void __launch_bounds__(SUMS ? kSumThreads : kTcThreads, 1)
 product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductParams p, const __grid_constant__ Plan plan,
                   bool vec) {
     using G = Geo<CG, BN>;
+    constexpr bool PARTS = A_ACROSS || B_ACROSS;         // a backward call: scratch memory for parts and runs
     extern __shared__ unsigned char smem_raw[];
     __shared__ Ctl ctl;
     unsigned char* ring = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -180,55 +189,57 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         uint32_t sent = 0, ragged = 0;
         for (int i = first; i < units && ok; i += step) {
             const Unit u = unit_at(plan, mt, slices, i);
-            if (u.s0 == u.s1) continue;
-            const int buf = it & 1;
-            const uint32_t d = tmem + (uint32_t)(buf * BN);
-            if (rank == 0) {
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_empty[buf], (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag))) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after_sync();
-            }
-            ++it;
-            for (int s = u.s0; s < u.s1; ++s, ++sent) {
-                const int stage = (int)(sent % G::STAGES), left = (int)min((int64_t)kSlice, k_end - (int64_t)s * kSlice);
-                unsigned char* at = ring + (size_t)stage * G::STAGE;
-                // stored rows past the counted ones may hold anything, and must not reach a sum, not even times zero
-                const bool clear = A_ACROSS && B_ACROSS && left < kSlice && k_end < p.k;
-                if (rank == 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], (sent / G::STAGES) & 1u, abort_flag));
-                else if (clear) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ctl.ragged, ragged, abort_flag));
-                if (!ok) break;
-                if (clear) {
-                    if (CG == 2 && rank == 0 && lane == 0) mbar_arrive_at(of_rank(&ctl.ragged, 1));
-                    const int per = (kSlice - left) * 8;
-                    for (int q = lane; q < per * (kBM + G::ROWS_B) / 64; q += 32) {
-                        const int c = q / per, r = q - c * per;
-                        *reinterpret_cast<uint4*>(at + c * 8192 + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (CG == 2) {
-                        if (rank == 1 && lane == 0) mbar_release_at(of_rank(&ctl.cleared, 0));
-                        if (rank == 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.cleared, ragged, abort_flag))) {
-                            ok = false;
-                            break;
-                        }
-                        ragged ^= 1u;
-                    }
-                }
+            for (int r0 = u.s0, r1; r0 < u.s1 && ok; r0 = r1) {
+                r1 = PARTS && u.s1 - r0 > plan.run ? r0 + plan.run : u.s1;
+                const int buf = it & 1;
+                const uint32_t d = tmem + (uint32_t)(buf * BN);
                 if (rank == 0) {
-                    tc_fence_after_sync();
-                    if (elect_one()) {
-                        // the address is the descriptor's low field, in units of 16 bytes
-                        const uint64_t ad = a_desc + (uint64_t)(uint32_t)(stage * (G::STAGE >> 4)), bd = b_desc + (uint64_t)(uint32_t)(stage * (G::STAGE >> 4));
-#pragma unroll
-                        for (int k = 0; k < kSlice / 16; ++k) mma<CG>(d, ad + (A_ACROSS ? k * 128 : k * 2), bd + (B_ACROSS ? k * 128 : k * 2), idesc, s > u.s0 || k > 0);
-                        commit<CG>(&ctl.empty[stage]);
-                        if (SUMS) commit<CG>(&ctl.done[stage]);
-                        if (s == u.s1 - 1) commit<CG>(&ctl.acc_full[buf]);
+                    if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_empty[buf], (uint32_t)(((it >> 1) & 1) ^ 1), abort_flag))) {
+                        ok = false;
+                        break;
                     }
-                    __syncwarp();
+                    tc_fence_after_sync();
+                }
+                ++it;
+                for (int s = r0; s < r1; ++s, ++sent) {
+                    const int stage = (int)(sent % G::STAGES), left = (int)min((int64_t)kSlice, k_end - (int64_t)s * kSlice);
+                    unsigned char* at = ring + (size_t)stage * G::STAGE;
+                    // stored rows past the counted ones may hold anything, and must not reach a sum, not even times zero
+                    const bool clear = A_ACROSS && B_ACROSS && left < kSlice && k_end < p.k;
+                    if (rank == 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ctl.full[stage], (sent / G::STAGES) & 1u, abort_flag));
+                    else if (clear) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&ctl.ragged, ragged, abort_flag));
+                    if (!ok) break;
+                    if (clear) {
+                        if (CG == 2 && rank == 0 && lane == 0) mbar_arrive_at(of_rank(&ctl.ragged, 1));
+                        const int per = (kSlice - left) * 8;
+                        for (int q = lane; q < per * (kBM + G::ROWS_B) / 64; q += 32) {
+                            const int c = q / per, r = q - c * per;
+                            *reinterpret_cast<uint4*>(at + c * 8192 + left * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (CG == 2) {
+                            if (rank == 1 && lane == 0) mbar_release_at(of_rank(&ctl.cleared, 0));
+                            if (rank == 0 && !__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.cleared, ragged, abort_flag))) {
+                                ok = false;
+                                break;
+                            }
+                            ragged ^= 1u;
+                        }
+                    }
+                    if (rank == 0) {
+                        tc_fence_after_sync();
+                        if (elect_one()) {
+                            // the address is the descriptor's low field, in units of 16 bytes
+                            const uint64_t ad = a_desc + (uint64_t)(uint32_t)(stage * (G::STAGE >> 4)), bd = b_desc + (uint64_t)(uint32_t)(stage * (G::STAGE >> 4));
+#pragma unroll
+                            for (int k = 0; k < kSlice / 16; ++k) mma<CG>(d, ad + (A_ACROSS ? k * 128 : k * 2), bd + (B_ACROSS ? k * 128 : k * 2), idesc, s > r0 || k > 0);
+                            commit<CG>(&ctl.empty[stage]);
+                            if (SUMS) commit<CG>(&ctl.done[stage]);
+                            if (s == r1 - 1) commit<CG>(&ctl.acc_full[buf]);
+                        }
+                        __syncwarp();
+                    }
                 }
             }
         }
@@ -297,98 +308,115 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (int i = first; i < units && ok; i += step) {
             const Unit u = unit_at(plan, mt, slices, i);
             const bool some = u.s0 < u.s1;   // else no term at all
-            const int buf = it & 1;
-            if (some) {
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_full[buf], (uint32_t)((it >> 1) & 1), abort_flag))) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after_sync();
-                ++it;
-            }
-            if (JOIN) {
-                // every CTA of the cluster is through with its ring: its shared memory takes the parts of 128 / cluster rows
-                last = u;
-                has = true;
-                cluster_sync_all();
-            }
             const int64_t row0 = ((int64_t)u.m * CG + rank) * kBM + quad * 32 + r8;
             const int rows = (int)max((int64_t)0, min((int64_t)32, m_end - row0 + r8));      // of the warp's 32 that count
-#pragma unroll 1
-            for (int c = 0; c < BN / 64; ++c) {
-                const int64_t col = (int64_t)u.n * BN + half * (BN / 2) + c * 32 + sub * 4;
-                const bool whole = vec && col + 4 <= p.n;
-                uint2 add[8];
-                if (res && whole && u.part < 0) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) add[q] = r8 + q * 4 < rows ? *reinterpret_cast<const uint2*>(res + (row0 + q * 4) * p.residual.stride + col) : make_uint2(0, 0);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) add[q] = make_uint2(0, 0);
-                }
-                float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (p.bias) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) bias[e] = col + e < p.n ? p.bias[col + e] : 0.0f;
-                }
-                uint32_t v[32];
+            // where a part goes, and where the runs before are: [rows of a tile][columns of a tile]
+            float* sums = !PARTS ? nullptr : u.part >= 0 ? plan.parts + (int64_t)u.part * CG * kBM * BN : (u.s1 - u.s0 > plan.run ? p.runs + (int64_t)first * CG * kBM * BN : nullptr);
+            if (sums) sums += (int64_t)(rank * kBM + quad * 32 + r8) * BN + half * (BN / 2) + sub * 4;
+            int s = u.s0;                    // the run's first slice
+            do {
+                const bool head = s == u.s0, whole_tile = !JOIN && (!PARTS || (u.part < 0 && u.s1 - s <= plan.run));
+                s += min(plan.run, u.s1 - s);
+                const int buf = it & 1;
                 if (some) {
-                    tmem_ld_32cols(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2) + c * 32), v);
-                    tmem_ld_wait();
-                    if (c == BN / 64 - 1) {
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (CG == 1) mbar_arrive(&ctl.acc_empty[buf]);
-                            else mbar_arrive_at(of_rank(&ctl.acc_empty[buf], 0));
-                        }
+                    if (!__all_sync(0xFFFFFFFFu, mbar_wait(&ctl.acc_full[buf], (uint32_t)((it >> 1) & 1), abort_flag))) {
+                        ok = false;
+                        break;
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = 0u;
+                    tc_fence_after_sync();
+                    ++it;
                 }
                 if (JOIN) {
-                    const int rows = kBM / plan.cluster, r = quad * 32 + lane;
-                    const uint32_t to = of_rank(ring, (uint32_t)(r / rows)) + (uint32_t)((((int)cluster_rank() * rows + r % rows) * BN + half * (BN / 2) + c * 32) * 4);
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        store_remote(to + (uint32_t)(e * 4), make_float4(__uint_as_float(v[e]), __uint_as_float(v[e + 1]), __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])));
-                    continue;
+                    // every CTA of the cluster is through with its ring: its shared memory takes the parts of 128 / cluster rows
+                    last = u;
+                    has = true;
+                    cluster_sync_all();
                 }
-                __syncwarp();                // the stage's readers of the chunk before are done
-#pragma unroll
-                for (int w = 0; w < 8; ++w)
-                    *reinterpret_cast<uint4*>(mine + lane * 32 + ((w ^ (lane & 7)) << 2)) = make_uint4(v[4 * w], v[4 * w + 1], v[4 * w + 2], v[4 * w + 3]);
-                __syncwarp();
-                if (u.part >= 0) {
-                    float* to = plan.parts + ((int64_t)u.part * CG + rank) * kBM * BN + (int64_t)(quad * 32 + r8) * BN + half * (BN / 2) + c * 32 + sub * 4;
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        *reinterpret_cast<float4*>(to + q * 4 * BN) = *reinterpret_cast<const float4*>(mine + (q * 4 + r8) * 32 + ((sub ^ ((q * 4 + r8) & 7)) << 2));
-                    continue;
-                }
-                if (whole) {
-                    const uint32_t at = smem_u32(mine + r8 * 32);
-                    uint16_t* to = out + row0 * p.out.stride + col;
-                    uint16_t* raw = pre ? pre + row0 * p.pre.stride + col : nullptr;
-                    if (p.act == AA_ACT_NONE) put_chunk<AA_ACT_NONE>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
-                    else if (p.act == AA_ACT_RELU) put_chunk<AA_ACT_RELU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
-                    else if (p.act == AA_ACT_GELU) put_chunk<AA_ACT_GELU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
-                    else put_chunk<AA_ACT_SILU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
-                } else {
 #pragma unroll 1
-                    for (int q0 = 0; q0 < 8; q0 += 4) {
-                        float z[16];
+                for (int c = 0; c < BN / 64; ++c) {
+                    const int64_t col = (int64_t)u.n * BN + half * (BN / 2) + c * 32 + sub * 4;
+                    const bool whole = vec && col + 4 <= p.n;
+                    uint2 add[8];
+                    if (res && whole && whole_tile) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int r = (q0 + q) * 4 + r8;
-                            const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
-                            z[q * 4] = f.x, z[q * 4 + 1] = f.y, z[q * 4 + 2] = f.z, z[q * 4 + 3] = f.w;
+                        for (int q = 0; q < 8; ++q) add[q] = r8 + q * 4 < rows ? *reinterpret_cast<const uint2*>(res + (row0 + q * 4) * p.residual.stride + col) : make_uint2(0, 0);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) add[q] = make_uint2(0, 0);
+                    }
+                    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (p.bias) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) bias[e] = col + e < p.n ? p.bias[col + e] : 0.0f;
+                    }
+                    uint32_t v[32];
+                    if (some) {
+                        tmem_ld_32cols(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2) + c * 32), v);
+                        tmem_ld_wait();
+                        if (c == BN / 64 - 1) {
+                            tc_fence_before_sync();
+                            __syncwarp();
+                            if (lane == 0) {
+                                if (CG == 1) mbar_arrive(&ctl.acc_empty[buf]);
+                                else mbar_arrive_at(of_rank(&ctl.acc_empty[buf], 0));
+                            }
                         }
-                        finish_quads<uint16_t, 4>(p, z, bias, row0 + q0 * 4, 4, m_end, col, false);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0u;
+                    }
+                    if (JOIN) {
+                        const int rows = kBM / plan.cluster, r = quad * 32 + lane;
+                        const uint32_t to = of_rank(ring, (uint32_t)(r / rows)) + (uint32_t)((((int)cluster_rank() * rows + r % rows) * BN + half * (BN / 2) + c * 32) * 4);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            store_remote(to + (uint32_t)(e * 4), make_float4(__uint_as_float(v[e]), __uint_as_float(v[e + 1]), __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])));
+                        continue;
+                    }
+                    __syncwarp();            // the stage's readers of the chunk before are done
+#pragma unroll
+                    for (int w = 0; w < 8; ++w)
+                        *reinterpret_cast<uint4*>(mine + lane * 32 + ((w ^ (lane & 7)) << 2)) = make_uint4(v[4 * w], v[4 * w + 1], v[4 * w + 2], v[4 * w + 3]);
+                    __syncwarp();
+                    if (sums) {
+                        // the places that this lane wrote and reads
+                        float* at = sums + c * 32;
+#pragma unroll
+                        for (int q = 0; q < 8; ++q, at += 4 * BN) {
+                            float4* own = reinterpret_cast<float4*>(mine + (q * 4 + r8) * 32 + ((sub ^ ((q * 4 + r8) & 7)) << 2));
+                            float4 f = *own;
+                            if (!head) {
+                                const float4 g = *reinterpret_cast<const float4*>(at);
+                                f = make_float4(g.x + f.x, g.y + f.y, g.z + f.z, g.w + f.w);
+                            }
+                            if (whole_tile) *own = f;
+                            else *reinterpret_cast<float4*>(at) = f;
+                        }
+                        if (!whole_tile) continue;
+                    }
+                    if (whole) {
+                        const uint32_t at = smem_u32(mine + r8 * 32);
+                        uint16_t* to = out + row0 * p.out.stride + col;
+                        uint16_t* raw = pre ? pre + row0 * p.pre.stride + col : nullptr;
+                        if (p.act == AA_ACT_NONE) put_chunk<AA_ACT_NONE>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
+                        else if (p.act == AA_ACT_RELU) put_chunk<AA_ACT_RELU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
+                        else if (p.act == AA_ACT_GELU) put_chunk<AA_ACT_GELU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
+                        else put_chunk<AA_ACT_SILU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
+                    } else {
+#pragma unroll 1
+                        for (int q0 = 0; q0 < 8; q0 += 4) {
+                            float z[16];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const int r = (q0 + q) * 4 + r8;
+                                const float4 f = *reinterpret_cast<const float4*>(mine + r * 32 + ((sub ^ (r & 7)) << 2));
+                                z[q * 4] = f.x, z[q * 4 + 1] = f.y, z[q * 4 + 2] = f.z, z[q * 4 + 3] = f.w;
+                            }
+                            finish_quads<uint16_t, 4>(p, z, bias, row0 + q0 * 4, 4, m_end, col, false);
+                        }
                     }
                 }
-            }
+            } while (PARTS && s < u.s1);
         }
     }
     if (JOIN) {
@@ -421,15 +449,18 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec, int clust
     const int64_t mt = (p.m + CG * kBM - 1) / (CG * kBM), nt = (p.n + BN - 1) / BN, tiles = mt * nt;
     const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA, SUMS, JOIN>;
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
-    const int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kThreads, G::SMEM, CG);
+    int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kThreads, G::SMEM, CG);
+    const bool runs = p.runs && p.k > (int64_t)kTcRun * kSlice;
+    if (runs) teams = (int)std::min<int64_t>(teams, p.run_floats / (CG * kBM * BN));       // a team has the memory of one tile
     if (teams < 1) return AA_ERR_CUDA;
-    const Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2, cluster);
+    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2, cluster);
+    if (runs) plan.run = kTcRun;
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
-    void* args[] = {&map_a, &map_b, &p, const_cast<Plan*>(&plan), &vec};
+    void* args[] = {&map_a, &map_b, &p, &plan, &vec};
     if (launch_clusters(c, kernel, (unsigned)(JOIN ? units : (units < teams ? units : teams) * CG), kThreads, args, G::SMEM, JOIN ? cluster : CG) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
     if (tail == 0 || JOIN) return AA_OK;
-    void* join[] = {&p, const_cast<Plan*>(&plan), &vec};
+    void* join[] = {&p, &plan, &vec};
     const int64_t threads = tail * CG * kBM * BN / 4;
     if (launch_overlapped(c, (const void*)product_join_kernel<uint16_t, CG * kBM, BN>, dim3((unsigned)(threads / 256)), dim3(256), join, 0, false) != cudaSuccess) return AA_ERR_CUDA;
     ++c->launches;
@@ -455,7 +486,7 @@ aa_status launch_majors(aa_ctx_impl* c, const ProductParams& p, bool vec) {
 bool product_tc_fits(const ProductParams& p) {
     const auto tma = [](const MatArg& a) { return (uintptr_t)a.data % 16 == 0 && a.stride % 8 == 0; };
     const int64_t tiles = ((p.m + kBM - 1) / kBM) * ((p.n + 63) / 64);
-    return tma(p.a) && tma(p.b) && p.m <= 0x3FFFFFFF && p.n <= 0x3FFFFFFF && p.k <= 0x3FFFFFFF && tiles < 0x3FFFFFF;
+    return tma(p.a) && tma(p.b) && p.m <= 0x3FFFFFFF && p.n <= 0x3FFFFFFF && p.k <= (p.runs ? 0x3FFFFFFFll : kTcTerms) && tiles < 0x3FFFFFF;
 }
 
 aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p) {
