@@ -8,7 +8,7 @@ import torch
 
 from paper_1905_03381_b200 import binding as B
 from paper_1905_03381_b200 import build
-from test_gpu_boss_step import BF16, DEV, HALF
+from test_gpu_boss_step import BF16, DEV, F32, HALF, c, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -32,6 +32,11 @@ def random(shape, seed, dtype=BF16, std=1.0):
 def below(got, bar):
     off = got.double().abs() - bar
     assert torch.all(off <= 0), f"off by {got.double().abs().max():.3e}, {off.max():.3e} above the bar"
+
+
+def close(got, want, bar):
+    assert torch.all(torch.isfinite(got))
+    below(got.double() - want, bar)
 
 
 def cancelling(rows, cols, seed, minus):
@@ -71,3 +76,81 @@ def test_long_contractions_keep_their_sums(aa):
     aa.aa_linear_grad(x, w, dout, aa.linear_grad_scratch(x, w), dx=dx)
     size = 2.0 * (dout[:, :k // 2].float() @ w[:k // 2].float()).double()
     below(dx, (2.0**-15 + k / 16384 * 2.0**-24) * size)
+
+
+ACT = {None: lambda z: z, "relu": torch.relu, "gelu": torch.nn.functional.gelu, "silu": torch.nn.functional.silu}
+
+
+# the first two of each: 54 and 153 tiles for 74 pairs of CTAs; the odd one has rows whose ends no vector meets
+@pytest.mark.parametrize("dtype,m,k,n", [(BF16, 1300, 72, 2056), (BF16, 2100, 264, 4104), (BF16, 1111, 520, 4101), (F32, 1300, 65, 2051)])
+@pytest.mark.parametrize("act", [None, "gelu", "relu"])
+def test_linear_on_tiles_of_pairs(aa, dtype, m, k, n, act):
+    x, w, bias = random((m, k), 1, dtype), random((n, k), 2, dtype, k ** -0.5), random((n,), 3, F32, 0.5)
+    res = random((m, n), 4, dtype)
+    out, pre = torch.empty_like(res), torch.empty_like(res)
+    for rows in (m, m - 77, 257, 1):
+        x[rows:] = float("nan")
+        res[rows:] = float("nan")
+        out.fill_(7.0), pre.fill_(7.0)
+        aa.aa_linear(x, w, out, bias=bias, activation=act, residual=res, pre=pre, count_dev=i32([rows]))
+        X, W = x[:rows].double(), w.double()
+        z = X @ W.t() + bias.double()
+        size = X.abs() @ W.t().abs() + bias.double().abs()
+        want = ACT[act](z) + res[:rows].double()
+        close(pre[:rows], z, c(k) * size + HALF[dtype] * z.abs())
+        close(out[:rows], want, 1.13 * c(k) * size + 2.0**-20 * z.abs().clamp(min=1.0) * (act is not None) + HALF[dtype] * want.abs() + 2.0**-22 * z.abs())
+        assert torch.all(out[rows:] == 7.0) and torch.all(pre[rows:] == 7.0)
+
+
+def check_grad(aa, dtype, m, k, n, act, counts, which=("dx", "dw", "dbias")):
+    """Counted rows have NaN behind them; counts are taken from the largest on."""
+    x, w, dout = random((m, k), 1, dtype), random((n, k), 2, dtype, k ** -0.5), random((m, n), 3, dtype)
+    pre, res = random((m, n), 4, dtype) if act else None, random((m, k), 5, dtype)
+    z = None if pre is None else pre.double().requires_grad_()
+    G = dout.double() if act is None else torch.autograd.grad(ACT[act](z), z, dout.double())[0]
+    absolute = 2.0**-20 * (act not in (None, "relu"))              # of a slope
+    rounded = 2.0**-8 if dtype == BF16 and act not in (None, "relu") else 0.0
+    scratch = aa.linear_grad_scratch(x, w, act)
+    for rows in counts:
+        for t in (x, dout, res) + (() if pre is None else (pre,)):
+            t[rows:] = float("nan")
+        scratch.fill_(255)                                        # NaN in every type
+        got = {"dx": torch.full_like(x, 7.0), "dw": torch.full_like(w, 7.0), "dbias": torch.full((n,), 7.0, device=DEV)}
+        got = {name: got[name] for name in which}
+        aa.aa_linear_grad(x, w, dout, scratch, activation=act, pre=pre, residual=res if "dx" in which else None, count_dev=i32([rows]), **got)
+        X, W, g, d = x[:rows].double(), w.double(), G[:rows], dout[:rows].double().abs()
+        if "dx" in which:
+            want = g @ W + res[:rows].double()
+            close(got["dx"][:rows], want, (c(n) + rounded) * (g.abs() @ W.abs()) + absolute * (d @ W.abs()) + (HALF[dtype] + 2.0**-22) * want.abs())
+            assert torch.all(got["dx"][rows:] == 7.0)
+        if "dw" in which:
+            want = g.t() @ X
+            close(got["dw"], want, (c(rows) + rounded) * (g.t().abs() @ X.abs()) + absolute * (d.t() @ X.abs()) + (HALF[dtype] + 2.0**-22) * want.abs())
+        if "dbias" in which:
+            close(got["dbias"], g.sum(0), c(rows) * g.abs().sum(0) + absolute * d.sum(0))
+
+
+@pytest.mark.parametrize("act", [None, "relu", "silu"])
+@pytest.mark.parametrize("m,k,n", [(5003, 520, 4616), (9001, 2312, 2320), (4999, 1000, 264)])
+def test_gradients_on_tiles_of_pairs(aa, m, k, n, act):
+    """Tiles of pairs in dx and dw: fewer than there are pairs, all of them cut; more, some of them cut; widths off the tiles.  Counts that end inside a slice of 64 tokens, at its
+    end, and that leave nothing."""
+    check_grad(aa, BF16, m, k, n, act, (m, m - 29, 4100, 128, 65, 64, 1, 0))
+
+
+@pytest.mark.parametrize("act", [None, "gelu"])
+def test_gradients_alone_on_tiles_of_pairs(aa, act):
+    for which in (("dx",), ("dw",), ("dbias",), ("dw", "dbias"), ("dx", "dw")):
+        check_grad(aa, BF16, 5003, 520, 4616, act, (4999,), which)
+
+
+@pytest.mark.parametrize("m,k,n", [(3000, 2312, 17000), (17001, 600, 2312), (33000, 264, 640), (300_000, 264, 640)])
+def test_gradients_whose_contractions_take_several_runs(aa, m, k, n):
+    """Runs of whole tiles and of cut ones, with the sums of dout beside them."""
+    check_grad(aa, BF16, m, k, n, None, (m, m - 29))
+
+
+@pytest.mark.parametrize("act", [None, "silu"])
+@pytest.mark.parametrize("m,k,n", [(2050, 1300, 2400), (2051, 1301, 2403)])
+def test_fp32_gradients_with_several_tiles_a_pair(aa, m, k, n, act):
+    check_grad(aa, F32, m, k, n, act, (m, m - 29, 65, 0))
