@@ -154,3 +154,53 @@ def test_gradients_whose_contractions_take_several_runs(aa, m, k, n):
 @pytest.mark.parametrize("m,k,n", [(2050, 1300, 2400), (2051, 1301, 2403)])
 def test_fp32_gradients_with_several_tiles_a_pair(aa, m, k, n, act):
     check_grad(aa, F32, m, k, n, act, (m, m - 29, 65, 0))
+
+
+# ---------------------------------------------------------------------------------------------------------------------- norm
+
+def norm_reference(x, gamma, eps):
+    c = x - x.mean(1, keepdim=True)
+    r = 1.0 / torch.sqrt((c * c).mean(1, keepdim=True) + eps)
+    h = c * r
+    return h, r, 2.0**-18 * (1.0 + h.abs()) + r * 2.0**-18 * x.abs().mean(1, keepdim=True)       # the last: what h may be off by
+
+
+def strided(m, n, seed, dtype, pad):
+    return random((m, n + pad), seed, dtype)[:, :n]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("m,n,pad", [(701, 4096, 0), (701, 4099, 0), (450, 5000, 0), (450, 5000, 3), (700, 8192, 0), (700, 8192, 1), (6001, 512, 0), (6001, 512, 5), (3001, 1024, 0), (2003, 2048, 0),
+                                     (20001, 64, 0), (20001, 100, 0), (1201, 3000, 1), (40, 8200, 0)])
+def test_norm_with_several_rows_a_group(aa, dtype, m, n, pad):
+    """More rows than the threads that are resident take at once; counts that leave an odd number of them to the last, with NaN behind; in place."""
+    x, d, res = (strided(m, n, seed, dtype, pad) for seed in (1, 2, 3))
+    x.mul_(1.5).add_(0.3)
+    gamma, beta = 1.0 + random((n,), 4, F32, 0.3), random((n,), 5, F32, 0.3)
+    scratch = aa.layer_norm_grad_scratch(x)
+    for rows in (m, m - 1, m // 2 + 1, 3):
+        for t in (x, d, res):
+            t[rows:] = float("nan")
+        live = {"count_dev": i32([rows])}
+        X, D = x[:rows].double(), d[:rows].double()
+        h, r, e = norm_reference(X, gamma, 1e-5)
+        g = D * gamma.double()
+        want = h * gamma.double() + beta.double()
+        out = torch.full_like(x, 7.0)
+        aa.aa_layer_norm(x, out, gamma=gamma, beta=beta, **live)
+        close(out[:rows], want, gamma.double().abs() * e + (HALF[dtype] + 2.0**-22) * want.abs())
+        assert torch.all(out[rows:] == 7.0)
+        mg, mgh = g.abs().mean(1, keepdim=True), (g * h).abs().mean(1, keepdim=True)
+        plain = r * (g - g.mean(1, keepdim=True) - h * (g * h).mean(1, keepdim=True))
+        bar = r * (2.0**-18 * (g.abs() + mg) + e * (mgh + mg) + h.abs() * ((g.abs() * e).mean(1, keepdim=True) + 2.0**-18 * mgh)) + 2.0**-17 * plain.abs()
+        for residual, onto in ((None, None), (res, None), (res, d), (None, x)):
+            dx = torch.full_like(x, 7.0) if onto is None else onto.clone()
+            a, b = (dx if onto is x else x), (dx if onto is d else d)
+            dg, db = torch.full((n,), 7.0, device=DEV), torch.full((n,), 7.0, device=DEV)
+            behind = dx[rows:].clone()
+            aa.aa_layer_norm_grad(a, b, dx, scratch, gamma=gamma, residual=residual, dgamma=dg, dbeta=db, **live)
+            want = plain + (0.0 if residual is None else res[:rows].double())
+            close(dx[:rows], want, bar + 2.0**-22 * want.abs() + HALF[dtype] * want.abs())
+            assert torch.equal(dx[rows:].view(torch.int32 if dtype == F32 else torch.int16), behind.view(torch.int32 if dtype == F32 else torch.int16))
+            close(dg, (D * h).sum(0), (D.abs() * e).sum(0) + c(rows) * (D * h).abs().sum(0))
+            close(db, D.sum(0), c(rows) * D.abs().sum(0))
