@@ -1,6 +1,6 @@
 // Products of linear layers on the 5th-generation tensor cores (tcgen05), bf16 operands that TMA can fetch.
 //
-// A persistent pair of CTAs (a cluster of two SMs) takes 256 x 256 tiles of C = A B^T, a single CTA 128 x BN tiles where there are few rows.  A warp fetches
+// A persistent pair of CTAs (a cluster of two SMs) takes 256 x 256 tiles of C = A B^T, a single CTA 128 x 64 tiles where there are few of those.  A warp fetches
 // 64-wide slices of its CTA's 128 rows of A and of its half of B into a ring (128-byte swizzle; an operand whose contraction runs across its
 // stored rows is fetched as it lies and read by the matrix unit in its other orientation, so nothing is ever transposed in memory).  One warp
 // of the pair issues the products (M = 256, N = BN, K = 16, four a slice), which read both CTAs' shared memory and leave 128 rows in each CTA's TMEM.
@@ -40,7 +40,7 @@ constexpr int kMaxStages = 8;
 template <int CG, int BN>
 struct Geo {
     static constexpr int A = kBM * 128, ROWS_B = BN / CG, B = ROWS_B * 128, STAGE = A + B;
-    static constexpr int STAGES = STAGE == 49152 ? 4 : (STAGE == 32768 ? 6 : 8);
+    static constexpr int STAGES = CG == 2 ? 6 : 8;
     static constexpr int TMEM = 2 * BN;
     static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + kEpilogue * kStageFloats * sizeof(float);
 };
@@ -453,7 +453,7 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec, int clust
     const bool runs = p.runs && p.k > (int64_t)kTcRun * kSlice;
     if (runs) teams = (int)std::min<int64_t>(teams, p.run_floats / (CG * kBM * BN));       // a team has the memory of one tile
     if (teams < 1) return AA_ERR_CUDA;
-    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, BN == 256 ? 0.4 : 0.2, cluster);
+    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, CG == 2 ? 0.4 : 0.2, cluster);
     if (runs) plan.run = kTcRun;
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     void* args[] = {&map_a, &map_b, &p, &plan, &vec};
@@ -492,12 +492,10 @@ bool product_tc_fits(const ProductParams& p) {
 aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p) {
     const auto quad = [](const MatArg& a) { return !a.data || ((uintptr_t)a.data % 8 == 0 && a.stride % 4 == 0); };
     const bool vec = quad(p.out) && quad(p.pre) && quad(p.residual);
-    // the widest tile moves the fewest bytes a product (256 x 256, 128 x 128 and 128 x 64: 8,192^3 721, 1,027 and 1,772 us, 4,096 x 1,024 -> 1,024 15, 17 and 25 us);
-    // narrower ones where it would leave more than half of the SMs idle (500 x 512 -> 2,048: 12.9, 12.6 and 12.4 us)
-    const int64_t mt = (p.m + kBM - 1) / kBM, sms = c->sm_count;
-    const auto tiles = [&](int bn) { return mt * ((p.n + bn - 1) / bn); };
-    if (2 * tiles(256) >= sms || (p.parts && p.k >= 16 * kSlice && tiles(256) * (p.k / (8 * kSlice)) >= sms)) return launch_majors<2, 256>(c, p, vec);
-    if (tiles(128) >= sms) return launch_majors<1, 128>(c, p, vec);
+    // the widest tile moves the fewest bytes a product (256 x 256 by pairs and 128 x 64: 8,192^3 721 and 1,772 us, 4,096 x 1,024 -> 1,024 15 and 25 us); narrow
+    // ones where it would leave more than half of the SMs idle (500 x 512 -> 2,048: 12.9 and 12.4 us)
+    const int64_t tiles = (p.m + kBM - 1) / kBM * ((p.n + 255) / 256), sms = c->sm_count;
+    if (2 * tiles >= sms || (p.parts && p.k >= 16 * kSlice && tiles * (p.k / (8 * kSlice)) >= sms)) return launch_majors<2, 256>(c, p, vec);
     return launch_majors<1, 64>(c, p, vec);
 }
 
