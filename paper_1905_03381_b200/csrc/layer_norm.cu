@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_
     using U = Shifted<T, E, TH>;
     constexpr int BYTES = SHIFT ? U::BYTES : S::BYTES;
     __shared__ __align__(8) float buf[2][TH / 32 * 2 * R];
-    extern __shared__ __align__(16) char ring[];     // [steps][R][x, dout, residual if there is one]; at the end the column sums
+    extern __shared__ __align__(16) char ring[];     // [steps, 1 or 2][R][x, dout, residual if there is one]; at the end the column sums
     grid_dependency_wait();
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
@@ -307,9 +307,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_
     for (int a = 0; a < steps; ++a) fetch(a * R * jump, a);
     int slot = 0;
     for (int64_t r = 0; lead + r < live; r += R * jump) {
-        if (steps >= 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
-        else if (steps == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-        else if (steps == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (steps == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
         if (SHIFT) __syncwarp();
         Raw<T, V, E> res[R];
