@@ -50,10 +50,17 @@ struct LinearScratch {
     size_t g, x, w, parts, runs, total;      // bytes
     bool copies;
 };
-// The parts of a cut tile are 256 KB in fp32 on each pair of SMs; three rounds of them (58 MB) leave little to balance.
-constexpr size_t kProductParts = 3ull * 74 * 256 * 256 * sizeof(float);
-// One tile a pair of SMs.
-constexpr size_t kProductRuns = 74ull * 256 * 256 * sizeof(float);
+// The parts of a cut tile are 256 KB in fp32 on each of a B200's 74 pairs of SMs; three rounds of them (58 MB) leave little to balance.  Runs: one tile a pair.
+constexpr int64_t kProductParts = 3ll * 74 * 256 * 256, kProductRuns = 74ll * 256 * 256;         // floats
+// What a product [m x n] over k can use of them, whatever its tiles are (256 x 256 at most, 64 columns at least): up to 16 parts of a tile and of its rows' sums (make_plan), of
+// four slices or more; runs where they are several.
+int64_t part_floats(int64_t m, int64_t n, int64_t k) {
+    const int64_t splits = std::min<int64_t>(16, (k + 63) / 64 / 4), tm = (m + 255) / 256, tn = (n + 255) / 256;
+    return splits < 2 ? 0 : std::min(kProductParts, std::min(tm * tn, kProductParts) * splits * (256 * 256 + 256 * 4));
+}
+int64_t run_floats(int64_t m, int64_t n, int64_t k) {
+    return k <= (int64_t)kTcRun * 64 ? 0 : std::min(kProductRuns, std::min((m + 255) / 256 * ((n + 255) / 256), kProductRuns) * 256 * 256);
+}
 int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
 LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
@@ -65,9 +72,8 @@ LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     if (act != AA_ACT_NONE || (s.copies && (wide || cols % 8 || !by_tma(x) || !by_tma(w)))) s.g = up((size_t)rows * (size_t)padded(cols) * each);
     if (s.copies && (wide || !by_tma(x))) s.x = up((size_t)rows * (size_t)padded(inner) * each);
     if (s.copies && (wide || !by_tma(w))) s.w = up((size_t)cols * (size_t)padded(inner) * each);
-    const size_t sums = up((size_t)kSlopeParts * (size_t)cols * sizeof(float));
-    s.parts = sums < kProductParts ? kProductParts : sums;
-    s.runs = !wide && std::max(rows, cols) > (int64_t)kTcRun * 64 ? kProductRuns : 0;
+    s.parts = up(std::max({kSlopeParts * cols, part_floats(rows, inner, cols), part_floats(cols, inner, rows)}) * sizeof(float));
+    if (!wide) s.runs = up(std::max(run_floats(rows, inner, cols), run_floats(cols, inner, rows)) * sizeof(float));
     s.total = s.g + s.x + s.w + s.parts + s.runs;
     return s;
 }

@@ -450,10 +450,16 @@ aa_status launch_tc(aa_ctx_impl* c, const ProductParams& in, bool vec, int clust
     const void* kernel = (const void*)product_tc_kernel<CG, BN, AA, BA, SUMS, JOIN>;
     if (allow_smem(c, kernel, G::SMEM) != AA_OK) return AA_ERR_CUDA;
     int teams = CG == 1 ? c->sm_count : resident_clusters(c, kernel, kThreads, G::SMEM, CG);
-    const bool runs = p.runs && p.k > (int64_t)kTcRun * kSlice;
-    if (runs) teams = (int)std::min<int64_t>(teams, p.run_floats / (CG * kBM * BN));       // a team has the memory of one tile
     if (teams < 1) return AA_ERR_CUDA;
-    Plan plan = make_plan(p, tiles, (int)nt, teams, (int64_t)CG * kBM * BN, CG * kBM, CG == 2 ? 0.4 : 0.2, cluster);
+    const auto plan_for = [&](int n) { return make_plan(p, tiles, (int)nt, n, (int64_t)CG * kBM * BN, CG * kBM, CG == 2 ? 0.4 : 0.2, cluster); };
+    Plan plan = plan_for(teams);
+    const bool runs = p.runs && p.k > (int64_t)kTcRun * kSlice;
+    // whole tile i < teams is team i's first, and a team has the memory of one tile
+    const int64_t places = p.run_floats / (CG * kBM * BN);
+    if (runs && std::min(plan.whole, teams) > places) {
+        if (places < 1) return AA_ERR_WORKSPACE;
+        plan = plan_for(teams = (int)places);
+    }
     if (runs) plan.run = kTcRun;
     const int64_t tail = tiles - plan.whole, units = plan.whole + tail * plan.splits;
     void* args[] = {&map_a, &map_b, &p, &plan, &vec};
