@@ -263,7 +263,7 @@ aa_status aa_layer_norm(aa_ctx* ctx, const aa_rows* x, const float* gamma, const
 aa_status aa_layer_norm_grad_scratch_bytes(const aa_rows* x, size_t* bytes) {
     if (!bytes || check_rows(x) != AA_OK) return AA_ERR_INVALID_ARG;
     if (x->cols > kMaxWidth) return AA_ERR_UNSUPPORTED;
-    const size_t stats = x->cols > kNormInRegisters ? ((size_t)x->rows * sizeof(float2) + 255) / 256 * 256 : 0;
+    const size_t stats = x->cols > kNormInRegisters ? ((size_t)x->rows * sizeof(NormStats) + 255) / 256 * 256 : 0;
     *bytes = stats + norm_scratch_floats(x->rows, x->cols) * sizeof(float);
     return AA_OK;
 }
@@ -301,8 +301,8 @@ aa_status aa_layer_norm_grad(aa_ctx* ctx, const aa_rows* x, const float* gamma, 
     p.gamma = gamma;
     p.eps = eps;
     p.ctl = c->ctl;
-    const size_t stats = n > kNormInRegisters ? ((size_t)x->rows * sizeof(float2) + 255) / 256 * 256 : 0;
-    p.stats = static_cast<float2*>(scratch);
+    const size_t stats = n > kNormInRegisters ? ((size_t)x->rows * sizeof(NormStats) + 255) / 256 * 256 : 0;
+    p.stats = static_cast<NormStats*>(scratch);
     if (dgamma || dbeta) p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + stats);
     return launch_layer_norm(c, p, x->dtype, true, dgamma, dbeta);
 }

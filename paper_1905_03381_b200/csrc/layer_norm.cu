@@ -6,8 +6,10 @@
 // Bound by memory where rows are short or fp32 (25,000 x 512 fp32: forward 18.8 us, 5.4 TB/s, backward 29 us, 5.3 TB/s; bf16 with residual 23 us, 4.5 TB/s), by
 // instructions and the latency of sums where an SM's warps share a row (3,001 x 4,099 fp32 backward: 39 us with both launches, the floor is 22).
 // 2 values a column pass forward, 3 or 4 backward.  A row stays in the registers of a group of threads (8 or 16 columns each) between its sums and its
-// result, so that memory is touched once; mean and variance are two rounds over registers, so that nothing cancels.  Backward the rounds carry
-// (sum x, sum g) and (sum c^2, sum g c): mean(g h) = r mean(g c), and no statistics are kept from the forward pass (two floats a row would save one round of
+// result, so that memory is touched once; mean and variance are two rounds over registers, so that nothing cancels.  A mean of fp32 numbers is off by a few parts in
+// 2^24, which is much where it is large against their spread (a constant row of 1,000.1 would get h = 0.02 with eps = 1e-5).  So the second round adds up c too:
+// with d = mean(c), c - d are the distances from the mean and mean(c^2) - d^2 is the variance.  bf16 numbers of one size add up exactly (8 bits, 8,192 columns).
+// Backward the rounds carry (sum x, sum g) and (sum c^2, sum g c, sum c): mean(g h) = r mean(g (c - d)), and no statistics are kept from the forward pass (two floats a row would save one round of
 // shuffles and no memory).  A group walks over rows of its own and adds up dout h and dout of its columns; the sums of a CTA's groups are joined in
 // shared memory, those of the CTAs by a second kernel, both in a fixed order.
 // Rows too long for registers are swept three times, and their columns are summed by a kernel of their own.
@@ -60,7 +62,7 @@ __device__ __forceinline__ float2 group_sum(float2 s, float2* buf) {
 // The same for K values.
 template <int G, int K>
 __device__ __forceinline__ void group_sums(float (&s)[K], float* buf) {
-    static_assert(K == 2 || K == 4, "");
+    static_assert(K == 2 || K == 4 || K == 8, "");
     if constexpr (K == 2 && G > 32) {        // the shorter chain of steps
         const float2 t = group_sum<G>(make_float2(s[0], s[1]), reinterpret_cast<float2*>(buf));
         s[0] = t.x;
@@ -69,17 +71,16 @@ __device__ __forceinline__ void group_sums(float (&s)[K], float* buf) {
     }
     const int lane = threadIdx.x & 31;
     // a warp halves the number of values a lane has with the first steps: value q ends up in the lanes with q = lane % K
-    float t;
-    if constexpr (K == 4) {
-        const bool up = lane & 2;
-        const float a = up ? s[2] : s[0], b = up ? s[3] : s[1];
-        const float c = __shfl_xor_sync(0xFFFFFFFFu, up ? s[0] : s[2], 2), d = __shfl_xor_sync(0xFFFFFFFFu, up ? s[1] : s[3], 2);
-        const bool odd = lane & 1;
-        t = (odd ? b + d : a + c) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a + c : b + d, 1);
-    } else {
-        const bool odd = lane & 1;
-        t = (odd ? s[1] : s[0]) + __shfl_xor_sync(0xFFFFFFFFu, odd ? s[0] : s[1], 1);
+    float w[K];
+#pragma unroll
+    for (int q = 0; q < K; ++q) w[q] = s[q];
+#pragma unroll
+    for (int o = K / 2; o > 0; o /= 2) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int q = 0; q < o; ++q) w[q] = (up ? w[q + o] : w[q]) + __shfl_xor_sync(0xFFFFFFFFu, up ? w[q] : w[q + o], o);
     }
+    float t = w[0];
 #pragma unroll
     for (int o = K; o < (G < 32 ? G : 32); o *= 2) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
     if constexpr (G > 32) {
@@ -127,6 +128,7 @@ struct Raw {
 template <typename T, int V, int E, int G>
 __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_kernel(NormParams p) {
     constexpr int TH = kThreadsOf<G>, N = E / V;
+    constexpr bool FINE = sizeof(T) == 4;    // the mean is corrected
     __shared__ float2 buf[2][32];
     grid_dependency_wait();
     grid_dependency_release();
@@ -160,21 +162,23 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_kerne
         if (r0 + jump < live) fetch(r0 + jump);
 #pragma unroll
         for (int j = 0; j < E; ++j) s.x += v[j];
-        const float mean = __fdiv_rn(group_sum<G>(s, buf[0]).x, (float)cols);     // exact for constant rows
+        const float mean = __fdiv_rn(group_sum<G>(s, buf[0]).x, (float)cols);
         s = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int j = 0; j < E; ++j) {
             v[j] = first + j / V * step < cols ? v[j] - mean : 0.0f;
             s.x = fmaf(v[j], v[j], s.x);
+            if (FINE) s.y += v[j];
         }
-        const float r = rsqrtf(group_sum<G>(s, buf[1]).x * inv + p.eps);
+        s = group_sum<G>(s, buf[1]);
+        const float d = FINE ? s.y * inv : 0.0f, r = rsqrtf((FINE ? fmaxf(fmaf(-d, s.y, s.x), 0.0f) : s.x) * inv + p.eps);
         T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = first + i * step;
             if (c >= cols || row >= live) continue;
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[i * V + e] = fmaf(v[i * V + e] * r, gm[i * V + e], bt[i * V + e]);
+            for (int e = 0; e < V; ++e) v[i * V + e] = fmaf((FINE ? v[i * V + e] - d : v[i * V + e]) * r, gm[i * V + e], bt[i * V + e]);
             store_elems<T, V>(out + c, v + i * V);
         }
     }
@@ -251,12 +255,13 @@ struct Shifted {
 template <typename T, int V, int E, int G, int R>
 __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_kernel(NormParams p, int steps) {
     constexpr int TH = kThreadsOf<G>, N = E / V;
-    constexpr bool SHIFT = V == 1;
+    constexpr bool SHIFT = V == 1, FINE = sizeof(T) == 4;
+    constexpr int K = FINE ? 4 : 2;          // sums of a row's second round
     static_assert(R == 1 || G >= 32, "a group's second row is skipped by whole warps");
     using S = Slot<T, V, E, TH>;
     using U = Shifted<T, E, TH>;
     constexpr int BYTES = SHIFT ? U::BYTES : S::BYTES;
-    __shared__ __align__(8) float buf[2][TH / 32 * 2 * R];
+    __shared__ __align__(8) float buf[2][TH / 32 * K * R];
     extern __shared__ __align__(16) char ring[];     // [steps, 1 or 2][R][x, dout, residual if there is one]; at the end the column sums
     grid_dependency_wait();
     grid_dependency_release();
@@ -345,30 +350,32 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_
         fetch(r + steps * R * jump, slot);
         slot = slot + 1 == steps ? 0 : slot + 1;
         group_sums<G>(s, buf[0]);
-        float mg[R];
+        float mg[R], t[K * R] = {};          // t: sums of c^2, c g, c
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             const float mean = __fdiv_rn(s[2 * q], (float)cols);
             mg[q] = s[2 * q + 1] * inv;
-            s[2 * q] = s[2 * q + 1] = 0.0f;
             const auto second_sums = [&](auto all) {
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     v[q][j] = all.value || first + j / V * step < cols ? v[q][j] - mean : 0.0f;
-                    s[2 * q] = fmaf(v[q][j], v[q][j], s[2 * q]);
-                    s[2 * q + 1] = fmaf(v[q][j], u[q][j] * gm[j], s[2 * q + 1]);
+                    t[K * q] = fmaf(v[q][j], v[q][j], t[K * q]);
+                    t[K * q + 1] = fmaf(v[q][j], u[q][j] * gm[j], t[K * q + 1]);
+                    if (FINE) t[K * q + 2] += v[q][j];
                 }
             };
             if (full) second_sums(std::true_type{});
             else second_sums(std::false_type{});
         }
-        group_sums<G>(s, buf[1]);
+        group_sums<G>(t, buf[1]);
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             const int64_t row = mine + r + q * jump;
             const bool on = (G >= 32 && q == 0) || row < live;
             if (q > 0 && !on) continue;
-            const float rs = rsqrtf(s[2 * q] * inv + p.eps), k = s[2 * q + 1] * inv * rs;
+            const float sum_c = FINE ? t[K * q + K - 2] : 0.0f, d = sum_c * inv;
+            const float rs = rsqrtf((FINE ? fmaxf(fmaf(-d, sum_c, t[K * q]), 0.0f) : t[K * q]) * inv + p.eps);
+            const float k = (FINE ? fmaf(-mg[q], sum_c, t[K * q + 1]) : t[K * q + 1]) * inv * rs;
             T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
             const auto finish = [&](auto all) {
 #pragma unroll
@@ -379,7 +386,7 @@ __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         const int j = i * V + e;
-                        const float h = v[q][j] * rs, w = on ? u[q][j] : 0.0f;
+                        const float h = (FINE ? v[q][j] - d : v[q][j]) * rs, w = on ? u[q][j] : 0.0f;
                         dg[j] = fmaf(w, h, dg[j]);
                         db[j] += w;
                         const float z = rs * (fmaf(u[q][j], gm[j], -mg[q]) - h * k);
@@ -439,9 +446,8 @@ __device__ __forceinline__ void sweep(const T* row, int64_t cols, F f) {
     }
 }
 
-// Mean and 1 / sqrt(var + eps) of a row.
 template <typename T, int V>
-__device__ __forceinline__ float2 row_stats(const NormParams& p, const T* x, float2 (*buf)[32]) {
+__device__ __forceinline__ NormStats row_stats(const NormParams& p, const T* x, float2 (*buf)[32]) {
     float2 s = make_float2(0.0f, 0.0f);
     sweep<T, V>(x, p.cols, [&](int64_t, const float* v) {
 #pragma unroll
@@ -451,9 +457,14 @@ __device__ __forceinline__ float2 row_stats(const NormParams& p, const T* x, flo
     s = make_float2(0.0f, 0.0f);
     sweep<T, V>(x, p.cols, [&](int64_t, const float* v) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) s.x = fmaf(v[e] - mean, v[e] - mean, s.x);
+        for (int e = 0; e < V; ++e) {
+            s.x = fmaf(v[e] - mean, v[e] - mean, s.x);
+            s.y += v[e] - mean;
+        }
     });
-    return make_float2(mean, 1.0f / sqrtf(group_sum<kSweep>(s, buf[1]).x / (float)p.cols + p.eps));
+    s = group_sum<kSweep>(s, buf[1]);
+    const float d = s.y / (float)p.cols;
+    return NormStats{mean, d, 1.0f / sqrtf(fmaxf(fmaf(-d, s.y, s.x), 0.0f) / (float)p.cols + p.eps), 0.0f};
 }
 
 template <typename T, int V>
@@ -465,16 +476,16 @@ __global__ void __launch_bounds__(kSweep) norm_sweep_kernel(NormParams p) {
     for (int64_t row = blockIdx.x; row < live; row += gridDim.x) {
         const T* x = static_cast<const T*>(p.x.data) + row * p.x.stride;
         T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
-        const float2 st = row_stats<T, V>(p, x, buf);
+        const NormStats st = row_stats<T, V>(p, x, buf);
         sweep<T, V>(x, p.cols, [&](int64_t c, float* v) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = fmaf((v[e] - st.x) * st.y, p.gamma ? p.gamma[c + e] : 1.0f, p.beta ? p.beta[c + e] : 0.0f);
+            for (int e = 0; e < V; ++e) v[e] = fmaf(st.h(v[e]), p.gamma ? p.gamma[c + e] : 1.0f, p.beta ? p.beta[c + e] : 0.0f);
             store_elems<T, V>(out + c, v);
         });
     }
 }
 
-// Sums of dout h and dout over runs of rows, before the rows' own kernel may overwrite x or dout.  stats: mean and r of each row.
+// Sums of dout h and dout over runs of rows, before the rows' own kernel may overwrite x or dout.
 template <typename T, int V>
 __global__ void __launch_bounds__(128) norm_columns_kernel(NormParams p) {
     grid_dependency_wait();
@@ -486,13 +497,13 @@ __global__ void __launch_bounds__(128) norm_columns_kernel(NormParams p) {
     float a[V] = {}, b[V] = {};
 #pragma unroll 4
     for (int64_t row = r0; row < r1; ++row) {
-        const float2 st = p.stats[row];
+        const NormStats st = p.stats[row];
         float d[V], x[V];
         load_elems<T, V>(static_cast<const T*>(p.dout.data) + row * p.dout.stride + c, d);
         load_elems<T, V>(static_cast<const T*>(p.x.data) + row * p.x.stride + c, x);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            a[e] = fmaf(d[e], (x[e] - st.x) * st.y, a[e]);
+            a[e] = fmaf(d[e], st.h(x[e]), a[e]);
             b[e] += d[e];
         }
     }
@@ -511,7 +522,7 @@ __global__ void __launch_bounds__(kSweep) norm_stats_kernel(NormParams p) {
     grid_dependency_release();
     const int64_t live = live_rows(p.live, p.ctl, blockIdx.x == 0 && threadIdx.x == 0);
     for (int64_t row = blockIdx.x; row < live; row += gridDim.x) {
-        const float2 st = row_stats<T, V>(p, static_cast<const T*>(p.x.data) + row * p.x.stride, buf);
+        const NormStats st = row_stats<T, V>(p, static_cast<const T*>(p.x.data) + row * p.x.stride, buf);
         if (threadIdx.x == 0) p.stats[row] = st;
     }
 }
@@ -527,7 +538,7 @@ __global__ void __launch_bounds__(kSweep) norm_grad_sweep_kernel(NormParams p) {
         const T *x = static_cast<const T*>(p.x.data) + row * p.x.stride, *d = static_cast<const T*>(p.dout.data) + row * p.dout.stride;
         const T* res = p.residual.data ? static_cast<const T*>(p.residual.data) + row * p.residual.stride : nullptr;
         T* out = static_cast<T*>(const_cast<void*>(p.out.data)) + row * p.out.stride;
-        const float2 st = p.stats[row];
+        const NormStats st = p.stats[row];
         float2 s = make_float2(0.0f, 0.0f);
         sweep<T, V>(d, p.cols, [&](int64_t c, const float* u) {
             float v[V];
@@ -536,18 +547,18 @@ __global__ void __launch_bounds__(kSweep) norm_grad_sweep_kernel(NormParams p) {
             for (int e = 0; e < V; ++e) {
                 const float g = u[e] * (p.gamma ? p.gamma[c + e] : 1.0f);
                 s.x += g;
-                s.y = fmaf(g, v[e] - st.x, s.y);
+                s.y = fmaf(g, st.h(v[e]), s.y);
             }
         });
         s = group_sum<kSweep>(s, buf);
-        const float mg = s.x * inv, k = s.y * inv * st.y;
+        const float mg = s.x * inv, k = s.y * inv;
         sweep<T, V>(d, p.cols, [&](int64_t c, const float* u) {
             float v[V], y[V];
             load_elems<T, V>(x + c, v);
             if (res) load_elems<T, V>(res + c, y);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float z = st.y * (u[e] * (p.gamma ? p.gamma[c + e] : 1.0f) - mg - (v[e] - st.x) * st.y * k);
+                const float z = st.r * (u[e] * (p.gamma ? p.gamma[c + e] : 1.0f) - mg - st.h(v[e]) * k);
                 y[e] = res ? z + y[e] : z;
             }
             store_elems<T, V>(out + c, y);

@@ -9,6 +9,14 @@ constexpr int kNormParts = 592;              // CTAs that leave column sums, at 
 constexpr int kSweepParts = 64;
 constexpr int64_t kNormInRegisters = 8192;   // columns of the longest row that stays in registers
 
+// Of a row too long for registers: its mean (mean + d, more exactly) and 1 / sqrt(var + eps).
+struct alignas(16) NormStats {
+    float mean, d, r, unused;
+#ifdef __CUDACC__
+    __device__ __forceinline__ float h(float x) const { return (x - mean - d) * r; }
+#endif
+};
+
 struct NormParams {
     MatArg x, dout, residual, out;           // dout: gradients only; residual nullable
     int64_t cols;
@@ -17,7 +25,7 @@ struct NormParams {
     const float* beta;
     float eps;
     float* parts;                            // column sums, [parts][2][cols]; null: neither dgamma nor dbeta is wanted
-    float2* stats;                           // [rows] (rows longer than kNormInRegisters)
+    NormStats* stats;                          // [rows] (rows longer than kNormInRegisters)
     Control* ctl;
 };
 

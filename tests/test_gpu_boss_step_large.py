@@ -204,3 +204,48 @@ def test_norm_with_several_rows_a_group(aa, dtype, m, n, pad):
             assert torch.equal(dx[rows:].view(torch.int32 if dtype == F32 else torch.int16), behind.view(torch.int32 if dtype == F32 else torch.int16))
             close(dg, (D * h).sum(0), (D.abs() * e).sum(0) + c(rows) * (D * h).abs().sum(0))
             close(db, D.sum(0), c(rows) * D.abs().sum(0))
+
+
+def far_bars(x, h, r):
+    """What h may be off by where the mean is corrected: the first one is off by 2^-18 mean|x| (test_gpu_boss_step), its correction by 2^-18 of that; sums and quotients 2^-18."""
+    return r * 2.0**-36 * x.abs().mean(1, keepdim=True) + 2.0**-18 * h.abs() + 2.0**-22
+
+
+@pytest.mark.parametrize("n", [5, 100, 512, 515, 1024, 2047, 4096, 4099, 5000, 8191, 9000])
+@pytest.mark.parametrize("value,eps", [(0.1, 1e-10), (1000.1, 1e-5), (-333.3, 1e-6)])
+def test_norm_of_constant_fp32_rows(aa, n, value, eps):
+    """h is 0, whatever the rounding of a sum of n equal numbers."""
+    m = 7
+    x, d = torch.full((m, n), value, device=DEV), random((m, n), 2, F32)
+    beta = random((n,), 3, F32)
+    out, dx, dg, db = torch.empty_like(x), torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    aa.aa_layer_norm(x, out, beta=beta, eps=eps)
+    r, h = eps**-0.5, torch.zeros((m, n), dtype=torch.float64, device=DEV)
+    e = far_bars(x.double(), h, r)
+    close(out, beta.double().expand(m, n), e + 2.0**-24 * beta.double().abs())
+    aa.aa_layer_norm_grad(x, d, dx, aa.layer_norm_grad_scratch(x), eps=eps, dgamma=dg, dbeta=db)
+    g = d.double()
+    want = r * (g - g.mean(1, keepdim=True))
+    # the variance that is left is 2^-18 of the square of the first mean's error: (2^-18 x)^2 2^-18 / eps of r at most
+    close(dx, want, r * 2.0**-18 * (g.abs() + g.abs().mean(1, keepdim=True)) + want.abs() * (2.0**-18 * (2.0**-18 * value) ** 2 / eps + 2.0**-20) + r * 4.0 * e)
+    close(dg, torch.zeros(n, dtype=torch.float64, device=DEV), (g.abs() * e).sum(0))
+
+
+@pytest.mark.parametrize("m,n,pad", [(40, 64, 0), (40, 512, 0), (40, 515, 0), (700, 1024, 0), (701, 4096, 0), (701, 4099, 0), (30, 6000, 1), (12, 9000, 0)])
+def test_norm_of_fp32_rows_far_from_zero(aa, m, n, pad):
+    x, d = strided(m, n, 1, F32, pad), strided(m, n, 2, F32, pad)
+    x.add_(1.0e4)
+    gamma = 1.0 + random((n,), 4, F32, 0.3)
+    h, r, _ = norm_reference(x.double(), gamma, 1e-5)
+    e = far_bars(x.double(), h, r)
+    out = torch.empty_like(x)
+    aa.aa_layer_norm(x, out, gamma=gamma)
+    close(out, h * gamma.double(), gamma.double().abs() * e + 2.0**-22 * h.abs())
+    dx, dg = torch.empty_like(x), torch.empty(n, device=DEV)
+    aa.aa_layer_norm_grad(x, d, dx, aa.layer_norm_grad_scratch(x), gamma=gamma, dgamma=dg)
+    D = d.double()
+    g = D * gamma.double()
+    mg, mgh = g.abs().mean(1, keepdim=True), (g * h).abs().mean(1, keepdim=True)
+    want = r * (g - g.mean(1, keepdim=True) - h * (g * h).mean(1, keepdim=True))
+    close(dx, want, r * (2.0**-18 * (g.abs() + mg) + e * (mgh + mg) + h.abs() * ((g.abs() * e).mean(1, keepdim=True) + 2.0**-18 * mgh)) + 2.0**-17 * want.abs())
+    close(dg, (D * h).sum(0), (D.abs() * e).sum(0) + c(m) * (D * h).abs().sum(0))
