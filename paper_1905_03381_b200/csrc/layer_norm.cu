@@ -4,7 +4,7 @@
 //   g = dout gamma,   dx = r (g - mean(g) - h mean(g h)) + residual,   dgamma = sum_rows dout h,  dbeta = sum_rows dout
 //
 // Bound by memory where rows are short or fp32 (25,000 x 512 fp32: forward 18.8 us, 5.4 TB/s, backward 29 us, 5.3 TB/s; bf16 with residual 23 us, 4.5 TB/s), by
-// instructions and the latency of sums where an SM's warps share a row (3,001 x 4,099 fp32 backward: 39 us with both launches, the floor is 22).
+// instructions and the latency of sums where an SM's warps share a row (3,001 x 4,099 fp32 backward: 41 us with both launches, the floor is 22).
 // 2 values a column pass forward, 3 or 4 backward.  A row stays in the registers of a group of threads (8 or 16 columns each) between its sums and its
 // result, so that memory is touched once; mean and variance are two rounds over registers, so that nothing cancels.  A mean of fp32 numbers is off by a few parts in
 // 2^24, which is much where it is large against their spread (a constant row of 1,000.1 would get h = 0.02 with eps = 1e-5).  So the second round adds up c too:
@@ -249,8 +249,8 @@ struct Shifted {
     }
 };
 
-// R rows of a group are worked on at a time - two where all warps of an SM are one group and registers allow: barriers and the latency of sums come once for
-// both (3,001 x 4,099 fp32: 41.7 us one by one, 39.4 in twos; groups of 256 threads gain nothing).  `steps` times R rows are under way; a step's place is
+// R rows of a group are worked on at a time - two where all warps of an SM are one group and registers hold both (10 columns a thread; with 11 they spill): barriers and the
+// latency of sums come once for both (3,001 x 4,099 fp32: 43.3 us one by one, 40.9 in twos; 2,600 x 4,700 bf16 35.0 and 34.4; groups of 256 threads gain nothing).  `steps` times R rows are under way; a step's place is
 // filled again as soon as its numbers are in registers.
 template <typename T, int V, int E, int G, int R>
 __global__ void __launch_bounds__(kThreadsOf<G>, 512 / kThreadsOf<G>) norm_grad_kernel(NormParams p, int steps) {
@@ -593,7 +593,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const float* parts, int 
 
 template <typename T, int V, int E, int G>
 aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
-    constexpr int TH = kThreadsOf<G>, groups = TH / G, R = G >= 512 && E <= 9 ? 2 : 1;
+    constexpr int TH = kThreadsOf<G>, groups = TH / G, R = G >= 512 && E <= 10 ? 2 : 1;
     const void* kernel = grad ? (const void*)norm_grad_kernel<T, V, E, G, R> : (const void*)norm_kernel<T, V, E, G>;
     // two steps, one where two would hold more than 150 KB an SM: more are slower (25,000 x 512 fp32: 29.1 us with two, 29.9 with three, 32.1 with four, 33.3 with
     // one; 6,000 x 2,048 with residual, 98 KB a step: 38.8 with one, 42.6 with two)
@@ -613,6 +613,14 @@ aa_status launch_rows(aa_ctx_impl* c, NormParams p, bool grad, int* n_parts) {
     ++c->launches;
     *n_parts = ctas;
     return AA_OK;
+}
+
+// 512 threads with E columns each or, if the row has more, with the next multiple of V.
+template <typename T, int V, int E>
+aa_status launch_wide(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
+    if constexpr (E < 16)
+        if (p.cols > 512 * E) return launch_wide<T, V, E + V>(c, p, grad, n);
+    return launch_rows<T, V, E, 512>(c, p, grad, n);
 }
 
 // The smallest group whose threads have 16 columns of bf16 each, or 8 of fp32 (more where no group is that wide, 8 where rows go in twos).
@@ -640,11 +648,8 @@ aa_status launch_width(aa_ctx_impl* c, const NormParams& p, bool grad, int* n) {
         if (p.cols <= 2048) return launch_rows<T, V, 8, 256>(c, p, grad, n);
         if (p.cols <= 4096) return launch_rows<T, V, 8, 512>(c, p, grad, n);
     }
-    if constexpr (V == 1)
-        if (p.cols <= 4608) return launch_rows<T, V, 9, 512>(c, p, grad, n);
-    if constexpr (V != 8)
-        if (p.cols <= 6144) return launch_rows<T, V, 12, 512>(c, p, grad, n);
-    return launch_rows<T, V, 16, 512>(c, p, grad, n);
+    // all of a CTA's threads hold the row: as many columns each as it takes (1,900 x 6,501 fp32, backward: 37.8 us with 13, 41.6 with 16; 2,400 x 5,100 bf16 34 with 10, 36 with 12)
+    return launch_wide<T, V, (8 / V + 1) * V>(c, p, grad, n);
 }
 
 template <typename T, int V>

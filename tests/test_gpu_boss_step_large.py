@@ -171,7 +171,7 @@ def strided(m, n, seed, dtype, pad):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("m,n,pad", [(701, 4096, 0), (701, 4099, 0), (450, 5000, 0), (450, 5000, 3), (700, 8192, 0), (700, 8192, 1), (6001, 512, 0), (6001, 512, 5), (3001, 1024, 0), (2003, 2048, 0),
-                                     (20001, 64, 0), (20001, 100, 0), (1201, 3000, 1), (40, 8200, 0)])
+                                     (20001, 64, 0), (20001, 100, 0), (1201, 3000, 1), (40, 8200, 0), (300, 4609, 0), (300, 5203, 0), (300, 6101, 0), (300, 6145, 0), (300, 7001, 0), (300, 7603, 0), (300, 6144, 0), (300, 6148, 0)])
 def test_norm_with_several_rows_a_group(aa, dtype, m, n, pad):
     """More rows than the threads that are resident take at once; counts that leave an odd number of them to the last, with NaN behind; in place."""
     x, d, res = (strided(m, n, seed, dtype, pad) for seed in (1, 2, 3))
