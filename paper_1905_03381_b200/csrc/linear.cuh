@@ -89,55 +89,67 @@ __device__ __forceinline__ float rcp_approx(float x) {
     return y;
 }
 
-// Normal distribution at z and its density's exponential e = exp(-z^2 / 2), which the gradient needs too.  The tail is Hastings' rational approximation
-// (Abramowitz and Stegun, 7.1.26): erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), within 1.5e-7; it shares e.
+// Normal distribution at z and its density's exponential e = exp(-z^2 / 2), which the gradient needs too.  FINE (fp32 matrices): by the functions of the library, good to
+// a few parts in 2^24.  Otherwise (results that are rounded to bf16) the tail is Hastings' rational approximation (Abramowitz and Stegun, 7.1.26):
+// erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + 0.3275911 x), within 1.5e-7, a two-thousandth of what bf16 keeps; it shares e
+// (8,000 x 256 -> 2,048 fp32 with GELU takes 92 us by it, 111 by the functions).
+template <bool FINE>
 __device__ __forceinline__ float normal_cdf(float z, float& e) {
     const float x = fabsf(z) * 0.70710678118654752f;
-    const float t = rcp_approx(fmaf(0.3275911f, x, 1.0f));
-    e = ex2_approx(z * z * -0.72134752044448170f);
-    float q = fmaf(t, 1.061405429f, -1.453152027f);
-    q = fmaf(t, q, 1.421413741f);
-    q = fmaf(t, q, -0.284496736f);
-    q = fmaf(t, q, 0.254829592f);
-    q = 0.5f * t * q * e;
+    float q;
+    if (FINE) {
+        e = expf(-0.5f * z * z);
+        q = 0.5f * erfcf(x);
+    } else {
+        const float t = rcp_approx(fmaf(0.3275911f, x, 1.0f));
+        e = ex2_approx(z * z * -0.72134752044448170f);
+        q = fmaf(t, 1.061405429f, -1.453152027f);
+        q = fmaf(t, q, 1.421413741f);
+        q = fmaf(t, q, -0.284496736f);
+        q = fmaf(t, q, 0.254829592f);
+        q = 0.5f * t * q * e;
+    }
     return z > 0.0f ? 1.0f - q : q;
 }
-__device__ __forceinline__ float logistic(float z) { return rcp_approx(1.0f + ex2_approx(z * -1.4426950408889634f)); }
+template <bool FINE>
+__device__ __forceinline__ float logistic(float z) {
+    return rcp_approx(1.0f + (FINE ? expf(-z) : ex2_approx(z * -1.4426950408889634f)));
+}
 
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float activate(float z) {
     if (ACT == AA_ACT_RELU) return z < 0.0f ? 0.0f : z;
     float e;
-    if (ACT == AA_ACT_GELU) return z * normal_cdf(z, e);
-    if (ACT == AA_ACT_SILU) return z * logistic(z);
+    if (ACT == AA_ACT_GELU) return z * normal_cdf<FINE>(z, e);
+    if (ACT == AA_ACT_SILU) return z * logistic<FINE>(z);
     return z;
 }
 // The same where the activation is known at run time: one branch for N values.
-template <int N>
+template <bool FINE, int N>
 __device__ __forceinline__ void activate_all(float (&z)[N], int act) {
     if (act == AA_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_RELU>(z[i]);
+        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_RELU, FINE>(z[i]);
     } else if (act == AA_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_GELU>(z[i]);
+        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_GELU, FINE>(z[i]);
     } else if (act == AA_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_SILU>(z[i]);
+        for (int i = 0; i < N; ++i) z[i] = activate<AA_ACT_SILU, FINE>(z[i]);
     }
 }
 
 // act'(z); relu'(0) = 0.
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float activation_slope(float z) {
     if (ACT == AA_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if (ACT == AA_ACT_GELU) {
         float e;
-        const float cdf = normal_cdf(z, e);
+        const float cdf = normal_cdf<FINE>(z, e);
         return fmaf(z * 0.39894228040143268f, e, cdf);
     }
     if (ACT == AA_ACT_SILU) {
-        const float s = logistic(z);
+        const float s = logistic<FINE>(z);
         return s * fmaf(z, 1.0f - s, 1.0f);
     }
     return 1.0f;

@@ -132,7 +132,7 @@ __device__ __forceinline__ void finish_quads(const ProductParams& p, float (&z)[
         }
     };
     if (pre) put(pre, p.pre.stride);
-    activate_all(z, p.act);
+    activate_all<sizeof(T) == 4>(z, p.act);
 #pragma unroll
     for (int i = 0; i < N * 4; ++i) z[i] += y[i];
     put(out, p.out.stride);

@@ -91,7 +91,7 @@ __device__ __forceinline__ void slope(const SlopeParams& p, float (*sums)[32 * (
                     float y[V];
                     values(zw[i], y);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) x[e] *= activation_slope<ACT>(y[e]);
+                    for (int e = 0; e < V; ++e) x[e] *= activation_slope<ACT, sizeof(T) == 4>(y[e]);
                 }
                 put(r + 8 * i, x);
 #pragma unroll

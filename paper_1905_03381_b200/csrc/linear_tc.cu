@@ -68,7 +68,7 @@ __device__ __forceinline__ void put_chunk(uint32_t stage, int sub, int r8, int r
             for (int e = 0; e < 4; ++e) z[e] += bias[e];
             if (raw) *reinterpret_cast<uint2*>(raw) = make_uint2(pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = activate<ACT>(z[e]);
+            for (int e = 0; e < 4; ++e) z[e] = activate<ACT, false>(z[e]);
             if (some) {
                 z[0] += bf16_lo(add[q].x);
                 z[1] += bf16_hi(add[q].x);

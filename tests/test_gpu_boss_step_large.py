@@ -249,3 +249,31 @@ def test_norm_of_fp32_rows_far_from_zero(aa, m, n, pad):
     want = r * (g - g.mean(1, keepdim=True) - h * (g * h).mean(1, keepdim=True))
     close(dx, want, r * (2.0**-18 * (g.abs() + mg) + e * (mgh + mg) + h.abs() * ((g.abs() * e).mean(1, keepdim=True) + 2.0**-18 * mgh)) + 2.0**-17 * want.abs())
     close(dg, (D * h).sum(0), (D.abs() * e).sum(0) + c(m) * (D * h).abs().sum(0))
+
+
+# --------------------------------------------------------------------------------------------------------------- activations
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_fp32_activations_and_slopes_number_by_number(aa, act):
+    """One weight of 1 and one term a sum, so that the call gives act(z) itself, and dbias of one row act'(z).  erfc and exp are good to 2^-21; their arguments, rounded twice, move
+    them by z^2 2^-23 of themselves."""
+    z = torch.cat([torch.linspace(-12.0, 12.0, 100_001, device=DEV), torch.linspace(-2.0, 2.0, 50_000, device=DEV)])
+    one, n = torch.ones((1, 1), device=DEV), z.numel()
+    Z = z.double()
+    e = 2.0**-21 + Z * Z * 2.0**-23
+    if act == "gelu":
+        q, phi = 0.5 * torch.special.erfc(Z.abs() * 0.5**0.5), torch.exp(-0.5 * Z * Z) * (0.5 / torch.pi) ** 0.5
+        cdf = torch.where(Z > 0, 1.0 - q, q)
+        want, slope = Z * cdf, cdf + Z * phi
+        bar, slope_bar = Z.abs() * (q * e + 2.0**-24 * (Z > 0)) + 2.0**-23 * want.abs(), q * e + Z.abs() * phi * e + 2.0**-23 * cdf
+    else:
+        s = torch.sigmoid(Z)
+        want, slope = Z * s, s * (1.0 + Z * (1.0 - s))
+        bar, slope_bar = want.abs() * 2.0**-20, s * (1.0 + Z.abs()) * 2.0**-22
+    for rows in (n, 12):                                          # tiles, and few rows
+        x, out = z[:rows, None].contiguous(), torch.empty((rows, 1), device=DEV)
+        aa.aa_linear(x, one, out, activation=act)
+        close(out[:, 0], want[:rows], bar[:rows])
+    w, pre, dout, db = torch.ones((n, 1), device=DEV), z[None, :].contiguous(), torch.ones((1, n), device=DEV), torch.empty(n, device=DEV)
+    aa.aa_linear_grad(one, w, dout, aa.linear_grad_scratch(one, w, act), dbias=db, activation=act, pre=pre)
+    close(db, slope, slope_bar)
