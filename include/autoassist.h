@@ -531,8 +531,8 @@ aa_status aa_linear(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, const float
  * Gradients of aa_linear from dout, the gradient of its output:  G = dout * act'(pre) (AA_ACT_NONE: G = dout, pre is NULL),
  *   dx = G w + residual,   dw = G^T x,   dbias = column sums of G.
  * dx, dw, dbias are nullable (not computed), written and not added to; residual (nullable, needs dx) is a gradient that reaches x past the layer, dx may
- * be residual itself.  dx and dw have the dtype of x and w, dbias is fp32.  With an activation and bf16 operands G is rounded to bf16 before the
- * two products (dbias sums it unrounded).  Sums run in an order that depends on the sizes alone, so equal calls give equal bits.
+ * be residual itself.  dx and dw have the dtype of x and w, dbias is fp32.  With an activation and bf16 operands G is rounded to bf16, as a gradient between two layers would be, before
+ * the two products (dbias sums it unrounded); fp32 operands keep all of it.  Sums run in an order that depends on the sizes alone, so equal calls give equal bits.
  * scratch: DEVICE memory of at least aa_linear_grad_scratch_bytes(...) bytes for these operands (strides and alignment count, too), 256-byte aligned; it holds nothing
  * between calls, and calls that may run at the same time need one each.
  */
@@ -561,7 +561,8 @@ aa_status aa_layer_norm_grad(aa_ctx* ctx, const aa_rows* x, const float* gamma, 
  *   g = grad_scale * grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   param = (1 - lr weight_decay) param - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps);   copy = param rounded to bf16.
  * grad_scale: nullable DEVICE scalar (for instance the factor of a clipped gradient norm).  If it is not finite the step writes nothing.
- * The call advances rule->t; the rule's values are read when the call is made, so that a captured graph replays one t.
+ * The call advances rule->t; the rule's values are read when the call is made, so that a captured graph replays one t: one lr, one bias correction and (8 bits) one set of
+ * draws, whose rounding is without bias over the elements then, but not over the steps.  A graph of a training step leaves this call outside, or is captured again.
  *
  * state_bits 32: m and v are fp32 [n].
  * state_bits 8:  m and root = sqrt(v) are e4m3 [n] in units of a power of two per block of 256 consecutive elements, m_scale and v_scale

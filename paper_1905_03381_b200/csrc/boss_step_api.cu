@@ -174,7 +174,8 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
     grad_x.part_floats = grad_w.part_floats = (int64_t)(need.parts / sizeof(float));
     grad_x.runs = grad_w.runs = need.runs ? parts + need.parts / sizeof(float) : nullptr;
     grad_x.run_floats = grad_w.run_floats = (int64_t)(need.runs / sizeof(float));
-    // G is a matrix of its own where there is an activation, or where dout is copied
+    // G is a matrix of its own where there is an activation, or where dout is copied.  In bf16 it is rounded: 25,000 x 512 -> 2,048 with GELU is off by 2.3e-3 of its results then, by
+    // 1.7e-3 if G kept 32 bits (the results' own rounding), for which both products, 97 of the call's 172 us, would be done twice.
     const bool copy_g = need.g > 0 && (act || planes || !by_tma(dout));
     const MatArg g = copy_g ? MatArg{at, padded(w->rows)} : mat(dout);
     const MatArg xs = need.x ? MatArg{at + need.g, padded(x->cols)} : mat(x), ws = need.w ? MatArg{at + need.g + need.x, padded(x->cols)} : mat(w);
