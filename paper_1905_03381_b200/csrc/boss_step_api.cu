@@ -45,21 +45,18 @@ constexpr int64_t kFewRowsOfCopies = 512, kWeightsOfCopies = 1 << 21;
 
 bool by_tma(const aa_rows* m) { return (uintptr_t)m->data % 16 == 0 && m->row_stride % 8 == 0; }
 
-// G, x and w as far as they are copied, then the column sums' parts or (later in the call) the products' parts, and the runs of long bf16 products.
+// G, x and w as far as they are copied, then the column sums' parts or (later in the call) the products' parts.
 struct LinearScratch {
-    size_t g, x, w, parts, runs, total;      // bytes
+    size_t g, x, w, parts, total;      // bytes
     bool copies;
 };
-// The parts of a cut tile are 256 KB in fp32 on each of a B200's 74 pairs of SMs; three rounds of them (58 MB) leave little to balance.  Runs: one tile a pair.
-constexpr int64_t kProductParts = 3ll * 74 * 256 * 256, kProductRuns = 74ll * 256 * 256;         // floats
+// The parts of a cut tile are 256 KB in fp32 on each of a B200's 74 pairs of SMs; three rounds of them (58 MB) leave little to balance.
+constexpr int64_t kProductParts = 3ll * 74 * 256 * 256;         // floats
 // What a product [m x n] over k can use of them, whatever its tiles are (256 x 256 at most, 64 columns at least): up to 16 parts of a tile and of its rows' sums (make_plan), of
-// four slices or more; runs where they are several.
+// four slices or more.
 int64_t part_floats(int64_t m, int64_t n, int64_t k) {
     const int64_t splits = std::min<int64_t>(16, (k + 63) / 64 / 4), tm = (m + 255) / 256, tn = (n + 255) / 256;
     return splits < 2 ? 0 : std::min(kProductParts, std::min(tm * tn, kProductParts) * splits * (256 * 256 + 256 * 4));
-}
-int64_t run_floats(int64_t m, int64_t n, int64_t k) {
-    return k <= (int64_t)kTcRun * 64 ? 0 : std::min(kProductRuns, std::min((m + 255) / 256 * ((n + 255) / 256), kProductRuns) * 256 * 256);
 }
 int64_t padded(int64_t cols) { return (cols + 7) / 8 * 8; }
 LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
@@ -73,8 +70,7 @@ LinearScratch linear_scratch(const aa_rows* x, const aa_rows* w, int act) {
     if (s.copies && (wide || !by_tma(x))) s.x = up((size_t)rows * (size_t)padded(inner) * each);
     if (s.copies && (wide || !by_tma(w))) s.w = up((size_t)cols * (size_t)padded(inner) * each);
     s.parts = up(std::max({kSlopeParts * cols, part_floats(rows, inner, cols), part_floats(cols, inner, rows)}) * sizeof(float));
-    if (!wide) s.runs = up(std::max(run_floats(rows, inner, cols), run_floats(cols, inner, rows)) * sizeof(float));
-    s.total = s.g + s.x + s.w + s.parts + s.runs;
+    s.total = s.g + s.x + s.w + s.parts;
     return s;
 }
 
@@ -172,8 +168,6 @@ aa_status aa_linear_grad(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, int32_
     grad_x.live = grad_w.live = live;
     grad_x.parts = grad_w.parts = parts;
     grad_x.part_floats = grad_w.part_floats = (int64_t)(need.parts / sizeof(float));
-    grad_x.runs = grad_w.runs = need.runs ? parts + need.parts / sizeof(float) : nullptr;
-    grad_x.run_floats = grad_w.run_floats = (int64_t)(need.runs / sizeof(float));
     // G is a matrix of its own where there is an activation, or where dout is copied.  In bf16 it is rounded: 25,000 x 512 -> 2,048 with GELU is off by 2.3e-3 of its results then, by
     // 1.7e-3 if G kept 32 bits (the results' own rounding), for which both products, 97 of the call's 172 us, would be done twice.
     const bool copy_g = need.g > 0 && (act || planes || !by_tma(dout));

@@ -34,18 +34,13 @@ struct ProductParams {
     MatArg residual, pre, out;   // nullable but out
     float* parts;            // scratch for tiles cut along the contraction, nullable (then bias, act and pre are empty)
     int64_t part_floats;
-    float* runs;             // scratch for the sums of the runs before of the tiles under way, nullable (linear_tc.cu)
-    int64_t run_floats;
     int64_t plane_a, plane_b;    // above 0: A and B are three planes of bf16 terms of fp32 numbers, so many elements apart
     float* a_sums;           // [m] sums of A over the contraction, nullable (a_across)
     Control* ctl;
 };
 
 aa_status launch_product(aa_ctx_impl* c, const ProductParams& p, int dtype);
-// What linear_tc.cu sums in TMEM: runs of so many slices of 64 terms, or contractions up to so many terms where there is no memory to add runs up in.
-constexpr int kTcRun = 256;
-constexpr int64_t kTcTerms = 1 << 15;
-// bf16 operands that TMA can fetch (16-byte aligned bases and rows), and runs where the contraction is long.
+// bf16 operands that TMA can fetch (16-byte aligned bases and rows).
 bool product_tc_fits(const ProductParams& p);
 aa_status launch_product_tc(aa_ctx_impl* c, const ProductParams& p);
 // At most 16 rows, forward.

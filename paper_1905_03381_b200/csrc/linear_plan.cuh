@@ -14,7 +14,6 @@ struct Plan {
     float* parts;                        // [part][rows of a tile][columns of a tile]
     float* sum_parts;                    // [part][rows of a tile]
     int cluster;                         // above 1: the parts of a tile are the CTAs of a cluster, which join them themselves (no scratch memory)
-    int run;                             // slices summed in TMEM (linear_tc.cu)
 };
 
 // CTAs that share a tile as a cluster, where there are few tiles and no scratch memory: as many as run at once, up to eight, with a
@@ -29,7 +28,7 @@ inline int tile_cluster(aa_ctx_impl* c, const void* kernel, int threads, size_t 
 // Splits of the tiles that do not fill a round of `teams`: the fewest slices one after the other, counting the parts' way through memory.
 // slice_us: what a slice of a tile takes.
 inline Plan make_plan(const ProductParams& p, int64_t tiles, int nt, int teams, int64_t tile_floats, int tile_rows, double slice_us, int cluster) {
-    Plan plan{nt, (int)tiles, 1, p.parts, nullptr, cluster, 0x7FFFFFFF};
+    Plan plan{nt, (int)tiles, 1, p.parts, nullptr, cluster};
     const int64_t slices = (p.k + kSlice - 1) / kSlice, whole = tiles / teams * teams, tail = tiles - whole;
     if (cluster > 1) plan.whole = 0, plan.splits = cluster;
     if (!p.parts) return plan;

@@ -1,7 +1,7 @@
 """Linear layers and layer normalisation at sizes that fill the GPU - tiles of pairs of CTAs, several of them one after the other, contractions cut or summed in runs,
 several rows a group of threads - against fp64 on the GPU.  Bars as in test_gpu_boss_step, and for the longest sums:
   bf16 sums: the matrix units round towards zero once in 16 terms, by half a step on average (2^-24 of the sum so far, which is half of the run's on average); runs of
-             16,384 terms are added up in fp32.  So 1,024 2^-24 / 2 = 2^-15 of the sum of absolute terms, and 2^-24 of it for each run.
+             2,048 terms are added up in fp32.  So 128 2^-24 / 2 = 2^-18 of the sum of absolute terms, and 2^-24 of it for each run.
 """
 import pytest
 import torch
@@ -56,7 +56,7 @@ def test_weights_gradients_of_many_tokens_keep_their_sums(aa):
     aa.aa_linear_grad(x, w, dout, aa.linear_grad_scratch(x, w), dw=dw, dbias=db)
     half = tokens // 2
     size = 2.0 * (x[:half].float().t() @ dout[:half].float()).t().double()
-    below(dw, (2.0**-15 + tokens / 16384 * 2.0**-24) * size)
+    below(dw, (2.0**-18 + tokens / 2048 * 2.0**-24) * size)
     # dbias: eight tokens at a time in fp32, rounded to nearest, of which a thread has every 32nd token
     below(db, tokens / 8 * 2.0**-24 * 2.0 * dout[:half].double().sum(0))
 
@@ -69,13 +69,13 @@ def test_long_contractions_keep_their_sums(aa):
     out = torch.empty((2048, 1100), dtype=BF16, device=DEV)
     aa.aa_linear(x, w, out)
     size = 2.0 * (x[:, :k // 2].float() @ w[:, :k // 2].float().t()).double()
-    below(out, (2.0**-15 + 2.0**-19) * size)                      # runs of 256 terms
+    below(out, (2.0**-18 + k / 2048 * 2.0**-24) * size)
     dout, w = cancelling(k, 1100, 5, True).t().contiguous(), cancelling(k, 2048, 6, False)
     x = torch.zeros((1100, 2048), dtype=BF16, device=DEV)
     dx = torch.empty_like(x)
     aa.aa_linear_grad(x, w, dout, aa.linear_grad_scratch(x, w), dx=dx)
     size = 2.0 * (dout[:, :k // 2].float() @ w[:k // 2].float()).double()
-    below(dx, (2.0**-15 + k / 16384 * 2.0**-24) * size)
+    below(dx, (2.0**-18 + k / 2048 * 2.0**-24) * size)
 
 
 ACT = {None: lambda z: z, "relu": torch.relu, "gelu": torch.nn.functional.gelu, "silu": torch.nn.functional.silu}
