@@ -532,7 +532,8 @@ aa_status aa_linear(aa_ctx* ctx, const aa_rows* x, const aa_rows* w, const float
  *   dx = G w + residual,   dw = G^T x,   dbias = column sums of G.
  * dx, dw, dbias are nullable (not computed), written and not added to; residual (nullable, needs dx) is a gradient that reaches x past the layer, dx may
  * be residual itself.  dx and dw have the dtype of x and w, dbias is fp32.  With an activation and bf16 operands G is rounded to bf16, as a gradient between two layers would be, before
- * the two products (dbias sums it unrounded); fp32 operands keep all of it.  Sums run in an order that depends on the sizes alone, so equal calls give equal bits.
+ * the two products (dbias sums it unrounded); fp32 operands keep all of it.  Sums run in an order that depends on sizes, strides, alignment
+ * and R alone, so equal calls give equal bits.
  * scratch: DEVICE memory of at least aa_linear_grad_scratch_bytes(...) bytes for these operands (strides and alignment count, too), 256-byte aligned; it holds nothing
  * between calls, and calls that may run at the same time need one each.
  */

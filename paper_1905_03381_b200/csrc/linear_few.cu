@@ -4,9 +4,9 @@
 // 16 rows of x as their N side; nothing is staged.  The order of the terms of a sum is free, so a lane fetches 8 neighbouring weights of two outputs
 // (16 or 32 bytes) and the 8 values of x that belong to them, and they are taken for the terms that the instruction's layout gives the
 // lane.  Where the outputs alone do not fill the GPU, the warps of a CTA share a sum's range and join in shared memory.
-// fp32 numbers go in as three bf16 terms (see linear_split.cu), which costs six instructions a weight whatever the rows; sums of 128 terms
-// leave the matrix unit's accumulator for ordinary additions.
-// 1 x 512 -> 32,000 bf16 (33 MB of weights, 5.0 us at the copy rate) takes 11 us from a cold L2, 14 by 128-row tiles on the tensor cores; 16 x 512 -> 32,000 fp32
+// fp32 numbers go in as three bf16 terms (see linear_split.cu), which costs six instructions a weight whatever the rows; sums of 64 terms
+// (bf16: 128) leave the matrix unit's accumulator for ordinary additions.
+// 1 x 512 -> 32,000 bf16 (33 MB of weights, 5.0 us at the copy rate) takes 8.3 us behind other launches and 11 alone, both from a cold L2 (14 by 128-row tiles on the tensor cores); 16 x 512 -> 32,000 fp32
 // 24 and 54, 16 x 8,192 -> 1,024 fp32 30 and 53.
 #include <type_traits>
 
