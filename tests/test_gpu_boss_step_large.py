@@ -9,6 +9,7 @@ import torch
 from paper_1905_03381_b200 import binding as B
 from paper_1905_03381_b200 import build
 from test_gpu_boss_step import BF16, DEV, F32, HALF, c, i32
+from test_gpu_boss_step_use import Layer
 
 pytestmark = pytest.mark.gpu
 
@@ -154,6 +155,50 @@ def test_gradients_whose_contractions_take_several_runs(aa, m, k, n):
 @pytest.mark.parametrize("m,k,n", [(2050, 1300, 2400), (2051, 1301, 2403)])
 def test_fp32_gradients_with_several_tiles_a_pair(aa, m, k, n, act):
     check_grad(aa, F32, m, k, n, act, (m, m - 29, 65, 0))
+
+
+def test_replayed_and_in_two_contexts_on_tiles_of_pairs():
+    """Two layers of pairs' tiles, each captured on a stream of its own, replayed at once with other counts than at capture: the bits of calls alone and outside of graphs."""
+    layers = []
+    for m, k, n in ((5003, 520, 4616), (3000, 2312, 4104)):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            ctx = B.AutoAssist(max_rows=64, max_d=64, device=DEV, stream=stream)
+            layer = Layer(ctx, BF16, m, k, n)
+            layer.run()
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                layer.run()
+        layers.append((stream, ctx, layer, graph, m))
+    torch.cuda.synchronize()
+
+    def fresh(layer, rows):
+        layer.count.fill_(rows)
+        for t in (layer.p, layer.m, layer.v):
+            t.zero_()
+
+    for less in (0, 29, 2900):
+        alone = []
+        for stream, _, layer, _, m in layers:
+            with torch.cuda.stream(stream):
+                fresh(layer, m - less)
+                layer.run()
+                alone.append(layer.results())
+            torch.cuda.synchronize()
+        for _ in range(3):
+            for stream, _, layer, graph, m in layers:
+                with torch.cuda.stream(stream):
+                    fresh(layer, m - less)
+                    graph.replay()
+        torch.cuda.synchronize()
+        for (stream, ctx, layer, _, _), want in zip(layers, alone):
+            with torch.cuda.stream(stream):
+                assert all(torch.equal(a, b) for a, b in zip(layer.results(), want))
+                layer.check()
+            assert ctx.aa_device_status() == B.AA_OK
+    for _, ctx, _, _, _ in layers:
+        ctx.close()
 
 
 # ---------------------------------------------------------------------------------------------------------------------- norm
