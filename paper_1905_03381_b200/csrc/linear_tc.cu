@@ -270,8 +270,8 @@ product_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     else if (p.act == AA_ACT_GELU) put_chunk<AA_ACT_GELU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
                     else put_chunk<AA_ACT_SILU>(at, sub, r8, rows, bias, res != nullptr, add, to, p.out.stride * 4, raw, p.pre.stride * 4);
                 } else {
-                    // (more rows at once would take the registers of the sums)
-                    constexpr int AT_ONCE = CG == 2 ? 2 : 4;
+                    // (128 more registers hold sums; four rows at once would spill)
+                    constexpr int AT_ONCE = CG == 2 && RUNS && SUMS ? 2 : 4;
 #pragma unroll 1
                     for (int q0 = 0; q0 < 8; q0 += AT_ONCE) {
                         float z[AT_ONCE * 4];
