@@ -322,3 +322,95 @@ def test_fp32_activations_and_slopes_number_by_number(aa, act):
     w, pre, dout, db = torch.ones((n, 1), device=DEV), z[None, :].contiguous(), torch.ones((1, n), device=DEV), torch.empty(n, device=DEV)
     aa.aa_linear_grad(one, w, dout, aa.linear_grad_scratch(one, w, act), dbias=db, activation=act, pre=pre)
     close(db, slope, slope_bar)
+
+
+# ------------------------------------------------------------------------------------------------------------------ surroundings
+
+def padded(m, n, seed, dtype, pad, shift=0):
+    """m x n with `shift` NaN before and `pad` NaN behind each row."""
+    whole = torch.full((m, shift + n + pad), float("nan"), dtype=dtype, device=DEV)
+    whole[:, shift:shift + n] = random((m, n), seed, dtype)
+    return whole, whole[:, shift:shift + n]
+
+
+def target(m, n, dtype, pad, shift=0):
+    whole = torch.full((m, shift + n + pad), 7.0, dtype=dtype, device=DEV)
+    return whole, whole[:, shift:shift + n]
+
+
+def untouched(whole, n, shift):
+    assert torch.all(whole[:, :shift] == 7.0) and torch.all(whole[:, shift + n:] == 7.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (16, 8), (3, 0), (5, 1), (0, 4)])
+@pytest.mark.parametrize("m,k,n", [(9, 72, 40), (140, 72, 136), (700, 515, 1001), (1300, 264, 2056)])
+def test_nothing_around_the_rows_is_read_into_them_or_written(aa, dtype, m, k, n, pad, shift):
+    (_, x), (_, w), (_, dout), (_, pre), (_, res) = (padded(a, b, i, dtype, pad, shift) for i, (a, b) in enumerate(((m, k), (n, k), (m, n), (m, n), (m, n)), 1))
+    w.mul_(k ** -0.5)
+    (out_whole, out), (z_whole, z) = (target(m, n, dtype, pad, shift) for _ in range(2))
+    aa.aa_linear(x, w, out, activation="relu", residual=res, pre=z)
+    want = x.double() @ w.double().t()
+    size = x.double().abs() @ w.double().t().abs()
+    close(z, want, c(k) * size + HALF[dtype] * want.abs())
+    want = want.clamp(min=0.0) + res.double()
+    close(out, want, c(k) * size + (HALF[dtype] + 2.0**-22) * want.abs() + 2.0**-22 * size)
+    untouched(out_whole, n, shift), untouched(z_whole, n, shift)
+    for act in (None, "relu"):
+        (dx_whole, dx), (dw_whole, dw) = target(m, k, dtype, pad, shift), target(n, k, dtype, pad, shift)
+        db = torch.empty(n, device=DEV)
+        aa.aa_linear_grad(x, w, dout, aa.linear_grad_scratch(x, w, act), dx=dx, dw=dw, dbias=db, activation=act, pre=pre if act else None)
+        g = dout.double() * (1.0 if act is None else (pre > 0).double())
+        for got, a, b, terms in ((dx, g, w.double(), n), (dw, g.t(), x.double(), m)):
+            want = a @ b
+            close(got, want, c(terms) * (a.abs() @ b.abs()) + (HALF[dtype] + 2.0**-22) * want.abs())
+        close(db, g.sum(0), c(m) * g.abs().sum(0))
+        untouched(dx_whole, k, shift), untouched(dw_whole, k, shift)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 0), (5, 1), (0, 4)])
+@pytest.mark.parametrize("m,n", [(9, 72), (700, 515), (300, 4099), (20, 9000)])
+def test_nothing_around_normalised_rows_is_read_or_written(aa, dtype, m, n, pad, shift):
+    (_, x), (_, d), (_, res) = (padded(m, n, i, dtype, pad, shift) for i in (1, 2, 3))
+    (out_whole, out), (dx_whole, dx) = (target(m, n, dtype, pad, shift) for _ in range(2))
+    dg, db = torch.full((n + 2,), 7.0, device=DEV), torch.full((n + 2,), 7.0, device=DEV)
+    aa.aa_layer_norm(x, out)
+    aa.aa_layer_norm_grad(x, d, dx, aa.layer_norm_grad_scratch(x), residual=res, dgamma=dg[1:-1], dbeta=db[1:-1])
+    h, r, e = norm_reference(x.double(), None, 1e-5)
+    close(out, h, e + HALF[dtype] * h.abs())
+    D = d.double()
+    mg, mgh = D.abs().mean(1, keepdim=True), (D * h).abs().mean(1, keepdim=True)
+    plain = r * (D - D.mean(1, keepdim=True) - h * (D * h).mean(1, keepdim=True))
+    want = plain + res.double()
+    bar = r * (2.0**-18 * (D.abs() + mg) + e * (mgh + mg) + h.abs() * ((D.abs() * e).mean(1, keepdim=True) + 2.0**-18 * mgh)) + 2.0**-17 * plain.abs()
+    close(dx, want, bar + 2.0**-22 * want.abs() + HALF[dtype] * want.abs())
+    close(dg[1:-1], (D * h).sum(0), (D.abs() * e).sum(0) + c(m) * (D * h).abs().sum(0))
+    close(db[1:-1], D.sum(0), c(m) * D.abs().sum(0))
+    untouched(out_whole, n, shift), untouched(dx_whole, n, shift)
+    assert all(v[0] == 7.0 and v[-1] == 7.0 for v in (dg, db))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_matrices_of_more_than_two_to_the_31_elements(aa, dtype):
+    m, k, n = 70_001, 64, 32_000
+    x, w, dout = random((m, k), 1, dtype), random((n, k), 2, dtype, 0.125), torch.empty((m, n), dtype=dtype, device=DEV)
+    for i in range(0, m, 10_000):
+        dout[i:i + 10_000] = random((min(10_000, m - i), n), 3 + i, dtype)
+    out = torch.empty_like(dout)
+    aa.aa_linear(x, w, out)
+    rows = torch.tensor([0, 1, 2**31 // n - 1, 2**31 // n, 2**31 // n + 1, m - 300, m - 1], device=DEV)
+    X, W = x[rows].double(), w.double()
+    want = X @ W.t()
+    close(out[rows], want, c(k) * (X.abs() @ W.t().abs()) + HALF[dtype] * want.abs())
+    del out
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, device=DEV)
+    aa.aa_linear_grad(x, w, dout, aa.linear_grad_scratch(x, w), dx=dx, dw=dw, dbias=db)
+    g = dout[rows].double()
+    want = g @ W
+    close(dx[rows], want, c(n) * (g.abs() @ W.abs()) + (HALF[dtype] + 2.0**-22) * want.abs())
+    cols = [0, 5, n // 2, n - 1]
+    g = dout[:, cols].double()
+    want = g.t() @ x.double()
+    close(dw[cols], want, c(m) * (g.t().abs() @ x.double().abs()) + (HALF[dtype] + 2.0**-22) * want.abs())
+    close(db[cols], g.sum(0), c(m) * g.abs().sum(0))
